@@ -538,6 +538,107 @@ QNN_API int qnn_logquant_combine(const int32_t *p, int groups, int64_t M, int64_
                                  void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* 8-bit operands with real-valued scales (language-model layers)             */
+/* ------------------------------------------------------------------------- */
+
+/* The calls of this section run the layers of a language model on 8-bit
+ * integers: a row of real values becomes int8 codes in -127..127 and ONE fp32
+ * scale, value = code * scale; a product multiplies codes exactly in int32 and
+ * applies the scale of the token (row of A) and of the output channel (row of
+ * B).  None of them needs a workspace, and every one may be captured in a CUDA
+ * graph.
+ *
+ * Element types of the real tensors: */
+#define QNN_TYPE_F32 0
+#define QNN_TYPE_BF16 1
+#define QNN_TYPE_F16 2
+
+/* Rules shared by the three calls that quantise rows:
+ *   scale[r] = max_k |t[r,k]| / 127,  code = round_half_even(t * (127 / max|t|)),
+ *   all in fp32; t is the row of values the call computes.
+ *  - codes  device, int8 [rows, ldq]: an operand in form QNN_FORM_I8 (16-byte
+ *           aligned, ldq a multiple of 16, ldq >= K rounded up to 32; whole
+ *           128-byte lines recommended).  Elements K .. roundup(K, 32) of every
+ *           row are written as 0, bytes beyond that are left untouched.
+ *  - scale  device, fp32 [rows]
+ *  - values device, [rows, ld_values] of values_type, or NULL: what the codes
+ *           stand for, code * scale rounded to values_type -- the operand a
+ *           training step uses beside the codes when it passes the gradient
+ *           straight through the quantiser.
+ *  - A row whose largest magnitude is below 2^-118 gives scale 0 and codes 0.
+ *    A row that holds (or computes) an infinity or a NaN, or whose sum of
+ *    squares overflows fp32, gives scale NaN and codes 0, so that everything
+ *    computed from it is NaN, as it would be without the quantiser.
+ *  - Real tensors need the alignment of their elements only; rows that are
+ *    16-byte aligned run fastest.
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (K or rows of 2^31 and more), CUDA. */
+
+/* t = x: weights [N, K] once (a scale for each output channel), or activations. */
+QNN_API int qnn_quantize_rows_i8(const void *x, int type, int64_t rows, int64_t K, int64_t ldx, void *codes, int64_t ldq,
+                                 float *scale, void *values, int values_type, int64_t ld_values, void *stream);
+
+/* Root-mean-square norm with the residual's addition:
+ *   s = x + residual (fp32),  t[k] = s[k] * gamma[k] / sqrt(mean_k s[k]^2 + eps)
+ * residual [rows, ldr] or NULL (s = x); gamma [K] or NULL (all one), both of x's
+ * type.  sum_out [rows, ld_sum] or NULL receives s rounded to that type, the next
+ * block's residual; it may be x or residual itself (same leading dimension). */
+QNN_API int qnn_rmsnorm_quant_i8(const void *x, const void *residual, int type, int64_t rows, int64_t K, int64_t ldx,
+                                 int64_t ldr, const void *gamma, float eps, void *codes, int64_t ldq, float *scale,
+                                 void *sum_out, int64_t ld_sum, void *values, int values_type, int64_t ld_values,
+                                 void *stream);
+
+/* Gated activation: t = gate / (1 + exp(-gate)) * up.  gate [rows, ldg] and up
+ * [rows, ldu] may be the two halves of one product's output. */
+QNN_API int qnn_silu_mul_quant_i8(const void *gate, const void *up, int type, int64_t rows, int64_t K, int64_t ldg,
+                                  int64_t ldu, void *codes, int64_t ldq, float *scale, void *values, int values_type,
+                                  int64_t ld_values, void *stream);
+
+/* out[m,n] = (float(sum_k a[m,k] * b[n,k]) * a_scale[m]) * b_scale[n] + bias[n],
+ * the sum exact in int32, the rest in fp32, rounded once to out_type.
+ *   a, b      device, int8 [M, lda], [N, ldb] (any codes in -128..127): 16-byte
+ *             aligned, lda and ldb multiples of 16 and >= K.  Bytes beyond K of a
+ *             row are not read into the sum: pads need not be zero.
+ *   a_scale   device, fp32 [M]; b_scale fp32 [N]; bias fp32 [N] or NULL
+ *   out       device, [M, ldo] of out_type, ldo >= N; rows that are 16-byte
+ *             aligned leave as bulk stores, others element by element
+ * K = 0 gives the bias.  Errors: INVALID_ARG, ALIGNMENT, OVERFLOW (K >= 2^17:
+ * 128 * 128 * K no longer fits int32), UNSUPPORTED (M or N above 2^30), CUDA. */
+QNN_API int qnn_gemm_i8_scaled(const void *a, int64_t lda, const float *a_scale, const void *b, int64_t ldb,
+                               const float *b_scale, const float *bias, int64_t M, int64_t N, int64_t K, void *out,
+                               int out_type, int64_t ldo, void *stream);
+
+/* Scores of given tokens from logits z [T, ldl] of `type`, one pass over them:
+ *   lse[t]       = log sum_v exp(z[t,v])
+ *   logprob[t]   = z[t, ids[t]] - lse[t]
+ *   entropy[t]   = - sum_v p log p,  p = exp(z - lse)
+ *   top_ids[t,j], top_logprob[t,j], j < topk <= min(V, 32): the topk largest
+ *                  logits in falling order, equal ones by rising index
+ * ids int64 [T]; an id outside 0..V-1 is "no token": logprob 0, and no gradient.
+ * logprob, entropy, lse, top_logprob: fp32; top_ids: int64; each may be NULL
+ * (ids may be NULL when logprob is; top_* only when topk = 0).
+ * A logit of -inf is a masked entry: probability 0.  A row with no other entries
+ * has lse -inf, every logprob -inf (a token's and the alternatives') and entropy
+ * 0.  A NaN or a +inf makes the row's numbers NaN (top_ids stay valid, NaN first).
+ * Statistics are held in fp32 relative to the running maximum, the sum of the
+ * entropy as sum e^(z-m) (z-m), which has one sign and does not cancel.
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (V >= 2^31, topk > 32), CUDA. */
+QNN_API int qnn_token_logprobs(const void *logits, int type, int64_t T, int64_t V, int64_t ldl, const int64_t *ids,
+                               float *logprob, float *entropy, float *lse, int topk, float *top_logprob,
+                               int64_t *top_ids, void *stream);
+
+/* Gradient of the scores with respect to the logits, from what the forward call
+ * left (lse, entropy) and the gradients that come back:
+ *   dz[t,v] = g_logprob[t] * ([v = ids[t]] - p) - g_entropy[t] * p * (log p + entropy[t])
+ * g_logprob (with ids) or g_entropy (with entropy) may be NULL: no such gradient.
+ * d_logits [T, ldd] of the logits' type, rounded once; it may be logits itself
+ * (ldd = ldl).  Masked entries and rows with nothing left get 0.  The top
+ * alternatives carry no gradient. */
+QNN_API int qnn_token_logprobs_backward(const void *logits, int type, int64_t T, int64_t V, int64_t ldl,
+                                        const int64_t *ids, const float *lse, const float *entropy,
+                                        const float *g_logprob, const float *g_entropy, void *d_logits, int64_t ldd,
+                                        void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* The ConvNet of Table 7                                                     */
 /* ------------------------------------------------------------------------- */
 

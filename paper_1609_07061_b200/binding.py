@@ -25,6 +25,7 @@ QNN_MODE_U01, QNN_MODE_PM1 = 0, 1
 QNN_OP_XNOR_GEMM, QNN_OP_BITPLANE_GEMM, QNN_OP_CONV2D, QNN_OP_MLP = 1, 2, 3, 4
 QNN_LAYER_CONV_U8, QNN_LAYER_CONV, QNN_LAYER_FC = 1, 2, 3
 QNN_NOALLOC_SCRATCH_BYTES = 8 << 20
+QNN_TYPE_F32, QNN_TYPE_BF16, QNN_TYPE_F16 = 0, 1, 2
 
 
 class QnnError(RuntimeError):
@@ -126,6 +127,12 @@ _SIGS = {
     "qnn_mlp_graph_destroy": (i32, [vp]),
     "qnn_mlp_layer_form": (i32, [ctypes.POINTER(qnn_mlp_layer), i32, i32, i32]),
     "qnn_mlp_workspace_bytes": (sz, [i64, i32, ctypes.POINTER(qnn_mlp_layer), i32, i32, i32]),
+    "qnn_quantize_rows_i8": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, vp, i32, i64, vp]),
+    "qnn_rmsnorm_quant_i8": (i32, [vp, vp, i32, i64, i64, i64, i64, vp, f32, vp, i64, vp, vp, i64, vp, i32, i64, vp]),
+    "qnn_silu_mul_quant_i8": (i32, [vp, vp, i32, i64, i64, i64, i64, vp, i64, vp, vp, i32, i64, vp]),
+    "qnn_gemm_i8_scaled": (i32, [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp]),
+    "qnn_token_logprobs": (i32, [vp, i32, i64, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp]),
+    "qnn_token_logprobs_backward": (i32, [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]),
     "qnn_workspace_bytes": (sz, [i32, i64, i64, i64, i32, i32, i32]),
     "qnn_select_algo": (i32, [i64, i64, i64, i32, i32, i32, i32]),
     "qnn_device_status": (i32, [vp]),
@@ -597,3 +604,76 @@ def qnn_xnor_gemm_noalloc(a, lda, b, ldb, M, N, K, out, ldo):
     For callers that cannot allocate device memory at call time.  Calls share the array, so keep them on one
     stream; the first call on a device should precede any stream capture."""
     _ck(_lib.qnn_xnor_gemm_noalloc(_p(a), lda, _p(b), ldb, M, N, K, _p(out), ldo, _stream()), "qnn_xnor_gemm_noalloc")
+
+
+_TYPES = {torch.float32: QNN_TYPE_F32, torch.bfloat16: QNN_TYPE_BF16, torch.float16: QNN_TYPE_F16}
+
+
+def _type(t: Optional[torch.Tensor], where: str, like: Optional[torch.Tensor] = None) -> int:
+    """QNN_TYPE_* of a real tensor; a second tensor that must share its type is checked (no pointer tells the C side)."""
+    if t is None:
+        return QNN_TYPE_F32
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{where}: {t.dtype} is none of float32, bfloat16, float16")
+    if like is not None and like.dtype != t.dtype:
+        raise TypeError(f"{where}: {like.dtype} where {t.dtype} is needed")
+    return code
+
+
+def _need(t: Optional[torch.Tensor], dtype: torch.dtype, where: str):
+    if t is not None and t.dtype != dtype:
+        raise TypeError(f"{where}: {t.dtype} where {dtype} is needed")
+    return None if t is None else t.data_ptr()
+
+
+def qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values=None, ld_values=0):
+    """Rows of x -> int8 codes and one fp32 scale a row (weights once, or activations); values: what the codes stand for."""
+    w = "qnn_quantize_rows_i8"
+    _ck(_lib.qnn_quantize_rows_i8(_p(x), _type(x, w), rows, K, ldx, _need(codes, torch.int8, w), ldq,
+                                  _need(scale, torch.float32, w), _p(values), _type(values, w), ld_values, _stream()), w)
+
+
+def qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out=None, ld_sum=0, values=None,
+                         ld_values=0):
+    """Root-mean-square norm of x + residual, scaled by gamma, as int8 codes and one scale a row; sum_out: x + residual."""
+    w = "qnn_rmsnorm_quant_i8"
+    t = _type(x, w, residual)
+    _type(x, w, gamma)
+    _type(x, w, sum_out)
+    _ck(_lib.qnn_rmsnorm_quant_i8(_p(x), _p(residual), t, rows, K, ldx, ldr, _p(gamma), eps, _need(codes, torch.int8, w), ldq,
+                                  _need(scale, torch.float32, w), _p(sum_out), ld_sum, _p(values), _type(values, w),
+                                  ld_values, _stream()), w)
+
+
+def qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values=None, ld_values=0):
+    """gate / (1 + exp(-gate)) * up as int8 codes and one scale a row."""
+    w = "qnn_silu_mul_quant_i8"
+    _ck(_lib.qnn_silu_mul_quant_i8(_p(gate), _p(up), _type(gate, w, up), rows, K, ldg, ldu, _need(codes, torch.int8, w), ldq,
+                                   _need(scale, torch.float32, w), _p(values), _type(values, w), ld_values, _stream()), w)
+
+
+def qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, M, N, K, out, ldo, bias=None):
+    """out[m, n] = sum_k a[m, k] b[n, k] * a_scale[m] * b_scale[n] + bias[n], in the type of `out`."""
+    w = "qnn_gemm_i8_scaled"
+    f = torch.float32
+    _ck(_lib.qnn_gemm_i8_scaled(_need(a, torch.int8, w), lda, _need(a_scale, f, w), _need(b, torch.int8, w), ldb,
+                                _need(b_scale, f, w), _need(bias, f, w), M, N, K, _p(out), _type(out, w), ldo, _stream()), w)
+
+
+def qnn_token_logprobs(logits, T, V, ldl, ids, logprob, entropy=None, lse=None, topk=0, top_logprob=None, top_ids=None):
+    """Log probabilities of the tokens `ids`, entropies, and the topk alternatives (ties to the lowest id)."""
+    w = "qnn_token_logprobs"
+    f = torch.float32
+    _ck(_lib.qnn_token_logprobs(_p(logits), _type(logits, w), T, V, ldl, _need(ids, torch.int64, w), _need(logprob, f, w),
+                                _need(entropy, f, w), _need(lse, f, w), topk, _need(top_logprob, f, w),
+                                _need(top_ids, torch.int64, w), _stream()), w)
+
+
+def qnn_token_logprobs_backward(logits, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d_logits, ldd):
+    """Gradient of log probabilities and entropies with respect to the logits."""
+    w = "qnn_token_logprobs_backward"
+    f = torch.float32
+    _ck(_lib.qnn_token_logprobs_backward(_p(logits), _type(logits, w, d_logits), T, V, ldl, _need(ids, torch.int64, w),
+                                         _need(lse, f, w), _need(entropy, f, w), _need(g_logprob, f, w),
+                                         _need(g_entropy, f, w), _p(d_logits), ldd, _stream()), w)

@@ -1,0 +1,428 @@
+// Rows of real values -> int8 codes and one scale a row: plain rows, a root-mean-square norm with the residual's
+// addition, a gated activation.
+//
+//   t[k]  = x[k]                                          (plain)
+//         = s[k] gamma[k] rstd,  s = x + residual,  rstd = 1 / sqrt(mean s^2 + eps)   (norm)
+//         = gate[k] / (1 + exp(-gate[k])) * up[k]         (gate)
+//   scale = max|t| / 127,  code = rn(t * 127 / max|t|)
+//
+// In the norm rstd is one positive number of the row, so it cancels in the codes: code = rn(u * 127 / max|u|) with
+// u = s gamma, and scale = rstd * max|u| / 127.  Sum of squares and maximum are then ONE reduction over the row, and a
+// row that stays in registers is read once and written once.
+//
+// Bound by HBM: 16-bit x and residual in, 16-bit sum and 8-bit codes out is 7 bytes an element.
+#include "qnn_types.cuh"
+
+namespace qnn {
+namespace {
+
+enum RowOp { ROW_PLAIN = 0, ROW_NORM = 1, ROW_GATE = 2 };
+
+struct RowArgs {
+    const void *x;                 // x, or the gate
+    const void *b;                 // residual (may be NULL), or up
+    const void *gamma;             // may be NULL
+    int64_t ldx, ldb;
+    int64_t rows;
+    int32_t K, KP;                 // KP = K rounded up to 32: codes are written up to there
+    float eps;
+    uint8_t *codes; int64_t ldq;
+    float *scale;
+    void *sum; int64_t ld_sum;     // may be NULL
+    void *values; int64_t ld_values; int values_type;   // may be NULL
+    int tpr;                       // threads per row, a multiple of 32
+};
+
+// 1.5 * 2^23: t * inv + MAGIC rounds to a whole number (to even at ties) and leaves it in the low bits of the float
+constexpr float MAGIC = 12582912.0f;
+
+__device__ __forceinline__ float silu(float a) { return __fdividef(a, 1.0f + __expf(-a)); }
+
+// what the reduction leaves a thread with: the factor that turns t into codes, the scale, and a mask for the codes
+struct RowScale {
+    float inv, scale;
+    uint32_t keep;
+};
+template <int OP>
+__device__ __forceinline__ RowScale row_scale(float ss, uint32_t top_bits, int32_t K, float eps)
+{
+    RowScale r;
+    const float top = __uint_as_float(top_bits);
+    r.inv = 0.0f; r.scale = 0.0f; r.keep = 0xffffffffu;
+    // bits above those of the largest finite float: an infinity or a NaN
+    bool bad = top_bits > 0x7f7fffffu;
+    if (OP == ROW_NORM) bad = bad || !(ss <= 3.402823466e38f);
+    if (bad) {
+        r.scale = __uint_as_float(0x7fc00000u);
+        r.keep = 0u;
+    } else if (top >= 3.0092655e-36f) {      // 2^-118: below it 127 / top may overflow, and the row counts as zero
+        r.inv = 127.0f / top;
+        r.scale = top / 127.0f;
+        if (OP == ROW_NORM) r.scale *= 1.0f / sqrtf(ss / (float)K + eps);
+    }
+    return r;
+}
+
+template <int W>
+__device__ __forceinline__ void store_codes(uint8_t *dst, const float (&f)[W], uint32_t keep)
+{
+    // f holds MAGIC + code: the code is the low byte
+    if constexpr (W == 8) {
+        uint32_t o[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t lo = __byte_perm(__float_as_uint(f[4 * h]), __float_as_uint(f[4 * h + 1]), 0x0040);
+            const uint32_t hi = __byte_perm(__float_as_uint(f[4 * h + 2]), __float_as_uint(f[4 * h + 3]), 0x0040);
+            o[h] = __byte_perm(lo, hi, 0x5410) & keep;
+        }
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(o[0], o[1]);
+    } else if constexpr (W == 2) {
+        *reinterpret_cast<uint16_t *>(dst) = (uint16_t)(__byte_perm(__float_as_uint(f[0]), __float_as_uint(f[1]), 0x0040) & keep);
+    } else {
+        *dst = (uint8_t)(__float_as_uint(f[0]) & keep);
+    }
+}
+
+template <typename V, int W>
+__device__ __forceinline__ void store_row_piece(void *base, int64_t row_off, int32_t k0, int32_t K, const float (&f)[W])
+{
+    V *dst = static_cast<V *>(base) + row_off + k0;
+    if (W == 1 || k0 + W <= K) {
+        store_floats<V, W>(dst, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (k0 + i < K) from_float(f[i], dst[i]);
+    }
+}
+template <int W>
+__device__ __forceinline__ void store_values(const RowArgs &p, int64_t row, int32_t k0, const float (&f)[W])
+{
+    const int64_t off = row * p.ld_values;
+    if (p.values_type == QNN_TYPE_F32) store_row_piece<float, W>(p.values, off, k0, p.K, f);
+    else if (p.values_type == QNN_TYPE_BF16) store_row_piece<__nv_bfloat16, W>(p.values, off, k0, p.K, f);
+    else store_row_piece<__half, W>(p.values, off, k0, p.K, f);
+}
+
+// a piece of a row in memory order; elements past K are zero (no load is issued for them)
+template <typename T, int W>
+__device__ __forceinline__ void load_row_piece(const T *row, int32_t k0, int32_t K, Piece<T, W> &v)
+{
+    if (W == 1 || k0 + W <= K) {
+        load_piece<T, W>(row + k0, v);
+    } else {
+        alignas(16) T t[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            t[i] = T(0.0f);
+            if (k0 + i < K) t[i] = row[k0 + i];
+        }
+        if constexpr (W == 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) * 2; ++i) v.w[i] = reinterpret_cast<const uint32_t *>(t)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) v.e[i] = t[i];
+        }
+    }
+}
+
+// t of one piece; adds to the sum of squares, and gives the sum s of the norm in `s`
+template <int OP, typename T, int W>
+__device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, const Piece<T, W> &bv, int32_t k0, float (&s)[W], float (&t)[W],
+                                       float &ss)
+{
+    float x[W], b[W];
+    piece_to_floats<T, W>(xv, x);
+    if (OP == ROW_GATE || (OP == ROW_NORM && p.b != nullptr)) piece_to_floats<T, W>(bv, b);
+    if (OP == ROW_PLAIN) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) t[i] = x[i];
+    } else if (OP == ROW_GATE) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) t[i] = silu(x[i]) * b[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            s[i] = p.b != nullptr ? x[i] + b[i] : x[i];
+            ss = fmaf(s[i], s[i], ss);
+            t[i] = s[i];
+        }
+        if (p.gamma != nullptr && k0 < p.K) {
+            Piece<T, W> gv;
+            float g[W];
+            load_row_piece<T, W>(static_cast<const T *>(p.gamma), k0, p.K, gv);
+            piece_to_floats<T, W>(gv, g);
+#pragma unroll
+            for (int i = 0; i < W; ++i) t[i] *= g[i];
+        }
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// A row of at most 8 * NV * tpr elements in registers: tpr threads own pieces of W elements, interleaved, so that a
+// warp's accesses are contiguous.  W = 8 needs 16-byte aligned rows, W = 2 aligned pairs, W = 1 nothing.
+template <int OP, typename T, int W, int NV>
+__global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
+{
+    constexpr int P = NV * 8 / W;                        // pieces per thread
+    constexpr int CH0 = W == 8 ? (sizeof(T) == 4 ? 2 : 4) : 8;   // pieces whose loads are in flight together
+    constexpr int CH = P < CH0 ? P : CH0;
+    __shared__ float sh_ss[16];
+    __shared__ uint32_t sh_top[16];
+    griddep_launch_dependents();
+    griddep_wait();
+
+    const int tpr = p.tpr;
+    const int sub = threadIdx.x / tpr, t0 = threadIdx.x - sub * tpr;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / tpr) + sub;
+    const bool live = row < p.rows;
+    const T *xr = static_cast<const T *>(p.x) + (live ? row : 0) * p.ldx;
+    const T *br = static_cast<const T *>(p.b) + (live ? row : 0) * p.ldb;
+    const bool with_b = OP == ROW_GATE || (OP == ROW_NORM && p.b != nullptr);
+    const int32_t K = live ? p.K : 0;
+
+    float t[P][W];
+    float ss = 0.0f;
+    uint32_t top = 0u;
+#pragma unroll
+    for (int c = 0; c < P; c += CH) {
+        Piece<T, W> xv[CH], bv[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int32_t k0 = ((c + j) * tpr + t0) * W;
+            if (k0 < K) load_row_piece<T, W>(xr, k0, K, xv[j]);
+            if (with_b && k0 < K) load_row_piece<T, W>(br, k0, K, bv[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int32_t k0 = ((c + j) * tpr + t0) * W;
+            if (k0 < K) {
+                float s[W];
+                row_op<OP, T, W>(p, xv[j], bv[j], k0, s, t[c + j], ss);
+                if (OP == ROW_NORM && p.sum != nullptr) store_row_piece<T, W>(p.sum, row * p.ld_sum, k0, K, s);
+#pragma unroll
+                for (int i = 0; i < W; ++i) top = max(top, __float_as_uint(t[c + j][i]) & 0x7fffffffu);
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i) t[c + j][i] = 0.0f;
+            }
+        }
+    }
+
+    if (OP == ROW_NORM) ss = warp_sum(ss);
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (tpr > 32) {
+        const int warp = threadIdx.x >> 5;
+        if ((threadIdx.x & 31) == 0) { sh_ss[warp] = ss; sh_top[warp] = top; }
+        __syncthreads();
+        const int w0 = sub * (tpr >> 5);
+        ss = 0.0f;
+        for (int w = 0; w < (tpr >> 5); ++w) { ss += sh_ss[w0 + w]; top = max(top, sh_top[w0 + w]); }
+    }
+    if (!live) return;
+    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
+    if (t0 == 0) p.scale[row] = r.scale;
+    uint8_t *cr = p.codes + row * p.ldq;
+#pragma unroll
+    for (int c = 0; c < P; ++c) {
+        const int32_t k0 = (c * tpr + t0) * W;
+        if (k0 < p.KP) {
+            float f[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) f[i] = fmaf(t[c][i], r.inv, MAGIC);
+            store_codes<W>(cr + k0, f, r.keep);
+            if (p.values != nullptr && k0 < K) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) f[i] = (f[i] - MAGIC) * r.scale;
+                store_values<W>(p, row, k0, f);
+            }
+        }
+    }
+}
+
+// Rows longer than the registers of a block hold: two passes over the row, the second mostly from L2.  sum_out may be x
+// or residual, so the first pass writes nothing and the second writes each element after reading it.
+template <int OP, typename T, int W>
+__global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
+{
+    __shared__ float sh_ss[16];
+    __shared__ uint32_t sh_top[16];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int64_t row = blockIdx.x;
+    const T *xr = static_cast<const T *>(p.x) + row * p.ldx;
+    const T *br = static_cast<const T *>(p.b) + row * p.ldb;
+    const bool with_b = OP == ROW_GATE || (OP == ROW_NORM && p.b != nullptr);
+    const int64_t step = (int64_t)blockDim.x * W;
+    float ss = 0.0f;
+    uint32_t top = 0u;
+    for (int64_t k0 = (int64_t)threadIdx.x * W; k0 < p.K; k0 += step) {
+        Piece<T, W> xv, bv;
+        float s[W], t[W];
+        load_row_piece<T, W>(xr, (int32_t)k0, p.K, xv);
+        if (with_b) load_row_piece<T, W>(br, (int32_t)k0, p.K, bv);
+        row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, ss);
+#pragma unroll
+        for (int i = 0; i < W; ++i) top = max(top, __float_as_uint(t[i]) & 0x7fffffffu);
+    }
+    if (OP == ROW_NORM) ss = warp_sum(ss);
+    top = __reduce_max_sync(0xffffffffu, top);
+    const int warp = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) { sh_ss[warp] = ss; sh_top[warp] = top; }
+    __syncthreads();
+    ss = 0.0f;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) { ss += sh_ss[w]; top = max(top, sh_top[w]); }
+    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
+    if (threadIdx.x == 0) p.scale[row] = r.scale;
+    uint8_t *cr = p.codes + row * p.ldq;
+    for (int64_t k0 = (int64_t)threadIdx.x * W; k0 < p.KP; k0 += step) {
+        float s[W], t[W], f[W], unused = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) t[i] = 0.0f;
+        if (k0 < p.K) {
+            Piece<T, W> xv, bv;
+            load_row_piece<T, W>(xr, (int32_t)k0, p.K, xv);
+            if (with_b) load_row_piece<T, W>(br, (int32_t)k0, p.K, bv);
+            row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, unused);
+            if (OP == ROW_NORM && p.sum != nullptr) store_row_piece<T, W>(p.sum, row * p.ld_sum, (int32_t)k0, p.K, s);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) f[i] = fmaf(t[i], r.inv, MAGIC);
+        store_codes<W>(cr + k0, f, r.keep);
+        if (p.values != nullptr && k0 < p.K) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) f[i] = (f[i] - MAGIC) * r.scale;
+            store_values<W>(p, row, (int32_t)k0, f);
+        }
+    }
+}
+
+constexpr int MAX_TPR = 512;
+
+template <int OP, typename T, int W>
+int launch_rows(RowArgs p, const char *what, cudaStream_t st)
+{
+    constexpr int MAX_NV = W == 8 ? 8 : 4;               // (narrow accesses need more registers an element)
+    const int64_t groups = ceil_div(p.KP, 8);            // a row in units of eight elements
+    if (groups > (int64_t)MAX_TPR * MAX_NV) {
+        QNN_CUDA(launch_pdl(row_quant_long_kernel<OP, T, W>, dim3((unsigned)p.rows), dim3(512), 0, st, p));
+        return check_launch(what);
+    }
+    // Few rows: as many threads a row as there are groups, for latency.  Many rows: two groups a thread.
+    int nv = (p.rows <= 2 * (int64_t)sm_count()) ? 1 : 2;
+    while (groups > (int64_t)MAX_TPR * nv) nv *= 2;
+    p.tpr = (int)(ceil_div(ceil_div(groups, nv), 32) * 32);
+    const int rpb = p.tpr >= 128 ? 1 : 128 / p.tpr;      // rows of short vectors share a block
+    const dim3 grid((unsigned)ceil_div(p.rows, rpb)), block((unsigned)(p.tpr * rpb));
+    switch (nv) {
+        case 1: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 1>, grid, block, 0, st, p)); break;
+        case 2: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 2>, grid, block, 0, st, p)); break;
+        case 4: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4>, grid, block, 0, st, p)); break;
+        default:
+            if constexpr (W == 8) QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 8>, grid, block, 0, st, p));
+            break;
+    }
+    return check_launch(what);
+}
+
+template <int OP, typename T>
+int launch_rows_w(const RowArgs &p, const char *what, cudaStream_t st)
+{
+    // widest access every row of every real tensor allows
+    auto fits = [&](size_t elems) {
+        auto ok = [&](const void *q, int64_t ld, size_t es) { return q == nullptr || (aligned(q, elems * es < 16 ? elems * es : 16) && (size_t)ld % (elems * es < 16 ? elems : 16 / es) == 0); };
+        const size_t vs = p.values_type == QNN_TYPE_F32 ? 4 : 2;
+        return ok(p.x, p.ldx, sizeof(T)) && ok(p.b, p.ldb, sizeof(T)) && ok(p.gamma, 0, sizeof(T)) && ok(p.sum, p.ld_sum, sizeof(T)) &&
+               ok(p.values, p.ld_values, vs);
+    };
+    if (fits(8)) return launch_rows<OP, T, 8>(p, what, st);
+    if (fits(2)) return launch_rows<OP, T, 2>(p, what, st);
+    return launch_rows<OP, T, 1>(p, what, st);
+}
+
+template <int OP>
+int quant_rows(RowArgs p, int type, int64_t K, const char *what, void *stream)
+{
+    QNN_REQUIRE(type_ok(type), QNN_ERR_INVALID_ARG, "%s: unknown element type %d", what, type);
+    QNN_REQUIRE(p.rows >= 0 && K >= 0, QNN_ERR_INVALID_ARG, "%s: negative size", what);
+    if (p.rows == 0 || K == 0) return QNN_OK;
+    QNN_REQUIRE(p.rows < ((int64_t)1 << 31) && K < ((int64_t)1 << 31) - 32, QNN_ERR_UNSUPPORTED, "%s: rows or K of 2^31 and more", what);
+    QNN_REQUIRE(p.x && p.codes && p.scale && (OP != ROW_GATE || p.b), QNN_ERR_INVALID_ARG, "%s: NULL pointer", what);
+    const int64_t kp = (int64_t)round_up((size_t)K, 32);
+    QNN_REQUIRE(p.ldx >= K && (!p.b || p.ldb >= K) && (!p.sum || p.ld_sum >= K), QNN_ERR_INVALID_ARG, "%s: leading dimension below K", what);
+    QNN_REQUIRE(p.ldq >= kp, QNN_ERR_INVALID_ARG, "%s: ldq below K rounded up to 32", what);
+    QNN_REQUIRE(aligned(p.codes, 16) && p.ldq % 16 == 0, QNN_ERR_ALIGNMENT, "%s: codes must be 16-byte aligned, ldq a multiple of 16", what);
+    const size_t es = (size_t)type_bytes(type);
+    QNN_REQUIRE(aligned(p.x, es) && aligned(p.b, es) && aligned(p.gamma, es) && aligned(p.sum, es) && aligned(p.scale, 4), QNN_ERR_ALIGNMENT,
+                "%s: a pointer is not aligned to its elements", what);
+    if (p.values) {
+        QNN_REQUIRE(type_ok(p.values_type), QNN_ERR_INVALID_ARG, "%s: unknown type %d of the values", what, p.values_type);
+        QNN_REQUIRE(p.ld_values >= K, QNN_ERR_INVALID_ARG, "%s: ld_values below K", what);
+        QNN_REQUIRE(aligned(p.values, (size_t)type_bytes(p.values_type)), QNN_ERR_ALIGNMENT, "%s: values are not aligned to their elements", what);
+    }
+    if (OP == ROW_NORM) {
+        QNN_REQUIRE(p.eps >= 0.0f, QNN_ERR_INVALID_ARG, "%s: eps is negative or NaN", what);
+        QNN_REQUIRE(p.sum == nullptr || p.sum != p.x || p.ld_sum == p.ldx, QNN_ERR_INVALID_ARG, "%s: sum_out over x needs the same leading dimension", what);
+        QNN_REQUIRE(p.sum == nullptr || p.sum != p.b || p.ld_sum == p.ldb, QNN_ERR_INVALID_ARG,
+                    "%s: sum_out over the residual needs the same leading dimension", what);
+    }
+    p.K = (int32_t)K;
+    p.KP = (int32_t)kp;
+    cudaStream_t st = as_stream(stream);
+    switch (type) {
+        case QNN_TYPE_F32: return launch_rows_w<OP, float>(p, what, st);
+        case QNN_TYPE_BF16: return launch_rows_w<OP, __nv_bfloat16>(p, what, st);
+        default: return launch_rows_w<OP, __half>(p, what, st);
+    }
+}
+
+}  // namespace
+}  // namespace qnn
+
+using namespace qnn;
+
+extern "C" {
+
+int qnn_quantize_rows_i8(const void *x, int type, int64_t rows, int64_t K, int64_t ldx, void *codes, int64_t ldq, float *scale, void *values,
+                         int values_type, int64_t ld_values, void *stream)
+{
+    RowArgs p{};
+    p.x = x; p.ldx = ldx; p.rows = rows;
+    p.codes = static_cast<uint8_t *>(codes); p.ldq = ldq; p.scale = scale;
+    p.values = values; p.values_type = values_type; p.ld_values = ld_values;
+    return quant_rows<ROW_PLAIN>(p, type, K, "qnn_quantize_rows_i8", stream);
+}
+
+int qnn_rmsnorm_quant_i8(const void *x, const void *residual, int type, int64_t rows, int64_t K, int64_t ldx, int64_t ldr, const void *gamma,
+                         float eps, void *codes, int64_t ldq, float *scale, void *sum_out, int64_t ld_sum, void *values, int values_type,
+                         int64_t ld_values, void *stream)
+{
+    RowArgs p{};
+    p.x = x; p.ldx = ldx; p.rows = rows;
+    p.b = residual; p.ldb = residual ? ldr : 0;
+    p.gamma = gamma; p.eps = eps;
+    p.codes = static_cast<uint8_t *>(codes); p.ldq = ldq; p.scale = scale;
+    p.sum = sum_out; p.ld_sum = ld_sum;
+    p.values = values; p.values_type = values_type; p.ld_values = ld_values;
+    return quant_rows<ROW_NORM>(p, type, K, "qnn_rmsnorm_quant_i8", stream);
+}
+
+int qnn_silu_mul_quant_i8(const void *gate, const void *up, int type, int64_t rows, int64_t K, int64_t ldg, int64_t ldu, void *codes, int64_t ldq,
+                          float *scale, void *values, int values_type, int64_t ld_values, void *stream)
+{
+    RowArgs p{};
+    p.x = gate; p.ldx = ldg; p.rows = rows;
+    p.b = up; p.ldb = ldu;
+    p.codes = static_cast<uint8_t *>(codes); p.ldq = ldq; p.scale = scale;
+    p.values = values; p.values_type = values_type; p.ld_values = ld_values;
+    return quant_rows<ROW_GATE>(p, type, K, "qnn_silu_mul_quant_i8", stream);
+}
+
+}  // extern "C"

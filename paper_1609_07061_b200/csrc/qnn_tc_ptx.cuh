@@ -156,6 +156,188 @@ __device__ __forceinline__ uint64_t make_kmajor_desc(uint32_t saddr)
     return d;
 }
 
+// One pipeline stage of the MMA warp as ONE instruction stream: poll the NEXT stage's full barrier, issue the
+// four K steps of this stage (+32 bytes of K = +2 in the descriptors' address field), commit them to this
+// stage's empty barrier, and only then read the poll's result -- the poll's latency hides behind the issue.
+// Returns non-zero when the next stage has already landed.
+template <int FORM>
+__device__ __forceinline__ uint32_t umma_stage(uint32_t next_full_bar, uint32_t next_parity, uint32_t d_tmem, uint32_t a_lo,
+                                               uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t accumulate_first,
+                                               uint32_t sf, uint32_t empty_bar)
+{
+    uint32_t ready;
+    if (FORM == QNN_FORM_FP4) {
+        asm volatile(
+            "{\n"
+            ".reg .pred P, Q, T;\n"
+            ".reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n"
+            ".reg .b32 t1, t2, t3, u1, u2, u3;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"
+            "setp.ne.b32 P, %7, 0;\n"
+            "setp.eq.b32 T, 0, 0;\n"
+            "add.u32 t1, %4, 2;\n add.u32 t2, %4, 4;\n add.u32 t3, %4, 6;\n"
+            "add.u32 u1, %5, 2;\n add.u32 u2, %5, 4;\n add.u32 u3, %5, 6;\n"
+            "mov.b64 a0, {%4, %10};\n mov.b64 a1, {t1, %10};\n mov.b64 a2, {t2, %10};\n mov.b64 a3, {t3, %10};\n"
+            "mov.b64 b0, {%5, %10};\n mov.b64 b1, {u1, %10};\n mov.b64 b2, {u2, %10};\n mov.b64 b3, {u3, %10};\n"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%3], a0, b0, %6, [%8], [%8], P;\n"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%3], a1, b1, %6, [%8], [%8], T;\n"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%3], a2, b2, %6, [%8], [%8], T;\n"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%3], a3, b3, %6, [%8], [%8], T;\n"
+            "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%9];\n"
+            "selp.u32 %0, 1, 0, Q;\n"
+            "}\n"
+            : "=r"(ready)
+            : "r"(next_full_bar), "r"(next_parity), "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate_first),
+              "r"(sf), "r"(empty_bar), "r"(desc_hi)
+            : "memory");
+    } else {
+        asm volatile(
+            "{\n"
+            ".reg .pred P, Q, T;\n"
+            ".reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n"
+            ".reg .b32 t1, t2, t3, u1, u2, u3;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"
+            "setp.ne.b32 P, %7, 0;\n"
+            "setp.eq.b32 T, 0, 0;\n"
+            "add.u32 t1, %4, 2;\n add.u32 t2, %4, 4;\n add.u32 t3, %4, 6;\n"
+            "add.u32 u1, %5, 2;\n add.u32 u2, %5, 4;\n add.u32 u3, %5, 6;\n"
+            "mov.b64 a0, {%4, %10};\n mov.b64 a1, {t1, %10};\n mov.b64 a2, {t2, %10};\n mov.b64 a3, {t3, %10};\n"
+            "mov.b64 b0, {%5, %10};\n mov.b64 b1, {u1, %10};\n mov.b64 b2, {u2, %10};\n mov.b64 b3, {u3, %10};\n"
+            "tcgen05.mma.cta_group::1.kind::i8 [%3], a0, b0, %6, P;\n"
+            "tcgen05.mma.cta_group::1.kind::i8 [%3], a1, b1, %6, T;\n"
+            "tcgen05.mma.cta_group::1.kind::i8 [%3], a2, b2, %6, T;\n"
+            "tcgen05.mma.cta_group::1.kind::i8 [%3], a3, b3, %6, T;\n"
+            "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%9];\n"
+            "selp.u32 %0, 1, 0, Q;\n"
+            "}\n"
+            : "=r"(ready)
+            : "r"(next_full_bar), "r"(next_parity), "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate_first),
+              "r"(sf), "r"(empty_bar), "r"(desc_hi)
+            : "memory");
+    }
+    return ready;
+}
+
+// The same stage for a CTA pair (issued by the leader CTA): one instruction multiplies the 256 x BN tile of both
+// CTAs; the commit arrives on this stage's empty barrier of BOTH CTAs.
+template <int FORM>
+__device__ __forceinline__ uint32_t umma_stage_pair(uint32_t next_full_bar, uint32_t next_parity, uint32_t d_tmem, uint32_t a_lo,
+                                                    uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t accumulate_first,
+                                                    uint32_t sf, uint32_t empty_bar)
+{
+    uint32_t ready;
+    if (FORM == QNN_FORM_FP4) {
+        asm volatile(
+            "{\n"
+            ".reg .pred P, Q, T;\n"
+            ".reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n"
+            ".reg .b32 t1, t2, t3, u1, u2, u3;\n"
+            ".reg .b16 both;\n"
+            "mov.b16 both, 3;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"
+            "setp.ne.b32 P, %7, 0;\n"
+            "setp.eq.b32 T, 0, 0;\n"
+            "add.u32 t1, %4, 2;\n add.u32 t2, %4, 4;\n add.u32 t3, %4, 6;\n"
+            "add.u32 u1, %5, 2;\n add.u32 u2, %5, 4;\n add.u32 u3, %5, 6;\n"
+            "mov.b64 a0, {%4, %10};\n mov.b64 a1, {t1, %10};\n mov.b64 a2, {t2, %10};\n mov.b64 a3, {t3, %10};\n"
+            "mov.b64 b0, {%5, %10};\n mov.b64 b1, {u1, %10};\n mov.b64 b2, {u2, %10};\n mov.b64 b3, {u3, %10};\n"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%3], a0, b0, %6, [%8], [%8], P;\n"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%3], a1, b1, %6, [%8], [%8], T;\n"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%3], a2, b2, %6, [%8], [%8], T;\n"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%3], a3, b3, %6, [%8], [%8], T;\n"
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%9], both;\n"
+            "selp.u32 %0, 1, 0, Q;\n"
+            "}\n"
+            : "=r"(ready)
+            : "r"(next_full_bar), "r"(next_parity), "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate_first),
+              "r"(sf), "r"(empty_bar), "r"(desc_hi)
+            : "memory");
+    } else {
+        asm volatile(
+            "{\n"
+            ".reg .pred P, Q, T;\n"
+            ".reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n"
+            ".reg .b32 t1, t2, t3, u1, u2, u3;\n"
+            ".reg .b16 both;\n"
+            "mov.b16 both, 3;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"
+            "setp.ne.b32 P, %7, 0;\n"
+            "setp.eq.b32 T, 0, 0;\n"
+            "add.u32 t1, %4, 2;\n add.u32 t2, %4, 4;\n add.u32 t3, %4, 6;\n"
+            "add.u32 u1, %5, 2;\n add.u32 u2, %5, 4;\n add.u32 u3, %5, 6;\n"
+            "mov.b64 a0, {%4, %10};\n mov.b64 a1, {t1, %10};\n mov.b64 a2, {t2, %10};\n mov.b64 a3, {t3, %10};\n"
+            "mov.b64 b0, {%5, %10};\n mov.b64 b1, {u1, %10};\n mov.b64 b2, {u2, %10};\n mov.b64 b3, {u3, %10};\n"
+            "tcgen05.mma.cta_group::2.kind::i8 [%3], a0, b0, %6, P;\n"
+            "tcgen05.mma.cta_group::2.kind::i8 [%3], a1, b1, %6, T;\n"
+            "tcgen05.mma.cta_group::2.kind::i8 [%3], a2, b2, %6, T;\n"
+            "tcgen05.mma.cta_group::2.kind::i8 [%3], a3, b3, %6, T;\n"
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%9], both;\n"
+            "selp.u32 %0, 1, 0, Q;\n"
+            "}\n"
+            : "=r"(ready)
+            : "r"(next_full_bar), "r"(next_parity), "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate_first),
+              "r"(sf), "r"(empty_bar), "r"(desc_hi)
+            : "memory");
+    }
+    return ready;
+}
+// accumulator-complete signal to both CTAs of a pair
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+{
+    asm volatile(
+        "{\n.reg .b16 both;\nmov.b16 both, 3;\n"
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], both;\n}\n"
+        ::"r"(bar) : "memory");
+}
+
+// TMA stage of one CTA of a pair: the loads land in this CTA's shared memory and report their bytes to the
+// LEADER's full barrier (`leader_full_bar`, a shared::cluster address); only the leader announces the bytes
+// (those of both CTAs).  No load is multicast.
+__device__ __forceinline__ uint32_t tma_stage_2d_pair(uint32_t next_empty_bar, uint32_t next_parity, uint32_t leader_full_bar,
+                                                      uint32_t tx_bytes_both, uint32_t is_leader, uint32_t dst_a,
+                                                      const CUtensorMap *map_a, int32_t ax, int32_t ay, uint32_t dst_b,
+                                                      const CUtensorMap *map_b, int32_t bx, int32_t by)
+{
+    uint32_t ready;
+    asm volatile(
+        "{\n"
+        ".reg .pred Q, L;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"
+        "setp.ne.b32 L, %13, 0;\n"
+        "@L mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%3], %4;\n"
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%5], [%6, {%7, %8}], [%3];\n"
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%9], [%10, {%11, %12}], [%3];\n"
+        "selp.u32 %0, 1, 0, Q;\n"
+        "}\n"
+        : "=r"(ready)
+        : "r"(next_empty_bar), "r"(next_parity), "r"(leader_full_bar), "r"(tx_bytes_both), "r"(dst_a), "l"(map_a), "r"(ax),
+          "r"(ay), "r"(dst_b), "l"(map_b), "r"(bx), "r"(by), "r"(is_leader)
+        : "memory");
+    return ready;
+}
+
+// One pipeline stage of the TMA warp the same way: poll the NEXT stage's empty barrier first, announce this
+// stage's bytes, issue its two loads, then read the poll's result.
+__device__ __forceinline__ uint32_t tma_stage_2d(uint32_t next_empty_bar, uint32_t next_parity, uint32_t full_bar, uint32_t tx_bytes,
+                                                 uint32_t dst_a, const CUtensorMap *map_a, int32_t ax, int32_t ay,
+                                                 uint32_t dst_b, const CUtensorMap *map_b, int32_t bx, int32_t by)
+{
+    uint32_t ready;
+    asm volatile(
+        "{\n"
+        ".reg .pred Q;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"
+        "mbarrier.arrive.expect_tx.shared::cta.b64 _, [%3], %4;\n"
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%5], [%6, {%7, %8}], [%3];\n"
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%9], [%10, {%11, %12}], [%3];\n"
+        "selp.u32 %0, 1, 0, Q;\n"
+        "}\n"
+        : "=r"(ready)
+        : "r"(next_empty_bar), "r"(next_parity), "r"(full_bar), "r"(tx_bytes), "r"(dst_a), "l"(map_a), "r"(ax), "r"(ay),
+          "r"(dst_b), "l"(map_b), "r"(bx), "r"(by)
+        : "memory");
+    return ready;
+}
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
