@@ -155,7 +155,10 @@ def _p(t: Optional[torch.Tensor]):
 
 
 def _stream():
-    # without a CUDA device only host-side validation can succeed; any launch then returns QNN_ERR_CUDA
+    # the current stream's handle without building a Stream object (this sits on every call's path); before CUDA is
+    # initialised only host-side validation can succeed, and any launch then returns QNN_ERR_CUDA
+    if torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
 
 

@@ -1357,14 +1357,16 @@ extern "C" int qnn_device_status(void *stream)
 {
     using namespace qnn;
     QNN_CUDA(cudaStreamSynchronize(as_stream(stream)));
-    int code = 0, code_fc = 0, code_sm = 0, code_i8s = 0;
+    int code = 0, code_fc = 0, code_sm = 0, code_i8s = 0, code_sc = 0;
     QNN_CUDA(status_read_clear(&code));
     if (int rc = fc_f32_status(&code_fc)) return rc;
     if (int rc = smallm_status(&code_sm)) return rc;
     if (int rc = gemm_i8s_status(&code_i8s)) return rc;
+    if (int rc = scores_status(&code_sc)) return rc;
     if (code == 0) code = code_fc;
     if (code == 0) code = code_sm;
     if (code == 0) code = code_i8s;
+    if (code == 0) code = code_sc;
     if (code != 0) return fail(QNN_ERR_TIMEOUT, "a bounded device-side wait ran out (wait site %d)", code);
     return QNN_OK;
 }

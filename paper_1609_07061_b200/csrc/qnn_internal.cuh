@@ -119,6 +119,7 @@ int smallm_status(int *code);
 // status word of the real-valued-weights layer kernel's bounded waits (its own translation unit): reads and clears it
 int fc_f32_status(int *code);
 int gemm_i8s_status(int *code);
+int scores_status(int *code);
 
 #ifdef __CUDACC__
 // Programmatic dependent launch.  A kernel launched through launch_pdl may be scheduled while the kernel before it in the

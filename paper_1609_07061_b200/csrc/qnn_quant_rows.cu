@@ -83,54 +83,19 @@ __device__ __forceinline__ void store_codes(uint8_t *dst, const float (&f)[W], u
     }
 }
 
-template <typename V, int W>
-__device__ __forceinline__ void store_row_piece(void *base, int64_t row_off, int32_t k0, int32_t K, const float (&f)[W])
-{
-    V *dst = static_cast<V *>(base) + row_off + k0;
-    if (W == 1 || k0 + W <= K) {
-        store_floats<V, W>(dst, f);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (k0 + i < K) from_float(f[i], dst[i]);
-    }
-}
 template <int W>
 __device__ __forceinline__ void store_values(const RowArgs &p, int64_t row, int32_t k0, const float (&f)[W])
 {
-    const int64_t off = row * p.ld_values;
-    if (p.values_type == QNN_TYPE_F32) store_row_piece<float, W>(p.values, off, k0, p.K, f);
-    else if (p.values_type == QNN_TYPE_BF16) store_row_piece<__nv_bfloat16, W>(p.values, off, k0, p.K, f);
-    else store_row_piece<__half, W>(p.values, off, k0, p.K, f);
-}
-
-// a piece of a row in memory order; elements past K are zero (no load is issued for them)
-template <typename T, int W>
-__device__ __forceinline__ void load_row_piece(const T *row, int32_t k0, int32_t K, Piece<T, W> &v)
-{
-    if (W == 1 || k0 + W <= K) {
-        load_piece<T, W>(row + k0, v);
-    } else {
-        alignas(16) T t[W];
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            t[i] = T(0.0f);
-            if (k0 + i < K) t[i] = row[k0 + i];
-        }
-        if constexpr (W == 8) {
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) * 2; ++i) v.w[i] = reinterpret_cast<const uint32_t *>(t)[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i) v.e[i] = t[i];
-        }
-    }
+    const int64_t at = row * p.ld_values + k0;
+    if (p.values_type == QNN_TYPE_BF16) store_floats<__nv_bfloat16, W>(static_cast<__nv_bfloat16 *>(p.values) + at, f);
+    else if (p.values_type == QNN_TYPE_F16) store_floats<__half, W>(static_cast<__half *>(p.values) + at, f);
+    else store_floats<float, W>(static_cast<float *>(p.values) + at, f);
 }
 
 // t of one piece; adds to the sum of squares, and gives the sum s of the norm in `s`
 template <int OP, typename T, int W>
 __device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, const Piece<T, W> &bv, int32_t k0, float (&s)[W], float (&t)[W],
-                                       float &ss)
+                                       f32x2 &ss)
 {
     float x[W], b[W];
     piece_to_floats<T, W>(xv, x);
@@ -142,21 +107,58 @@ __device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, 
 #pragma unroll
         for (int i = 0; i < W; ++i) t[i] = silu(x[i]) * b[i];
     } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            s[i] = p.b != nullptr ? x[i] + b[i] : x[i];
-            ss = fmaf(s[i], s[i], ss);
-            t[i] = s[i];
-        }
-        if (p.gamma != nullptr && k0 < p.K) {
+        float g[W];
+        if (p.gamma != nullptr) {
             Piece<T, W> gv;
-            float g[W];
-            load_row_piece<T, W>(static_cast<const T *>(p.gamma), k0, p.K, gv);
+            load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv);
             piece_to_floats<T, W>(gv, g);
+        } else {
 #pragma unroll
-            for (int i = 0; i < W; ++i) t[i] *= g[i];
+            for (int i = 0; i < W; ++i) g[i] = 1.0f;
+        }
+        if constexpr (W == 1) {
+            s[0] = p.b != nullptr ? x[0] + b[0] : x[0];
+            ss = fma2(pair(s[0], 0.0f), pair(s[0], 0.0f), ss);
+            t[0] = s[0] * g[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 2) {
+                f32x2 s2 = pair(x[i], x[i + 1]);
+                if (p.b != nullptr) s2 = add2(s2, pair(b[i], b[i + 1]));
+                unpair(s2, s[i], s[i + 1]);
+                ss = fma2(s2, s2, ss);
+                unpair(mul2(s2, pair(g[i], g[i + 1])), t[i], t[i + 1]);
+            }
         }
     }
+}
+// MAGIC + code of W elements, and the values the codes stand for
+template <int W>
+__device__ __forceinline__ void to_codes(const float (&t)[W], float inv, float (&f)[W])
+{
+    if constexpr (W == 1) {
+        f[0] = fmaf(t[0], inv, MAGIC);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; i += 2) unpair(fma2(pair(t[i], t[i + 1]), pair(inv, inv), pair(MAGIC, MAGIC)), f[i], f[i + 1]);
+    }
+}
+template <int W>
+__device__ __forceinline__ void to_values(float (&f)[W], float scale)
+{
+    if constexpr (W == 1) {
+        f[0] = (f[0] - MAGIC) * scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; i += 2)
+            unpair(mul2(add2(pair(f[i], f[i + 1]), pair(-MAGIC, -MAGIC)), pair(scale, scale)), f[i], f[i + 1]);
+    }
+}
+__device__ __forceinline__ float pair_sum(f32x2 v)
+{
+    float a, b;
+    unpair(v, a, b);
+    return a + b;
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -167,7 +169,9 @@ __device__ __forceinline__ float warp_sum(float v)
 }
 
 // A row of at most 8 * NV * tpr elements in registers: tpr threads own pieces of W elements, interleaved, so that a
-// warp's accesses are contiguous.  W = 8 needs 16-byte aligned rows, W = 2 aligned pairs, W = 1 nothing.
+// warp's accesses are contiguous.  W divides K; W = 8 needs 16-byte aligned rows, W = 2 aligned pairs, W = 1 nothing.
+// (A kernel that also took rows ending inside a piece spent 41 instructions an element instead of 16 on the 8192 x 4096
+// norm: the element-wise ends of every load and store are predicated, not branched around.)
 template <int OP, typename T, int W, int NV>
 __global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
 {
@@ -189,26 +193,28 @@ __global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
     const int32_t K = live ? p.K : 0;
 
     float t[P][W];
-    float ss = 0.0f;
-    uint32_t top = 0u;
+    f32x2 ss2 = 0ull;
+    float topf = 0.0f;
 #pragma unroll
     for (int c = 0; c < P; c += CH) {
         Piece<T, W> xv[CH], bv[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int32_t k0 = ((c + j) * tpr + t0) * W;
-            if (k0 < K) load_row_piece<T, W>(xr, k0, K, xv[j]);
-            if (with_b && k0 < K) load_row_piece<T, W>(br, k0, K, bv[j]);
+            if (k0 < K) {
+                load_piece<T, W>(xr + k0, xv[j]);
+                if (with_b) load_piece<T, W>(br + k0, bv[j]);
+            }
         }
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int32_t k0 = ((c + j) * tpr + t0) * W;
             if (k0 < K) {
                 float s[W];
-                row_op<OP, T, W>(p, xv[j], bv[j], k0, s, t[c + j], ss);
-                if (OP == ROW_NORM && p.sum != nullptr) store_row_piece<T, W>(p.sum, row * p.ld_sum, k0, K, s);
+                row_op<OP, T, W>(p, xv[j], bv[j], k0, s, t[c + j], ss2);
+                if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
 #pragma unroll
-                for (int i = 0; i < W; ++i) top = max(top, __float_as_uint(t[c + j][i]) & 0x7fffffffu);
+                for (int i = 0; i < W; ++i) topf = max_nan(topf, fabsf(t[c + j][i]));
             } else {
 #pragma unroll
                 for (int i = 0; i < W; ++i) t[c + j][i] = 0.0f;
@@ -216,8 +222,9 @@ __global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
         }
     }
 
-    if (OP == ROW_NORM) ss = warp_sum(ss);
-    top = __reduce_max_sync(0xffffffffu, top);
+    float ss = 0.0f;
+    if (OP == ROW_NORM) ss = warp_sum(pair_sum(ss2));
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(topf) & 0x7fffffffu);
     if (tpr > 32) {
         const int warp = threadIdx.x >> 5;
         if ((threadIdx.x & 31) == 0) { sh_ss[warp] = ss; sh_top[warp] = top; }
@@ -235,12 +242,10 @@ __global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
         const int32_t k0 = (c * tpr + t0) * W;
         if (k0 < p.KP) {
             float f[W];
-#pragma unroll
-            for (int i = 0; i < W; ++i) f[i] = fmaf(t[c][i], r.inv, MAGIC);
+            to_codes<W>(t[c], r.inv, f);
             store_codes<W>(cr + k0, f, r.keep);
             if (p.values != nullptr && k0 < K) {
-#pragma unroll
-                for (int i = 0; i < W; ++i) f[i] = (f[i] - MAGIC) * r.scale;
+                to_values<W>(f, r.scale);
                 store_values<W>(p, row, k0, f);
             }
         }
@@ -261,19 +266,20 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     const T *br = static_cast<const T *>(p.b) + row * p.ldb;
     const bool with_b = OP == ROW_GATE || (OP == ROW_NORM && p.b != nullptr);
     const int64_t step = (int64_t)blockDim.x * W;
-    float ss = 0.0f;
-    uint32_t top = 0u;
+    f32x2 ss2 = 0ull;
+    float topf = 0.0f;
     for (int64_t k0 = (int64_t)threadIdx.x * W; k0 < p.K; k0 += step) {
         Piece<T, W> xv, bv;
         float s[W], t[W];
-        load_row_piece<T, W>(xr, (int32_t)k0, p.K, xv);
-        if (with_b) load_row_piece<T, W>(br, (int32_t)k0, p.K, bv);
-        row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, ss);
+        load_piece<T, W>(xr + k0, xv);
+        if (with_b) load_piece<T, W>(br + k0, bv);
+        row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, ss2);
 #pragma unroll
-        for (int i = 0; i < W; ++i) top = max(top, __float_as_uint(t[i]) & 0x7fffffffu);
+        for (int i = 0; i < W; ++i) topf = max_nan(topf, fabsf(t[i]));
     }
-    if (OP == ROW_NORM) ss = warp_sum(ss);
-    top = __reduce_max_sync(0xffffffffu, top);
+    float ss = 0.0f;
+    if (OP == ROW_NORM) ss = warp_sum(pair_sum(ss2));
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(topf) & 0x7fffffffu);
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) { sh_ss[warp] = ss; sh_top[warp] = top; }
     __syncthreads();
@@ -283,22 +289,21 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     if (threadIdx.x == 0) p.scale[row] = r.scale;
     uint8_t *cr = p.codes + row * p.ldq;
     for (int64_t k0 = (int64_t)threadIdx.x * W; k0 < p.KP; k0 += step) {
-        float s[W], t[W], f[W], unused = 0.0f;
+        float s[W], t[W], f[W];
+        f32x2 unused = 0ull;
 #pragma unroll
         for (int i = 0; i < W; ++i) t[i] = 0.0f;
         if (k0 < p.K) {
             Piece<T, W> xv, bv;
-            load_row_piece<T, W>(xr, (int32_t)k0, p.K, xv);
-            if (with_b) load_row_piece<T, W>(br, (int32_t)k0, p.K, bv);
+            load_piece<T, W>(xr + k0, xv);
+            if (with_b) load_piece<T, W>(br + k0, bv);
             row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, unused);
-            if (OP == ROW_NORM && p.sum != nullptr) store_row_piece<T, W>(p.sum, row * p.ld_sum, (int32_t)k0, p.K, s);
+            if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
         }
-#pragma unroll
-        for (int i = 0; i < W; ++i) f[i] = fmaf(t[i], r.inv, MAGIC);
+        to_codes<W>(t, r.inv, f);
         store_codes<W>(cr + k0, f, r.keep);
         if (p.values != nullptr && k0 < p.K) {
-#pragma unroll
-            for (int i = 0; i < W; ++i) f[i] = (f[i] - MAGIC) * r.scale;
+            to_values<W>(f, r.scale);
             store_values<W>(p, row, (int32_t)k0, f);
         }
     }
@@ -335,8 +340,9 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st)
 template <int OP, typename T>
 int launch_rows_w(const RowArgs &p, const char *what, cudaStream_t st)
 {
-    // widest access every row of every real tensor allows
+    // widest access that every row of every real tensor allows and that the row length is a multiple of
     auto fits = [&](size_t elems) {
+        if (p.K % (int)elems != 0) return false;
         auto ok = [&](const void *q, int64_t ld, size_t es) { return q == nullptr || (aligned(q, elems * es < 16 ? elems * es : 16) && (size_t)ld % (elems * es < 16 ? elems : 16 / es) == 0); };
         const size_t vs = p.values_type == QNN_TYPE_F32 ? 4 : 2;
         return ok(p.x, p.ldx, sizeof(T)) && ok(p.b, p.ldb, sizeof(T)) && ok(p.gamma, 0, sizeof(T)) && ok(p.sum, p.ld_sum, sizeof(T)) &&

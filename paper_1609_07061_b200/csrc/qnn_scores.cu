@@ -13,13 +13,16 @@
 // 64-bit keys (value, ~index), which makes the result independent of the order in which candidates are found.
 //
 // Backward: dz = g_lp ([v = id] - p) - g_H p (log p + H), element by element from lse and the entropy.
+#include <type_traits>
+#include <atomic>
 #include "qnn_types.cuh"
+#include "qnn_tc_ptx.cuh"
 
 namespace qnn {
 namespace {
 
 constexpr int MAX_TOP = 32;
-constexpr int CAND = 1024;            // candidates a CTA can hold; more (masses of equal logits) take the slow exact path
+constexpr int CAND = 512;             // candidates a CTA can hold; more (masses of equal logits) take the slow exact path
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float FAR = -1000.0f;       // e^-1000 is 0 in fp32
 constexpr uint32_t INF_BITS = 0x7f800000u;
@@ -30,12 +33,6 @@ __device__ __forceinline__ float exp2_approx(float x)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 // order-preserving map of floats to unsigned: -inf < ... < +inf < NaN, and -0 = +0
@@ -65,17 +62,18 @@ struct Granules {
     }
     __device__ __forceinline__ int64_t count() const { return ((int64_t)V + shift + E - 1) / E; }
     __device__ __forceinline__ int64_t first(int64_t g) const { return g * E - shift; }
-    // raw words of granule g; elements outside the row read as -inf and are not touched
+    // granules first_full() .. end_full() - 1 lie wholly inside the row
+    __device__ __forceinline__ int64_t first_full() const { return shift > 0; }
+    __device__ __forceinline__ int64_t end_full() const { return ((int64_t)V + shift) / E; }
+    __device__ __forceinline__ const uint4 *at(int64_t g) const { return reinterpret_cast<const uint4 *>(row + first(g)); }
+    // any granule: elements outside the row read as -inf and are not touched
     __device__ __forceinline__ uint4 load(int64_t g) const
     {
+        if (g >= first_full() && g < end_full()) return *at(g);
         const int64_t v0 = first(g);
-        if (v0 >= 0 && v0 + E <= V) return *reinterpret_cast<const uint4 *>(row + v0);
         alignas(16) T t[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            t[i] = T(neg_inf());
-            if (v0 + i >= 0 && v0 + i < V) t[i] = row[v0 + i];
-        }
+#pragma unroll 1
+        for (int i = 0; i < E; ++i) t[i] = (v0 + i >= 0 && v0 + i < V) ? row[v0 + i] : T(neg_inf());
         return *reinterpret_cast<const uint4 *>(t);
     }
     static __device__ __forceinline__ void floats(const uint4 &w, float (&f)[E])
@@ -113,9 +111,134 @@ __device__ __forceinline__ Stats join(Stats a, Stats b)
     return a;
 }
 
+// Below this magnitude of the reference (the running maximum, or lse) the element loops clamp the LOGITS at -2^60 (f16: at
+// its lowest value) instead of the differences: on packed 16-bit pairs that is half an instruction an element, e^ of such an
+// element is 0 all the same, and its difference stays finite.  References beyond it take the plain loops.
+// (f16 has no room below its lowest value: the reference must be well above it for e^ of a clamped element to be 0.)
+template <typename T>
+__device__ __forceinline__ bool calm_at(float ref)
+{
+    if (std::is_same<T, __half>::value) return ref > -64000.0f && ref < 1e15f;
+    return fabsf(ref) < 1e15f;
+}
+
+// largest of the 16-bit pairs of two words (a NaN stays), and the clamp
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b, __nv_bfloat16)
+{
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b, __half)
+{
+    const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b, float) { return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b))); }
+__device__ __forceinline__ float top_of(uint32_t w, float) { return __uint_as_float(w); }
+template <typename T>
+__device__ __forceinline__ float top_of(uint32_t w, T)
+{
+    float lo, hi;
+    unpack2(w, lo, hi, T());
+    return max_nan(lo, hi);
+}
+// the elements of a granule as pairs, clamped
+__device__ __forceinline__ void calm_pairs(const uint4 &w, f32x2 (&z)[4], __nv_bfloat16)
+{
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    const uint32_t low = 0xDD80DD80u;            // -2^60 twice
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 c = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&x[i]), *reinterpret_cast<const __nv_bfloat162 *>(&low));
+        float lo, hi;
+        unpack2(*reinterpret_cast<const uint32_t *>(&c), lo, hi, __nv_bfloat16());
+        z[i] = pair(lo, hi);
+    }
+}
+__device__ __forceinline__ void calm_pairs(const uint4 &w, f32x2 (&z)[4], __half)
+{
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    const uint32_t low = 0xFBFFFBFFu;            // -65504 twice
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 c = __hmax2(*reinterpret_cast<const __half2 *>(&x[i]), *reinterpret_cast<const __half2 *>(&low));
+        const float2 f = __half22float2(c);
+        z[i] = pair(f.x, f.y);
+    }
+}
+__device__ __forceinline__ void calm_pairs(const uint4 &w, f32x2 (&z)[2], float)
+{
+    const float low = -1.152921504606846976e18f;  // -2^60
+    z[0] = pair(fmaxf(__uint_as_float(w.x), low), fmaxf(__uint_as_float(w.y), low));
+    z[1] = pair(fmaxf(__uint_as_float(w.z), low), fmaxf(__uint_as_float(w.w), low));
+}
+
+// Running statistics of one thread: m, and s and u as two partial sums each.
+struct Running {
+    float m;
+    f32x2 s, u;
+    __device__ __forceinline__ Stats stats() const
+    {
+        float a, b, c, d;
+        unpair(s, a, b);
+        unpair(u, c, d);
+        return {m, a + b, c + d};
+    }
+};
+// adds N granules (words of elements outside the row are -inf); returns their largest element
+template <typename T, int N>
+__device__ __forceinline__ float add_granules(Running &a, const uint4 (&w)[N])
+{
+    constexpr int E = Granules<T>::E;
+    uint32_t top = max_words(max_words(w[0].x, w[0].y, T()), max_words(w[0].z, w[0].w, T()), T());
+#pragma unroll
+    for (int j = 1; j < N; ++j) top = max_words(top, max_words(max_words(w[j].x, w[j].y, T()), max_words(w[j].z, w[j].w, T()), T()), T());
+    const float b = top_of(top, T());
+    if (!(b <= a.m)) {
+        const float to = max_nan(a.m, b);
+        const float d = fmaxf(a.m - to, FAR);
+        const float c = exp2_approx(d * LOG2E);
+        a.u = mul2(fma2(a.s, pair(d, d), a.u), pair(c, c));
+        a.s = mul2(a.s, pair(c, c));
+        a.m = to;
+    }
+    if (calm_at<T>(a.m)) {
+        const f32x2 nm = pair(-a.m, -a.m), l2e = pair(LOG2E, LOG2E);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            f32x2 z[E / 2];
+            calm_pairs(w[j], z, T());
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                const f32x2 x = add2(z[i], nm);
+                float lo, hi;
+                unpair(mul2(x, l2e), lo, hi);
+                const f32x2 e = pair(exp2_approx(lo), exp2_approx(hi));
+                a.s = add2(a.s, e);
+                a.u = fma2(e, x, a.u);
+            }
+        }
+    } else if (a.m != neg_inf()) {
+        // (unrolled: a loop over w[j] would put the granules of EVERY call into local memory)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float f[E];
+            Granules<T>::floats(w[j], f);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float x = fmaxf(f[i] - a.m, FAR);
+                const f32x2 e = pair(exp2_approx(x * LOG2E), 0.0f);
+                a.s = add2(a.s, e);
+                a.u = fma2(e, pair(x, 0.0f), a.u);
+            }
+        }
+    }
+    return b;
+}
+
 struct ScoreArgs {
     const void *logits;
-    int64_t ldl;
+    int64_t T, ldl;
     int32_t V;
     const int64_t *ids;
     float *logprob, *entropy, *lse;
@@ -124,15 +247,8 @@ struct ScoreArgs {
     int64_t *top_ids;
 };
 
-__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_barrier() { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t peer_addr(const void *p, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    return r;
-}
+__device__ __forceinline__ uint32_t peer_addr(const void *p, uint32_t rank) { return map_to_cta(smem_u32(p), rank); }
 __device__ __forceinline__ float peer_f32(uint32_t a)
 {
     float v;
@@ -146,207 +262,321 @@ __device__ __forceinline__ unsigned long long peer_u64(uint32_t a)
     return v;
 }
 
-template <int THREADS>
+// THREADS threads add, one more warp loads.  Rows stream through a ring of STAGES chunks of THREADS * U granules in shared
+// memory, filled by bulk copies, so that what is in flight does not depend on how far the adding threads are.
+template <int THREADS, int U, int STAGES>
 struct ScoreShared {
-    Stats part[THREADS / 32];
+    static constexpr int CHUNK = THREADS * U;       // granules
+    static constexpr int GL = THREADS / 32;         // lanes a group: 32 groups of threads
+    static_assert(GL >= 4 && GL <= 32 && MAX_TOP <= 32, "groups");
+    uint4 ring[STAGES][CHUNK];
+    unsigned long long full[STAGES], empty[STAGES]; // barriers
+    int abort_flag;
+    int n_cand, n_one, n_all;
     Stats mine;                                     // this CTA's statistics, read by the cluster's first CTA
+    alignas(16) uint32_t group[32];                 // largest element of each group of threads, as order keys
+    float2 part[THREADS / 32];                      // s and u of each warp
+    uint32_t one[THREADS];                          // threads that hold candidates in one chunk: chunk * THREADS + thread
+    uint32_t all[THREADS];                          // ... perhaps in several
     unsigned long long best[MAX_TOP];               // this CTA's largest keys, falling; 0 = none
     unsigned long long cand[CAND];
-    uint32_t group[64];
-    int flagged[THREADS];
-    int n_flagged, n_cand;
-    uint32_t bound;
     unsigned long long round_best[THREADS / 32];
 };
 
-// The topk largest keys of `n` candidates into out[0..topk), falling; keys are distinct, so every rank is taken once.
-template <int THREADS>
-__device__ __forceinline__ void rank_candidates(const unsigned long long *cand, int n, int topk, unsigned long long *out)
+// The topk largest keys of `n` candidates, each handed with its rank to put(rank, key); keys are distinct (0 = none), so
+// every rank is taken once.
+template <int THREADS, class Put>
+__device__ __forceinline__ void rank_candidates(const unsigned long long *cand, int n, int topk, Put put)
 {
     for (int c = threadIdx.x; c < n; c += THREADS) {
         const unsigned long long k = cand[c];
         if (k == 0ull) continue;
         int rank = 0;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) rank += cand[j] > k;
-        if (rank < topk) out[rank] = k;
+        if (rank < topk) put(rank, k);
     }
 }
 
-template <typename T, int THREADS, int U>
-__global__ void __launch_bounds__(THREADS) scores_kernel(const ScoreArgs p)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n"
+                 "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%2], [%3], %1, [%0];"
+                 ::"r"(bar), "r"(bytes), "r"(dst), "l"(src) : "memory");
+}
+template <int THREADS>
+__device__ __forceinline__ void adders_sync() { asm volatile("barrier.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+
+// One CTA (or one cluster of them) a row, RESIDENT CTAs an SM: while one joins its statistics and finds its alternatives, the
+// others stream.  (CTAs that walk several rows and load ahead across them were slower, 97 against 90 us on 2048 x 131072
+// without alternatives: SMs differ in how fast they stream, and the hardware hands out rows as they finish.)
+template <typename T, int THREADS, int U, int STAGES, int RESIDENT>
+__global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const ScoreArgs p)
 {
     using G = Granules<T>;
+    using SH = ScoreShared<THREADS, U, STAGES>;
     constexpr int E = G::E;
-    __shared__ ScoreShared<THREADS> sh;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    SH &sh = *reinterpret_cast<SH *>(smem_raw);
+    volatile int *abort_flag = &sh.abort_flag;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), THREADS / 32); }
+        *abort_flag = 0;
+        sh.n_cand = 0; sh.n_one = 0; sh.n_all = 0;
+        fence_async_shared();
+    }
+    __syncthreads();
     griddep_launch_dependents();
     griddep_wait();
-    const uint32_t csize = cluster_size(), crank = cluster_rank();
+    const uint32_t csize = cluster_size(), crank = csize > 1 ? cluster_ctarank() : 0u;
     const int64_t t = blockIdx.x / csize;
-    const G row(static_cast<const T *>(p.logits) + t * p.ldl, p.V);
-    // this CTA's granules
-    const int64_t all = row.count(), per = (all + csize - 1) / csize;
-    const int64_t g0 = per * crank < all ? per * crank : all;
-    const int64_t g1 = g0 + per < all ? g0 + per : all;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const G row(static_cast<const T *>(p.logits) + t * p.ldl, p.V);
+    // this CTA's whole granules of the row
+    int64_t g0, g1;
+    {
+        const int64_t f0 = row.first_full(), n = row.end_full() - f0, share = (n + csize - 1) / csize;
+        g0 = f0 + (share * crank < n ? share * crank : n);
+        g1 = f0 + (share * (crank + 1) < n ? share * (crank + 1) : n);
+    }
+    int stage = 0;
+    uint32_t phase = 0;
 
-    Stats a = {neg_inf(), 0.0f, 0.0f};
-    for (int64_t g = g0 + tid; g < g1; g += (int64_t)THREADS * U) {
-        uint4 w[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-            if (g + (int64_t)j * THREADS < g1) w[j] = row.load(g + (int64_t)j * THREADS);
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            if (g + (int64_t)j * THREADS >= g1) break;
-            float f[E];
-            G::floats(w[j], f);
-            float b = f[0];
-#pragma unroll
-            for (int i = 1; i < E; ++i) b = max_nan(b, f[i]);
-            if (!(b <= a.m)) rescale(a, max_nan(a.m, b));
-            if (a.m == neg_inf()) continue;
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float x = fmaxf(f[i] - a.m, FAR);
-                const float e = exp2_approx(x * LOG2E);
-                a.s += e;
-                a.u = fmaf(e, x, a.u);
+    if (warp == THREADS / 32) {
+        if (lane == 0) {
+            for (int64_t g = g0; g < g1; g += SH::CHUNK) {
+                if (!mbar_wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag, 21)) break;
+                const int64_t n = g1 - g < SH::CHUNK ? g1 - g : SH::CHUNK;
+                bulk_load(smem_u32(sh.ring[stage]), row.at(g), (uint32_t)(n * 16), smem_u32(&sh.full[stage]));
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
+            if (*abort_flag)
+                for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies in flight land before shared memory is released
         }
+        __syncwarp();
+        if (csize > 1) {                                 // the barriers of a cluster count every warp
+            cluster_sync_all();
+            cluster_sync_all();
+        }
+        return;
     }
-    const float mine = a.m;                          // the largest of this thread's elements
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Stats b;
-        b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-        b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-        b.u = __shfl_xor_sync(0xffffffffu, a.u, o);
-        // (lower lane first on both sides, so that all lanes hold the same bits)
-        a = (lane & o) ? join(b, a) : join(a, b);
-    }
-    if (lane == 0) sh.part[warp] = a;
 
     const int topk = p.topk;
-    if (topk > 0) {
-        constexpr int GL = THREADS >= 512 ? 8 : 4;   // lanes a group: THREADS / GL groups, at least MAX_TOP of them
-        constexpr int NG = THREADS / GL;
-        static_assert(NG >= MAX_TOP && NG <= 64, "groups");
-        float gm = mine;
+    // the token's logit is on its way while the row streams
+    int64_t id = -1;
+    float token = 0.0f;
+    if (tid == 0 && crank == 0 && p.logprob != nullptr) {
+        id = p.ids[t];
+        if (id >= 0 && id < p.V) token = to_float(row.row[id]);
+    }
+    Running run = {neg_inf(), 0ull, 0ull};
+    float second = neg_inf();                        // the largest element outside this thread's best chunk
+    uint32_t best_chunk = 0, chunk = 0;
+    for (int64_t g = g0; g < g1; g += SH::CHUNK, ++chunk) {
+        // (a wait that runs out raises the status word; the row is then finished on what the ring holds)
+        (void)mbar_wait(smem_u32(&sh.full[stage]), phase, abort_flag, 22);
+        const int n = g1 - g < SH::CHUNK ? (int)(g1 - g) : SH::CHUNK;
+        uint4 w[U];
+        if (n == SH::CHUNK) {
 #pragma unroll
-        for (int o = GL / 2; o > 0; o >>= 1) gm = max_nan(gm, __shfl_xor_sync(0xffffffffu, gm, o));
-        if ((lane & (GL - 1)) == 0) sh.group[tid / GL] = order_key(gm);
-        if (tid == 0) { sh.n_flagged = 0; sh.n_cand = 0; }
-        if (tid < MAX_TOP) sh.best[tid] = 0ull;
-        __syncthreads();
-        if (tid < NG) {                              // the group maximum of rank topk - 1 (ties by group number)
-            const uint32_t k = sh.group[tid];
-            int rank = 0;
-#pragma unroll 8
-            for (int j = 0; j < NG; ++j) rank += (sh.group[j] > k) || (sh.group[j] == k && j < tid);
-            if (rank == topk - 1) sh.bound = k;
-        }
-        __syncthreads();
-        const uint32_t bound = sh.bound;
-        if (g0 + tid < g1 && order_key(mine) >= bound) sh.flagged[atomicAdd(&sh.n_flagged, 1)] = tid;
-        __syncthreads();
-        const int nf = sh.n_flagged;
-        for (int f = warp; f < nf; f += THREADS / 32) {
-            for (int64_t g = g0 + sh.flagged[f] + (int64_t)lane * THREADS; g < g1; g += (int64_t)32 * THREADS) {
-                float z[E];
-                G::floats(row.load(g), z);
-                const int64_t v0 = row.first(g);
+            for (int j = 0; j < U; ++j) w[j] = sh.ring[stage][j * THREADS + tid];
+        } else {
+            constexpr uint32_t fill = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;   // -inf
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const int64_t v = v0 + i;
-                    const uint32_t k = order_key(z[i]);
-                    if (k >= bound && v >= 0 && v < p.V) {
-                        const int at = atomicAdd(&sh.n_cand, 1);
-                        if (at < CAND) sh.cand[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)v;
-                    }
-                }
+            for (int j = 0; j < U; ++j) {
+                w[j] = make_uint4(fill, fill, fill, fill);
+                if (j * THREADS + tid < n) w[j] = sh.ring[stage][j * THREADS + tid];
             }
         }
-        __syncthreads();
-        if (sh.n_cand <= CAND) {
-            rank_candidates<THREADS>(sh.cand, sh.n_cand, topk, sh.best);
-        } else {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        const float before = run.m;
+        float b = neg_inf();
+        if (n > THREADS) {
+            b = add_granules<T, U>(run, w);
+        } else if (tid < n) {
+            const uint4 only[1] = {w[0]};
+            b = add_granules<T, 1>(run, only);
+        }
+        second = fmaxf(second, fminf(before, b));
+        if (b > before) best_chunk = chunk;
+    }
+    // Granules that the row only shares with its neighbours: the head is thread 0's, the tail thread 1's, of the first
+    // CTA.  (A row inside one granule is a head.)
+    const bool head = row.first_full() > 0, tail = row.end_full() < row.count() && row.count() > row.first_full();
+    const bool has_edge = crank == 0 && ((tid == 0 && head) || (tid == 1 && tail));
+    const int64_t edge = tid == 0 ? 0 : row.count() - 1;
+    if (has_edge) {
+        const uint4 only[1] = {row.load(edge)};
+        (void)add_granules<T, 1>(run, only);
+    }
+    const float mine = run.m;                        // the largest of this thread's elements
+    // the row's (or part's) maximum, through the groups' maxima
+    float gm = mine;
+#pragma unroll
+    for (int o = SH::GL / 2; o > 0; o >>= 1) gm = max_nan(gm, __shfl_xor_sync(0xffffffffu, gm, o));
+    if ((lane & (SH::GL - 1)) == 0) sh.group[tid / SH::GL] = order_key(gm);
+    adders_sync<THREADS>();
+    const uint32_t gkey = sh.group[lane];
+    Stats a = run.stats();
+    {
+        const float m = order_value(__reduce_max_sync(0xffffffffu, gkey));
+        if (m != neg_inf()) rescale(a, m);           // (all -inf: s and u are 0)
+        else a.m = m;
+    }
+    // s and u of the block: every thread has scaled its own to the common maximum, plain sums are left
+    float s = a.s, u = a.u;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        u += __shfl_xor_sync(0xffffffffu, u, o);
+    }
+    if (lane == 0) sh.part[warp] = make_float2(s, u);
+    uint32_t bound = 0u;
+    if (topk > 0) {
+        // the topk-th largest of the groups' maxima: the smallest one that fewer than topk are above
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(&sh.group[j]);
+            above += (int)(o.x > gkey) + (int)(o.y > gkey) + (int)(o.z > gkey) + (int)(o.w > gkey);
+        }
+        bound = __reduce_min_sync(0xffffffffu, above < topk ? gkey : 0xffffffffu);
+        // threads that hold candidates: in their best chunk alone, or perhaps elsewhere too
+        if (order_key(mine) >= bound) {
+            if (order_key(second) >= bound || mine != mine) sh.all[atomicAdd(&sh.n_all, 1)] = (uint32_t)tid;
+            else if (run.m > neg_inf()) sh.one[atomicAdd(&sh.n_one, 1)] = best_chunk * THREADS + (uint32_t)tid;
+        }
+    }
+    adders_sync<THREADS>();
+    a.s = 0.0f; a.u = 0.0f;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) { a.s += sh.part[i].x; a.u += sh.part[i].y; }
+
+    bool listed = false;                             // the keys stand in sh.best, not in sh.cand
+    if (topk > 0) {
+        auto offer = [&](const uint4 &words, int64_t v0) {
+            float z[E];
+            G::floats(words, z);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const uint32_t k = order_key(z[i]);
+                if (k >= bound && v0 + i >= 0 && v0 + i < p.V) {
+                    const int at = atomicAdd(&sh.n_cand, 1);
+                    if (at < CAND) sh.cand[at] = ((unsigned long long)k << 32) | (uint32_t)~(uint32_t)(v0 + i);
+                }
+            }
+        };
+        const int n_one = sh.n_one * U;
+        for (int i = tid; i < n_one; i += THREADS) {
+            const uint32_t e = sh.one[i / U], c = e / THREADS;
+            const int64_t g = g0 + (int64_t)c * SH::CHUNK + (i % U) * THREADS + (e - c * THREADS);
+            if (g < g1) offer(*row.at(g), row.first(g));
+        }
+        const uint32_t per = (uint32_t)((g1 - g0 + THREADS - 1) / THREADS);
+        const int64_t n_all = (int64_t)sh.n_all * per;
+        for (int64_t i = tid; i < n_all; i += THREADS) {
+            const uint32_t f = (uint32_t)(i / per);
+            const int64_t g = g0 + sh.all[f] + (i - (int64_t)f * per) * THREADS;
+            if (g < g1) offer(*row.at(g), row.first(g));
+        }
+        if (has_edge && order_key(mine) >= bound) offer(row.load(edge), row.first(edge));
+        adders_sync<THREADS>();
+        if (sh.n_cand > CAND) {
             // Masses of equal logits at the bound (a row almost wholly masked, a constant row): topk passes, each
             // finding the largest key below the last one.
+            listed = true;
+            if (tid < MAX_TOP) sh.best[tid] = 0ull;
             unsigned long long last = ~0ull;
             for (int j = 0; j < topk; ++j) {
                 unsigned long long b = 0ull;
-                for (int64_t g = g0 + tid; g < g1; g += THREADS) {
+                auto look = [&](const uint4 &words, int64_t v0) {
                     float z[E];
-                    G::floats(row.load(g), z);
-                    const int64_t v0 = row.first(g);
+                    G::floats(words, z);
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
                         const int64_t v = v0 + i;
                         const unsigned long long k = ((unsigned long long)order_key(z[i]) << 32) | (uint32_t)~(uint32_t)v;
                         if (v >= 0 && v < p.V && k < last && k > b) b = k;
                     }
-                }
+                };
+                for (int64_t g = g0 + tid; g < g1; g += THREADS) look(*row.at(g), row.first(g));
+                if (has_edge) look(row.load(edge), row.first(edge));
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
                     const unsigned long long c = __shfl_xor_sync(0xffffffffu, b, o);
                     b = c > b ? c : b;
                 }
+                adders_sync<THREADS>();
                 if (lane == 0) sh.round_best[warp] = b;
-                __syncthreads();
+                adders_sync<THREADS>();
                 b = 0ull;
-                for (int w = 0; w < THREADS / 32; ++w) b = sh.round_best[w] > b ? sh.round_best[w] : b;
+                for (int i = 0; i < THREADS / 32; ++i) b = sh.round_best[i] > b ? sh.round_best[i] : b;
                 if (tid == 0) sh.best[j] = b;
                 last = b;
-                __syncthreads();
                 if (b == 0ull) break;                // fewer than topk elements in this CTA's part
             }
+            adders_sync<THREADS>();
         }
     }
-    __syncthreads();
-    a = sh.part[0];
-    for (int w = 1; w < THREADS / 32; ++w) a = join(a, sh.part[w]);
 
     if (csize > 1) {
         if (tid == 0) sh.mine = a;
-        cluster_barrier();
+        if (topk > 0 && !listed) {
+            if (tid < MAX_TOP) sh.best[tid] = 0ull;
+            adders_sync<THREADS>();
+            rank_candidates<THREADS>(sh.cand, sh.n_cand, topk, [&](int rank, unsigned long long k) { sh.best[rank] = k; });
+        }
+        __syncwarp();
+        cluster_sync_all();
         if (crank == 0) {
-            if (topk > 0) {                          // the CTAs' lists side by side
-                for (int c = tid; c < (int)csize * topk; c += THREADS) {
-                    const int r = c / topk;
-                    sh.cand[c] = peer_u64(peer_addr(&sh.best[c - r * topk], (uint32_t)r));
-                }
+            for (int c = tid; c < (int)csize * topk; c += THREADS) {         // the CTAs' lists side by side
+                const int r = c / topk;
+                sh.cand[c] = peer_u64(peer_addr(&sh.best[c - r * topk], (uint32_t)r));
             }
-            for (uint32_t r = 1; r < csize; ++r) {
-                const uint32_t at = peer_addr(&sh.mine, r);
-                const Stats b = {peer_f32(at), peer_f32(at + 4), peer_f32(at + 8)};
-                a = join(a, b);
-            }
-            if (topk > 0) {
-                __syncthreads();
-                rank_candidates<THREADS>(sh.cand, (int)csize * topk, topk, sh.best);
-                __syncthreads();
+            // every warp joins the CTAs' statistics: lane r reads those of CTA r (their number is a power of two)
+            const uint32_t at = peer_addr(&sh.mine, (uint32_t)lane & (csize - 1));
+            a = {peer_f32(at), peer_f32(at + 4), peer_f32(at + 8)};
+            for (uint32_t o = 1; o < csize; o <<= 1) {
+                Stats b;
+                b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+                b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+                b.u = __shfl_xor_sync(0xffffffffu, a.u, o);
+                a = (lane & o) ? join(b, a) : join(a, b);    // (the same order on both sides: all lanes hold the same bits)
             }
         }
-        cluster_barrier();                           // nobody leaves while its shared memory is being read
-        if (crank != 0) return;
+        __syncwarp();
+        cluster_sync_all();                              // nobody leaves while its shared memory is being read
+        listed = false;
+        if (crank == 0) {
+            if (tid == 0) sh.n_cand = (int)csize * topk;
+            adders_sync<THREADS>();
+        }
     }
 
-    const bool none = a.m == neg_inf();              // a row with nothing left
-    const bool bad = !(a.m < __uint_as_float(INF_BITS));
-    const float logs = logf(a.s);
-    auto logp = [&](float z) { return bad ? quiet_nan() : none ? neg_inf() : (z - a.m) - logs; };
-    if (tid == 0) {
-        if (p.lse) p.lse[t] = bad ? quiet_nan() : none ? neg_inf() : a.m + logs;
-        if (p.entropy) p.entropy[t] = bad ? quiet_nan() : none ? 0.0f : logs - a.u / a.s;
-        if (p.logprob) {
-            const int64_t id = p.ids[t];
-            p.logprob[t] = (id >= 0 && id < p.V) ? logp(to_float(row.row[id])) : 0.0f;
+    if (crank == 0) {
+        const bool none = a.m == neg_inf();          // a row with nothing left
+        const bool bad = !(a.m < __uint_as_float(INF_BITS));
+        const float logs = logf(a.s);
+        auto logp = [&](float z) { return bad ? quiet_nan() : none ? neg_inf() : (z - a.m) - logs; };
+        if (tid == 0) {
+            if (p.lse) p.lse[t] = bad ? quiet_nan() : none ? neg_inf() : a.m + logs;
+            if (p.entropy) p.entropy[t] = bad ? quiet_nan() : none ? 0.0f : logs - a.u / a.s;
+            if (p.logprob) p.logprob[t] = (id >= 0 && id < p.V) ? logp(token) : 0.0f;
+        }
+        auto put = [&](int rank, unsigned long long k) {
+            if (p.top_logprob) p.top_logprob[t * topk + rank] = logp(order_value((uint32_t)(k >> 32)));
+            if (p.top_ids) p.top_ids[t * topk + rank] = (int64_t)(uint32_t)~(uint32_t)k;
+        };
+        if (listed) {
+            if (tid < topk) put(tid, sh.best[tid]);
+        } else if (topk > 0) {
+            rank_candidates<THREADS>(sh.cand, sh.n_cand, topk, put);
         }
     }
-    if (tid < topk) {
-        const unsigned long long k = sh.best[tid];
-        if (p.top_logprob) p.top_logprob[t * topk + tid] = logp(order_value((uint32_t)(k >> 32)));
-        if (p.top_ids) p.top_ids[t * topk + tid] = (int64_t)(uint32_t)~(uint32_t)k;
+    if (*abort_flag) {
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
 }
 
@@ -363,6 +593,20 @@ struct ScoreGradArgs {
 
 constexpr int GRAD_THREADS = 256, GRAD_U = 4;
 
+struct GradRow {
+    float lse, gh, h, gl, c;       // dz = -p (c + g_H log p), plus g_lp at the token
+    int64_t id;
+    bool none;
+    __device__ __forceinline__ float grad(float z, int64_t v) const
+    {
+        if (none || z == neg_inf()) return 0.0f;
+        const float x = fmaxf(z - lse, FAR);
+        float d = -exp2_approx(x * LOG2E) * fmaf(gh, x, c);
+        if (v == id) d += gl;
+        return lse != lse ? lse : d;
+    }
+};
+
 // VEC: logits and gradient rows lie alike modulo 16 bytes, so a granule of one is a granule of the other
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(GRAD_THREADS) scores_grad_kernel(const ScoreGradArgs p)
@@ -375,82 +619,114 @@ __global__ void __launch_bounds__(GRAD_THREADS) scores_grad_kernel(const ScoreGr
     const uint32_t part = blockIdx.x - (uint32_t)t * p.parts;
     const G row(static_cast<const T *>(p.logits) + t * p.ldl, p.V);
     T *dst = static_cast<T *>(p.d) + t * p.ldd;
-    const float lse = p.lse[t];
-    const float gh = p.g_entropy ? p.g_entropy[t] : 0.0f, h = p.g_entropy ? p.entropy[t] : 0.0f;
-    const int64_t id = p.g_logprob ? p.ids[t] : -1;
-    const float gl = (id >= 0 && id < p.V) ? p.g_logprob[t] : 0.0f;
-    const bool none = lse == neg_inf();
-    const float c = fmaf(gh, h, gl);                 // dz = -p (c + g_H log p), plus g_lp at the token
-    auto grad = [&](float z, int64_t v) {
-        if (none || z == neg_inf()) return 0.0f;
-        const float x = fmaxf(z - lse, FAR);
-        const float pr = exp2_approx(x * LOG2E);
-        float d = -pr * fmaf(gh, x, c);
-        if (v == id) d += gl;
-        return lse != lse ? lse : d;
-    };
+    GradRow r;
+    r.lse = p.lse[t];
+    r.gh = p.g_entropy ? p.g_entropy[t] : 0.0f;
+    r.h = p.g_entropy ? p.entropy[t] : 0.0f;
+    r.id = p.g_logprob ? p.ids[t] : -1;
+    r.gl = (r.id >= 0 && r.id < p.V) ? p.g_logprob[t] : 0.0f;
+    r.none = r.lse == neg_inf();
+    r.c = fmaf(r.gh, r.h, r.gl);
     if (VEC) {
-        const int64_t all = row.count(), base = (int64_t)part * (GRAD_THREADS * GRAD_U) + threadIdx.x;
+        const int64_t all = row.count(), f0 = row.first_full(), f1 = row.end_full();
+        const int64_t base = (int64_t)part * (GRAD_THREADS * GRAD_U) + threadIdx.x;
         uint4 w[GRAD_U];
-#pragma unroll
-        for (int j = 0; j < GRAD_U; ++j)
-            if (base + j * GRAD_THREADS < all) w[j] = row.load(base + j * GRAD_THREADS);
 #pragma unroll
         for (int j = 0; j < GRAD_U; ++j) {
             const int64_t g = base + j * GRAD_THREADS;
-            if (g >= all) break;
-            const int64_t v0 = row.first(g);
-            float f[E];
-            G::floats(w[j], f);
+            if (g >= f0 && g < f1) w[j] = *row.at(g);
+        }
+        const bool calm = calm_at<T>(r.lse) && fabsf(r.gh) < 1e15f && fabsf(r.c) < 1e15f;
+        const f32x2 nlse = pair(-r.lse, -r.lse), l2e = pair(LOG2E, LOG2E), ngh = pair(-r.gh, -r.gh), nc = pair(-r.c, -r.c);
 #pragma unroll
-            for (int i = 0; i < E; ++i) f[i] = grad(f[i], v0 + i);
-            if (v0 >= 0 && v0 + E <= p.V) {
+        for (int j = 0; j < GRAD_U; ++j) {
+            const int64_t g = base + j * GRAD_THREADS;
+            const int64_t v0 = row.first(g);
+            if (g >= f0 && g < f1) {
+                float f[E];
+                if (calm) {
+                    f32x2 z[E / 2];
+                    calm_pairs(w[j], z, T());
+#pragma unroll
+                    for (int i = 0; i < E / 2; ++i) {
+                        const f32x2 x = add2(z[i], nlse);
+                        float lo, hi;
+                        unpair(mul2(x, l2e), lo, hi);
+                        unpair(mul2(pair(exp2_approx(lo), exp2_approx(hi)), fma2(ngh, x, nc)), f[2 * i], f[2 * i + 1]);
+                    }
+                    const int64_t at = r.id - v0;
+                    if (at >= 0 && at < E) {             // the token's own entry, unless it is masked
+                        float z1[E];
+                        G::floats(w[j], z1);
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            if (i == at && z1[i] != neg_inf()) f[i] += r.gl;
+                    }
+                } else {
+                    G::floats(w[j], f);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) f[i] = r.grad(f[i], v0 + i);
+                }
                 if constexpr (E == 8) store_floats<T, 8>(dst + v0, f);
                 else *reinterpret_cast<float4 *>(dst + v0) = make_float4(f[0], f[1], f[2], f[3]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < E; ++i)
-                    if (v0 + i >= 0 && v0 + i < p.V) from_float(f[i], dst[v0 + i]);
+            } else if (g < all) {                        // a granule the row only shares
+#pragma unroll 1
+                for (int64_t v = v0 < 0 ? 0 : v0; v < v0 + E && v < p.V; ++v) from_float(r.grad(to_float(row.row[v]), v), dst[v]);
             }
         }
     } else {
         const int64_t v1 = (int64_t)(part + 1) * (GRAD_THREADS * GRAD_U * E);
         for (int64_t v = (int64_t)part * (GRAD_THREADS * GRAD_U * E) + threadIdx.x; v < v1 && v < p.V; v += GRAD_THREADS)
-            from_float(grad(to_float(row.row[v]), v), dst[v]);
+            from_float(r.grad(to_float(row.row[v]), v), dst[v]);
     }
 }
 
-template <typename T, int THREADS, int U>
-int launch_scores_cfg(const ScoreArgs &p, int64_t T_rows, int cluster, cudaStream_t st)
+template <typename T, int THREADS, int U, int STAGES, int RESIDENT>
+int launch_scores_cfg(const ScoreArgs &p, int cluster, cudaStream_t st)
 {
+    auto kern = scores_kernel<T, THREADS, U, STAGES, RESIDENT>;
+    constexpr size_t smem = sizeof(ScoreShared<THREADS, U, STAGES>);
+    static_assert(smem * RESIDENT + 1024 * RESIDENT <= 228 * 1024, "shared memory of an SM");
+    // the shared-memory opt-in is per kernel and device: asked for once each (racing first calls set the same attribute)
+    static std::atomic<bool> done[64];
+    int dev = 0;
+    QNN_CUDA(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64 || !done[dev].load(std::memory_order_acquire)) {
+        QNN_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(T_rows * cluster));
-    cfg.blockDim = dim3(THREADS);
+    cfg.gridDim = dim3((unsigned)(p.T * cluster));
+    cfg.blockDim = dim3(THREADS + 32);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     unsigned na = 0;
-    attr[na].id = cudaLaunchAttributeClusterDimension;
-    attr[na].val.clusterDim.x = (unsigned)cluster; attr[na].val.clusterDim.y = 1; attr[na].val.clusterDim.z = 1;
-    ++na;
+    if (cluster > 1) {
+        attr[na].id = cudaLaunchAttributeClusterDimension;
+        attr[na].val.clusterDim.x = (unsigned)cluster; attr[na].val.clusterDim.y = 1; attr[na].val.clusterDim.z = 1;
+        ++na;
+    }
     if (pdl_enabled()) {
         attr[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[na].val.programmaticStreamSerializationAllowed = 1;
         ++na;
     }
     cfg.attrs = attr; cfg.numAttrs = na;
-    QNN_CUDA(cudaLaunchKernelEx(&cfg, scores_kernel<T, THREADS, U>, p));
+    QNN_CUDA(cudaLaunchKernelEx(&cfg, kern, p));
     return check_launch("qnn_token_logprobs");
 }
 
 template <typename T>
-int launch_scores(const ScoreArgs &p, int64_t rows, cudaStream_t st)
+int launch_scores(const ScoreArgs &p, cudaStream_t st)
 {
     const int64_t granules = (int64_t)p.V / Granules<T>::E + 1;
-    // Short rows: small blocks, several rows to an SM.  Few long rows: a cluster of CTAs shares a row.
-    if (granules <= 512) return launch_scores_cfg<T, 128, 4>(p, rows, 1, st);
     int cluster = 1;
-    while (cluster < 8 && rows * cluster * 2 <= 2 * (int64_t)sm_count() && granules / (cluster * 2) >= 512) cluster *= 2;
-    return launch_scores_cfg<T, 512, 4>(p, rows, cluster, st);
+    while (cluster < 8 && p.T * cluster * 2 <= 2 * (int64_t)sm_count() && granules / (cluster * 2) >= 512) cluster *= 2;
+    // Threads a CTA: more rows at a time where rows are short (2048 x 16384 bf16 with 8 alternatives: 128 threads 24 us, 256
+    // threads 31 us), shorter rows' ends where they are long (2048 x 131072: 100 and 99 us, 4 x 128000: 22 and 15 us).
+    if (granules <= 4096) return launch_scores_cfg<T, 128, 4, 3, 7>(p, cluster, st);
+    return launch_scores_cfg<T, 256, 4, 3, 4>(p, cluster, st);
 }
 
 template <typename T>
@@ -482,6 +758,13 @@ int check_logits(const char *what, const void *logits, int type, int64_t T, int6
 }
 
 }  // namespace
+
+int scores_status(int *code)
+{
+    QNN_CUDA(status_read_clear(code));
+    return QNN_OK;
+}
+
 }  // namespace qnn
 
 using namespace qnn;
@@ -503,14 +786,14 @@ int qnn_token_logprobs(const void *logits, int type, int64_t T, int64_t V, int64
     QNN_REQUIRE(aligned(ids, 8) && aligned(top_ids, 8) && aligned(logprob, 4) && aligned(entropy, 4) && aligned(lse, 4) && aligned(top_logprob, 4),
                 QNN_ERR_ALIGNMENT, "%s: a pointer is not aligned to its elements", what);
     ScoreArgs p{};
-    p.logits = logits; p.ldl = ldl; p.V = (int32_t)V;
+    p.logits = logits; p.T = T; p.ldl = ldl; p.V = (int32_t)V;
     p.ids = ids; p.logprob = logprob; p.entropy = entropy; p.lse = lse;
     p.topk = topk; p.top_logprob = top_logprob; p.top_ids = top_ids;
     cudaStream_t st = as_stream(stream);
     switch (type) {
-        case QNN_TYPE_F32: return launch_scores<float>(p, T, st);
-        case QNN_TYPE_BF16: return launch_scores<__nv_bfloat16>(p, T, st);
-        default: return launch_scores<__half>(p, T, st);
+        case QNN_TYPE_F32: return launch_scores<float>(p, st);
+        case QNN_TYPE_BF16: return launch_scores<__nv_bfloat16>(p, st);
+        default: return launch_scores<__half>(p, st);
     }
 }
 

@@ -47,6 +47,27 @@ __device__ __forceinline__ void from_float(float x, float &o) { o = x; }
 __device__ __forceinline__ void from_float(float x, __nv_bfloat16 &o) { o = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void from_float(float x, __half &o) { o = __float2half_rn(x); }
 
+// Two fp32 values in one 64-bit register pair: sm_100 adds, multiplies and fuses pairs with one instruction, which halves
+// the issue slots of the element loops.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair(float lo, float hi)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(f32x2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+// maximum that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // W consecutive elements in registers as they lie in memory.  W = 8 is one or two 16-byte accesses, W = 2 one access of
 // a pair, W = 1 a single element; the address must be a multiple of min(16, W * sizeof(T)) bytes.
 template <typename T, int W>
