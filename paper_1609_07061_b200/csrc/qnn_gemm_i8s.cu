@@ -193,26 +193,38 @@ gemm_i8s_wide_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
         uint32_t iter = 0;
         bool ok = true;
         int32_t tn = (int32_t)((blockIdx.x / CTAS) / tiles_m), tm = (int32_t)((blockIdx.x / CTAS) - (uint32_t)tn * tiles_m);
-        int32_t tn_parked = -1;
+        // Channel scales, biases and the token's scale of a tile are fetched into registers while the tile before it is
+        // drained, and parked in shared memory when its turn comes: their latency never sits between two tiles.
+        constexpr int CPL = S::NBW * S::CB / 32;                 // channels a lane fetches
+        float s_next[CPL], b_next[CPL], sa_next;
+        auto fetch = [&](int32_t ftm, int32_t ftn) {
+            const int64_t m = ((int64_t)ftm * CTAS + rank) * BM + q * 32 + lane;
+            sa_next = m < p.M ? __ldg(p.a_scale + m) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                const int blk = grp + (i * 32 / S::CB) * G;
+                const int64_t n = (int64_t)ftn * BN + blk * S::CB + (i * 32) % S::CB + lane;
+                const bool in = blk < S::NB && n < p.N;
+                s_next[i] = in ? __ldg(p.b_scale + n) : 0.0f;
+                b_next[i] = in && p.bias ? __ldg(p.bias + n) : 0.0f;
+            }
+        };
+        if (blockIdx.x / CTAS < num_tiles) fetch(tm, tn);
         for (uint32_t t = blockIdx.x / CTAS; t < num_tiles && ok; t += gridDim.x / CTAS, ++iter) {
             const uint32_t as = iter & 1u, aphase = (iter >> 1) & 1u;
             const int64_t ntile = (int64_t)tn * BN;
             const int64_t m0 = ((int64_t)tm * CTAS + rank) * BM + q * 32;       // the row of the warp's lane 0
-            const float sa = m0 + lane < p.M ? __ldg(p.a_scale + m0 + lane) : 0.0f;
-            if (tn != tn_parked) {                               // consecutive tiles mostly share their columns
-                tn_parked = tn;
-                __syncwarp();
-                for (int b = 0; b < S::NBW; ++b) {
-                    for (int c = lane; c < S::CB; c += 32) {
-                        const int blk = grp + b * G;
-                        const int64_t n = ntile + blk * S::CB + c;
-                        const bool in = blk < S::NB && n < p.N;
-                        cs[b * S::CB + c] = in ? __ldg(p.b_scale + n) : 0.0f;
-                        cb[b * S::CB + c] = (in && p.bias) ? __ldg(p.bias + n) : 0.0f;
-                    }
-                }
-                __syncwarp();
+            const float sa = sa_next;
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                cs[i * 32 + lane] = s_next[i];
+                cb[i * 32 + lane] = b_next[i];
             }
+            __syncwarp();
+            tm += (int32_t)step_m; tn += (int32_t)step_n;        // the next tile's coordinates
+            if (tm >= (int32_t)tiles_m) { tm -= (int32_t)tiles_m; ++tn; }
+            if (t + gridDim.x / CTAS < num_tiles) fetch(tm, tn);
             // the tensor-memory loads below are warp-collective: leave the loop only as a whole warp
             if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(as), aphase, abort_flag, 14))) { ok = false; break; }
             tc_fence_after();
@@ -256,16 +268,18 @@ gemm_i8s_wide_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
                     // rows of any alignment: lanes along the columns, element by element
                     __syncwarp();
                     const int rows = p.M - m0 < 32 ? (int)(p.M - m0) : 32;
-                    TOUT *dst = static_cast<TOUT *>(p.out) + m0 * p.ldo + n0;
-#pragma unroll 4
-                    for (int r = 0; r < rows; ++r) {
+                    TOUT *dst = static_cast<TOUT *>(p.out) + m0 * p.ldo + n0 + lane;
+#pragma unroll 8
+                    for (int r = 0; r < 32; ++r) {
+                        if (r < rows) {
 #pragma unroll
-                        for (int h = 0; h < S::CB / 32; ++h) {
-                            const int c = h * 32 + lane;
-                            const int byte = c * (int)sizeof(TOUT);
-                            const TOUT x = *reinterpret_cast<const TOUT *>(stg + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
-                            if (n0 + c < p.N) dst[(int64_t)r * p.ldo + c] = x;
+                            for (int h = 0; h < S::CB / 32; ++h) {
+                                const int byte = (h * 32 + lane) * (int)sizeof(TOUT);
+                                const TOUT x = *reinterpret_cast<const TOUT *>(stg + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+                                if (n0 + h * 32 + lane < p.N) dst[h * 32] = x;
+                            }
                         }
+                        dst += p.ldo;
                     }
                     __syncwarp();
                 }
@@ -277,8 +291,6 @@ gemm_i8s_wide_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
                 if (CTAS == 2) mbar_arrive_cluster(map_to_cta(tempty_bar(as), 0));
                 else mbar_arrive(tempty_bar(as));
             }
-            tm += (int32_t)step_m; tn += (int32_t)step_n;
-            if (tm >= (int32_t)tiles_m) { tm -= (int32_t)tiles_m; ++tn; }
         }
         if (lane == 0) bulk_wait_all();                          // stores must have read shared memory before it goes away
         __syncwarp();
@@ -314,18 +326,18 @@ struct NarrowCfg {
     static_assert((2 * STAGES + 1) * 8 + 8 <= 128, "barriers");
 };
 
-__device__ __forceinline__ int32_t ld_peer_i32(uint32_t addr)
+__device__ __forceinline__ int4 ld_peer_i32x4(uint32_t addr)
 {
-    int32_t v;
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
 
-template <int BN, typename TOUT>
+template <int BN, typename TOUT, int SPLIT>
 __global__ void __launch_bounds__(NARROW_THREADS, 2)
-gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const I8sParams p,
-                       const int split)
+gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const I8sParams p)
 {
+    constexpr int split = SPLIT;
     using S = NarrowCfg<BN>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -351,6 +363,8 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), S::TMEM);
+    if (warp == 2 && lane < 2)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &tmap_w : &tmap_x) : "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -426,17 +440,35 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         // every CTA of the cluster reaches both barriers, whatever became of its waits
         cluster_sync_all();
         if (warp >= 2 && ok) {
-            const int n_local = threadIdx.x - 64;
-            const int64_t n = (int64_t)tn * BM + n_local;
-            if (n < p.N) {
-                const float sb = __ldg(p.b_scale + n), bi = p.bias ? __ldg(p.bias + n) : 0.0f;
-                for (int j = (int)rank; j < nt; j += split) {
-                    const uint32_t at = smem_u32(part + j * BM + n_local);
-                    int32_t s = 0;
-                    for (int r = 0; r < split; ++r) s += ld_peer_i32(map_to_cta(at, (uint32_t)r));
-                    const int64_t m = (int64_t)tm * BN + j;
-                    const float f = fmaf(__int2float_rn(s) * __ldg(p.a_scale + m), sb, bi);
-                    from_float(f, static_cast<TOUT *>(p.out)[m * p.ldo + n]);
+            // a warp takes one token at a time, a lane four channels of it: one 16-byte read from every CTA of the cluster
+            const int64_t n = (int64_t)tn * BM + 4 * lane;
+            float sb[4], bi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sb[i] = n + i < p.N ? __ldg(p.b_scale + n + i) : 0.0f;
+                bi[i] = n + i < p.N && p.bias ? __ldg(p.bias + n + i) : 0.0f;
+            }
+#pragma unroll 2
+            for (int j = (int)rank + (warp - 2) * split; j < nt; j += 4 * split) {
+                const uint32_t at = smem_u32(part + j * BM + 4 * lane);
+                const int64_t m = (int64_t)tm * BN + j;
+                const float sa = __ldg(p.a_scale + m);
+                int4 v[SPLIT];
+#pragma unroll
+                for (int r = 0; r < SPLIT; ++r) v[r] = ld_peer_i32x4(map_to_cta(at, (uint32_t)r));
+                int4 s = v[0];
+#pragma unroll
+                for (int r = 1; r < SPLIT; ++r) { s.x += v[r].x; s.y += v[r].y; s.z += v[r].z; s.w += v[r].w; }
+                const float f[4] = {fmaf(__int2float_rn(s.x) * sa, sb[0], bi[0]), fmaf(__int2float_rn(s.y) * sa, sb[1], bi[1]),
+                                    fmaf(__int2float_rn(s.z) * sa, sb[2], bi[2]), fmaf(__int2float_rn(s.w) * sa, sb[3], bi[3])};
+                TOUT *dst = static_cast<TOUT *>(p.out) + m * p.ldo + n;
+                if (n + 4 <= p.N && (reinterpret_cast<uintptr_t>(dst) & (4 * sizeof(TOUT) - 1)) == 0) {
+                    if constexpr (sizeof(TOUT) == 4) *reinterpret_cast<float4 *>(dst) = make_float4(f[0], f[1], f[2], f[3]);
+                    else *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2(f[0], f[1], TOUT()), pack2(f[2], f[3], TOUT()));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (n + i < p.N) from_float(f[i], dst[i]);
                 }
             }
         }
@@ -449,6 +481,106 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc<1>(tmem_base, S::TMEM);
+}
+
+// ---- a handful of tokens ---------------------------------------------------------------------------------------
+//
+// Bound by reading the weights once, and at 2.6 us of it (16.8 MB) by latency: a launch, one round of loads, a sum.  So no
+// shared-memory staging and no tensor memory: a warp reads GEMV_R rows of weights 16 bytes a lane, multiplies by the tokens'
+// codes (which stay in L1) four at a time on the integer units (dp4a), and sums over its lanes.  K may be cut among the warps
+// of a block, whose partial sums meet in shared memory.
+
+__device__ __forceinline__ uint4 load_codes(const uint8_t *row, int32_t k) { return __ldg(reinterpret_cast<const uint4 *>(row + k)); }
+// the same with the codes from K on taken as 0 (only one factor of a product needs it)
+__device__ __forceinline__ uint4 load_codes_to(const uint8_t *row, int32_t k, int32_t K)
+{
+    uint4 v = load_codes(row, k);
+    const int left = K - k;                                  // >= 1
+    if (left < 16) {
+        auto keep = [&](int first) { const int n = left - first; return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; };
+        v.x &= keep(0); v.y &= keep(4); v.z &= keep(8); v.w &= keep(12);
+    }
+    return v;
+}
+__device__ __forceinline__ int32_t dot16(const uint4 &a, const uint4 &b, int32_t s)
+{
+    s = __dp4a((int)a.x, (int)b.x, s);
+    s = __dp4a((int)a.y, (int)b.y, s);
+    s = __dp4a((int)a.z, (int)b.z, s);
+    return __dp4a((int)a.w, (int)b.w, s);
+}
+
+template <int MT, int GEMV_R, int GEMV_U, typename TOUT>
+__global__ void __launch_bounds__(256) gemv_i8s_kernel(const uint8_t *__restrict__ a, int64_t lda, const uint8_t *__restrict__ b, int64_t ldb,
+                                                       const int32_t K, const int ksplit, const I8sParams p)
+{
+    __shared__ int32_t part[8][GEMV_R * MT];
+    griddep_launch_dependents();
+    griddep_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per_block = 8 / ksplit;                        // row groups of a block
+    const int64_t n0 = ((int64_t)blockIdx.x * per_block + warp / ksplit) * GEMV_R;
+    const int32_t share = (((K + 15) / 16 + ksplit - 1) / ksplit) * 16;    // codes of a warp's part of K
+    const int32_t k0 = share * (warp % ksplit), k1 = k0 + share < K ? k0 + share : K;
+    int32_t acc[GEMV_R][MT];
+#pragma unroll
+    for (int r = 0; r < GEMV_R; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[r][m] = 0;
+    const uint8_t *br[GEMV_R], *ar[MT];
+#pragma unroll
+    for (int r = 0; r < GEMV_R; ++r) br[r] = b + (n0 + r < p.N ? n0 + r : p.N - 1) * ldb;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) ar[m] = a + (m < p.M ? m : p.M - 1) * lda;
+    int32_t k = k0 + 16 * lane;
+    // whole rounds: GEMV_U x GEMV_R loads of weights in flight
+    for (; k + 512 * (GEMV_U - 1) + 16 <= k1; k += 512 * GEMV_U) {
+        uint4 w[GEMV_U][GEMV_R];
+#pragma unroll
+        for (int u = 0; u < GEMV_U; ++u)
+#pragma unroll
+            for (int r = 0; r < GEMV_R; ++r) w[u][r] = load_codes(br[r], k + 512 * u);
+#pragma unroll
+        for (int u = 0; u < GEMV_U; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const uint4 x = load_codes(ar[m], k + 512 * u);
+#pragma unroll
+                for (int r = 0; r < GEMV_R; ++r) acc[r][m] = dot16(w[u][r], x, acc[r][m]);
+            }
+    }
+    for (; k < k1; k += 512) {
+        uint4 w[GEMV_R];
+#pragma unroll
+        for (int r = 0; r < GEMV_R; ++r) w[r] = load_codes(br[r], k);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const uint4 x = load_codes_to(ar[m], k, K);
+#pragma unroll
+            for (int r = 0; r < GEMV_R; ++r) acc[r][m] = dot16(w[r], x, acc[r][m]);
+        }
+    }
+    int32_t mine = 0;                                        // lane r * MT + m keeps sum (r, m)
+#pragma unroll
+    for (int r = 0; r < GEMV_R; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int32_t s = __reduce_add_sync(0xffffffffu, acc[r][m]);
+            if (lane == r * MT + m) mine = s;
+        }
+    if (ksplit > 1) {
+        if (lane < GEMV_R * MT) part[warp][lane] = mine;
+        __syncthreads();
+        if (warp % ksplit != 0) return;
+        if (lane < GEMV_R * MT)
+            for (int i = 1; i < ksplit; ++i) mine += part[warp + i][lane];
+    }
+    const int64_t n = n0 + lane / MT;
+    const int m = lane % MT;
+    if (lane < GEMV_R * MT && n < p.N && m < p.M) {
+        const float f = fmaf(__int2float_rn(mine) * __ldg(p.a_scale + m), __ldg(p.b_scale + n), p.bias ? __ldg(p.bias + n) : 0.0f);
+        from_float(f, static_cast<TOUT *>(p.out)[m * p.ldo + n]);
+    }
 }
 
 // K = 0: the bias alone
@@ -525,27 +657,35 @@ struct I8sCall {
     int64_t lda, ldb, K;
 };
 
-template <int BN, typename TOUT>
-int launch_narrow(const I8sCall &c, I8sParams p, cudaStream_t st)
+template <int BN, typename TOUT, int SPLIT>
+int launch_narrow_split(const I8sCall &c, I8sParams p, cudaStream_t st)
 {
     using S = NarrowCfg<BN>;
-    auto kern = gemm_i8s_narrow_kernel<BN, TOUT>;
+    auto kern = gemm_i8s_narrow_kernel<BN, TOUT, SPLIT>;
     static std::atomic<bool> done[64];
     if (int rc = opt_in(kern, S::TOTAL, done)) return rc;
     CUtensorMap mw, mx;
     if (int rc = make_map_codes(&mw, c.b, p.N, c.K, c.ldb, BM)) return rc;
     if (int rc = make_map_codes(&mx, c.a, p.M, c.K, c.lda, BN)) return rc;
-    p.tiles_n = (int32_t)ceil_div(p.N, BM);
-    p.tiles_m = (int32_t)ceil_div(p.M, BN);
     p.idesc = i8_idesc(BM, BN);
-    const int64_t tiles = (int64_t)p.tiles_n * p.tiles_m;
-    int split = 1;
-    while (split < 8 && tiles * split * 2 <= 2 * (int64_t)sm_count() && p.num_kb / (split * 2) >= 2) split *= 2;
-    QNN_REQUIRE(tiles * split < ((int64_t)1 << 31), QNN_ERR_UNSUPPORTED, "qnn_gemm_i8_scaled: too many output tiles");
+    const int64_t ctas = (int64_t)p.tiles_n * p.tiles_m * SPLIT;
+    QNN_REQUIRE(ctas < ((int64_t)1 << 31), QNN_ERR_UNSUPPORTED, "qnn_gemm_i8_scaled: too many output tiles");
     profile_before(st);
-    QNN_CUDA(launch_clustered(kern, (unsigned)(tiles * split), NARROW_THREADS, S::TOTAL, split, st, mw, mx, p, split));
+    QNN_CUDA(launch_clustered(kern, (unsigned)ctas, NARROW_THREADS, S::TOTAL, SPLIT, st, mw, mx, p));
     profile_after(st);
     return check_launch("qnn_gemm_i8_scaled");
+}
+template <int BN, typename TOUT>
+int launch_narrow(const I8sCall &c, I8sParams p, int split, cudaStream_t st)
+{
+    p.tiles_n = (int32_t)ceil_div(p.N, BM);
+    p.tiles_m = (int32_t)ceil_div(p.M, BN);
+    switch (split) {
+        case 1: return launch_narrow_split<BN, TOUT, 1>(c, p, st);
+        case 2: return launch_narrow_split<BN, TOUT, 2>(c, p, st);
+        case 4: return launch_narrow_split<BN, TOUT, 4>(c, p, st);
+        default: return launch_narrow_split<BN, TOUT, 8>(c, p, st);
+    }
 }
 
 template <int BN, int CTAS, typename TOUT>
@@ -610,6 +750,22 @@ int pairs_resident()
     return v - 1;
 }
 
+template <int MT, int GEMV_R, int GEMV_U, typename TOUT>
+int launch_gemv(const I8sCall &c, const I8sParams &p, cudaStream_t st)
+{
+    // K is cut until there are about sixteen warps for every SM (or a warp's part is a single round of loads)
+    const int64_t groups = ceil_div(p.N, GEMV_R);
+    int ksplit = 1;
+    while (ksplit < 8 && groups * ksplit * 2 <= 16 * (int64_t)sm_count() && c.K / (ksplit * 2) >= 512) ksplit *= 2;
+    const int64_t blocks = ceil_div(groups, 8 / ksplit);
+    QNN_REQUIRE(blocks < ((int64_t)1 << 31), QNN_ERR_UNSUPPORTED, "qnn_gemm_i8_scaled: too many output channels");
+    profile_before(st);
+    QNN_CUDA(launch_pdl(gemv_i8s_kernel<MT, GEMV_R, GEMV_U, TOUT>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const uint8_t *>(c.a), c.lda,
+                        static_cast<const uint8_t *>(c.b), c.ldb, (int32_t)c.K, ksplit, p));
+    profile_after(st);
+    return check_launch("qnn_gemm_i8_scaled");
+}
+
 template <typename TOUT>
 int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
 {
@@ -619,13 +775,60 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
                             static_cast<TOUT *>(p.out), p.ldo));
         return check_launch("qnn_gemm_i8_scaled");
     }
-    if (p.M <= 16) return launch_narrow<16, TOUT>(c, p, st);
-    if (p.M <= 32) return launch_narrow<32, TOUT>(c, p, st);
-    if (p.M <= 64) return launch_narrow<64, TOUT>(c, p, st);
-    if (p.M <= 128) return launch_narrow<128, TOUT>(c, p, st);
-    const int pairs = pairs_resident();
-    if (pairs >= 8 && ceil_div(p.M, 256) * ceil_div(p.N, 256) >= pairs) return launch_wide<256, 2, TOUT>(c, p, pairs, st);
-    return launch_wide<128, 1, TOUT>(c, p, sm_count(), st);
+    // A handful of tokens: the weights go through the integer units.  One or two tokens always (4096 x 4096: 3.3 us against
+    // 5.3 us on the tensor cores, 16384 x 4096: 12.3 against 14.6 us); up to four while the weights are at most 32 MB
+    // (4096 x 4096: 3.6 against 5.4, 11008 x 2048: 5.5 against 6.0, but 16384 x 4096: 20.3 against 14.8), up to eight while
+    // they are at most 8 MB (1024 x 8192: 3.9 against 5.1, but 4096 x 4096: 5.9 against 5.4).
+    const int64_t weights = p.N * c.K;
+    if (p.M == 1) return launch_gemv<1, 2, 4, TOUT>(c, p, st);
+    if (p.M == 2) return launch_gemv<2, 2, 4, TOUT>(c, p, st);
+    if (p.M <= 4 && weights <= (int64_t)32 << 20) return launch_gemv<4, 4, 4, TOUT>(c, p, st);
+    if (p.M <= 8 && weights <= (int64_t)8 << 20) return launch_gemv<8, 4, 1, TOUT>(c, p, st);
+
+    // On the tensor cores the time of a launch is, within about 10 % over M = 16 .. 4096, N = 1024 .. 16384, K = 1024 .. 8192,
+    //   start + waves * (K blocks a CTA walks * time of a block + hand-over)      (us, fitted to the sweep)
+    // with the constants below; the cheapest configuration runs.  100 x 4096 x 4096: narrow 8.6, wide 64 columns 9.2;
+    // 100 x 11008 x 2048: narrow 10.0, wide 128 columns 7.7; 701 x 2047 x 1111: wide 64 columns 8.2, 128 columns 6.6, pairs of
+    // 256 columns 9.2; 701 x 4096 x 4096: 22.8, 19.8, and pairs of 128 / 192 / 256 columns 18.1 / 13.2 / 15.1.
+    struct Config { int rows, cols; float start, block, hand; };
+    static const Config wide[] = {{128, 64, 3.2f, 0.21f, 0.1f}, {128, 128, 3.7f, 0.27f, 0.2f}, {256, 128, 4.2f, 0.235f, 0.3f},
+                                  {256, 192, 4.8f, 0.285f, 0.5f}, {256, 256, 5.5f, 0.34f, 0.7f}};
+    const int sms = sm_count(), pairs = pairs_resident();
+    int best = -1;
+    float cost = 0.0f;
+    for (int i = 0; i < 5; ++i) {
+        const int workers = wide[i].rows == 128 ? sms : pairs;
+        if (workers < 1) continue;
+        const int64_t tiles = ceil_div(p.M, wide[i].rows) * ceil_div(p.N, wide[i].cols);
+        const float t = wide[i].start + (float)ceil_div(tiles, workers) * (wide[i].block * (float)p.num_kb + wide[i].hand);
+        if (best < 0 || t < cost) { best = i; cost = t; }
+    }
+    {
+        // narrow tiles, K cut until the CTAs are about one for every SM: few tokens, or few channels and a long K
+        static const Config narrow[] = {{16, 0, 3.0f, 0.28f, 0.5f}, {32, 0, 3.5f, 0.29f, 0.6f}, {64, 0, 4.4f, 0.31f, 0.8f}, {128, 0, 5.5f, 0.36f, 1.2f}};
+        const int i = p.M <= 16 ? 0 : p.M <= 32 ? 1 : p.M <= 64 ? 2 : 3;
+        const int64_t tiles = ceil_div(p.N, BM) * ceil_div(p.M, narrow[i].rows);
+        int split = 1;
+        while (split < 8 && tiles * split * 2 <= (int64_t)sms * 5 / 4 && p.num_kb / (split * 2) >= 2) split *= 2;
+        const int64_t ctas = tiles * split;
+        const float t = (float)ceil_div(ctas, 2 * sms) * (narrow[i].start + narrow[i].block * (float)ceil_div(p.num_kb, split) * (ctas > sms ? 1.4f : 1.0f)) +
+                        (split > 1 ? narrow[i].hand : 0.0f);
+        if (t < cost) {
+            switch (i) {
+                case 0: return launch_narrow<16, TOUT>(c, p, split, st);
+                case 1: return launch_narrow<32, TOUT>(c, p, split, st);
+                case 2: return launch_narrow<64, TOUT>(c, p, split, st);
+                default: return launch_narrow<128, TOUT>(c, p, split, st);
+            }
+        }
+    }
+    switch (best) {
+        case 0: return launch_wide<64, 1, TOUT>(c, p, sms, st);
+        case 1: return launch_wide<128, 1, TOUT>(c, p, sms, st);
+        case 2: return launch_wide<128, 2, TOUT>(c, p, pairs, st);
+        case 3: return launch_wide<192, 2, TOUT>(c, p, pairs, st);
+        default: return launch_wide<256, 2, TOUT>(c, p, pairs, st);
+    }
 }
 
 }  // namespace
