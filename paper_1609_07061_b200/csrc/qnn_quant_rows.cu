@@ -170,17 +170,16 @@ __device__ __forceinline__ float warp_sum(float v)
 
 // A row of at most 8 * NV * tpr elements in registers: tpr threads own pieces of W elements, interleaved, so that a
 // warp's accesses are contiguous.  W divides K; W = 8 needs 16-byte aligned rows, W = 2 aligned pairs, W = 1 nothing.
-// (A kernel that also took rows ending inside a piece spent 41 instructions an element instead of 16 on the 8192 x 4096
+// (A kernel that also took rows ending inside a piece spent 41 instructions an element instead of 18 on the 8192 x 4096
 // norm: the element-wise ends of every load and store are predicated, not branched around.)
-template <int OP, typename T, int W, int NV>
-__global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
+template <int OP, typename T, int W, int NV, int MAXREG = 128>
+__global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(const RowArgs p)
 {
     constexpr int P = NV * 8 / W;                        // pieces per thread
     constexpr int CH0 = W == 8 ? (sizeof(T) == 4 ? 2 : 4) : 8;   // pieces whose loads are in flight together
     constexpr int CH = P < CH0 ? P : CH0;
     __shared__ float sh_ss[16];
     __shared__ uint32_t sh_top[16];
-    griddep_launch_dependents();
     griddep_wait();
 
     const int tpr = p.tpr;
@@ -222,6 +221,8 @@ __global__ void __launch_bounds__(512) row_quant_kernel(const RowArgs p)
         }
     }
 
+    // the row is in: the next kernel may be scheduled now (allowed to start at once, its blocks pile up on the free SMs)
+    griddep_launch_dependents();
     float ss = 0.0f;
     if (OP == ROW_NORM) ss = warp_sum(pair_sum(ss2));
     uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(topf) & 0x7fffffffu);
@@ -320,8 +321,13 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st)
         QNN_CUDA(launch_pdl(row_quant_long_kernel<OP, T, W>, dim3((unsigned)p.rows), dim3(512), 0, st, p));
         return check_launch(what);
     }
-    // Few rows: as many threads a row as there are groups, for latency.  Many rows: two groups a thread.
-    int nv = (p.rows <= 2 * (int64_t)sm_count()) ? 1 : 2;
+    // Groups a thread.  Few rows: one, for latency.  Many rows: two while that gives blocks of at most 128 threads; small blocks
+    // stream best, so four for longer rows (norm, bf16, 8192 rows: K = 4096 48.7 against 50.9 us with two, K = 8192 92.3 against
+    // 107.6; 1200 rows of 4096 11.5 against 10.6, so there two), but not in fp32, whose loads need twice the registers
+    // (8192 x 4096: 80.7 against 76.3).
+    const int64_t sms = sm_count();
+    int nv = p.rows <= 2 * sms ? 1 : 2;
+    if (nv == 2 && sizeof(T) == 2 && (groups > 512 || (groups > 256 && p.rows >= 16 * sms))) nv = 4;
     while (groups > (int64_t)MAX_TPR * nv) nv *= 2;
     p.tpr = (int)(ceil_div(ceil_div(groups, nv), 32) * 32);
     const int rpb = p.tpr >= 128 ? 1 : 128 / p.tpr;      // rows of short vectors share a block
@@ -329,7 +335,18 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st)
     switch (nv) {
         case 1: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 1>, grid, block, 0, st, p)); break;
         case 2: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 2>, grid, block, 0, st, p)); break;
-        case 4: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4>, grid, block, 0, st, p)); break;
+        case 4:
+            if constexpr (OP == ROW_GATE && W == 8 && sizeof(T) == 2) {
+                // 64 registers a thread let 1024 threads of an SM run: two blocks of 384, a quarter of them idle.  56 let three
+                // run, at the price of a few spills (4096 x 12288 f16: 56.7 against 60.9 us; 8192 wide, where four blocks of
+                // 256 fit anyway, 38.1 against 36.4).
+                if (1024 / block.x * block.x < 820) {
+                    QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4, 56>, grid, block, 0, st, p));
+                    break;
+                }
+            }
+            QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4>, grid, block, 0, st, p));
+            break;
         default:
             if constexpr (W == 8) QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 8>, grid, block, 0, st, p));
             break;

@@ -22,7 +22,8 @@ namespace qnn {
 namespace {
 
 constexpr int MAX_TOP = 32;
-constexpr int CAND = 512;             // candidates a CTA can hold; more (masses of equal logits) take the slow exact path
+constexpr int MAX_CLUSTER = 8;        // CTAs that share a row
+constexpr int CAND = 256;             // candidates a CTA can hold; more (masses of equal logits) take the slow exact path
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float FAR = -1000.0f;       // e^-1000 is 0 in fp32
 constexpr uint32_t INF_BITS = 0x7f800000u;
@@ -249,18 +250,18 @@ struct ScoreArgs {
 
 __device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t peer_addr(const void *p, uint32_t rank) { return map_to_cta(smem_u32(p), rank); }
-__device__ __forceinline__ float peer_f32(uint32_t a)
+// asynchronous stores into another CTA's shared memory that report their bytes to a barrier there
+__device__ __forceinline__ void send_u64(uint32_t a, unsigned long long v, uint32_t bar)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.u64 [%0], %1, [%2];" ::"r"(a), "l"(v), "r"(bar) : "memory");
 }
-__device__ __forceinline__ unsigned long long peer_u64(uint32_t a)
+__device__ __forceinline__ void send_f32x4(uint32_t a, float x, float y, float z, float w, uint32_t bar)
 {
-    unsigned long long v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-    return v;
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // THREADS threads add, one more warp loads.  Rows stream through a ring of STAGES chunks of THREADS * U granules in shared
 // memory, filled by bulk copies, so that what is in flight does not depend on how far the adding threads are.
@@ -268,18 +269,21 @@ template <int THREADS, int U, int STAGES>
 struct ScoreShared {
     static constexpr int CHUNK = THREADS * U;       // granules
     static constexpr int GL = THREADS / 32;         // lanes a group: 32 groups of threads
-    static_assert(GL >= 4 && GL <= 32 && MAX_TOP <= 32, "groups");
+    static_assert(GL >= 4 && GL <= 32 && MAX_TOP <= 32 && MAX_CLUSTER * MAX_TOP <= CAND, "groups");
     uint4 ring[STAGES][CHUNK];
     unsigned long long full[STAGES], empty[STAGES]; // barriers
     int abort_flag;
     int n_cand, n_one, n_all;
-    Stats mine;                                     // this CTA's statistics, read by the cluster's first CTA
+    // in the cluster's first CTA: what every CTA found -- its statistics and at most MAX_TOP keys, 0 = none
+    unsigned long long gathered;                    // barrier
+    alignas(16) float4 theirs[MAX_CLUSTER];
+    unsigned long long theirs_best[MAX_CLUSTER][MAX_TOP];
     alignas(16) uint32_t group[32];                 // largest element of each group of threads, as order keys
     float2 part[THREADS / 32];                      // s and u of each warp
     uint32_t one[THREADS];                          // threads that hold candidates in one chunk: chunk * THREADS + thread
     uint32_t all[THREADS];                          // ... perhaps in several
     unsigned long long best[MAX_TOP];               // this CTA's largest keys, falling; 0 = none
-    unsigned long long cand[CAND];
+    alignas(16) unsigned long long cand[CAND];
     unsigned long long round_best[THREADS / 32];
 };
 
@@ -290,11 +294,14 @@ __device__ __forceinline__ void rank_candidates(const unsigned long long *cand, 
 {
     for (int c = threadIdx.x; c < n; c += THREADS) {
         const unsigned long long k = cand[c];
-        if (k == 0ull) continue;
         int rank = 0;
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) rank += cand[j] > k;
-        if (rank < topk) put(rank, k);
+        for (int j = 0; j + 1 < n; j += 2) {
+            const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(cand + j);
+            rank += (int)(o.x > k) + (int)(o.y > k);
+        }
+        if ((n & 1) && cand[n - 1] > k) ++rank;
+        if (rank < topk && k != 0ull) put(rank, k);
     }
 }
 
@@ -321,14 +328,19 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
     volatile int *abort_flag = &sh.abort_flag;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), THREADS / 32); }
+        mbar_init(smem_u32(&sh.gathered), 1);
         *abort_flag = 0;
         sh.n_cand = 0; sh.n_one = 0; sh.n_all = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
+        // what the CTAs of a cluster send to the first one
+        const uint32_t expected = cluster_size() * (16u + (p.topk > 0 ? 8u * MAX_TOP : 0u));
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(&sh.gathered)), "r"(expected) : "memory");
     }
     __syncthreads();
-    griddep_launch_dependents();
-    griddep_wait();
     const uint32_t csize = cluster_size(), crank = csize > 1 ? cluster_ctarank() : 0u;
+    if (csize > 1) cluster_arrive();                     // nothing is sent before the first CTA's barrier stands
+    griddep_wait();
     const int64_t t = blockIdx.x / csize;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const G row(static_cast<const T *>(p.logits) + t * p.ldl, p.V);
@@ -354,10 +366,7 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
                 for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies in flight land before shared memory is released
         }
         __syncwarp();
-        if (csize > 1) {                                 // the barriers of a cluster count every warp
-            cluster_sync_all();
-            cluster_sync_all();
-        }
+        if (csize > 1) cluster_wait();
         return;
     }
 
@@ -402,6 +411,9 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         second = fmaxf(second, fminf(before, b));
         if (b > before) best_chunk = chunk;
     }
+    // The row is in: the next kernel may be scheduled now.  (Allowed to start at once, its CTAs pile up on the SMs that are
+    // still free, several to one, and stay there.)
+    griddep_launch_dependents();
     // Granules that the row only shares with its neighbours: the head is thread 0's, the tail thread 1's, of the first
     // CTA.  (A row inside one granule is a head.)
     const bool head = row.first_full() > 0, tail = row.end_full() < row.count() && row.count() > row.first_full();
@@ -521,36 +533,54 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         }
     }
 
+    if (*abort_flag) {                                   // copies in flight land before shared memory is released
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
     if (csize > 1) {
-        if (tid == 0) sh.mine = a;
-        if (topk > 0 && !listed) {
+        // every CTA sends what it found to the first one, which goes on alone: at most MAX_TOP keys each
+        int n_mine = topk > 0 ? sh.n_cand : 0;
+        if (topk > 0 && !listed && n_mine > MAX_TOP) {
             if (tid < MAX_TOP) sh.best[tid] = 0ull;
             adders_sync<THREADS>();
-            rank_candidates<THREADS>(sh.cand, sh.n_cand, topk, [&](int rank, unsigned long long k) { sh.best[rank] = k; });
+            rank_candidates<THREADS>(sh.cand, n_mine, topk, [&](int rank, unsigned long long k) { sh.best[rank] = k; });
+            adders_sync<THREADS>();
+            listed = true;
         }
+        if (listed) n_mine = topk;
         __syncwarp();
-        cluster_sync_all();
-        if (crank == 0) {
-            for (int c = tid; c < (int)csize * topk; c += THREADS) {         // the CTAs' lists side by side
-                const int r = c / topk;
-                sh.cand[c] = peer_u64(peer_addr(&sh.best[c - r * topk], (uint32_t)r));
-            }
-            // every warp joins the CTAs' statistics: lane r reads those of CTA r (their number is a power of two)
-            const uint32_t at = peer_addr(&sh.mine, (uint32_t)lane & (csize - 1));
-            a = {peer_f32(at), peer_f32(at + 4), peer_f32(at + 8)};
-            for (uint32_t o = 1; o < csize; o <<= 1) {
-                Stats b;
-                b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-                b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-                b.u = __shfl_xor_sync(0xffffffffu, a.u, o);
-                a = (lane & o) ? join(b, a) : join(a, b);    // (the same order on both sides: all lanes hold the same bits)
-            }
+        cluster_wait();
+        const uint32_t bar = peer_addr(&sh.gathered, 0);
+        if (warp == 0) {
+            if (topk > 0) send_u64(peer_addr(&sh.theirs_best[crank][lane], 0), lane < n_mine ? (listed ? sh.best[lane] : sh.cand[lane]) : 0ull, bar);
+            if (lane == 0) send_f32x4(peer_addr(&sh.theirs[crank], 0), a.m, a.s, a.u, 0.0f, bar);
         }
+        if (crank != 0) return;
+        (void)mbar_wait(smem_u32(&sh.gathered), 0, abort_flag, 23);
         __syncwarp();
-        cluster_sync_all();                              // nobody leaves while its shared memory is being read
+        // every warp joins the CTAs' statistics: lane r holds those of CTA r (their number is a power of two)
+        const float4 theirs = sh.theirs[lane & (csize - 1)];
+        a = {theirs.x, theirs.y, theirs.z};
+        for (uint32_t o = 1; o < csize; o <<= 1) {
+            Stats b;
+            b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+            b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+            b.u = __shfl_xor_sync(0xffffffffu, a.u, o);
+            a = (lane & o) ? join(b, a) : join(a, b);    // (the same order on both sides: all lanes hold the same bits)
+        }
         listed = false;
-        if (crank == 0) {
-            if (tid == 0) sh.n_cand = (int)csize * topk;
+        if (topk > 0) {
+            // their keys side by side, in any order
+            adders_sync<THREADS>();                      // (this CTA's own candidates have been sent)
+            if (tid == 0) sh.n_cand = 0;
+            adders_sync<THREADS>();
+            for (uint32_t r = warp; r < csize; r += THREADS / 32) {
+                const unsigned long long k = sh.theirs_best[r][lane];
+                const uint32_t have = __ballot_sync(0xffffffffu, k != 0ull);
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&sh.n_cand, __popc(have));
+                at = __shfl_sync(0xffffffffu, at, 0);
+                if (k != 0ull) sh.cand[at + __popc(have & ((1u << lane) - 1u))] = k;
+            }
             adders_sync<THREADS>();
         }
     }
@@ -574,9 +604,6 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         } else if (topk > 0) {
             rank_candidates<THREADS>(sh.cand, sh.n_cand, topk, put);
         }
-    }
-    if (*abort_flag) {
-        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
 }
 
@@ -721,8 +748,14 @@ template <typename T>
 int launch_scores(const ScoreArgs &p, cudaStream_t st)
 {
     const int64_t granules = (int64_t)p.V / Granules<T>::E + 1;
+    // CTAs a row (128000 bf16 with 5 alternatives, 1 / 2 / 4 / 8 CTAs): 16 rows 13.6 / 10.0 / 8.0 / 7.4 us, 33 rows 13.9 / 10.0 /
+    // 8.5 / 9.5, 64 rows 14.1 / 10.5 / 9.6 / 10.8, 100 rows 14.2 / 12.5 / 13.3 / 16.3, 296 rows 24.2 / 21.8 / 28.8, 400 rows
+    // 28.5 / 31.4: two while they fit the SMs at four each, four at two each, eight at one each.  A CTA's part stays long
+    // enough for its threads to have work.
+    const int64_t sms = sm_count();
     int cluster = 1;
-    while (cluster < 8 && p.T * cluster * 2 <= 2 * (int64_t)sm_count() && granules / (cluster * 2) >= 512) cluster *= 2;
+    for (int c = 2; c <= MAX_CLUSTER; c *= 2)
+        if (p.T * c <= sms * 8 / c && granules / c >= 512) cluster = c;
     // Threads a CTA: more rows at a time where rows are short (2048 x 16384 bf16 with 8 alternatives: 128 threads 24 us, 256
     // threads 31 us), shorter rows' ends where they are long (2048 x 131072: 100 and 99 us, 4 x 128000: 22 and 15 us).
     if (granules <= 4096) return launch_scores_cfg<T, 128, 4, 3, 7>(p, cluster, st);
