@@ -170,7 +170,7 @@ __device__ __forceinline__ float warp_sum(float v)
 
 // A row of at most 8 * NV * tpr elements in registers: tpr threads own pieces of W elements, interleaved, so that a
 // warp's accesses are contiguous.  W divides K; W = 8 needs 16-byte aligned rows, W = 2 aligned pairs, W = 1 nothing.
-// (A kernel that also took rows ending inside a piece spent 41 instructions an element instead of 18 on the 8192 x 4096
+// (A kernel that also took rows ending inside a piece spent 41 instructions an element instead of 27 on the 8192 x 4096
 // norm: the element-wise ends of every load and store are predicated, not branched around.)
 template <int OP, typename T, int W, int NV, int MAXREG = 128>
 __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(const RowArgs p)

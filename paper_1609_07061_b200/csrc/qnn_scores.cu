@@ -269,7 +269,7 @@ template <int THREADS, int U, int STAGES>
 struct ScoreShared {
     static constexpr int CHUNK = THREADS * U;       // granules
     static constexpr int GL = THREADS / 32;         // lanes a group: 32 groups of threads
-    static_assert(GL >= 4 && GL <= 32 && MAX_TOP <= 32 && MAX_CLUSTER * MAX_TOP <= CAND, "groups");
+    static_assert(GL >= 2 && GL <= 32 && MAX_TOP <= 32 && MAX_CLUSTER * MAX_TOP <= CAND, "groups");
     uint4 ring[STAGES][CHUNK];
     unsigned long long full[STAGES], empty[STAGES]; // barriers
     int abort_flag;
@@ -756,10 +756,12 @@ int launch_scores(const ScoreArgs &p, cudaStream_t st)
     int cluster = 1;
     for (int c = 2; c <= MAX_CLUSTER; c *= 2)
         if (p.T * c <= sms * 8 / c && granules / c >= 512) cluster = c;
-    // Threads a CTA: more rows at a time where rows are short (2048 x 16384 bf16 with 8 alternatives: 128 threads 24 us, 256
-    // threads 31 us), shorter rows' ends where they are long (2048 x 131072: 100 and 99 us, 4 x 128000: 22 and 15 us).
-    if (granules <= 4096) return launch_scores_cfg<T, 128, 4, 3, 7>(p, cluster, st);
-    return launch_scores_cfg<T, 256, 4, 3, 4>(p, cluster, st);
+    // Threads a CTA: fewer a row, and so more rows on an SM, where rows are short and many -- the joins cost instructions in
+    // every warp.  bf16, 8 alternatives: 4096 x 2000 with 64 / 128 threads 14.7 / 21.9 us, 3519 x 6784 22.0 / 25.3, but
+    // 200 x 6784 7.0 / 6.1; with 128 / 256 threads 4329 x 37184 (20 alternatives) 87.4 / 91.7, 2048 x 131072 97.1 / 95.5.
+    if (cluster > 1 || granules > 8192) return launch_scores_cfg<T, 256, 4, 3, 4>(p, cluster, st);
+    if (granules <= 1024 && p.T > 7 * sms) return launch_scores_cfg<T, 64, 4, 3, 12>(p, cluster, st);
+    return launch_scores_cfg<T, 128, 4, 2, 8>(p, cluster, st);
 }
 
 template <typename T>
