@@ -51,6 +51,9 @@ struct WideCfg {
     static_assert(STAGES >= 3 && TMEM <= 512 && BN % CB == 0 && (2 * STAGES + 4) * 8 + 8 <= 256, "configuration");
 };
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // 32 accumulator columns of one row -> scaled values; sb / bi: this block's channel scales and biases in shared memory
 __device__ __forceinline__ void scale32(const uint32_t (&v)[32], float sa, const float *sb, const float *bi, float (&f)[32])
 {
@@ -269,17 +272,14 @@ gemm_i8s_wide_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
                     __syncwarp();
                     const int rows = p.M - m0 < 32 ? (int)(p.M - m0) : 32;
                     TOUT *dst = static_cast<TOUT *>(p.out) + m0 * p.ldo + n0 + lane;
-#pragma unroll 8
-                    for (int r = 0; r < 32; ++r) {
-                        if (r < rows) {
+#pragma unroll (sizeof(TOUT) == 4 ? 8 : 4)
+                    for (int r = 0; r < rows; ++r, dst += p.ldo) {
 #pragma unroll
-                            for (int h = 0; h < S::CB / 32; ++h) {
-                                const int byte = (h * 32 + lane) * (int)sizeof(TOUT);
-                                const TOUT x = *reinterpret_cast<const TOUT *>(stg + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
-                                if (n0 + h * 32 + lane < p.N) dst[h * 32] = x;
-                            }
+                        for (int h = 0; h < S::CB / 32; ++h) {
+                            const int byte = (h * 32 + lane) * (int)sizeof(TOUT);
+                            const TOUT x = *reinterpret_cast<const TOUT *>(stg + r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15));
+                            if (n0 + h * 32 + lane < p.N) dst[h * 32] = x;
                         }
-                        dst += p.ldo;
                     }
                     __syncwarp();
                 }
@@ -317,13 +317,19 @@ struct NarrowCfg {
     static constexpr int A_BYTES = BM * BKB;                            // weights
     static constexpr int B_BYTES = BN * BKB;                            // tokens
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-    // two CTAs fit an SM: one CTA's set-up and join overlap the other's stream of weights
-    static constexpr int STAGES = (108 * 1024) / STAGE_BYTES > 6 ? 6 : (108 * 1024) / STAGE_BYTES;
-    static constexpr int BAR_OFFSET = STAGES * STAGE_BYTES;
+    // How the partial sums of a cluster meet.  Up to 16 tokens every thread sends its few to the CTA that joins them, which
+    // waits on a barrier of its own: no cluster-wide barrier after the products (16 x 4096 x 4096: 5.1 us against 5.6 us).  With
+    // more tokens the stores are too many (100 tokens: 10.2 against 8.5 us): sums go to shared memory, over the operand
+    // stages, and are read from there in 16-byte pieces.
+    static constexpr bool PUSH = BN == 16;
+    // two CTAs fit an SM: one's set-up and join overlap the other's stream of weights
+    static constexpr int STAGES = BN == 16 ? 5 : (108 * 1024) / STAGE_BYTES > 6 ? 6 : (108 * 1024) / STAGE_BYTES;
+    static constexpr int JOIN_OFFSET = STAGES * STAGE_BYTES;
+    static constexpr int BAR_OFFSET = JOIN_OFFSET + (PUSH ? BM * BN * 4 : 0);
     static constexpr int TOTAL = BAR_OFFSET + 128 + 1024;
     static constexpr int TMEM = tmem_cols(BN);
-    static_assert(STAGES * STAGE_BYTES >= BN * BM * 4, "the partial sums reuse the stages");
-    static_assert((2 * STAGES + 1) * 8 + 8 <= 128, "barriers");
+    static_assert(PUSH || STAGES * STAGE_BYTES >= BN * BM * 4, "the partial sums reuse the stages");
+    static_assert((2 * STAGES + 2) * 8 + 8 <= 128 && 2 * (TOTAL + 1024) <= 228 * 1024, "configuration");
 };
 
 __device__ __forceinline__ int4 ld_peer_i32x4(uint32_t addr)
@@ -332,13 +338,34 @@ __device__ __forceinline__ int4 ld_peer_i32x4(uint32_t addr)
     asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
+// asynchronous store of W int32 into another CTA's shared memory that reports its bytes to a barrier there
+template <int W>
+__device__ __forceinline__ void send_i32(uint32_t addr, const uint32_t *v, uint32_t bar)
+{
+    if constexpr (W == 4)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                     ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(bar) : "memory");
+    else
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];"
+                     ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
 
 template <int BN, typename TOUT, int SPLIT>
 __global__ void __launch_bounds__(NARROW_THREADS, 2)
 gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const I8sParams p)
 {
-    constexpr int split = SPLIT;
     using S = NarrowCfg<BN>;
+    constexpr int split = SPLIT;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -347,20 +374,30 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     auto full_bar = [&](int s) { return bar0 + 8u * (uint32_t)s; };
     auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(S::STAGES + s); };
     const uint32_t done_bar = bar0 + 8u * (uint32_t)(2 * S::STAGES);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 1));
+    const uint32_t join_bar = done_bar + 8u;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 2));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x % (uint32_t)split;                // = the CTA's rank in its cluster
     const uint32_t tile = blockIdx.x / (uint32_t)split;
     const int32_t tn = (int32_t)(tile % (uint32_t)p.tiles_n), tm = (int32_t)(tile / (uint32_t)p.tiles_n);
     const int32_t kb0 = (int32_t)((int64_t)p.num_kb * rank / split), kb1 = (int32_t)((int64_t)p.num_kb * (rank + 1) / split);
+    const int32_t nt = p.M - (int64_t)tm * BN < BN ? (int32_t)(p.M - (int64_t)tm * BN) : BN;   // tokens of this tile
+    // (PUSH) CTA r of a cluster joins tokens r * TPO .. r * TPO + TPO - 1, W of them to a store
+    constexpr int TPO = BN / SPLIT, W = TPO < 4 ? TPO : 4;
+    const int32_t own = nt - (int32_t)rank * TPO;                      // ... of which it has this many
+    const int32_t own_groups = own <= 0 ? 0 : own >= TPO ? TPO / W : (own + W - 1) / W;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
         mbar_init(done_bar, 1);
+        mbar_init(join_bar, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        // what the CTAs of the cluster send here
+        if (S::PUSH && SPLIT > 1)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(join_bar), "r"((uint32_t)(SPLIT * BM * own_groups * W * 4)) : "memory");
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(tmem_slot), S::TMEM);
     if (warp == 2 && lane < 2)
@@ -369,11 +406,10 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    if (S::PUSH && SPLIT > 1) cluster_arrive();                        // nothing is sent before every CTA's barrier stands
     griddep_launch_dependents();                                       // (after the allocation, as above)
     griddep_wait();
 
-    const int32_t nt = p.M - (int64_t)tm * BN < BN ? (int32_t)(p.M - (int64_t)tm * BN) : BN;   // tokens of this tile
-    int32_t *part = reinterpret_cast<int32_t *>(gen);                  // [token][128 channels], over the operand stages
     bool ok = true;
     if (warp == 0) {
         if (lane == 0) {
@@ -408,35 +444,62 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             tc_fence_after();
             const int n_local = q * 32 + lane;
             const int64_t n = (int64_t)tn * BM + n_local;
-            const float sb = (split == 1 && n < p.N) ? __ldg(p.b_scale + n) : 0.0f;
-            const float bi = (split == 1 && n < p.N && p.bias) ? __ldg(p.bias + n) : 0.0f;
+            const float sb = n < p.N ? __ldg(p.b_scale + n) : 0.0f, bi = n < p.N && p.bias ? __ldg(p.bias + n) : 0.0f;
+            auto store = [&](int j, int32_t sum) {               // token j of the tile, this thread's channel
+                const int64_t m = (int64_t)tm * BN + j;
+                if (n < p.N) from_float(fmaf(__int2float_rn(sum) * __ldg(p.a_scale + m), sb, bi), static_cast<TOUT *>(p.out)[m * p.ldo + n]);
+            };
+            if (S::PUSH && SPLIT > 1) cluster_wait();
+            int32_t *dump = reinterpret_cast<int32_t *>(gen);    // (not PUSH) [token][128 channels], over the operand stages
 #pragma unroll 1
             for (int c = 0; c < nt; c += 16) {
                 uint32_t v[16];
-                asm volatile(
-                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-                    "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                    : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
-                      "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-                    : "r"(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c) : "memory");
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
+                if (SPLIT == 1) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (c + j < nt) {
-                        if (split > 1) {
-                            part[(c + j) * BM + n_local] = (int32_t)v[j];
-                        } else if (n < p.N) {
-                            const int64_t m = (int64_t)tm * BN + c + j;
-                            const float f = fmaf(__int2float_rn((int32_t)v[j]) * __ldg(p.a_scale + m), sb, bi);
-                            from_float(f, static_cast<TOUT *>(p.out)[m * p.ldo + n]);
-                        }
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < nt) store(c + j, (int32_t)v[j]);
+                } else if constexpr (!S::PUSH) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < nt) dump[(c + j) * BM + n_local] = (int32_t)v[j];
+                } else {
+                    // W tokens of this channel to the CTA that joins them: [sender][group of W tokens][channel][W]
+#pragma unroll
+                    for (int g = 0; g < 16; g += W) {
+                        const int j = c + g, owner = j / TPO;
+                        if (j < nt)
+                            send_i32<W>(map_to_cta(base + (uint32_t)(S::JOIN_OFFSET + (((int)rank * (TPO / W) + (j - owner * TPO) / W) * BM + n_local) * W * 4), (uint32_t)owner),
+                                        v + g, map_to_cta(join_bar, (uint32_t)owner));
+                    }
+                }
+            }
+            if (S::PUSH && SPLIT > 1 && own_groups > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait(join_bar, 0, abort_flag, 18));
+                const int32_t *part = reinterpret_cast<const int32_t *>(gen + S::JOIN_OFFSET) + n_local * W;
+                for (int g = 0; g < own_groups && ok; ++g) {
+                    int32_t sum[W];
+#pragma unroll
+                    for (int i = 0; i < W; ++i) sum[i] = 0;
+#pragma unroll
+                    for (int r = 0; r < SPLIT; ++r) {
+                        alignas(16) int32_t x[W];
+                        if constexpr (W == 4) *reinterpret_cast<int4 *>(x) = *reinterpret_cast<const int4 *>(part + (r * (TPO / W) + g) * BM * W);
+                        else *reinterpret_cast<int2 *>(x) = *reinterpret_cast<const int2 *>(part + (r * (TPO / W) + g) * BM * W);
+#pragma unroll
+                        for (int i = 0; i < W; ++i) sum[i] += x[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const int j = (int)rank * TPO + g * W + i;
+                        if (j < nt) store(j, sum[i]);
                     }
                 }
             }
         }
     }
     __syncwarp();
-    if (split > 1) {
+    if (!S::PUSH && SPLIT > 1) {
         // every CTA of the cluster reaches both barriers, whatever became of its waits
         cluster_sync_all();
         if (warp >= 2 && ok) {
@@ -450,7 +513,7 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             }
 #pragma unroll 2
             for (int j = (int)rank + (warp - 2) * split; j < nt; j += 4 * split) {
-                const uint32_t at = smem_u32(part + j * BM + 4 * lane);
+                const uint32_t at = base + (uint32_t)((j * BM + 4 * lane) * 4);
                 const int64_t m = (int64_t)tm * BN + j;
                 const float sa = __ldg(p.a_scale + m);
                 int4 v[SPLIT];
@@ -775,15 +838,13 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
                             static_cast<TOUT *>(p.out), p.ldo));
         return check_launch("qnn_gemm_i8_scaled");
     }
-    // A handful of tokens: the weights go through the integer units.  One or two tokens always (4096 x 4096: 3.3 us against
-    // 5.3 us on the tensor cores, 16384 x 4096: 12.3 against 14.6 us); up to four while the weights are at most 32 MB
-    // (4096 x 4096: 3.6 against 5.4, 11008 x 2048: 5.5 against 6.0, but 16384 x 4096: 20.3 against 14.8), up to eight while
-    // they are at most 8 MB (1024 x 8192: 3.9 against 5.1, but 4096 x 4096: 5.9 against 5.4).
-    const int64_t weights = p.N * c.K;
+    // A handful of tokens: the weights go through the integer units.  One or two tokens always (4096 x 4096: 3.4 us against
+    // 4.9 us on the tensor cores, 16384 x 4096: 12.3 against 14.6 us), up to four while the weights are at most 32 MB
+    // (4096 x 4096: 3.6 against 4.9, 11008 x 2048: 5.3 against 5.7, but 16384 x 4096: 20.3 against 14.8; with eight tokens
+    // 4096 x 4096 takes 5.9 us).
     if (p.M == 1) return launch_gemv<1, 2, 4, TOUT>(c, p, st);
     if (p.M == 2) return launch_gemv<2, 2, 4, TOUT>(c, p, st);
-    if (p.M <= 4 && weights <= (int64_t)32 << 20) return launch_gemv<4, 4, 4, TOUT>(c, p, st);
-    if (p.M <= 8 && weights <= (int64_t)8 << 20) return launch_gemv<8, 4, 1, TOUT>(c, p, st);
+    if (p.M <= 4 && p.N * c.K <= (int64_t)32 << 20) return launch_gemv<4, 4, 4, TOUT>(c, p, st);
 
     // On the tensor cores the time of a launch is, within about 10 % over M = 16 .. 4096, N = 1024 .. 16384, K = 1024 .. 8192,
     //   start + waves * (K blocks a CTA walks * time of a block + hand-over)      (us, fitted to the sweep)
