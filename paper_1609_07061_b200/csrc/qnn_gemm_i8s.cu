@@ -838,20 +838,26 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
                             static_cast<TOUT *>(p.out), p.ldo));
         return check_launch("qnn_gemm_i8_scaled");
     }
-    // A handful of tokens: the weights go through the integer units.  One or two tokens always (4096 x 4096: 3.4 us against
-    // 4.9 us on the tensor cores, 16384 x 4096: 12.3 against 14.6 us), up to four while the weights are at most 32 MB
-    // (4096 x 4096: 3.6 against 4.9, 11008 x 2048: 5.3 against 5.7, but 16384 x 4096: 20.3 against 14.8; with eight tokens
-    // 4096 x 4096 takes 5.9 us).
-    if (p.M == 1) return launch_gemv<1, 2, 4, TOUT>(c, p, st);
-    if (p.M == 2) return launch_gemv<2, 2, 4, TOUT>(c, p, st);
-    if (p.M <= 4 && p.N * c.K <= (int64_t)32 << 20) return launch_gemv<4, 4, 4, TOUT>(c, p, st);
+    // A handful of tokens: the weights go through the integer units.  One token always (4096 x 4096: 3.4 us against 4.9 us on the
+    // tensor cores, 28672 x 4096: 20.9 against 21.4; rows of at most 1024 codes four to a warp: 131072 x 1024 22.7 against
+    // 30.5 us two to a warp).  Two to four tokens while the weights are at most 32 MB (two: 4096 x 4096 3.8 against 4.9, but
+    // 131072 x 1024 34.4 against 29.2; four: 4096 x 4096 3.6 against 4.9, 11008 x 2048 5.3 against 5.7, but 16384 x 4096 20.3
+    // against 14.8), three and four not for the shortest rows (16384 x 512: 4.8 against 4.0).  Eight tokens: 5.9 us for 4096 x
+    // 4096.
+    if (p.M == 1) return c.K <= 1024 ? launch_gemv<1, 4, 1, TOUT>(c, p, st) : launch_gemv<1, 2, 4, TOUT>(c, p, st);
+    if (p.M <= 4 && p.N * c.K <= (int64_t)32 << 20) {
+        if (p.M == 2) return launch_gemv<2, 4, 1, TOUT>(c, p, st);
+        if (c.K >= 1024) return launch_gemv<4, 4, 4, TOUT>(c, p, st);
+    }
 
-    // On the tensor cores the time of a launch is, within about 10 % over M = 16 .. 4096, N = 1024 .. 16384, K = 1024 .. 8192,
-    //   start + waves * (K blocks a CTA walks * time of a block + hand-over)      (us, fitted to the sweep)
+    // On the tensor cores the time of a launch is, within about 15 % over M = 3 .. 4096, N = 128 .. 131072, K = 128 .. 16384,
+    //   wide    start + waves * (K blocks * block + hand-over)
+    //   narrow  waves * start + (K blocks of a CTA) * max(block, CTAs an SM * stream) + hand-over      (us, fitted to sweeps)
     // with the constants below; the cheapest configuration runs.  100 x 4096 x 4096: narrow 8.6, wide 64 columns 9.2;
-    // 100 x 11008 x 2048: narrow 10.0, wide 128 columns 7.7; 701 x 2047 x 1111: wide 64 columns 8.2, 128 columns 6.6, pairs of
-    // 256 columns 9.2; 701 x 4096 x 4096: 22.8, 19.8, and pairs of 128 / 192 / 256 columns 18.1 / 13.2 / 15.1.
-    struct Config { int rows, cols; float start, block, hand; };
+    // 100 x 11008 x 2048: narrow 10.0, wide 128 columns 7.7; 16 x 131072 x 4096: narrow 85, wide 116 .. 200; 701 x 2047 x 1111:
+    // wide 64 columns 8.2, 128 columns 6.6, pairs of 256 columns 9.2; 701 x 4096 x 4096: 22.8, 19.8, and pairs of 128 / 192 / 256
+    // columns 18.1 / 13.2 / 15.1.
+    struct Config { int rows, cols; float start, block, hand; };            // us
     static const Config wide[] = {{128, 64, 3.2f, 0.21f, 0.1f}, {128, 128, 3.7f, 0.27f, 0.2f}, {256, 128, 4.2f, 0.235f, 0.3f},
                                   {256, 192, 4.8f, 0.285f, 0.5f}, {256, 256, 5.5f, 0.34f, 0.7f}};
     const int sms = sm_count(), pairs = pairs_resident();
@@ -865,15 +871,24 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
         if (best < 0 || t < cost) { best = i; cost = t; }
     }
     {
-        // narrow tiles, K cut until the CTAs are about one for every SM: few tokens, or few channels and a long K
-        static const Config narrow[] = {{16, 0, 3.0f, 0.28f, 0.5f}, {32, 0, 3.5f, 0.29f, 0.6f}, {64, 0, 4.4f, 0.31f, 0.8f}, {128, 0, 5.5f, 0.36f, 1.2f}};
+        // narrow tiles, K cut until the CTAs are about one for every SM: few tokens, or few channels and a long K.  The weights
+        // (and with many CTAs an SM nothing else) set the pace; wide tiles stream them less well, which counts when all that
+        // there is to do is to stream them.
+        struct Narrow { int cols; float start, block, stream, hand; };
+        static const Narrow narrow[] = {{16, 3.0f, 0.28f, 0.34f, 0.3f}, {32, 3.5f, 0.29f, 0.34f, 0.6f}, {64, 4.4f, 0.31f, 0.38f, 0.8f},
+                                        {128, 5.5f, 0.36f, 0.42f, 1.2f}};
         const int i = p.M <= 16 ? 0 : p.M <= 32 ? 1 : p.M <= 64 ? 2 : 3;
-        const int64_t tiles = ceil_div(p.N, BM) * ceil_div(p.M, narrow[i].rows);
+        const int64_t tiles = ceil_div(p.N, BM) * ceil_div(p.M, narrow[i].cols);
         int split = 1;
         while (split < 8 && tiles * split * 2 <= (int64_t)sms * 5 / 4 && p.num_kb / (split * 2) >= 2) split *= 2;
         const int64_t ctas = tiles * split;
-        const float t = (float)ceil_div(ctas, 2 * sms) * (narrow[i].start + narrow[i].block * (float)ceil_div(p.num_kb, split) * (ctas > sms ? 1.4f : 1.0f)) +
-                        (split > 1 ? narrow[i].hand : 0.0f);
+        const float an_sm = (float)ctas / (float)sms * narrow[i].stream;
+        const float t = (float)ceil_div(ctas, 2 * sms) * narrow[i].start +
+                        (float)ceil_div(p.num_kb, split) * (an_sm > narrow[i].block ? an_sm : narrow[i].block) + (split > 1 ? narrow[i].hand : 0.0f);
+        if (p.M <= 128) {
+            const float stream = 4.0f + 1.35f * (float)(p.N * c.K) * 1e-6f / 6.5f;   // (6.5 MB a us)
+            if (cost < stream) cost = stream;
+        }
         if (t < cost) {
             switch (i) {
                 case 0: return launch_narrow<16, TOUT>(c, p, split, st);
