@@ -269,14 +269,28 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     const int64_t step = (int64_t)blockDim.x * W;
     f32x2 ss2 = 0ull;
     float topf = 0.0f;
-    for (int64_t k0 = (int64_t)threadIdx.x * W; k0 < p.K; k0 += step) {
-        Piece<T, W> xv, bv;
-        float s[W], t[W];
-        load_piece<T, W>(xr + k0, xv);
-        if (with_b) load_piece<T, W>(br + k0, bv);
-        row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, ss2);
+    // CH pieces a round, their loads in flight together
+    constexpr int CH = 2;
+    for (int64_t k = (int64_t)threadIdx.x * W; k < p.K; k += CH * step) {
+        Piece<T, W> xv[CH], bv[CH];
 #pragma unroll
-        for (int i = 0; i < W; ++i) topf = max_nan(topf, fabsf(t[i]));
+        for (int c = 0; c < CH; ++c) {
+            const int64_t k0 = k + c * step;
+            if (k0 < p.K) {
+                load_piece<T, W>(xr + k0, xv[c]);
+                if (with_b) load_piece<T, W>(br + k0, bv[c]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t k0 = k + c * step;
+            if (k0 < p.K) {
+                float s[W], t[W];
+                row_op<OP, T, W>(p, xv[c], bv[c], (int32_t)k0, s, t, ss2);
+#pragma unroll
+                for (int i = 0; i < W; ++i) topf = max_nan(topf, fabsf(t[i]));
+            }
+        }
     }
     float ss = 0.0f;
     if (OP == ROW_NORM) ss = warp_sum(pair_sum(ss2));
@@ -289,23 +303,34 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
     if (threadIdx.x == 0) p.scale[row] = r.scale;
     uint8_t *cr = p.codes + row * p.ldq;
-    for (int64_t k0 = (int64_t)threadIdx.x * W; k0 < p.KP; k0 += step) {
-        float s[W], t[W], f[W];
-        f32x2 unused = 0ull;
+    for (int64_t k = (int64_t)threadIdx.x * W; k < p.KP; k += CH * step) {
+        Piece<T, W> xv[CH], bv[CH];
 #pragma unroll
-        for (int i = 0; i < W; ++i) t[i] = 0.0f;
-        if (k0 < p.K) {
-            Piece<T, W> xv, bv;
-            load_piece<T, W>(xr + k0, xv);
-            if (with_b) load_piece<T, W>(br + k0, bv);
-            row_op<OP, T, W>(p, xv, bv, (int32_t)k0, s, t, unused);
-            if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
+        for (int c = 0; c < CH; ++c) {
+            const int64_t k0 = k + c * step;
+            if (k0 < p.K) {
+                load_piece<T, W>(xr + k0, xv[c]);
+                if (with_b) load_piece<T, W>(br + k0, bv[c]);
+            }
         }
-        to_codes<W>(t, r.inv, f);
-        store_codes<W>(cr + k0, f, r.keep);
-        if (p.values != nullptr && k0 < p.K) {
-            to_values<W>(f, r.scale);
-            store_values<W>(p, row, (int32_t)k0, f);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int64_t k0 = k + c * step;
+            if (k0 >= p.KP) break;
+            float s[W], t[W], f[W];
+            f32x2 unused = 0ull;
+#pragma unroll
+            for (int i = 0; i < W; ++i) t[i] = 0.0f;
+            if (k0 < p.K) {
+                row_op<OP, T, W>(p, xv[c], bv[c], (int32_t)k0, s, t, unused);
+                if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
+            }
+            to_codes<W>(t, r.inv, f);
+            store_codes<W>(cr + k0, f, r.keep);
+            if (p.values != nullptr && k0 < p.K) {
+                to_values<W>(f, r.scale);
+                store_values<W>(p, row, (int32_t)k0, f);
+            }
         }
     }
 }
@@ -315,9 +340,11 @@ constexpr int MAX_TPR = 512;
 template <int OP, typename T, int W>
 int launch_rows(RowArgs p, const char *what, cudaStream_t st)
 {
-    constexpr int MAX_NV = W == 8 ? 8 : 4;               // (narrow accesses need more registers an element)
+    // (narrow accesses: more instructions an element, so long rows take the rolled loops of the other kernel)
+    constexpr int MAX_NV = W == 8 ? 8 : 2;
+    constexpr int64_t MAX_GROUPS = W == 8 ? (int64_t)MAX_TPR * MAX_NV : W == 2 ? 1024 : 256;
     const int64_t groups = ceil_div(p.KP, 8);            // a row in units of eight elements
-    if (groups > (int64_t)MAX_TPR * MAX_NV) {
+    if (groups > MAX_GROUPS) {
         QNN_CUDA(launch_pdl(row_quant_long_kernel<OP, T, W>, dim3((unsigned)p.rows), dim3(512), 0, st, p));
         return check_launch(what);
     }
@@ -327,7 +354,7 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st)
     // (8192 x 4096: 80.7 against 76.3).
     const int64_t sms = sm_count();
     int nv = p.rows <= 2 * sms ? 1 : 2;
-    if (nv == 2 && sizeof(T) == 2 && (groups > 512 || (groups > 256 && p.rows >= 16 * sms))) nv = 4;
+    if (nv == 2 && W == 8 && sizeof(T) == 2 && (groups > 512 || (groups > 256 && p.rows >= 16 * sms))) nv = 4;
     while (groups > (int64_t)MAX_TPR * nv) nv *= 2;
     p.tpr = (int)(ceil_div(ceil_div(groups, nv), 32) * 32);
     const int rpb = p.tpr >= 128 ? 1 : 128 / p.tpr;      // rows of short vectors share a block
@@ -345,7 +372,7 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st)
                     break;
                 }
             }
-            QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4>, grid, block, 0, st, p));
+            if constexpr (W == 8) QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4>, grid, block, 0, st, p));
             break;
         default:
             if constexpr (W == 8) QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 8>, grid, block, 0, st, p));
