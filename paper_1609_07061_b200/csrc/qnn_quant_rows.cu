@@ -36,7 +36,11 @@ struct RowArgs {
 // 1.5 * 2^23: t * inv + MAGIC rounds to a whole number (to even at ties) and leaves it in the low bits of the float
 constexpr float MAGIC = 12582912.0f;
 
-__device__ __forceinline__ float silu(float a) { return __fdividef(a, 1.0f + __expf(-a)); }
+// two to the power, and reciprocal, on the special-function unit; results below the normal range are 0
+__device__ __forceinline__ float exp2_sfu(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float rcp_sfu(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// a / (1 + e^-a): below a = -127 or so the sum is infinite and its reciprocal 0, the limit (but -inf gives -inf * 0, a NaN)
+__device__ __forceinline__ float silu(float a) { return a * rcp_sfu(1.0f + exp2_sfu(a * -1.4426950408889634f)); }
 
 // what the reduction leaves a thread with: the factor that turns t into codes, the scale, and a mask for the codes
 struct RowScale {
@@ -104,8 +108,18 @@ __device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, 
 #pragma unroll
         for (int i = 0; i < W; ++i) t[i] = x[i];
     } else if (OP == ROW_GATE) {
+        if constexpr (W == 1) {
+            t[0] = silu(x[0]) * b[0];
+        } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) t[i] = silu(x[i]) * b[i];
+            for (int i = 0; i < W; i += 2) {             // the same on pairs
+                const f32x2 a2 = pair(x[i], x[i + 1]);
+                float e0, e1, d0, d1;
+                unpair(mul2(a2, pair(-1.4426950408889634f, -1.4426950408889634f)), e0, e1);
+                unpair(add2(pair(exp2_sfu(e0), exp2_sfu(e1)), pair(1.0f, 1.0f)), d0, d1);
+                unpair(mul2(mul2(a2, pair(rcp_sfu(d0), rcp_sfu(d1))), pair(b[i], b[i + 1])), t[i], t[i + 1]);
+            }
+        }
     } else {
         float g[W];
         if (p.gamma != nullptr) {
