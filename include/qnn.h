@@ -596,8 +596,9 @@ QNN_API int qnn_silu_mul_quant_i8(const void *gate, const void *up, int type, in
 /* out[m,n] = (float(sum_k a[m,k] * b[n,k]) * a_scale[m]) * b_scale[n] + bias[n],
  * the sum exact in int32, the rest in fp32, rounded once to out_type.
  *   a, b      device, int8 [M, lda], [N, ldb] (any codes in -128..127): 16-byte
- *             aligned, lda and ldb multiples of 16 and >= K.  Bytes beyond K of a
- *             row are not read into the sum: pads need not be zero.
+ *             aligned, lda and ldb multiples of 16 and >= K.  Rows are read in
+ *             16-byte pieces, but what stands beyond K does not enter the sum: pads
+ *             need not be zero.
  *   a_scale   device, fp32 [M]; b_scale fp32 [N]; bias fp32 [N] or NULL
  *   out       device, [M, ldo] of out_type, ldo >= N; rows that are 16-byte
  *             aligned leave as bulk stores, others element by element
@@ -621,7 +622,7 @@ QNN_API int qnn_gemm_i8_scaled(const void *a, int64_t lda, const float *a_scale,
  * 0.  A NaN or a +inf makes the row's numbers NaN (top_ids stay valid, NaN first).
  * Statistics are held in fp32 relative to the running maximum, the sum of the
  * entropy as sum e^(z-m) (z-m), which has one sign and does not cancel.
- * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (V >= 2^31, topk > 32), CUDA. */
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (V > 2^30, T >= 2^28, topk > 32), CUDA. */
 QNN_API int qnn_token_logprobs(const void *logits, int type, int64_t T, int64_t V, int64_t ldl, const int64_t *ids,
                                float *logprob, float *entropy, float *lse, int topk, float *top_logprob,
                                int64_t *top_ids, void *stream);

@@ -61,17 +61,17 @@ struct Granules {
     {
         shift = (int32_t)((reinterpret_cast<uintptr_t>(r) & 15u) / sizeof(T));
     }
-    __device__ __forceinline__ int64_t count() const { return ((int64_t)V + shift + E - 1) / E; }
-    __device__ __forceinline__ int64_t first(int64_t g) const { return g * E - shift; }
+    __device__ __forceinline__ int32_t count() const { return (V + shift + E - 1) / E; }
+    __device__ __forceinline__ int32_t first(int32_t g) const { return g * E - shift; }
     // granules first_full() .. end_full() - 1 lie wholly inside the row
-    __device__ __forceinline__ int64_t first_full() const { return shift > 0; }
-    __device__ __forceinline__ int64_t end_full() const { return ((int64_t)V + shift) / E; }
-    __device__ __forceinline__ const uint4 *at(int64_t g) const { return reinterpret_cast<const uint4 *>(row + first(g)); }
+    __device__ __forceinline__ int32_t first_full() const { return shift > 0; }
+    __device__ __forceinline__ int32_t end_full() const { return (V + shift) / E; }
+    __device__ __forceinline__ const uint4 *at(int32_t g) const { return reinterpret_cast<const uint4 *>(row + first(g)); }
     // any granule: elements outside the row read as -inf and are not touched
-    __device__ __forceinline__ uint4 load(int64_t g) const
+    __device__ __forceinline__ uint4 load(int32_t g) const
     {
         if (g >= first_full() && g < end_full()) return *at(g);
-        const int64_t v0 = first(g);
+        const int32_t v0 = first(g);
         alignas(16) T t[E];
 #pragma unroll 1
         for (int i = 0; i < E; ++i) t[i] = (v0 + i >= 0 && v0 + i < V) ? row[v0 + i] : T(neg_inf());
@@ -345,20 +345,20 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const G row(static_cast<const T *>(p.logits) + t * p.ldl, p.V);
     // this CTA's whole granules of the row
-    int64_t g0, g1;
+    int32_t g0, g1;
     {
-        const int64_t f0 = row.first_full(), n = row.end_full() - f0, share = (n + csize - 1) / csize;
-        g0 = f0 + (share * crank < n ? share * crank : n);
-        g1 = f0 + (share * (crank + 1) < n ? share * (crank + 1) : n);
+        const int32_t f0 = row.first_full(), n = row.end_full() - f0, share = (n + (int32_t)csize - 1) / (int32_t)csize;
+        g0 = f0 + min(share * (int32_t)crank, n);
+        g1 = f0 + min(share * ((int32_t)crank + 1), n);
     }
     int stage = 0;
     uint32_t phase = 0;
 
     if (warp == THREADS / 32) {
         if (lane == 0) {
-            for (int64_t g = g0; g < g1; g += SH::CHUNK) {
+            for (int32_t g = g0; g < g1; g += SH::CHUNK) {
                 if (!mbar_wait(smem_u32(&sh.empty[stage]), phase ^ 1u, abort_flag, 21)) break;
-                const int64_t n = g1 - g < SH::CHUNK ? g1 - g : SH::CHUNK;
+                const int32_t n = min(g1 - g, SH::CHUNK);
                 bulk_load(smem_u32(sh.ring[stage]), row.at(g), (uint32_t)(n * 16), smem_u32(&sh.full[stage]));
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
@@ -381,10 +381,10 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
     Running run = {neg_inf(), 0ull, 0ull};
     float second = neg_inf();                        // the largest element outside this thread's best chunk
     uint32_t best_chunk = 0, chunk = 0;
-    for (int64_t g = g0; g < g1; g += SH::CHUNK, ++chunk) {
+    for (int32_t g = g0; g < g1; g += SH::CHUNK, ++chunk) {
         // (a wait that runs out raises the status word; the row is then finished on what the ring holds)
         (void)mbar_wait(smem_u32(&sh.full[stage]), phase, abort_flag, 22);
-        const int n = g1 - g < SH::CHUNK ? (int)(g1 - g) : SH::CHUNK;
+        const int n = min(g1 - g, SH::CHUNK);
         uint4 w[U];
         if (n == SH::CHUNK) {
 #pragma unroll
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
     // CTA.  (A row inside one granule is a head.)
     const bool head = row.first_full() > 0, tail = row.end_full() < row.count() && row.count() > row.first_full();
     const bool has_edge = crank == 0 && ((tid == 0 && head) || (tid == 1 && tail));
-    const int64_t edge = tid == 0 ? 0 : row.count() - 1;
+    const int32_t edge = tid == 0 ? 0 : row.count() - 1;
     if (has_edge) {
         const uint4 only[1] = {row.load(edge)};
         (void)add_granules<T, 1>(run, only);
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
 
     bool listed = false;                             // the keys stand in sh.best, not in sh.cand
     if (topk > 0) {
-        auto offer = [&](const uint4 &words, int64_t v0) {
+        auto offer = [&](const uint4 &words, int32_t v0) {
             float z[E];
             G::floats(words, z);
 #pragma unroll
@@ -483,14 +483,14 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         const int n_one = sh.n_one * U;
         for (int i = tid; i < n_one; i += THREADS) {
             const uint32_t e = sh.one[i / U], c = e / THREADS;
-            const int64_t g = g0 + (int64_t)c * SH::CHUNK + (i % U) * THREADS + (e - c * THREADS);
+            const int32_t g = g0 + (int32_t)(c * SH::CHUNK + (i % U) * THREADS + (e - c * THREADS));
             if (g < g1) offer(*row.at(g), row.first(g));
         }
         const uint32_t per = (uint32_t)((g1 - g0 + THREADS - 1) / THREADS);
-        const int64_t n_all = (int64_t)sh.n_all * per;
-        for (int64_t i = tid; i < n_all; i += THREADS) {
+        const uint32_t n_all = (uint32_t)sh.n_all * per;
+        for (uint32_t i = tid; i < n_all; i += THREADS) {
             const uint32_t f = (uint32_t)(i / per);
-            const int64_t g = g0 + sh.all[f] + (i - (int64_t)f * per) * THREADS;
+            const int32_t g = g0 + (int32_t)(sh.all[f] + (i - f * per) * THREADS);
             if (g < g1) offer(*row.at(g), row.first(g));
         }
         if (has_edge && order_key(mine) >= bound) offer(row.load(edge), row.first(edge));
@@ -503,17 +503,17 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
             unsigned long long last = ~0ull;
             for (int j = 0; j < topk; ++j) {
                 unsigned long long b = 0ull;
-                auto look = [&](const uint4 &words, int64_t v0) {
+                auto look = [&](const uint4 &words, int32_t v0) {
                     float z[E];
                     G::floats(words, z);
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        const int64_t v = v0 + i;
+                        const int32_t v = v0 + i;
                         const unsigned long long k = ((unsigned long long)order_key(z[i]) << 32) | (uint32_t)~(uint32_t)v;
                         if (v >= 0 && v < p.V && k < last && k > b) b = k;
                     }
                 };
-                for (int64_t g = g0 + tid; g < g1; g += THREADS) look(*row.at(g), row.first(g));
+                for (int32_t g = g0 + tid; g < g1; g += THREADS) look(*row.at(g), row.first(g));
                 if (has_edge) look(row.load(edge), row.first(edge));
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
@@ -616,6 +616,7 @@ struct ScoreGradArgs {
     void *d;
     int64_t ldd;
     uint32_t parts;                 // CTAs a row
+    int32_t span;                   // granules a CTA, whole rounds of GRAD_THREADS * GRAD_U
 };
 
 constexpr int GRAD_THREADS = 256, GRAD_U = 4;
@@ -655,21 +656,25 @@ __global__ void __launch_bounds__(GRAD_THREADS) scores_grad_kernel(const ScoreGr
     r.none = r.lse == neg_inf();
     r.c = fmaf(r.gh, r.h, r.gl);
     if (VEC) {
-        const int64_t all = row.count(), f0 = row.first_full(), f1 = row.end_full();
-        const int64_t base = (int64_t)part * (GRAD_THREADS * GRAD_U) + threadIdx.x;
-        uint4 w[GRAD_U];
-#pragma unroll
-        for (int j = 0; j < GRAD_U; ++j) {
-            const int64_t g = base + j * GRAD_THREADS;
-            if (g >= f0 && g < f1) w[j] = *row.at(g);
-        }
+        const int32_t f0 = row.first_full(), f1 = row.end_full();
+        // the token's place in the row; -E where there is none
+        const int32_t id = r.id >= 0 && r.id < p.V ? (int32_t)r.id : -E;
         const bool calm = calm_at<T>(r.lse) && fabsf(r.gh) < 1e15f && fabsf(r.c) < 1e15f;
         const f32x2 nlse = pair(-r.lse, -r.lse), l2e = pair(LOG2E, LOG2E), ngh = pair(-r.gh, -r.gh), nc = pair(-r.c, -r.c);
+        const int32_t g1 = min(f1, (int32_t)(part + 1) * p.span);
+#pragma unroll 1
+        for (int32_t base = (int32_t)part * p.span + (int32_t)threadIdx.x; base < g1; base += GRAD_THREADS * GRAD_U) {
+            uint4 w[GRAD_U];
 #pragma unroll
-        for (int j = 0; j < GRAD_U; ++j) {
-            const int64_t g = base + j * GRAD_THREADS;
-            const int64_t v0 = row.first(g);
-            if (g >= f0 && g < f1) {
+            for (int j = 0; j < GRAD_U; ++j) {
+                const int32_t g = base + j * GRAD_THREADS;
+                if (g >= f0 && g < g1) w[j] = *row.at(g);
+            }
+#pragma unroll
+            for (int j = 0; j < GRAD_U; ++j) {
+                const int32_t g = base + j * GRAD_THREADS;
+                if (g < f0 || g >= g1) continue;
+                const int32_t v0 = row.first(g);
                 float f[E];
                 if (calm) {
                     f32x2 z[E / 2];
@@ -681,7 +686,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) scores_grad_kernel(const ScoreGr
                         unpair(mul2(x, l2e), lo, hi);
                         unpair(mul2(pair(exp2_approx(lo), exp2_approx(hi)), fma2(ngh, x, nc)), f[2 * i], f[2 * i + 1]);
                     }
-                    const int64_t at = r.id - v0;
+                    const int32_t at = id - v0;
                     if (at >= 0 && at < E) {             // the token's own entry, unless it is masked
                         float z1[E];
                         G::floats(w[j], z1);
@@ -696,14 +701,18 @@ __global__ void __launch_bounds__(GRAD_THREADS) scores_grad_kernel(const ScoreGr
                 }
                 if constexpr (E == 8) store_floats<T, 8>(dst + v0, f);
                 else *reinterpret_cast<float4 *>(dst + v0) = make_float4(f[0], f[1], f[2], f[3]);
-            } else if (g < all) {                        // a granule the row only shares
-#pragma unroll 1
-                for (int64_t v = v0 < 0 ? 0 : v0; v < v0 + E && v < p.V; ++v) from_float(r.grad(to_float(row.row[v]), v), dst[v]);
             }
         }
+        // granules that the row only shares with its neighbours (a row inside one granule is a head)
+        const bool head = f0 > 0, tail = f1 < row.count() && row.count() > f0;
+        if (part == 0 && ((threadIdx.x == 0 && head) || (threadIdx.x == 1 && tail))) {
+            const int32_t v0 = row.first(threadIdx.x == 0 ? 0 : row.count() - 1);
+#pragma unroll 1
+            for (int32_t v = max(v0, 0); v < v0 + E && v < p.V; ++v) from_float(r.grad(to_float(row.row[v]), v), dst[v]);
+        }
     } else {
-        const int64_t v1 = (int64_t)(part + 1) * (GRAD_THREADS * GRAD_U * E);
-        for (int64_t v = (int64_t)part * (GRAD_THREADS * GRAD_U * E) + threadIdx.x; v < v1 && v < p.V; v += GRAD_THREADS)
+        const int64_t v1 = (int64_t)(part + 1) * p.span * E;
+        for (int64_t v = (int64_t)part * p.span * E + threadIdx.x; v < v1 && v < p.V; v += GRAD_THREADS)
             from_float(r.grad(to_float(row.row[v]), v), dst[v]);
     }
 }
@@ -769,7 +778,12 @@ int launch_scores_grad(ScoreGradArgs p, int64_t rows, cudaStream_t st)
 {
     constexpr int E = Granules<T>::E;
     const int64_t granules = (int64_t)p.V / E + 2;
-    p.parts = (uint32_t)ceil_div(granules, GRAD_THREADS * GRAD_U);
+    // Rounds a CTA: in 16 bits up to four while the SMs have eight CTAs each, to spread the set-up (2048 x 131072 bf16, kept up
+    // for seconds: 165 against 173 us -- the power limit makes instructions count); in fp32 one (925 x 100544: 108 against 116).
+    int64_t rounds = sizeof(T) == 4 ? 1 : rows * granules / ((int64_t)GRAD_THREADS * GRAD_U * 8 * sm_count());
+    rounds = rounds < 1 ? 1 : rounds > 4 ? 4 : rounds;
+    p.span = (int32_t)(GRAD_THREADS * GRAD_U * rounds);
+    p.parts = (uint32_t)ceil_div(granules, p.span);
     const bool vec = (reinterpret_cast<uintptr_t>(p.logits) & 15u) == (reinterpret_cast<uintptr_t>(p.d) & 15u) &&
                      (p.ldl * (int64_t)sizeof(T)) % 16 == (p.ldd * (int64_t)sizeof(T)) % 16;
     QNN_REQUIRE(rows * (int64_t)p.parts < ((int64_t)1 << 31), QNN_ERR_UNSUPPORTED, "qnn_token_logprobs_backward: too many elements for one launch");
@@ -783,7 +797,7 @@ int check_logits(const char *what, const void *logits, int type, int64_t T, int6
 {
     QNN_REQUIRE(type_ok(type), QNN_ERR_INVALID_ARG, "%s: unknown element type %d", what, type);
     QNN_REQUIRE(T >= 0 && V >= 0, QNN_ERR_INVALID_ARG, "%s: negative size", what);
-    QNN_REQUIRE(V < ((int64_t)1 << 31) - 64 && T < ((int64_t)1 << 28), QNN_ERR_UNSUPPORTED, "%s: V of 2^31 or T of 2^28 and more", what);
+    QNN_REQUIRE(V <= ((int64_t)1 << 30) && T < ((int64_t)1 << 28), QNN_ERR_UNSUPPORTED, "%s: V above 2^30 or T of 2^28 and more", what);
     if (T == 0) return QNN_OK;
     QNN_REQUIRE(V >= 1, QNN_ERR_INVALID_ARG, "%s: V is 0", what);
     QNN_REQUIRE(logits != nullptr, QNN_ERR_INVALID_ARG, "%s: logits is NULL", what);
