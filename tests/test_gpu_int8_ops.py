@@ -540,3 +540,50 @@ def test_side_stream_and_graph(q):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
     assert q.qnn_device_status() == 0
+
+
+def test_every_call_is_one_launch(q):
+    """One kernel a call, counted by the library that both the ctypes and the CPython entry share."""
+    M, K, N, V = 5, 200, 300, 1000
+    x = torch.randn(M, K, device="cuda")
+    w = torch.randn(N, K, device="cuda")
+    codes, wc = torch.empty(M, 224, dtype=torch.int8, device="cuda"), torch.empty(N, 224, dtype=torch.int8, device="cuda")
+    s, ws = torch.empty(M, device="cuda"), torch.empty(N, device="cuda")
+    out, z = torch.empty(M, N, device="cuda"), torch.randn(M, V, device="cuda")
+    ids = torch.randint(0, V, (M,), device="cuda")
+    lp, h, lse = (torch.empty(M, device="cuda") for _ in range(3))
+    calls = [lambda: q.qnn_quantize_rows_i8(w, N, K, K, wc, 224, ws),
+             lambda: q.qnn_rmsnorm_quant_i8(x, None, M, K, K, K, None, 1e-5, codes, 224, s),
+             lambda: q.qnn_silu_mul_quant_i8(x, x, M, K, K, K, codes, 224, s),
+             lambda: q.qnn_gemm_i8_scaled(codes, 224, s, wc, 224, ws, M, N, K, out, N),
+             lambda: q.qnn_token_logprobs(z, M, V, V, ids, lp, entropy=h, lse=lse),
+             lambda: q.qnn_token_logprobs_backward(z, M, V, V, ids, lse, h, lp, h, z, V)]
+    for call in calls:
+        before = q.qnn_launch_count()
+        call()
+        assert q.qnn_launch_count() == before + 1
+    torch.cuda.synchronize()
+    assert q.qnn_device_status() == 0
+
+
+@pytest.mark.parametrize("M", [1, 2, 4, 9, 16, 40, 130, 600])
+def test_product_repeats_bit_for_bit(q, M):
+    """The same call again and again gives the same bits, also where K is cut among CTAs or warps."""
+    g = gen(M)
+    a = torch.randint(-128, 128, (M, 4096), generator=g, device="cuda", dtype=torch.int8)
+    b = torch.randint(-128, 128, (520, 4096), generator=g, device="cuda", dtype=torch.int8)
+    sa, sb = torch.rand(M, generator=g, device="cuda"), torch.rand(520, generator=g, device="cuda")
+    outs = [torch.empty(M, 520, dtype=torch.bfloat16, device="cuda") for _ in range(8)]
+    for o in outs:
+        q.qnn_gemm_i8_scaled(a, 4096, sa, b, 4096, sb, M, 520, 4096, o, 520)
+    assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+@pytest.mark.parametrize("T,V", [(1, 128000), (6, 90001), (40, 30000), (2000, 3000)])
+def test_scores_repeat_bit_for_bit(q, T, V):
+    """Rows shared by several CTAs, candidates found in any order: the same numbers and alternatives every time."""
+    z = (torch.randn(T, V, generator=gen(T), device="cuda") * 3).bfloat16()
+    ids = torch.randint(0, V, (T,), generator=gen(V), device="cuda")
+    first = run_scores(q, z, ids, 10, V)
+    for _ in range(6):
+        assert all(torch.equal(a, b) for a, b in zip(run_scores(q, z, ids, 10, V), first))
