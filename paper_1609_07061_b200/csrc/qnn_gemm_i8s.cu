@@ -2,11 +2,15 @@
 //   out[m, n] = (float(sum_k a[m,k] b[n,k]) * a_scale[m]) * b_scale[n] + bias[n]
 // The sum is exact in int32 (tcgen05 kind::i8 accumulates there), so it does not depend on tiles or splits.
 //
-// Two kernels:
+// Three kernels:
 //  - wide: persistent; tokens are the tile's 128 (a CTA pair: 256) rows, channels its columns.  Warp 0 loads by TMA, warp 1
-//    multiplies into one of two accumulator stages in tensor memory, the other warps scale and store the previous tile.
-//  - narrow, for few tokens: bound by the bytes of the weights, so weights are the tile's 128 rows and the tokens its 16..128
-//    columns; K is cut among the CTAs of a cluster, whose int32 partial sums meet in shared memory.
+//    multiplies into one of two accumulator stages in tensor memory, the other warps scale and store the previous tile.  Bound
+//    by the tensor cores: 10000 x 4096 x 4096 in 110 us, 3050 T operations/s, their pipe busy 79 % of the time (nine waves of
+//    tiles for 8.65; repeated for seconds the power limit holds it at 128 us).
+//  - narrow, for few tokens: bound by the bytes of the weights and by latency, so weights are the tile's 128 rows and the tokens
+//    its 16..128 columns; K is cut among the CTAs of a cluster, whose int32 partial sums meet in shared memory.  16 x 131072 x
+//    4096: 85 us, 6.3 TB/s of weights; 100 x 4096 x 4096: 7.7 us.
+//  - integer units, for one to four tokens: 1 x 4096 x 4096 in 3.4 us (4.9 TB/s of weights, launch and all).
 // All device-side waits are bounded.
 #include <cuda.h>
 #include <atomic>
@@ -319,17 +323,22 @@ struct NarrowCfg {
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     // How the partial sums of a cluster meet.  Up to 16 tokens every thread sends its few to the CTA that joins them, which
     // waits on a barrier of its own: no cluster-wide barrier after the products (16 x 4096 x 4096: 5.1 us against 5.6 us).  With
-    // more tokens the stores are too many (100 tokens: 10.2 against 8.5 us): sums go to shared memory, over the operand
-    // stages, and are read from there in 16-byte pieces.
+    // more tokens the stores are too many (100 tokens: 1.7 us slower): sums go to shared memory, over the operand stages, and
+    // are read from there in 16-byte pieces; so they are where K is not cut, to be stored along the channels (100 x 16384 x
+    // 4096: 16.6 us, by thread and column 19.9).
     static constexpr bool PUSH = BN == 16;
-    // two CTAs fit an SM: one's set-up and join overlap the other's stream of weights
-    static constexpr int STAGES = BN == 16 ? 5 : (108 * 1024) / STAGE_BYTES > 6 ? 6 : (108 * 1024) / STAGE_BYTES;
+    // Up to 64 tokens two CTAs fit an SM: one's set-up and join overlap the other's stream of weights.  With 128 a stage is so
+    // large that two CTAs would have three each, too little in flight: one CTA with six (100 x 4096 x 4096: 7.7 us against 8.7 us,
+    // 128 x 16384 x 4096 19.9 against 24.5).
+    static constexpr int RESIDENT = BN == 128 ? 1 : 2;
+    static constexpr int STAGES = BN == 128 ? 6 : BN == 16 ? 5 : (108 * 1024) / STAGE_BYTES > 6 ? 6 : (108 * 1024) / STAGE_BYTES;
     static constexpr int JOIN_OFFSET = STAGES * STAGE_BYTES;
     static constexpr int BAR_OFFSET = JOIN_OFFSET + (PUSH ? BM * BN * 4 : 0);
-    static constexpr int TOTAL = BAR_OFFSET + 128 + 1024;
+    static constexpr int SCALE_OFFSET = BAR_OFFSET + 128;               // the tokens' scales
+    static constexpr int TOTAL = SCALE_OFFSET + BN * 4 + 1024;
     static constexpr int TMEM = tmem_cols(BN);
     static_assert(PUSH || STAGES * STAGE_BYTES >= BN * BM * 4, "the partial sums reuse the stages");
-    static_assert((2 * STAGES + 2) * 8 + 8 <= 128 && 2 * (TOTAL + 1024) <= 228 * 1024, "configuration");
+    static_assert((2 * STAGES + 2) * 8 + 8 <= 128 && RESIDENT * (TOTAL + 1024) <= 228 * 1024, "configuration");
 };
 
 __device__ __forceinline__ int4 ld_peer_i32x4(uint32_t addr)
@@ -361,7 +370,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16])
 }
 
 template <int BN, typename TOUT, int SPLIT>
-__global__ void __launch_bounds__(NARROW_THREADS, 2)
+__global__ void __launch_bounds__(NARROW_THREADS, NarrowCfg<BN>::RESIDENT)
 gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const I8sParams p)
 {
     using S = NarrowCfg<BN>;
@@ -377,6 +386,7 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     const uint32_t join_bar = done_bar + 8u;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 2));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    float *token_scale = reinterpret_cast<float *>(gen + S::SCALE_OFFSET);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x % (uint32_t)split;                // = the CTA's rank in its cluster
     const uint32_t tile = blockIdx.x / (uint32_t)split;
@@ -439,15 +449,22 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         }
     } else {
         const int q = warp & 3;
+        const int n_local = q * 32 + lane;
+        const int64_t n = (int64_t)tn * BM + n_local;
+        // the scales are fetched while the products run
+        if (n_local < nt) token_scale[n_local] = __ldg(p.a_scale + (int64_t)tm * BN + n_local);
+        float sb = 0.0f, bi = 0.0f;
+        if (S::PUSH) {
+            if (n < p.N) sb = __ldg(p.b_scale + n);
+            if (n < p.N && p.bias) bi = __ldg(p.bias + n);
+            asm volatile("barrier.sync 1, 128;" ::: "memory");
+        }
         ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag, 17));
         if (ok) {
             tc_fence_after();
-            const int n_local = q * 32 + lane;
-            const int64_t n = (int64_t)tn * BM + n_local;
-            const float sb = n < p.N ? __ldg(p.b_scale + n) : 0.0f, bi = n < p.N && p.bias ? __ldg(p.bias + n) : 0.0f;
             auto store = [&](int j, int32_t sum) {               // token j of the tile, this thread's channel
                 const int64_t m = (int64_t)tm * BN + j;
-                if (n < p.N) from_float(fmaf(__int2float_rn(sum) * __ldg(p.a_scale + m), sb, bi), static_cast<TOUT *>(p.out)[m * p.ldo + n]);
+                if (n < p.N) from_float(fmaf(__int2float_rn(sum) * token_scale[j], sb, bi), static_cast<TOUT *>(p.out)[m * p.ldo + n]);
             };
             if (S::PUSH && SPLIT > 1) cluster_wait();
             int32_t *dump = reinterpret_cast<int32_t *>(gen);    // (not PUSH) [token][128 channels], over the operand stages
@@ -455,14 +472,14 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             for (int c = 0; c < nt; c += 16) {
                 uint32_t v[16];
                 tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c, v);
-                if (SPLIT == 1) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c + j < nt) store(c + j, (int32_t)v[j]);
-                } else if constexpr (!S::PUSH) {
+                if constexpr (!S::PUSH) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         if (c + j < nt) dump[(c + j) * BM + n_local] = (int32_t)v[j];
+                } else if (SPLIT == 1) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < nt) store(c + j, (int32_t)v[j]);
                 } else {
                     // W tokens of this channel to the CTA that joins them: [sender][group of W tokens][channel][W]
 #pragma unroll
@@ -499,29 +516,38 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         }
     }
     __syncwarp();
-    if (!S::PUSH && SPLIT > 1) {
+    if (!S::PUSH) {
+        // A warp takes a few tokens at a time, a lane four channels of them: 16 16-byte reads from the CTAs of the cluster are on
+        // their way before the first is used.
+        const int64_t n = (int64_t)tn * BM + 4 * lane;
+        float sb[4], bi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sb[i] = n + i < p.N ? __ldg(p.b_scale + n + i) : 0.0f;
+            bi[i] = n + i < p.N && p.bias ? __ldg(p.bias + n + i) : 0.0f;
+        }
         // every CTA of the cluster reaches both barriers, whatever became of its waits
-        cluster_sync_all();
-        if (warp >= 2 && ok) {
-            // a warp takes one token at a time, a lane four channels of it: one 16-byte read from every CTA of the cluster
-            const int64_t n = (int64_t)tn * BM + 4 * lane;
-            float sb[4], bi[4];
+        if (SPLIT > 1) cluster_sync_all();
+        else __syncthreads();
+        constexpr int AT_ONCE = 16 / SPLIT, STRIDE = SPLIT * (NARROW_THREADS / 32);
+#pragma unroll 1
+        for (int j0 = (int)rank + warp * SPLIT; j0 < nt; j0 += AT_ONCE * STRIDE) {
+            int4 v[AT_ONCE][SPLIT];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sb[i] = n + i < p.N ? __ldg(p.b_scale + n + i) : 0.0f;
-                bi[i] = n + i < p.N && p.bias ? __ldg(p.bias + n + i) : 0.0f;
-            }
-#pragma unroll 2
-            for (int j = (int)rank + (warp - 2) * split; j < nt; j += 4 * split) {
-                const uint32_t at = base + (uint32_t)((j * BM + 4 * lane) * 4);
+            for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                for (int r = 0; r < SPLIT; ++r)
+                    if (j0 + i * STRIDE < nt)
+                        v[i][r] = ld_peer_i32x4(map_to_cta(base + (uint32_t)(((j0 + i * STRIDE) * BM + 4 * lane) * 4), (uint32_t)r));
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int j = j0 + i * STRIDE;
+                if (j >= nt) break;
                 const int64_t m = (int64_t)tm * BN + j;
-                const float sa = __ldg(p.a_scale + m);
-                int4 v[SPLIT];
+                const float sa = token_scale[j];
+                int4 s = v[i][0];
 #pragma unroll
-                for (int r = 0; r < SPLIT; ++r) v[r] = ld_peer_i32x4(map_to_cta(at, (uint32_t)r));
-                int4 s = v[0];
-#pragma unroll
-                for (int r = 1; r < SPLIT; ++r) { s.x += v[r].x; s.y += v[r].y; s.z += v[r].z; s.w += v[r].w; }
+                for (int r = 1; r < SPLIT; ++r) { s.x += v[i][r].x; s.y += v[i][r].y; s.z += v[i][r].z; s.w += v[i][r].w; }
                 const float f[4] = {fmaf(__int2float_rn(s.x) * sa, sb[0], bi[0]), fmaf(__int2float_rn(s.y) * sa, sb[1], bi[1]),
                                     fmaf(__int2float_rn(s.z) * sa, sb[2], bi[2]), fmaf(__int2float_rn(s.w) * sa, sb[3], bi[3])};
                 TOUT *dst = static_cast<TOUT *>(p.out) + m * p.ldo + n;
@@ -530,12 +556,12 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
                     else *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2(f[0], f[1], TOUT()), pack2(f[2], f[3], TOUT()));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (n + i < p.N) from_float(f[i], dst[i]);
+                    for (int k = 0; k < 4; ++k)
+                        if (n + k < p.N) from_float(f[k], dst[k]);
                 }
             }
         }
-        cluster_sync_all();                // nobody leaves while its partial sums are being read
+        if (SPLIT > 1) cluster_sync_all();                // nobody leaves while its partial sums are being read
     }
     if (*abort_flag) {
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
@@ -658,7 +684,7 @@ __global__ void __launch_bounds__(256) bias_rows_kernel(int64_t M, int64_t N, co
     }
 }
 
-int make_map(CUtensorMap *map, CUtensorMapDataType type, int64_t es, const void *base, int64_t rows, int64_t cols, int64_t ld_bytes, int box_rows,
+int make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t rows, int64_t cols, int64_t ld_bytes, int box_rows,
              int box_cols, CUtensorMapL2promotion promo)
 {
     EncodeTiledFn fn = encode_fn();
@@ -667,7 +693,6 @@ int make_map(CUtensorMap *map, CUtensorMapDataType type, int64_t es, const void 
     cuuint64_t strides[1] = {(cuuint64_t)ld_bytes};
     cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
-    (void)es;
     CUresult r = fn(map, type, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     promo, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     QNN_REQUIRE(r == CUDA_SUCCESS, QNN_ERR_CUDA, "qnn_gemm_i8_scaled: cuTensorMapEncodeTiled failed with code %d", (int)r);
@@ -675,7 +700,7 @@ int make_map(CUtensorMap *map, CUtensorMapDataType type, int64_t es, const void 
 }
 int make_map_codes(CUtensorMap *map, const void *base, int64_t rows, int64_t K, int64_t ld, int box_rows)
 {
-    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, K, ld, box_rows, BKB, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, rows, K, ld, box_rows, BKB, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 constexpr uint32_t i8_idesc(int m, int n) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
@@ -767,7 +792,7 @@ int launch_wide(const I8sCall &c, I8sParams p, int workers, cudaStream_t st)
     p.tma_out = aligned(p.out, 16) && (p.ldo * sizeof(TOUT)) % 16 == 0 && (p.N * sizeof(TOUT)) % 16 == 0;
     if (p.tma_out) {
         const CUtensorMapDataType dt = sizeof(TOUT) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
-        if (int rc = make_map(&mo, dt, sizeof(TOUT), p.out, p.M, p.N, p.ldo * (int64_t)sizeof(TOUT), 32, S::CB, CU_TENSOR_MAP_L2_PROMOTION_NONE))
+        if (int rc = make_map(&mo, dt, p.out, p.M, p.N, p.ldo * (int64_t)sizeof(TOUT), 32, S::CB, CU_TENSOR_MAP_L2_PROMOTION_NONE))
             return rc;
     }
     p.tiles_n = (int32_t)ceil_div(p.N, BN);
@@ -813,6 +838,44 @@ int pairs_resident()
     return v - 1;
 }
 
+// Clusters of `split` CTAs of the narrow kernel for up to 128 tokens, one CTA an SM, that are resident at once: SMs / split less
+// what the GPU's groups of SMs leave over (eights: 15 of 18, fours: 33 of 37).  Asked for once per device.
+template <int SPLIT>
+int narrow_clusters_of()
+{
+    static std::atomic<int> cached[64];                 // 0 = not asked yet
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    int v = cached[dev].load(std::memory_order_acquire);
+    if (v == 0) {
+        using S = NarrowCfg<128>;
+        auto kern = gemm_i8s_narrow_kernel<128, __nv_bfloat16, SPLIT>;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::TOTAL) == cudaSuccess) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(SPLIT * (unsigned)sm_count());
+            cfg.blockDim = dim3(NARROW_THREADS);
+            cfg.dynamicSmemBytes = S::TOTAL;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = SPLIT; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr; cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&v, kern, &cfg) != cudaSuccess) { (void)cudaGetLastError(); v = 0; }
+        }
+        if (v < 1) v = 1;
+        cached[dev].store(v, std::memory_order_release);
+    }
+    return v;
+}
+int narrow_clusters(int split)
+{
+    switch (split) {
+        case 1: return sm_count();
+        case 2: return narrow_clusters_of<2>();
+        case 4: return narrow_clusters_of<4>();
+        default: return narrow_clusters_of<8>();
+    }
+}
+
 template <int MT, int GEMV_R, int GEMV_U, typename TOUT>
 int launch_gemv(const I8sCall &c, const I8sParams &p, cudaStream_t st)
 {
@@ -853,8 +916,8 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
     // On the tensor cores the time of a launch is, within about 15 % over M = 3 .. 4096, N = 128 .. 131072, K = 128 .. 16384,
     //   wide    start + waves * (K blocks * block + hand-over)
     //   narrow  waves * start + (K blocks of a CTA) * max(block, CTAs an SM * stream) + hand-over      (us, fitted to sweeps)
-    // with the constants below; the cheapest configuration runs.  100 x 4096 x 4096: narrow 8.6, wide 64 columns 9.2;
-    // 100 x 11008 x 2048: narrow 10.0, wide 128 columns 7.7; 16 x 131072 x 4096: narrow 85, wide 116 .. 200; 701 x 2047 x 1111:
+    // with the constants below; the cheapest configuration runs.  100 x 4096 x 4096: narrow 7.8, wide 64 columns 9.2;
+    // 100 x 11008 x 2048: narrow 9.8, wide 128 columns 7.7; 16 x 131072 x 4096: narrow 85, wide 116 .. 200; 701 x 2047 x 1111:
     // wide 64 columns 8.2, 128 columns 6.6, pairs of 256 columns 9.2; 701 x 4096 x 4096: 22.8, 19.8, and pairs of 128 / 192 / 256
     // columns 18.1 / 13.2 / 15.1.
     struct Config { int rows, cols; float start, block, hand; };            // us
@@ -873,17 +936,20 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
     {
         // narrow tiles, K cut until the CTAs are about one for every SM: few tokens, or few channels and a long K.  The weights
         // (and with many CTAs an SM nothing else) set the pace; wide tiles stream them less well, which counts when all that
-        // there is to do is to stream them.
+        // there is to do is to stream them.  128 columns have one CTA an SM: K is cut while all clusters are resident at once
+        // (100 x 2048 x 4096: 7.2 us in 16 clusters of four, 11.9 in 16 of eight, of which 15 fit).
         struct Narrow { int cols; float start, block, stream, hand; };
         static const Narrow narrow[] = {{16, 3.0f, 0.28f, 0.34f, 0.3f}, {32, 3.5f, 0.29f, 0.34f, 0.6f}, {64, 4.4f, 0.31f, 0.38f, 0.8f},
-                                        {128, 5.5f, 0.36f, 0.42f, 1.2f}};
+                                        {128, 5.0f, 0.26f, 0.44f, 0.6f}};
         const int i = p.M <= 16 ? 0 : p.M <= 32 ? 1 : p.M <= 64 ? 2 : 3;
         const int64_t tiles = ceil_div(p.N, BM) * ceil_div(p.M, narrow[i].cols);
         int split = 1;
-        while (split < 8 && tiles * split * 2 <= (int64_t)sms * 5 / 4 && p.num_kb / (split * 2) >= 2) split *= 2;
+        while (split < 8 && p.num_kb / (split * 2) >= 2 &&
+               (i == 3 ? tiles <= narrow_clusters(split * 2) : tiles * split * 2 <= (int64_t)sms * 5 / 4)) split *= 2;
+        const int64_t waves = i == 3 ? ceil_div(tiles, narrow_clusters(split)) : ceil_div(tiles * split, 2 * sms);
         const int64_t ctas = tiles * split;
         const float an_sm = (float)ctas / (float)sms * narrow[i].stream;
-        const float t = (float)ceil_div(ctas, 2 * sms) * narrow[i].start +
+        const float t = (float)waves * narrow[i].start +
                         (float)ceil_div(p.num_kb, split) * (an_sm > narrow[i].block ? an_sm : narrow[i].block) + (split > 1 ? narrow[i].hand : 0.0f);
         if (p.M <= 128) {
             const float stream = 4.0f + 1.35f * (float)(p.N * c.K) * 1e-6f / 6.5f;   // (6.5 MB a us)
