@@ -758,19 +758,25 @@ template <typename T>
 int launch_scores(const ScoreArgs &p, cudaStream_t st)
 {
     const int64_t granules = (int64_t)p.V / Granules<T>::E + 1;
-    // CTAs a row (128000 bf16 with 5 alternatives, 1 / 2 / 4 / 8 CTAs): 16 rows 13.6 / 10.0 / 8.0 / 7.4 us, 33 rows 13.9 / 10.0 /
-    // 8.5 / 9.5, 64 rows 14.1 / 10.5 / 9.6 / 10.8, 100 rows 14.2 / 12.5 / 13.3 / 16.3, 296 rows 24.2 / 21.8 / 28.8, 400 rows
-    // 28.5 / 31.4: two while they fit the SMs at four each, four at two each, eight at one each.  A CTA's part stays long
-    // enough for its threads to have work.
+    // CTAs a row.  128000 bf16 with 5 alternatives, 1 / 2 / 4 / 8 CTAs: 16 rows 13.6 / 10.0 / 7.6 / 6.9 us, 33 rows 14.0 / 10.1 / 8.1 /
+    // 8.9, 64 rows 13.8 / 10.1 / 9.2 / 10.1, 74 rows 14.1 / 10.3 / 11.6 / 13.0, 100 rows 14.2 / 12.0 / 12.8 / 15.6, 296 rows 23.7 /
+    // 21.3 / 27.7, 400 rows 26.8 / 30.1: two while they fit the SMs at four each, four at two each, eight at one each, less the
+    // SMs that clusters of four and eight leave over.  And a part must be long enough to be worth a join, the more so the more
+    // CTAs share an SM: 32000, 4 rows 6.1 / 5.4 / 5.1 / 5.5, 100 rows 7.0 / 6.8 / 7.5, 296 rows 8.5 / 9.3; 16384, 64 rows 5.6 / 5.2 / 6.1,
+    // 100 rows 5.2 / 5.6; 50000, 200 rows 10.5 / 12.0.
     const int64_t sms = sm_count();
     int cluster = 1;
-    for (int c = 2; c <= MAX_CLUSTER; c *= 2)
-        if (p.T * c <= sms * 8 / c && granules / c >= 512) cluster = c;
+    for (int c = 2; c <= MAX_CLUSTER; c *= 2) {
+        const int64_t ctas = p.T * c, least = ctas <= sms ? 768 : ctas <= 2 * sms ? 1536 : 6144;
+        if (ctas * 10 <= sms * 8 / c * (c == 2 ? 10 : 9) && granules / c >= least) cluster = c;
+    }
     // Threads a CTA: fewer a row, and so more rows on an SM, where rows are short and many -- the joins cost instructions in
-    // every warp.  bf16, 8 alternatives: 4096 x 2000 with 64 / 128 threads 14.7 / 21.9 us, 3519 x 6784 22.0 / 25.3, but
-    // 200 x 6784 7.0 / 6.1; with 128 / 256 threads 4329 x 37184 (20 alternatives) 87.4 / 91.7, 2048 x 131072 97.1 / 95.5.
-    if (cluster > 1 || granules > 8192) return launch_scores_cfg<T, 256, 4, 3, 4>(p, cluster, st);
-    if (granules <= 1024 && p.T > 7 * sms) return launch_scores_cfg<T, 64, 4, 3, 12>(p, cluster, st);
+    // every warp.  bf16, 8 alternatives, 64 / 128 / 256 threads: 592 x 2000 4.4 / 5.0 / 5.8 us, 4096 x 2000 13.6 / 20.1 / 33.4,
+    // 296 x 4000 5.5 / 4.4 / 5.0, 296 x 8000 6.8 / 5.7 / 5.1, 444 x 8000 7.0 / 6.1 / 6.7, 4096 x 8000 27.4 / 28.4 / 40.8, 592 x 50000
+    // 21.7 / 19.9 / 17.8, 1024 x 50000 33.7 / 28.4 / 29.5, 2048 x 131072 119 / 98 / 95.
+    if (cluster > 1 || granules > 8192 || (granules > 640 && p.T <= 2 * sms) || (granules > 5000 && p.T <= 4 * sms))
+        return launch_scores_cfg<T, 256, 4, 3, 4>(p, cluster, st);
+    if (granules <= 320 || (granules <= 1024 && p.T > 7 * sms)) return launch_scores_cfg<T, 64, 4, 3, 12>(p, cluster, st);
     return launch_scores_cfg<T, 128, 4, 2, 8>(p, cluster, st);
 }
 
