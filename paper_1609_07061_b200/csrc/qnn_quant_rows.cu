@@ -182,6 +182,21 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// the row's sum of squares and maximum from those of its n <= 16 warps, in every lane: lane l looks at warp l's (a loop over the
+// warps: gate 4096 x 12288 61.0 against 59.1 us kept up for seconds, norm 1 x 4096 2.1 against 1.9)
+template <int OP>
+__device__ __forceinline__ void join_warps(const float *sh_ss, const uint32_t *sh_top, int w0, int n, float &ss, uint32_t &top)
+{
+    const int lane = threadIdx.x & 31;
+    top = __reduce_max_sync(0xffffffffu, lane < n ? sh_top[w0 + lane] : 0u);
+    if (OP == ROW_NORM) {
+        ss = lane < n ? sh_ss[w0 + lane] : 0.0f;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        ss = __shfl_sync(0xffffffffu, ss, 0);
+    }
+}
+
 // A row of at most 8 * NV * tpr elements in registers: tpr threads own pieces of W elements, interleaved, so that a
 // warp's accesses are contiguous.  W divides K; W = 8 needs 16-byte aligned rows, W = 2 aligned pairs, W = 1 nothing.
 // (A kernel that also took rows ending inside a piece spent 41 instructions an element instead of 27 on the 8192 x 4096
@@ -242,11 +257,9 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(cons
     uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(topf) & 0x7fffffffu);
     if (tpr > 32) {
         const int warp = threadIdx.x >> 5;
-        if ((threadIdx.x & 31) == 0) { sh_ss[warp] = ss; sh_top[warp] = top; }
+        if ((threadIdx.x & 31) == 0) { if (OP == ROW_NORM) sh_ss[warp] = ss; sh_top[warp] = top; }
         __syncthreads();
-        const int w0 = sub * (tpr >> 5);
-        ss = 0.0f;
-        for (int w = 0; w < (tpr >> 5); ++w) { ss += sh_ss[w0 + w]; top = max(top, sh_top[w0 + w]); }
+        join_warps<OP>(sh_ss, sh_top, sub * (tpr >> 5), tpr >> 5, ss, top);
     }
     if (!live) return;
     const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
@@ -310,10 +323,9 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     if (OP == ROW_NORM) ss = warp_sum(pair_sum(ss2));
     uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(topf) & 0x7fffffffu);
     const int warp = threadIdx.x >> 5;
-    if ((threadIdx.x & 31) == 0) { sh_ss[warp] = ss; sh_top[warp] = top; }
+    if ((threadIdx.x & 31) == 0) { if (OP == ROW_NORM) sh_ss[warp] = ss; sh_top[warp] = top; }
     __syncthreads();
-    ss = 0.0f;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) { ss += sh_ss[w]; top = max(top, sh_top[w]); }
+    join_warps<OP>(sh_ss, sh_top, 0, (int)(blockDim.x >> 5), ss, top);
     const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
     if (threadIdx.x == 0) p.scale[row] = r.scale;
     uint8_t *cr = p.codes + row * p.ldq;
