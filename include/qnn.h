@@ -565,7 +565,8 @@ QNN_API int qnn_logquant_combine(const int32_t *p, int groups, int64_t M, int64_
  *           stand for, code * scale rounded to values_type -- the operand a
  *           training step uses beside the codes when it passes the gradient
  *           straight through the quantiser.
- *  - A row whose largest magnitude is below 2^-118 gives scale 0 and codes 0.
+ *  - A row whose largest magnitude is below 2^-118 gives scale 0 and codes 0;
+ *    K = 0 gives scale 0 and touches nothing else.
  *    A row that holds (or computes) an infinity or a NaN, or whose sum of
  *    squares overflows fp32, gives scale NaN and codes 0, so that everything
  *    computed from it is NaN, as it would be without the quantiser.

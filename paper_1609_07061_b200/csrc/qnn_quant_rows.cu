@@ -428,8 +428,13 @@ int quant_rows(RowArgs p, int type, int64_t K, const char *what, void *stream)
 {
     QNN_REQUIRE(type_ok(type), QNN_ERR_INVALID_ARG, "%s: unknown element type %d", what, type);
     QNN_REQUIRE(p.rows >= 0 && K >= 0, QNN_ERR_INVALID_ARG, "%s: negative size", what);
-    if (p.rows == 0 || K == 0) return QNN_OK;
+    if (p.rows == 0) return QNN_OK;
     QNN_REQUIRE(p.rows < ((int64_t)1 << 31) && K < ((int64_t)1 << 31) - 32, QNN_ERR_UNSUPPORTED, "%s: rows or K of 2^31 and more", what);
+    if (K == 0) {                                        // rows of nothing: no codes, and the scale of a row of zeros
+        QNN_REQUIRE(p.scale && aligned(p.scale, 4), QNN_ERR_INVALID_ARG, "%s: scale is NULL or not aligned to its elements", what);
+        QNN_CUDA(cudaMemsetAsync(p.scale, 0, (size_t)p.rows * 4, as_stream(stream)));
+        return QNN_OK;
+    }
     QNN_REQUIRE(p.x && p.codes && p.scale && (OP != ROW_GATE || p.b), QNN_ERR_INVALID_ARG, "%s: NULL pointer", what);
     const int64_t kp = (int64_t)round_up((size_t)K, 32);
     QNN_REQUIRE(p.ldx >= K && (!p.b || p.ldb >= K) && (!p.sum || p.ld_sum >= K), QNN_ERR_INVALID_ARG, "%s: leading dimension below K", what);

@@ -246,6 +246,16 @@ def test_product_largest_sums(q, M, N):
     assert torch.equal(out, want.float())
 
 
+def test_quantisers_without_k_give_scale_zero(q):
+    c = torch.full((5, 32), 7, dtype=torch.int8, device="cuda")
+    x = torch.ones(5, 32, device="cuda")
+    for call in (lambda s: q.qnn_quantize_rows_i8(x, 5, 0, 32, c, 32, s), lambda s: q.qnn_rmsnorm_quant_i8(x, None, 5, 0, 32, 32, None, 0.0, c, 32, s),
+                 lambda s: q.qnn_silu_mul_quant_i8(x, x, 5, 0, 32, 32, c, 32, s)):
+        s = torch.full((6,), 3.0, device="cuda")
+        call(s)
+        assert s.tolist() == [0.0] * 5 + [3.0] and (c == 7).all()
+
+
 def test_product_without_k_is_the_bias(q):
     for dtype in TYPES:
         s, bias = torch.ones(64, device="cuda"), torch.randn(50, device="cuda")
