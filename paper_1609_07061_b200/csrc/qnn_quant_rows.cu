@@ -10,7 +10,8 @@
 // u = s gamma, and scale = rstd * max|u| / 127.  Sum of squares and maximum are then ONE reduction over the row, and a
 // row that stays in registers is read once and written once.
 //
-// Bound by HBM: 16-bit x and residual in, 16-bit sum and 8-bit codes out is 7 bytes an element.
+// Bound by HBM: 16-bit x and residual in, 16-bit sum, 8-bit codes and their 16-bit values out is 9 bytes an element; norm
+// 8192 x 4096 bf16 49 us (6.2 TB/s), gate 4096 x 12288 f16 54 us (6.5 TB/s), one row of 4096 1.9 us.
 #include "qnn_types.cuh"
 
 namespace qnn {
@@ -96,10 +97,10 @@ __device__ __forceinline__ void store_values(const RowArgs &p, int64_t row, int3
     else store_floats<float, W>(static_cast<float *>(p.values) + at, f);
 }
 
-// t of one piece; adds to the sum of squares, and gives the sum s of the norm in `s`
-template <int OP, typename T, int W>
-__device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, const Piece<T, W> &bv, int32_t k0, float (&s)[W], float (&t)[W],
-                                       f32x2 &ss)
+// t of one piece; adds to the sum of squares, and gives the sum s of the norm in `s`; weights(gv) loads the piece's gamma
+template <int OP, typename T, int W, class Weights>
+__device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, const Piece<T, W> &bv, float (&s)[W], float (&t)[W], f32x2 &ss,
+                                       const Weights &weights)
 {
     float x[W], b[W];
     piece_to_floats<T, W>(xv, x);
@@ -124,7 +125,7 @@ __device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, 
         float g[W];
         if (p.gamma != nullptr) {
             Piece<T, W> gv;
-            load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv);
+            weights(gv);
             piece_to_floats<T, W>(gv, g);
         } else {
 #pragma unroll
@@ -239,7 +240,8 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(cons
             const int32_t k0 = ((c + j) * tpr + t0) * W;
             if (k0 < K) {
                 float s[W];
-                row_op<OP, T, W>(p, xv[j], bv[j], k0, s, t[c + j], ss2);
+                row_op<OP, T, W>(p, xv[j], bv[j], s, t[c + j], ss2,
+                                 [&](Piece<T, W> &gv) { load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv); });
                 if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
 #pragma unroll
                 for (int i = 0; i < W; ++i) topf = max_nan(topf, fabsf(t[c + j][i]));
@@ -280,6 +282,289 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(cons
     }
 }
 
+// ---- rows that start or end inside 16 bytes ----------------------------------------------------------------------
+
+// bytes sh .. sh + 15 of the 32 bytes lo, hi
+template <int ES>
+__device__ __forceinline__ uint4 shift_units(const uint4 &lo, const uint4 &hi, int sh)
+{
+    const uint32_t in[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    uint32_t a[6], b[5];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) a[i] = sh & 8 ? in[i + 2] : in[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) b[i] = sh & 4 ? a[i + 1] : a[i];
+    if (ES == 4) return make_uint4(b[0], b[1], b[2], b[3]);
+    const uint32_t sel = sh & 2 ? 0x5432u : 0x3210u;
+    return make_uint4(__byte_perm(b[0], b[1], sel), __byte_perm(b[1], b[2], sel), __byte_perm(b[2], b[3], sel), __byte_perm(b[3], b[4], sel));
+}
+// A row of a real tensor as aligned 16-byte units.
+template <typename T>
+struct UnitRow {
+    static constexpr int E = 16 / (int)sizeof(T);
+    const T *row;
+    int32_t K;
+    int off;                // bytes from the unit that the row starts in to its start
+    bool before, after;     // the rest of its first / last unit is the tensor's too (another row, or the gap to it)
+    __device__ __forceinline__ UnitRow(const void *p, int64_t r, int64_t ld, int64_t rows, int32_t k)
+        : row(static_cast<const T *>(p) + r * ld), K(k), off((int)(reinterpret_cast<uintptr_t>(row) & 15u)), before(r > 0), after(r + 1 < rows) {}
+    // whether all units of a warp's piece from element k on are the row's own (k: the same in all lanes)
+    __device__ __forceinline__ bool inside(int32_t k) const { return (k > 0 || off == 0) && k + 256 + E <= K; }
+    // the aligned 16 bytes that begin at element k; elements from K on are 0, those before the row anything
+    __device__ __forceinline__ uint4 load(int32_t k) const
+    {
+        if (k >= 0 && k <= K - E) return *reinterpret_cast<const uint4 *>(row + k);
+        if (k >= K) return make_uint4(0u, 0u, 0u, 0u);
+        if ((k >= 0 || before) && (k <= K - E || after)) {
+            uint4 v = *reinterpret_cast<const uint4 *>(row + k);
+            const int left = (K - k) * (int)sizeof(T);
+            auto keep = [&](int at) { const int n = left - at; return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; };
+            v.x &= keep(0); v.y &= keep(4); v.z &= keep(8); v.w &= keep(12);
+            return v;
+        }
+        return load_edge(k);
+    }
+    // element by element: the unit reaches beyond the tensor
+    __device__ __forceinline__ uint4 load_edge(int32_t k) const
+    {
+        uint32_t e[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            e[i] = 0u;
+            if (k + i >= 0 && k + i < K) {
+                if constexpr (sizeof(T) == 4) e[i] = reinterpret_cast<const uint32_t *>(row)[k + i];
+                else e[i] = reinterpret_cast<const uint16_t *>(row)[k + i];
+            }
+        }
+        if constexpr (sizeof(T) == 4) return make_uint4(e[0], e[1], e[2], e[3]);
+        else return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    }
+};
+// 16 aligned bytes to element k on of a row; elements outside 0 .. K - 1 are not stored
+template <typename T>
+__device__ __forceinline__ void store_unit(T *row, int32_t k, uint4 v, int32_t K)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if (k >= 0 && k <= K - E) {
+        *reinterpret_cast<uint4 *>(row + k) = v;
+    } else if (k < K) {
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if (k + i >= 0 && k + i < K) {
+                if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(row)[k + i] = x[i];
+                else reinterpret_cast<uint16_t *>(row)[k + i] = (uint16_t)(i & 1 ? x[i / 2] >> 16 : x[i / 2]);
+            }
+        }
+    }
+}
+
+// eight elements from k0 (a multiple of 8) on: the units they lie in, then shifted
+template <typename T>
+struct Units {
+    static constexpr int N = (int)sizeof(T) / 2;         // units of a piece
+    uint4 u[N + 1];
+    __device__ __forceinline__ void load(const UnitRow<T> &r, int32_t k0, bool inside)
+    {
+        const int32_t k = k0 - r.off / (int)sizeof(T);
+        if (inside) {                                    // (all lanes)
+            const uint4 *at = reinterpret_cast<const uint4 *>(r.row + k);
+#pragma unroll
+            for (int n = 0; n <= N; ++n) u[n] = at[n];
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) u[n] = r.load(k + n * r.E);
+            u[N] = r.off != 0 ? r.load(k + 8) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    __device__ __forceinline__ void piece(int off, Piece<T, 8> &v) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint4 x = shift_units<(int)sizeof(T)>(u[n], u[n + 1], off);
+            v.w[4 * n] = x.x; v.w[4 * n + 1] = x.y; v.w[4 * n + 2] = x.z; v.w[4 * n + 3] = x.w;
+        }
+    }
+};
+// Stores a warp's pieces of a row, piece by piece along it, lanes side by side: a unit of memory is put together from a lane's
+// elements and those of the lane before, so that all but a row's ends are whole aligned stores.
+template <typename T>
+struct RunStore {
+    static constexpr int N = (int)sizeof(T) / 2, E = 16 / (int)sizeof(T);
+    T *row;
+    int off;
+    int32_t K;
+    uint4 last;             // the last unit of this lane's piece before (of lane 31 at first: of the warp before)
+    uint4 held;             // lane 0: its first unit, when the one before it is not known yet
+    __device__ __forceinline__ RunStore(T *r, int32_t k)
+        : row(r), off((int)(reinterpret_cast<uintptr_t>(r) & 15u)), K(k), last(make_uint4(0u, 0u, 0u, 0u)), held(last) {}
+    static __device__ __forceinline__ void pack(const float (&f)[8], uint4 (&u)[N])
+    {
+        if constexpr (N == 1) {
+            u[0] = make_uint4(pack2(f[0], f[1], T()), pack2(f[2], f[3], T()), pack2(f[4], f[5], T()), pack2(f[6], f[7], T()));
+        } else {
+            u[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+            u[N - 1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+        }
+    }
+    // hold: keep the run's first unit for release()
+    __device__ __forceinline__ void put(const float (&f)[8], int32_t k0, bool hold)
+    {
+        const int lane = threadIdx.x & 31;
+        const bool inside = (k0 - lane * 8 > 0 || off == 0) && k0 - lane * 8 + 256 <= K;
+        uint4 u[N];
+        pack(f, u);
+        if (off == 0) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (inside) *reinterpret_cast<uint4 *>(row + k0 + n * E) = u[n];
+                else store_unit<T>(row, k0 + n * E, u[n], K);
+            }
+            return;
+        }
+        const int from = (lane + 31) & 31;
+        const bool top = lane == 31;
+        uint4 before;
+        before.x = __shfl_sync(0xffffffffu, top ? last.x : u[N - 1].x, from);
+        before.y = __shfl_sync(0xffffffffu, top ? last.y : u[N - 1].y, from);
+        before.z = __shfl_sync(0xffffffffu, top ? last.z : u[N - 1].z, from);
+        before.w = __shfl_sync(0xffffffffu, top ? last.w : u[N - 1].w, from);
+        last = u[N - 1];
+        if (hold) held = u[0];
+        const int32_t k = k0 - off / (int)sizeof(T);
+        const uint4 x = shift_units<(int)sizeof(T)>(before, u[0], 16 - off), y = shift_units<(int)sizeof(T)>(u[0], u[N - 1], 16 - off);
+        if (inside) {
+            if (!(hold && lane == 0)) *reinterpret_cast<uint4 *>(row + k) = x;
+            if (N == 2) *reinterpret_cast<uint4 *>(row + k + E) = y;
+        } else {
+            if (!(hold && lane == 0)) store_unit<T>(row, k, x, K);
+            if (N == 2) store_unit<T>(row, k + E, y, K);
+        }
+        // the row ends here: what lies past the last unit
+        if (top && k0 + 8 >= K && k + 8 < K)
+            store_unit<T>(row, k + 8, shift_units<(int)sizeof(T)>(u[N - 1], make_uint4(0u, 0u, 0u, 0u), 16 - off), K);
+    }
+    __device__ __forceinline__ void release(int32_t first, const uint4 &before)
+    {
+        if ((threadIdx.x & 31) == 0 && off != 0)
+            store_unit<T>(row, first - off / (int)sizeof(T), shift_units<(int)sizeof(T)>(before, held, 16 - off), K);
+    }
+};
+
+// A row of any alignment in registers: a warp owns a run of P * 256 elements, lane by lane eight, and the real tensors move in
+// aligned units of 16 bytes whatever their offsets, which may differ from tensor to tensor.  A unit's elements are shifted
+// into place by selects and byte permutes (15 a unit and direction), so what bounds it is instructions: 3000 x 11009 bf16, norm 116 us
+// (2.0 TB/s), gate 71 us (3.3 TB/s); element by element 148 and 119.  The register limits let two blocks of 350 threads
+// run on an SM (gate 3000 x 11009 116 us without them).
+template <int OP, typename T, int P, int MAXREG = P == 4 ? 80 : 64>
+__global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_ragged_kernel(const RowArgs p)
+{
+    constexpr int CH = P == 1 || sizeof(T) == 4 ? 1 : 2; // pieces whose loads are in flight together
+    __shared__ float sh_ss[16];
+    __shared__ uint32_t sh_top[16];
+    // what the next warp needs to complete the first units of its run: t of a run's last eight elements, their last unit of sums
+    __shared__ float4 sh_t[16][2];
+    __shared__ uint4 sh_sum[16];
+    griddep_wait();
+
+    const int tpr = p.tpr, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int sub = threadIdx.x / tpr, w = (threadIdx.x - sub * tpr) >> 5;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / tpr) + sub;
+    const bool live = row < p.rows;
+    const int64_t rr = live ? row : 0;
+    const int32_t K = live ? p.K : 0, first = w * (P * 256);
+    const bool with_b = OP == ROW_GATE || (OP == ROW_NORM && p.b != nullptr);
+    const UnitRow<T> xr(p.x, rr, p.ldx, p.rows, K), br(p.b, rr, p.ldb, p.rows, K), gr(p.gamma, 0, 0, 1, K);
+
+    float t[P][8];
+    f32x2 ss2 = 0ull;
+    float topf = 0.0f;
+    const bool keep_sum = OP == ROW_NORM && p.sum != nullptr;
+    RunStore<T> sums(static_cast<T *>(p.sum) + (keep_sum ? rr : 0) * p.ld_sum, K);
+#pragma unroll
+    for (int c = 0; c < P; c += CH) {
+        Units<T> xv[CH], bv[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int32_t k = first + (c + j) * 256;
+            if (k < K) {
+                xv[j].load(xr, k + lane * 8, xr.inside(k));
+                if (with_b) bv[j].load(br, k + lane * 8, br.inside(k));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int32_t k = first + (c + j) * 256;
+            if (k < K) {                                 // (elements from K on are zeros, and give t = 0)
+                float s[8];
+                Piece<T, 8> xp, bp;
+                xv[j].piece(xr.off, xp);
+                if (with_b) bv[j].piece(br.off, bp);
+                row_op<OP, T, 8>(p, xp, bp, s, t[c + j], ss2, [&](Piece<T, 8> &gv) {
+                    Units<T> g;
+                    g.load(gr, k + lane * 8, gr.inside(k));
+                    g.piece(gr.off, gv);
+                });
+                if (keep_sum) sums.put(s, k + lane * 8, c + j == 0 && w > 0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) topf = max_nan(topf, fabsf(t[c + j][i]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[c + j][i] = 0.0f;
+            }
+        }
+    }
+
+    griddep_launch_dependents();
+    float ss = 0.0f;
+    if (OP == ROW_NORM) ss = warp_sum(pair_sum(ss2));
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(topf) & 0x7fffffffu);
+    if (tpr > 32) {
+        if (lane == 0) { if (OP == ROW_NORM) sh_ss[warp] = ss; sh_top[warp] = top; }
+        if (lane == 31) {
+            sh_t[warp][0] = make_float4(t[P - 1][0], t[P - 1][1], t[P - 1][2], t[P - 1][3]);
+            sh_t[warp][1] = make_float4(t[P - 1][4], t[P - 1][5], t[P - 1][6], t[P - 1][7]);
+            if (keep_sum) sh_sum[warp] = sums.last;
+        }
+        __syncthreads();
+        join_warps<OP>(sh_ss, sh_top, sub * (tpr >> 5), tpr >> 5, ss, top);
+        if (keep_sum && w > 0 && first < K) sums.release(first, sh_sum[warp - 1]);
+    }
+    if (!live) return;
+    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
+    if (w == 0 && lane == 0) p.scale[row] = r.scale;
+    uint8_t *cr = p.codes + row * p.ldq;
+    auto finish = [&](auto type) {
+        using V = decltype(type);
+        RunStore<V> values(static_cast<V *>(p.values) + (p.values != nullptr ? row * p.ld_values : 0), K);
+        if (p.values != nullptr && w > 0 && values.off != 0) {
+            const float4 a = sh_t[warp - 1][0], b = sh_t[warp - 1][1];
+            const float e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            float f[8];
+            uint4 u[RunStore<V>::N];
+            to_codes<8>(e, r.inv, f);
+            to_values<8>(f, r.scale);
+            RunStore<V>::pack(f, u);
+            values.last = u[RunStore<V>::N - 1];
+        }
+#pragma unroll
+        for (int c = 0; c < P; ++c) {
+            const int32_t k = first + c * 256, k0 = k + lane * 8;
+            if (k >= p.KP) break;
+            float f[8];
+            to_codes<8>(t[c], r.inv, f);
+            if (k0 < p.KP) store_codes<8>(cr + k0, f, r.keep);
+            if (p.values != nullptr && k < K) {
+                to_values<8>(f, r.scale);
+                values.put(f, k0, false);
+            }
+        }
+    };
+    if (p.values_type == QNN_TYPE_BF16) finish(__nv_bfloat16());
+    else if (p.values_type == QNN_TYPE_F16) finish(__half());
+    else finish(float());
+}
+
 // Rows longer than the registers of a block hold: two passes over the row, the second mostly from L2.  sum_out may be x
 // or residual, so the first pass writes nothing and the second writes each element after reading it.
 template <int OP, typename T, int W>
@@ -313,7 +598,8 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
             const int64_t k0 = k + c * step;
             if (k0 < p.K) {
                 float s[W], t[W];
-                row_op<OP, T, W>(p, xv[c], bv[c], (int32_t)k0, s, t, ss2);
+                row_op<OP, T, W>(p, xv[c], bv[c], s, t, ss2,
+                                 [&](Piece<T, W> &gv) { load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv); });
 #pragma unroll
                 for (int i = 0; i < W; ++i) topf = max_nan(topf, fabsf(t[i]));
             }
@@ -348,7 +634,8 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
 #pragma unroll
             for (int i = 0; i < W; ++i) t[i] = 0.0f;
             if (k0 < p.K) {
-                row_op<OP, T, W>(p, xv[c], bv[c], (int32_t)k0, s, t, unused);
+                row_op<OP, T, W>(p, xv[c], bv[c], s, t, unused,
+                                 [&](Piece<T, W> &gv) { load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv); });
                 if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
             }
             to_codes<W>(t, r.inv, f);
@@ -408,6 +695,25 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st)
 }
 
 template <int OP, typename T>
+int launch_ragged(RowArgs p, const char *what, cudaStream_t st)
+{
+    // Pieces a lane: one for few rows, for latency, and in fp32 (norm 4000 x 2003: 34.6 us against 40.2 with two); two else (norm
+    // 4000 x 2003 bf16: 27.3 against 32.9 with one and 32.3 with four).
+    const int64_t groups = ceil_div(p.KP, 8);
+    int pieces = p.rows <= 2 * (int64_t)sm_count() || sizeof(T) == 4 || groups <= 32 ? 1 : 2;
+    while (groups > (int64_t)MAX_TPR * pieces) pieces *= 2;
+    p.tpr = (int)(ceil_div(groups, 32 * pieces) * 32);
+    const int rpb = p.tpr >= 128 ? 1 : 128 / p.tpr;
+    const dim3 grid((unsigned)ceil_div(p.rows, rpb)), block((unsigned)(p.tpr * rpb));
+    switch (pieces) {
+        case 1: QNN_CUDA(launch_pdl(row_quant_ragged_kernel<OP, T, 1>, grid, block, 0, st, p)); break;
+        case 2: QNN_CUDA(launch_pdl(row_quant_ragged_kernel<OP, T, 2>, grid, block, 0, st, p)); break;
+        default: QNN_CUDA(launch_pdl(row_quant_ragged_kernel<OP, T, 4>, grid, block, 0, st, p)); break;
+    }
+    return check_launch(what);
+}
+
+template <int OP, typename T>
 int launch_rows_w(const RowArgs &p, const char *what, cudaStream_t st)
 {
     // widest access that every row of every real tensor allows and that the row length is a multiple of
@@ -419,7 +725,14 @@ int launch_rows_w(const RowArgs &p, const char *what, cudaStream_t st)
                ok(p.values, p.ld_values, vs);
     };
     if (fits(8)) return launch_rows<OP, T, 8>(p, what, st);
-    if (fits(2)) return launch_rows<OP, T, 2>(p, what, st);
+    // Rows that end inside 16 bytes: in pairs where all tensors lie alike and a block's registers hold the row (bf16 norm 5000 x
+    // 4098 51 us, shifted units 70; gate 36 and 51), and for the norm of many longer rows in pairs too, in two passes (2000 x
+    // 11010 66 and 76); else shifted units (2000 x 11010 gate 47 us, 66 in pairs; 64 x 11009 norm 6.9, 13; 5000 x 4097 norm 70, by
+    // single elements 97, gate 51, 84; 1 x 4097 norm 3.6, 6.0).  Single elements are left to the shortest rows and those that
+    // no block holds.
+    const bool pairs = fits(2), held = p.KP <= 8 * 4 * MAX_TPR;
+    if (pairs && (p.KP <= 8192 || !held || (OP == ROW_NORM && p.rows > 2 * (int64_t)sm_count()))) return launch_rows<OP, T, 2>(p, what, st);
+    if (held && p.KP >= 256) return launch_ragged<OP, T>(p, what, st);
     return launch_rows<OP, T, 1>(p, what, st);
 }
 

@@ -246,6 +246,49 @@ def test_product_largest_sums(q, M, N):
     assert torch.equal(out, want.float())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,K", [(1, 257), (3, 300), (2, 1031), (5, 4099), (301, 519), (2, 9001), (400, 2051)])
+def test_quantisers_tensors_at_different_offsets(q, rows, K, dtype):
+    """Every tensor starts elsewhere in its 16 bytes, and so does every row; the outputs are those of aligned tensors, bit for bit,
+    and nothing beside the rows is written."""
+    g = gen(rows + K)
+    wide = (K + 15) // 8 * 8
+
+    def at(off, ld):
+        return torch.full((rows * ld + 16,), 7.0, dtype=dtype, device="cuda")[off:off + rows * ld].view(rows, ld)
+
+    x, r = (torch.randn(rows, wide, generator=g, device="cuda").to(dtype) for _ in range(2))
+    gamma = (1 + 0.3 * torch.randn(wide, generator=g, device="cuda")).to(dtype)
+    x2, r2, s2 = at(1, K), at(3, K + 2), at(5, K + 1)
+    x2.copy_(x[:, :K]); r2[:, :K].copy_(r[:, :K])
+    gamma2 = torch.empty(wide + 8, dtype=dtype, device="cuda")[7:7 + K]
+    gamma2.copy_(gamma[:K])
+    for vt in TYPES:
+        one, two = Quantised(rows, K, values=vt, ld_values=wide), Quantised(rows, K, values=vt, ld_values=K + 3)
+        total = torch.empty(rows, wide, dtype=dtype, device="cuda")
+        q.qnn_rmsnorm_quant_i8(x, r, rows, K, wide, wide, gamma, 1e-5, one.codes.t, one.ldq, one.scale.t, sum_out=total, ld_sum=wide,
+                               values=one.values.t, ld_values=one.ldv)
+        q.qnn_rmsnorm_quant_i8(x2, r2, rows, K, K, K + 2, gamma2, 1e-5, two.codes.t, two.ldq, two.scale.t, sum_out=s2, ld_sum=K + 1,
+                               values=two.values.t, ld_values=two.ldv)
+        assert torch.equal(s2[:, :K], total[:, :K]) and (s2[:, K:] == 7).all()
+        top = one.codes.t[:, :K].int() - two.codes.t[:, :K].int()
+        # (the sum of squares is added in another order, which moves the scale by roundings, not the codes)
+        assert not top.any()
+        assert ((one.scale.t - two.scale.t).abs() <= 1e-5 * one.scale.t).all()
+        # in place: over x, and over the residual
+        for over, ld in ((0, K), (1, K + 2)):
+            a, b = x2.clone(), r2.clone()
+            o = Quantised(rows, K, values=vt, ld_values=K + 3)
+            q.qnn_rmsnorm_quant_i8(a, b, rows, K, K, K + 2, gamma2, 1e-5, o.codes.t, o.ldq, o.scale.t, sum_out=(a, b)[over], ld_sum=ld,
+                                   values=o.values.t, ld_values=o.ldv)
+            assert torch.equal((a, b)[over][:, :K], total[:, :K]) and torch.equal(o.codes.t, two.codes.t)
+        one, two = Quantised(rows, K, values=vt, ld_values=wide), Quantised(rows, K, values=vt, ld_values=K + 3)
+        q.qnn_silu_mul_quant_i8(x, r, rows, K, wide, wide, one.codes.t, one.ldq, one.scale.t, values=one.values.t, ld_values=one.ldv)
+        q.qnn_silu_mul_quant_i8(x2, r2, rows, K, K, K + 2, two.codes.t, two.ldq, two.scale.t, values=two.values.t, ld_values=two.ldv)
+        assert torch.equal(one.codes.t, two.codes.t) and torch.equal(one.scale.t, two.scale.t)
+        assert torch.equal(one.values.t[:, :K], two.values.t[:, :K])
+
+
 def test_quantisers_without_k_give_scale_zero(q):
     c = torch.full((5, 32), 7, dtype=torch.int8, device="cuda")
     x = torch.ones(5, 32, device="cuda")
