@@ -154,11 +154,15 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+_initialized = torch.cuda.is_initialized
+_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream():
     # the current stream's handle without building a Stream object (this sits on every call's path); before CUDA is
     # initialised only host-side validation can succeed, and any launch then returns QNN_ERR_CUDA
-    if torch.cuda.is_initialized():
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if _initialized():
+        return _raw_stream(_device())
     return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
 
 
@@ -610,97 +614,49 @@ def qnn_xnor_gemm_noalloc(a, lda, b, ldb, M, N, K, out, ldo):
 
 
 # The 8-bit language-model calls are made once per layer and token: they go through a CPython module (_qnn_calls, built next
-# to the library) whose functions convert their arguments in nanoseconds; ctypes needs 2 us for as many.
+# to the library) that checks the tensors' types and converts the arguments in nanoseconds; ctypes needs 2 us for as many.
 from . import _qnn_calls  # noqa: E402  (after the library's own check above)
-
-_TYPES = {torch.float32: QNN_TYPE_F32, torch.bfloat16: QNN_TYPE_BF16, torch.float16: QNN_TYPE_F16}
-_f32, _i8, _i64 = torch.float32, torch.int8, torch.int64
-
-
-def _wrong(where: str, got, needed: str):
-    raise TypeError(f"{where}: {got} where {needed} is needed")
-
-
-def _real(t: torch.Tensor, where: str) -> int:
-    """QNN_TYPE_* of a real tensor."""
-    code = _TYPES.get(t.dtype)
-    return _wrong(where, t.dtype, "float32, bfloat16 or float16") if code is None else code
-
-
-def _need(t: Optional[torch.Tensor], dtype: torch.dtype, where: str):
-    """Pointer of a tensor whose type the C side cannot see."""
-    if t is None:
-        return None
-    if t.dtype is not dtype:
-        _wrong(where, t.dtype, str(dtype))
-    return t.data_ptr()
-
-
-def _values(values, where):
-    return (None, 0) if values is None else (values.data_ptr(), _real(values, where))
 
 
 def qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values=None, ld_values=0):
     """Rows of x -> int8 codes and one fp32 scale a row (weights once, or activations); values: what the codes stand for."""
-    w = "qnn_quantize_rows_i8"
-    vp_, vt = _values(values, w)
-    s = _qnn_calls.qnn_quantize_rows_i8(_p(x), QNN_TYPE_F32 if x is None else _real(x, w), rows, K, ldx, _need(codes, _i8, w), ldq,
-                                        _need(scale, _f32, w), vp_, vt, ld_values, _stream())
+    s = _qnn_calls.qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values, ld_values, _stream())
     if s:
-        raise QnnError(s, w)
+        raise QnnError(s, "qnn_quantize_rows_i8")
 
 
 def qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out=None, ld_sum=0, values=None,
                          ld_values=0):
     """Root-mean-square norm of x + residual, scaled by gamma, as int8 codes and one scale a row; sum_out: x + residual."""
-    w = "qnn_rmsnorm_quant_i8"
-    dt = _f32 if x is None else x.dtype
-    vp_, vt = _values(values, w)
-    s = _qnn_calls.qnn_rmsnorm_quant_i8(_p(x), _need(residual, dt, w), QNN_TYPE_F32 if x is None else _real(x, w), rows, K, ldx, ldr,
-                                        _need(gamma, dt, w), eps, _need(codes, _i8, w), ldq, _need(scale, _f32, w),
-                                        _need(sum_out, dt, w), ld_sum, vp_, vt, ld_values, _stream())
+    s = _qnn_calls.qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out, ld_sum, values,
+                                        ld_values, _stream())
     if s:
-        raise QnnError(s, w)
+        raise QnnError(s, "qnn_rmsnorm_quant_i8")
 
 
 def qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values=None, ld_values=0):
     """gate / (1 + exp(-gate)) * up as int8 codes and one scale a row."""
-    w = "qnn_silu_mul_quant_i8"
-    vp_, vt = _values(values, w)
-    s = _qnn_calls.qnn_silu_mul_quant_i8(_p(gate), _need(up, _f32 if gate is None else gate.dtype, w),
-                                         QNN_TYPE_F32 if gate is None else _real(gate, w), rows, K, ldg, ldu, _need(codes, _i8, w),
-                                         ldq, _need(scale, _f32, w), vp_, vt, ld_values, _stream())
+    s = _qnn_calls.qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values, ld_values, _stream())
     if s:
-        raise QnnError(s, w)
+        raise QnnError(s, "qnn_silu_mul_quant_i8")
 
 
 def qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, M, N, K, out, ldo, bias=None):
     """out[m, n] = sum_k a[m, k] b[n, k] * a_scale[m] * b_scale[n] + bias[n], in the type of `out`."""
-    w = "qnn_gemm_i8_scaled"
-    s = _qnn_calls.qnn_gemm_i8_scaled(_need(a, _i8, w), lda, _need(a_scale, _f32, w), _need(b, _i8, w), ldb, _need(b_scale, _f32, w),
-                                      _need(bias, _f32, w), M, N, K, _p(out), QNN_TYPE_F32 if out is None else _real(out, w), ldo,
-                                      _stream())
+    s = _qnn_calls.qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, _stream())
     if s:
-        raise QnnError(s, w)
+        raise QnnError(s, "qnn_gemm_i8_scaled")
 
 
 def qnn_token_logprobs(logits, T, V, ldl, ids, logprob, entropy=None, lse=None, topk=0, top_logprob=None, top_ids=None):
     """Log probabilities of the tokens `ids`, entropies, and the topk alternatives (ties to the lowest id)."""
-    w = "qnn_token_logprobs"
-    s = _qnn_calls.qnn_token_logprobs(_p(logits), QNN_TYPE_F32 if logits is None else _real(logits, w), T, V, ldl,
-                                      _need(ids, _i64, w), _need(logprob, _f32, w), _need(entropy, _f32, w), _need(lse, _f32, w),
-                                      topk, _need(top_logprob, _f32, w), _need(top_ids, _i64, w), _stream())
+    s = _qnn_calls.qnn_token_logprobs(logits, T, V, ldl, ids, logprob, entropy, lse, topk, top_logprob, top_ids, _stream())
     if s:
-        raise QnnError(s, w)
+        raise QnnError(s, "qnn_token_logprobs")
 
 
 def qnn_token_logprobs_backward(logits, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d_logits, ldd):
     """Gradient of log probabilities and entropies with respect to the logits."""
-    w = "qnn_token_logprobs_backward"
-    dt = _f32 if logits is None else logits.dtype
-    s = _qnn_calls.qnn_token_logprobs_backward(_p(logits), QNN_TYPE_F32 if logits is None else _real(logits, w), T, V, ldl,
-                                               _need(ids, _i64, w), _need(lse, _f32, w), _need(entropy, _f32, w),
-                                               _need(g_logprob, _f32, w), _need(g_entropy, _f32, w), _need(d_logits, dt, w), ldd,
-                                               _stream())
+    s = _qnn_calls.qnn_token_logprobs_backward(logits, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d_logits, ldd, _stream())
     if s:
-        raise QnnError(s, w)
+        raise QnnError(s, "qnn_token_logprobs_backward")
