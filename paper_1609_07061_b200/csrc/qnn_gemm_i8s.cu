@@ -10,7 +10,7 @@
 //  - narrow, for few tokens: bound by the bytes of the weights and by latency, so weights are the tile's 128 rows and the tokens
 //    its 16..128 columns; K is cut among the CTAs of a cluster, whose int32 partial sums meet in shared memory.  16 x 131072 x
 //    4096: 85 us, 6.3 TB/s of weights; 100 x 4096 x 4096: 7.7 us.
-//  - integer units, for one to four tokens: 1 x 4096 x 4096 in 3.4 us (4.9 TB/s of weights, launch and all).
+//  - integer units, for one to four tokens: 1 x 4096 x 4096 in 2.8 us (6.1 TB/s of weights, launch and all).
 // All device-side waits are bounded.
 #include <cuda.h>
 #include <atomic>
@@ -604,7 +604,6 @@ __global__ void __launch_bounds__(256) gemv_i8s_kernel(const uint8_t *__restrict
                                                        const int32_t K, const int ksplit, const I8sParams p)
 {
     __shared__ int32_t part[8][GEMV_R * MT];
-    griddep_launch_dependents();
     griddep_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per_block = 8 / ksplit;                        // row groups of a block
@@ -649,6 +648,9 @@ __global__ void __launch_bounds__(256) gemv_i8s_kernel(const uint8_t *__restrict
             for (int r = 0; r < GEMV_R; ++r) acc[r][m] = dot16(w[r], x, acc[r][m]);
         }
     }
+    // the weights are in: the next kernel may be scheduled now (allowed to start at once, its blocks pile up on the SMs that are
+    // free, several to one, and stay there: 1 x 4096 x 4096 2.8 against 3.4 us)
+    griddep_launch_dependents();
     int32_t mine = 0;                                        // lane r * MT + m keeps sum (r, m)
 #pragma unroll
     for (int r = 0; r < GEMV_R; ++r)
@@ -901,10 +903,10 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
                             static_cast<TOUT *>(p.out), p.ldo));
         return check_launch("qnn_gemm_i8_scaled");
     }
-    // A handful of tokens: the weights go through the integer units.  One token always (4096 x 4096: 3.4 us against 4.9 us on the
+    // A handful of tokens: the weights go through the integer units.  One token always (4096 x 4096: 2.8 us against 4.9 us on the
     // tensor cores, 28672 x 4096: 20.9 against 21.4; rows of at most 1024 codes four to a warp: 131072 x 1024 22.7 against
-    // 30.5 us two to a warp).  Two to four tokens while the weights are at most 32 MB (two: 4096 x 4096 3.8 against 4.9, but
-    // 131072 x 1024 34.4 against 29.2; four: 4096 x 4096 3.6 against 4.9, 11008 x 2048 5.3 against 5.7, but 16384 x 4096 20.3
+    // 30.5 us two to a warp).  Two to four tokens while the weights are at most 32 MB (two: 4096 x 4096 3.2 against 4.9, but
+    // 131072 x 1024 34.4 against 29.2; four: 4096 x 4096 3.5 against 4.9, 11008 x 2048 4.9 against 5.7, but 16384 x 4096 20.3
     // against 14.8), three and four not for the shortest rows (16384 x 512: 4.8 against 4.0).  Eight tokens: 5.9 us for 4096 x
     // 4096.
     if (p.M == 1) return c.K <= 1024 ? launch_gemv<1, 4, 1, TOUT>(c, p, st) : launch_gemv<1, 2, 4, TOUT>(c, p, st);

@@ -572,7 +572,6 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
 {
     __shared__ float sh_ss[16];
     __shared__ uint32_t sh_top[16];
-    griddep_launch_dependents();
     griddep_wait();
     const int64_t row = blockIdx.x;
     const T *xr = static_cast<const T *>(p.x) + row * p.ldx;
@@ -611,6 +610,7 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) { if (OP == ROW_NORM) sh_ss[warp] = ss; sh_top[warp] = top; }
     __syncthreads();
+    griddep_launch_dependents();
     join_warps<OP>(sh_ss, sh_top, 0, (int)(blockDim.x >> 5), ss, top);
     const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
     if (threadIdx.x == 0) p.scale[row] = r.scale;
