@@ -322,7 +322,7 @@ struct NarrowCfg {
     static constexpr int B_BYTES = BN * BKB;                            // tokens
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     // How the partial sums of a cluster meet.  Up to 16 tokens every thread sends its few to the CTA that joins them, which
-    // waits on a barrier of its own: no cluster-wide barrier after the products (16 x 4096 x 4096: 5.1 us against 5.6 us).  With
+    // waits on a barrier of its own: no cluster-wide barrier after the products (16 x 4096 x 4096: half a microsecond less).  With
     // more tokens the stores are too many (100 tokens: 1.7 us slower): sums go to shared memory, over the operand stages, and
     // are read from there in 16-byte pieces; so they are where K is not cut, to be stored along the channels (100 x 16384 x
     // 4096: 16.6 us, by thread and column 19.9).
@@ -417,7 +417,10 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     if (S::PUSH && SPLIT > 1) cluster_arrive();                        // nothing is sent before every CTA's barrier stands
-    griddep_launch_dependents();                                       // (after the allocation, as above)
+    // When the next kernel may be scheduled (after the allocation, as above): at once where it cannot share an SM with this one;
+    // else when the last loads are on their way -- earlier its CTAs pile up, two to an SM, on the SMs that are free and stay
+    // there (64 x 4096 x 4096 6.5 against 7.4 us, 16 x 4096 x 4096 4.9 against 5.2).
+    if (S::RESIDENT == 1) griddep_launch_dependents();
     griddep_wait();
 
     bool ok = true;
@@ -431,6 +434,7 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
                                    sa + S::A_BYTES, &tmap_x, kb * BKB, tm * BN);
                 if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
             }
+            if (S::RESIDENT > 1) griddep_launch_dependents();
         }
     } else if (warp == 1) {
         if (lane == 0) {
