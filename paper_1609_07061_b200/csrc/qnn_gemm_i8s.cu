@@ -945,8 +945,8 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
         // there is to do is to stream them.  128 columns have one CTA an SM: K is cut while all clusters are resident at once
         // (100 x 2048 x 4096: 7.2 us in 16 clusters of four, 11.9 in 16 of eight, of which 15 fit).
         struct Narrow { int cols; float start, block, stream, hand; };
-        static const Narrow narrow[] = {{16, 3.0f, 0.28f, 0.34f, 0.3f}, {32, 3.5f, 0.29f, 0.34f, 0.6f}, {64, 4.4f, 0.31f, 0.38f, 0.8f},
-                                        {128, 5.0f, 0.26f, 0.44f, 0.6f}};
+        static const Narrow narrow[] = {{16, 3.0f, 0.28f, 0.34f, 0.3f}, {32, 3.5f, 0.31f, 0.28f, 0.3f}, {64, 4.0f, 0.22f, 0.38f, 0.3f},
+                                        {128, 5.0f, 0.31f, 0.46f, 0.6f}};
         const int i = p.M <= 16 ? 0 : p.M <= 32 ? 1 : p.M <= 64 ? 2 : 3;
         const int64_t tiles = ceil_div(p.N, BM) * ceil_div(p.M, narrow[i].cols);
         int split = 1;
