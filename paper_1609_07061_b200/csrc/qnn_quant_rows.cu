@@ -32,9 +32,10 @@ struct RowArgs {
     void *sum; int64_t ld_sum;     // may be NULL
     void *values; int64_t ld_values; int values_type;   // may be NULL
     int tpr;                       // threads per row, a multiple of 32
+    float one;                     // 1, from memory: see to_codes
 };
 
-// 1.5 * 2^23: t * inv + MAGIC rounds to a whole number (to even at ties) and leaves it in the low bits of the float
+// 1.5 * 2^23: x + MAGIC rounds to a whole number (to even at ties) and leaves it in the low bits of the float
 constexpr float MAGIC = 12582912.0f;
 
 // two to the power, and reciprocal, on the special-function unit; results below the normal range are 0
@@ -147,15 +148,18 @@ __device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, 
         }
     }
 }
-// MAGIC + code of W elements, and the values the codes stand for
+// MAGIC + code of W elements, and the values the codes stand for.  The product is rounded to fp32 before MAGIC is added, as the
+// definition says; fused into one operation, t = max / 2 (63.5, common among 16-bit values) follows the rounding error of 127 / max
+// to 63 or 64 instead of being a tie.  (ptxas fuses mul.rn.f32x2 and add.rn.f32x2: the sum is a fused operation of its own,
+// product * one + MAGIC, with a `one` that only the host knows.)
 template <int W>
-__device__ __forceinline__ void to_codes(const float (&t)[W], float inv, float (&f)[W])
+__device__ __forceinline__ void to_codes(const float (&t)[W], float inv, float one, float (&f)[W])
 {
     if constexpr (W == 1) {
-        f[0] = fmaf(t[0], inv, MAGIC);
+        f[0] = __fadd_rn(__fmul_rn(t[0], inv), MAGIC);
     } else {
 #pragma unroll
-        for (int i = 0; i < W; i += 2) unpair(fma2(pair(t[i], t[i + 1]), pair(inv, inv), pair(MAGIC, MAGIC)), f[i], f[i + 1]);
+        for (int i = 0; i < W; i += 2) unpair(fma2(mul2(pair(t[i], t[i + 1]), pair(inv, inv)), pair(one, one), pair(MAGIC, MAGIC)), f[i], f[i + 1]);
     }
 }
 template <int W>
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(cons
         const int32_t k0 = (c * tpr + t0) * W;
         if (k0 < p.KP) {
             float f[W];
-            to_codes<W>(t[c], r.inv, f);
+            to_codes<W>(t[c], r.inv, p.one, f);
             store_codes<W>(cr + k0, f, r.keep);
             if (p.values != nullptr && k0 < K) {
                 to_values<W>(f, r.scale);
@@ -542,7 +546,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_ragged_kern
             const float e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
             float f[8];
             uint4 u[RunStore<V>::N];
-            to_codes<8>(e, r.inv, f);
+            to_codes<8>(e, r.inv, p.one, f);
             to_values<8>(f, r.scale);
             RunStore<V>::pack(f, u);
             values.last = u[RunStore<V>::N - 1];
@@ -552,7 +556,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_ragged_kern
             const int32_t k = first + c * 256, k0 = k + lane * 8;
             if (k >= p.KP) break;
             float f[8];
-            to_codes<8>(t[c], r.inv, f);
+            to_codes<8>(t[c], r.inv, p.one, f);
             if (k0 < p.KP) store_codes<8>(cr + k0, f, r.keep);
             if (p.values != nullptr && k < K) {
                 to_values<8>(f, r.scale);
@@ -638,7 +642,7 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
                                  [&](Piece<T, W> &gv) { load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv); });
                 if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
             }
-            to_codes<W>(t, r.inv, f);
+            to_codes<W>(t, r.inv, p.one, f);
             store_codes<W>(cr + k0, f, r.keep);
             if (p.values != nullptr && k0 < p.K) {
                 to_values<W>(f, r.scale);
@@ -769,6 +773,7 @@ int quant_rows(RowArgs p, int type, int64_t K, const char *what, void *stream)
     }
     p.K = (int32_t)K;
     p.KP = (int32_t)kp;
+    p.one = 1.0f;
     cudaStream_t st = as_stream(stream);
     switch (type) {
         case QNN_TYPE_F32: return launch_rows_w<OP, float>(p, what, st);

@@ -640,3 +640,38 @@ def test_scores_repeat_bit_for_bit(q, T, V):
     first = run_scores(q, z, ids, 10, V)
     for _ in range(6):
         assert all(torch.equal(a, b) for a, b in zip(run_scores(q, z, ids, 10, V), first))
+
+
+# ---- rounding of the codes -----------------------------------------------------------------------------------------
+
+def codes_by_definition(t):
+    """round_half_even(t * (127 / max|t|)) in fp32, and max|t| / 127 (numpy: every operation rounded once)."""
+    top = np.abs(t).max(1, keepdims=True)
+    return np.rint(t * (np.float32(127.0) / top)).astype(np.int8), (top / np.float32(127.0))[:, 0]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,K", [(400, 16), (300, 512), (64, 1031), (40, 4098), (9, 16400), (5, 20001)])
+def test_codes_are_the_definition_bit_for_bit(q, rows, K, dtype):
+    """Rows full of ties (t = max * n / 254 with n odd, as nearly as the type holds it): the product is rounded to fp32, then to
+    a whole number, in every kernel that quantises; no tolerance."""
+    g = gen(rows + K)
+    top = torch.rand(rows, 1, generator=g, device="cuda") + 0.5
+    n = torch.randint(-127, 127, (rows, K), generator=g, device="cuda") * 2 + 1
+    x = (top * n / 254).to(dtype)
+    x[:, ::3] = (top * 0.5).to(dtype)                    # 63.5 exactly
+    x[:, 1] = top[:, 0].to(dtype)
+    o = Quantised(rows, K)
+    q.qnn_quantize_rows_i8(x, rows, K, K, o.codes.t, o.ldq, o.scale.t)
+    codes, scale = codes_by_definition(x.float().cpu().numpy())
+    assert np.array_equal(o.codes.t[:, :K].cpu().numpy(), codes)
+    assert np.array_equal(o.scale.t.cpu().numpy(), scale)
+    # the norm: u = (x + r) gamma rounds twice more, its factor 1 / rms cancels
+    r = torch.randn(rows, K, generator=g, device="cuda").to(dtype) if K % 2 else None
+    gamma = torch.exp2(torch.randint(-2, 3, (K,), generator=g, device="cuda").float()).to(dtype) if K % 3 else None
+    o = Quantised(rows, K)
+    q.qnn_rmsnorm_quant_i8(x, r, rows, K, K, K, gamma, 1e-5, o.codes.t, o.ldq, o.scale.t)
+    u = x.float().cpu().numpy()
+    u = u + r.float().cpu().numpy() if r is not None else u
+    u = u * gamma.float().cpu().numpy() if gamma is not None else u
+    assert np.array_equal(o.codes.t[:, :K].cpu().numpy(), codes_by_definition(u)[0])
