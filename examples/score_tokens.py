@@ -37,6 +37,8 @@ class Weights8:
     @staticmethod
     def of(w: torch.Tensor) -> "Weights8":
         N, K = w.shape
+        if w.stride(1) != 1:
+            raise ValueError("the elements of a row of the weights must lie next to each other")
         codes = torch.empty(N, pitch(K), dtype=torch.int8, device=w.device)
         scale = torch.empty(N, dtype=torch.float32, device=w.device)
         q.qnn_quantize_rows_i8(w, N, K, w.stride(0), codes, pitch(K), scale)
@@ -56,8 +58,15 @@ class Scorer:
     def __init__(self, embedding: torch.Tensor, blocks: List[Block], gamma: torch.Tensor, head: Weights8, max_tokens: int,
                  max_top: int = 8, eps: float = 1e-5):
         self.embedding, self.blocks, self.gamma, self.head, self.eps = embedding, blocks, gamma, head, eps
+        self.max_tokens, self.max_top = max_tokens, max_top
         dev, dt, T = embedding.device, embedding.dtype, max_tokens
-        self.width, self.hidden, self.vocab = embedding.shape[1], blocks[0].down.K, head.N
+        self.width, self.hidden, self.vocab = embedding.shape[1], blocks[0].down.K if blocks else 0, head.N
+        w, h = self.width, self.hidden
+        for i, b in enumerate(blocks):
+            if (b.gate_up.N, b.gate_up.K, b.down.N, b.down.K, b.gamma.numel()) != (2 * h, w, w, h, w):
+                raise ValueError(f"block {i}: weights of another width or hidden width than {w}, {h}")
+        if head.K != w or gamma.numel() != w:
+            raise ValueError(f"the last norm or the vocabulary product is not {w} wide")
 
         def buf(*shape, dtype=dt):
             return torch.empty(*shape, dtype=dtype, device=dev)
@@ -70,6 +79,22 @@ class Scorer:
         # (flat: the calls write [tokens, top] rows next to each other)
         self.top_logprob, self.top_ids = buf(T * max_top, dtype=torch.float32), buf(T * max_top, dtype=torch.int64)
 
+    def check(self, top: int = 0, **per_token: Optional[torch.Tensor]) -> int:
+        """Number of tokens of a call; every argument that the buffers or the calls below could not hold is refused here, on the
+        host (the calls take pointers and sizes, and see no buffer's end)."""
+        given = {name: t for name, t in per_token.items() if t is not None}
+        T = next(iter(given.values())).numel()
+        if T > self.max_tokens:
+            raise ValueError(f"{T} tokens, but the buffers hold {self.max_tokens}")
+        if not 0 <= top <= min(self.max_top, self.vocab):
+            raise ValueError(f"{top} alternatives, but the buffers hold {self.max_top} and the vocabulary {self.vocab}")
+        for name, t in given.items():
+            if t.numel() != T:
+                raise ValueError(f"{name} has {t.numel()} elements for {T} tokens")
+            if not t.is_contiguous() or t.device != self.embedding.device:
+                raise ValueError(f"{name} must be contiguous and on {self.embedding.device}")
+        return T
+
     def norm(self, T: int, gamma: torch.Tensor, first: bool) -> None:
         """residual = x + residual (or x), and its norm as codes."""
         d = self.width
@@ -81,7 +106,7 @@ class Scorer:
 
     def score(self, tokens: torch.Tensor, targets: torch.Tensor, top: int = 5) -> Dict[str, torch.Tensor]:
         """Log probabilities of `targets`, entropies and the `top` alternatives, one row a token."""
-        T, h = tokens.numel(), self.hidden
+        T, h = self.check(top, tokens=tokens, targets=targets), self.hidden
         torch.index_select(self.embedding, 0, tokens, out=self.x[:T])
         for i, b in enumerate(self.blocks):
             self.norm(T, b.gamma, first=i == 0)
@@ -97,12 +122,13 @@ class Scorer:
 
     def logits_gradient(self, targets: torch.Tensor, g_logprob: torch.Tensor, g_entropy: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Gradient of the last score() with respect to its logits, written over them."""
-        T, V = targets.numel(), self.vocab
+        T, V = self.check(targets=targets, g_logprob=g_logprob, g_entropy=g_entropy), self.vocab
         q.qnn_token_logprobs_backward(self.logits, T, V, V, targets, self.lse, self.entropy, g_logprob, g_entropy, self.logits, V)
         return self.logits[:T]
 
 
-def random_scorer(width: int, hidden: int, vocab: int, blocks: int, max_tokens: int, seed: int = 0, dtype=torch.bfloat16) -> Scorer:
+def random_scorer(width: int, hidden: int, vocab: int, blocks: int, max_tokens: int, seed: int = 0, dtype=torch.bfloat16,
+                  max_top: int = 8) -> Scorer:
     """A model of random weights of the usual magnitudes."""
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
@@ -112,7 +138,7 @@ def random_scorer(width: int, hidden: int, vocab: int, blocks: int, max_tokens: 
     bs = [Block((1 + 0.1 * normal(width)).to(dtype), Weights8.of(normal(2 * hidden, width, scale=width ** -0.5)),
                 Weights8.of(normal(width, hidden, scale=hidden ** -0.5))) for _ in range(blocks)]
     return Scorer(normal(vocab, width).to(dtype), bs, torch.ones(width, dtype=dtype, device="cuda"),
-                  Weights8.of(normal(vocab, width, scale=2.0 * width ** -0.5)), max_tokens)
+                  Weights8.of(normal(vocab, width, scale=2.0 * width ** -0.5)), max_tokens, max_top)
 
 
 def main() -> None:
@@ -125,7 +151,7 @@ def main() -> None:
     ap.add_argument("--top", type=int, default=5)
     ap.add_argument("--grad", action="store_true", help="also the gradient of the mean log probability")
     a = ap.parse_args()
-    m = random_scorer(a.width, a.hidden, a.vocab, a.blocks, a.tokens)
+    m = random_scorer(a.width, a.hidden, a.vocab, a.blocks, a.tokens, max_top=a.top)
     ids = torch.randint(0, a.vocab, (a.tokens + 1,), device="cuda")
     tokens, targets = ids[:-1].contiguous(), ids[1:].contiguous()
     runs = 20
