@@ -742,6 +742,19 @@ QNN_API int qnn_device_status(void *stream);
  * path of an installation; never needed in normal operation. */
 QNN_API int qnn_selftest_wait_timeout(void *stream);
 
+/* Diagnostic: the failure path of the kernels whose thread blocks send partial
+ * results to one another.  Runs one small instance (an int8 product of 16
+ * tokens, or the scores of one row) in which one block sends nothing and
+ * another sends a millisecond late, while the receivers wait for a short time
+ * only.  They give up, stay until the late block has sent and ended, and
+ * return: qnn_device_status() then gives QNN_ERR_TIMEOUT once and QNN_OK after
+ * that, and the context stays fully usable.  scratch: device memory, 16-byte
+ * aligned, at least QNN_SELFTEST_CLUSTER_BYTES; its contents are overwritten. */
+#define QNN_SELFTEST_PRODUCT 0
+#define QNN_SELFTEST_SCORES 1
+#define QNN_SELFTEST_CLUSTER_BYTES (128 * 1024)
+QNN_API int qnn_selftest_cluster_timeout(int which, void *scratch, size_t scratch_bytes, void *stream);
+
 /* Measurement aid: arms two cudaEvent_t handles (passed as void*) on the calling
  * thread.  The next matrix-product call made by this thread records `start`
  * immediately before and `stop` immediately after its product kernel (not

@@ -26,6 +26,8 @@ QNN_OP_XNOR_GEMM, QNN_OP_BITPLANE_GEMM, QNN_OP_CONV2D, QNN_OP_MLP = 1, 2, 3, 4
 QNN_LAYER_CONV_U8, QNN_LAYER_CONV, QNN_LAYER_FC = 1, 2, 3
 QNN_NOALLOC_SCRATCH_BYTES = 8 << 20
 QNN_TYPE_F32, QNN_TYPE_BF16, QNN_TYPE_F16 = 0, 1, 2
+QNN_SELFTEST_PRODUCT, QNN_SELFTEST_SCORES = 0, 1
+QNN_SELFTEST_CLUSTER_BYTES = 128 << 10
 
 
 class QnnError(RuntimeError):
@@ -137,6 +139,7 @@ _SIGS = {
     "qnn_select_algo": (i32, [i64, i64, i64, i32, i32, i32, i32]),
     "qnn_device_status": (i32, [vp]),
     "qnn_selftest_wait_timeout": (i32, [vp]),
+    "qnn_selftest_cluster_timeout": (i32, [i32, vp, sz, vp]),
     "qnn_pipe_peak_launch": (i32, [i32, i32, ctypes.POINTER(ctypes.c_double), vp]),
     "qnn_launch_count": (ctypes.c_uint64, []),
     "qnn_set_kernel_events": (i32, [vp, vp]),
@@ -575,6 +578,12 @@ def qnn_device_status() -> int:
 def qnn_selftest_wait_timeout():
     """Launches the diagnostic kernel whose bounded wait runs out; the next qnn_device_status() reports it once."""
     _ck(_lib.qnn_selftest_wait_timeout(_stream()), "qnn_selftest_wait_timeout")
+
+
+def qnn_selftest_cluster_timeout(which, scratch):
+    """A product (QNN_SELFTEST_PRODUCT) or scores call one of whose thread blocks sends nothing and another late; see qnn.h."""
+    n = 0 if scratch is None else scratch.numel() * scratch.element_size()
+    _ck(_lib.qnn_selftest_cluster_timeout(which, _p(scratch), n, _stream()), "qnn_selftest_cluster_timeout")
 
 
 QNN_PIPE_TENSOR_FP4, QNN_PIPE_TENSOR_I8, QNN_PIPE_POPC = 1, 2, 3

@@ -55,9 +55,6 @@ struct WideCfg {
     static_assert(STAGES >= 3 && TMEM <= 512 && BN % CB == 0 && (2 * STAGES + 4) * 8 + 8 <= 256, "configuration");
 };
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // 32 accumulator columns of one row -> scaled values; sb / bi: this block's channel scales and biases in shared memory
 __device__ __forceinline__ void scale32(const uint32_t (&v)[32], float sa, const float *sb, const float *bi, float (&f)[32])
 {
@@ -301,10 +298,7 @@ gemm_i8s_wide_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
     }
 
     __syncwarp();
-    if (*abort_flag) {
-        // give copies and products still in flight time to land before shared and tensor memory are released
-        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    }
+    if (*abort_flag) let_flights_land();
     tc_fence_before();
     __syncthreads();
     if (CTAS == 2) cluster_sync_all();     // the peer no longer touches this CTA's barriers, shared or tensor memory
@@ -369,7 +363,8 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16])
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
-template <int BN, typename TOUT, int SPLIT>
+// SELFTEST: CTA 1 of a cluster gives up before it sends, CTA 2 sends late, and the others wait for a short time only.
+template <int BN, typename TOUT, int SPLIT, bool SELFTEST = false>
 __global__ void __launch_bounds__(NARROW_THREADS, NarrowCfg<BN>::RESIDENT)
 gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const I8sParams p)
 {
@@ -464,13 +459,16 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             asm volatile("barrier.sync 1, 128;" ::: "memory");
         }
         ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag, 17));
+        if (S::PUSH && SPLIT > 1) cluster_wait();
+        if (SELFTEST && rank == 1) { *abort_flag = 1; ok = false; }
+        if (SELFTEST && rank == 2)
+            for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         if (ok) {
             tc_fence_after();
             auto store = [&](int j, int32_t sum) {               // token j of the tile, this thread's channel
                 const int64_t m = (int64_t)tm * BN + j;
                 if (n < p.N) from_float(fmaf(__int2float_rn(sum) * token_scale[j], sb, bi), static_cast<TOUT *>(p.out)[m * p.ldo + n]);
             };
-            if (S::PUSH && SPLIT > 1) cluster_wait();
             int32_t *dump = reinterpret_cast<int32_t *>(gen);    // (not PUSH) [token][128 channels], over the operand stages
 #pragma unroll 1
             for (int c = 0; c < nt; c += 16) {
@@ -496,7 +494,7 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
                 }
             }
             if (S::PUSH && SPLIT > 1 && own_groups > 0) {
-                ok = __all_sync(0xffffffffu, mbar_wait(join_bar, 0, abort_flag, 18));
+                ok = __all_sync(0xffffffffu, mbar_wait(join_bar, 0, abort_flag, 18, SELFTEST ? 64u : WAIT_LIMIT));
                 const int32_t *part = reinterpret_cast<const int32_t *>(gen + S::JOIN_OFFSET) + n_local * W;
                 for (int g = 0; g < own_groups && ok; ++g) {
                     int32_t sum[W];
@@ -520,6 +518,7 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         }
     }
     __syncwarp();
+    if (S::PUSH && SPLIT > 1 && warp < 2) cluster_wait();               // (as the other warps did above)
     if (!S::PUSH) {
         // A warp takes a few tokens at a time, a lane four channels of them: 16 16-byte reads from the CTAs of the cluster are on
         // their way before the first is used.
@@ -567,12 +566,14 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         }
         if (SPLIT > 1) cluster_sync_all();                // nobody leaves while its partial sums are being read
     }
-    if (*abort_flag) {
-        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    }
     tc_fence_before();
-    __syncthreads();
+    const bool aborted = __syncthreads_or(*abort_flag) != 0;
     tc_fence_after();
+    if (aborted) {
+        // (PUSH) the CTAs of the cluster may not have sent everything yet
+        if (S::PUSH && SPLIT > 1) stay_for_cluster();
+        else let_flights_land();
+    }
     if (warp == 1) tmem_dealloc<1>(tmem_base, S::TMEM);
 }
 
@@ -751,11 +752,11 @@ struct I8sCall {
     int64_t lda, ldb, K;
 };
 
-template <int BN, typename TOUT, int SPLIT>
+template <int BN, typename TOUT, int SPLIT, bool SELFTEST = false>
 int launch_narrow_split(const I8sCall &c, I8sParams p, cudaStream_t st)
 {
     using S = NarrowCfg<BN>;
-    auto kern = gemm_i8s_narrow_kernel<BN, TOUT, SPLIT>;
+    auto kern = gemm_i8s_narrow_kernel<BN, TOUT, SPLIT, SELFTEST>;
     static std::atomic<bool> done[64];
     if (int rc = opt_in(kern, S::TOTAL, done)) return rc;
     CUtensorMap mw, mx;
@@ -980,6 +981,19 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
 }
 
 }  // namespace
+
+int gemm_i8s_selftest(uint8_t *scratch, cudaStream_t st)
+{
+    // 16 tokens of 512 codes and 128 channels: four CTAs, a K block each
+    I8sParams p{};
+    p.M = 16; p.N = BM; p.num_kb = 4; p.tiles_n = p.tiles_m = 1;
+    const I8sCall c = {scratch, scratch + 16 * 512, 512, 512, 512};
+    float *f = reinterpret_cast<float *>(scratch + (16 + BM) * 512);
+    p.a_scale = f; p.b_scale = f + 16;
+    p.out = f + 16 + BM; p.ldo = BM;
+    static_assert((16 + BM) * 512 + (16 + BM + 16 * BM) * 4 <= CLUSTER_SELFTEST_BYTES, "scratch");
+    return launch_narrow_split<16, float, 4, true>(c, p, st);
+}
 
 int gemm_i8s_status(int *code)
 {

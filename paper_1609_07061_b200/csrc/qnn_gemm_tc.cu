@@ -1353,6 +1353,18 @@ extern "C" int qnn_selftest_wait_timeout(void *stream)
     return check_launch("qnn_selftest_wait_timeout");
 }
 
+extern "C" int qnn_selftest_cluster_timeout(int which, void *scratch, size_t scratch_bytes, void *stream)
+{
+    using namespace qnn;
+    const char *what = "qnn_selftest_cluster_timeout";
+    QNN_REQUIRE(which == QNN_SELFTEST_PRODUCT || which == QNN_SELFTEST_SCORES, QNN_ERR_INVALID_ARG, "%s: unknown test %d", what, which);
+    QNN_REQUIRE(scratch != nullptr && aligned(scratch, 16) && scratch_bytes >= (size_t)CLUSTER_SELFTEST_BYTES, QNN_ERR_WORKSPACE,
+                "%s: scratch is NULL, misaligned or smaller than %d bytes", what, CLUSTER_SELFTEST_BYTES);
+    cudaStream_t st = as_stream(stream);
+    QNN_CUDA(cudaMemsetAsync(scratch, 0, (size_t)CLUSTER_SELFTEST_BYTES, st));
+    return which == QNN_SELFTEST_PRODUCT ? gemm_i8s_selftest(static_cast<uint8_t *>(scratch), st) : scores_selftest(static_cast<uint8_t *>(scratch), st);
+}
+
 extern "C" int qnn_device_status(void *stream)
 {
     using namespace qnn;

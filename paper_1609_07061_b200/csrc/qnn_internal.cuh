@@ -120,6 +120,10 @@ int smallm_status(int *code);
 int fc_f32_status(int *code);
 int gemm_i8s_status(int *code);
 int scores_status(int *code);
+// the calls whose CTAs send to one another, with one that sends nothing and one that is late (qnn_selftest_cluster_timeout)
+constexpr int CLUSTER_SELFTEST_BYTES = QNN_SELFTEST_CLUSTER_BYTES;
+int gemm_i8s_selftest(uint8_t *scratch, cudaStream_t st);
+int scores_selftest(uint8_t *scratch, cudaStream_t st);
 
 #ifdef __CUDACC__
 // Programmatic dependent launch.  A kernel launched through launch_pdl may be scheduled while the kernel before it in the

@@ -260,8 +260,6 @@ __device__ __forceinline__ void send_f32x4(uint32_t a, float x, float y, float z
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
                  ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // THREADS threads add, one more warp loads.  Rows stream through a ring of STAGES chunks of THREADS * U granules in shared
 // memory, filled by bulk copies, so that what is in flight does not depend on how far the adding threads are.
@@ -317,7 +315,8 @@ __device__ __forceinline__ void adders_sync() { asm volatile("barrier.sync 1, %0
 // One CTA (or one cluster of them) a row, RESIDENT CTAs an SM: while one joins its statistics and finds its alternatives, the
 // others stream.  (CTAs that walk several rows and load ahead across them were slower, 97 against 90 us on 2048 x 131072
 // without alternatives: SMs differ in how fast they stream, and the hardware hands out rows as they finish.)
-template <typename T, int THREADS, int U, int STAGES, int RESIDENT>
+// SELFTEST: CTA 1 of a cluster ends without sending what it found, CTA 2 sends late, and the first one waits for a short time only.
+template <typename T, int THREADS, int U, int STAGES, int RESIDENT, bool SELFTEST = false>
 __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const ScoreArgs p)
 {
     using G = Granules<T>;
@@ -362,8 +361,7 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
                 bulk_load(smem_u32(sh.ring[stage]), row.at(g), (uint32_t)(n * 16), smem_u32(&sh.full[stage]));
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
-            if (*abort_flag)
-                for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies in flight land before shared memory is released
+            if (*abort_flag) let_flights_land();
         }
         __syncwarp();
         if (csize > 1) cluster_wait();
@@ -537,9 +535,7 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         }
     }
 
-    if (*abort_flag) {                                   // copies in flight land before shared memory is released
-        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    }
+    if (*abort_flag) let_flights_land();
     if (csize > 1) {
         // every CTA sends what it found to the first one, which goes on alone: at most MAX_TOP keys each
         int n_mine = topk > 0 ? sh.n_cand : 0;
@@ -553,13 +549,16 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         if (listed) n_mine = topk;
         __syncwarp();
         cluster_wait();
+        if (SELFTEST && crank == 1) return;
+        if (SELFTEST && crank == 2)
+            for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         const uint32_t bar = peer_addr(&sh.gathered, 0);
         if (warp == 0) {
             if (topk > 0) send_u64(peer_addr(&sh.theirs_best[crank][lane], 0), lane < n_mine ? (listed ? sh.best[lane] : sh.cand[lane]) : 0ull, bar);
             if (lane == 0) send_f32x4(peer_addr(&sh.theirs[crank], 0), a.m, a.s, a.u, 0.0f, bar);
         }
         if (crank != 0) return;
-        (void)mbar_wait(smem_u32(&sh.gathered), 0, abort_flag, 23);
+        (void)mbar_wait(smem_u32(&sh.gathered), 0, abort_flag, 23, SELFTEST ? 64u : WAIT_LIMIT);
         __syncwarp();
         // every warp joins the CTAs' statistics: lane r holds those of CTA r (their number is a power of two)
         const float4 theirs = sh.theirs[lane & (csize - 1)];
@@ -605,6 +604,8 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
         } else if (topk > 0) {
             rank_candidates<THREADS>(sh.cand, csize > 1 ? sh.n_join : sh.n_cand, topk, put);
         }
+        // the others may not have sent everything yet
+        if (csize > 1 && __any_sync(0xffffffffu, *abort_flag)) stay_for_cluster();
     }
 }
 
@@ -719,10 +720,10 @@ __global__ void __launch_bounds__(GRAD_THREADS) scores_grad_kernel(const ScoreGr
     }
 }
 
-template <typename T, int THREADS, int U, int STAGES, int RESIDENT>
+template <typename T, int THREADS, int U, int STAGES, int RESIDENT, bool SELFTEST = false>
 int launch_scores_cfg(const ScoreArgs &p, int cluster, cudaStream_t st)
 {
-    auto kern = scores_kernel<T, THREADS, U, STAGES, RESIDENT>;
+    auto kern = scores_kernel<T, THREADS, U, STAGES, RESIDENT, SELFTEST>;
     constexpr size_t smem = sizeof(ScoreShared<THREADS, U, STAGES>);
     static_assert(smem * RESIDENT + 1024 * RESIDENT <= 228 * 1024, "shared memory of an SM");
     // the shared-memory opt-in is per kernel and device: asked for once each (racing first calls set the same attribute)
@@ -815,6 +816,17 @@ int check_logits(const char *what, const void *logits, int type, int64_t T, int6
 }
 
 }  // namespace
+
+int scores_selftest(uint8_t *scratch, cudaStream_t st)
+{
+    // one row of 16384 zeros, four CTAs, eight alternatives
+    ScoreArgs p{};
+    p.logits = scratch; p.T = 1; p.V = 16384; p.ldl = 16384; p.topk = 8;
+    float *f = reinterpret_cast<float *>(scratch) + 16384;
+    p.lse = f; p.entropy = f + 1; p.top_logprob = f + 2;
+    static_assert((16384 + 2 + 8) * 4 <= CLUSTER_SELFTEST_BYTES, "scratch");
+    return launch_scores_cfg<float, 256, 4, 3, 4, true>(p, 4, st);
+}
 
 int scores_status(int *code)
 {

@@ -118,6 +118,21 @@ __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// After a wait that ran out: time for copies and products still in flight to land before shared and tensor memory go away.
+__device__ __forceinline__ void let_flights_land()
+{
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+}
+// A CTA that gave up must not end while others of its cluster may still store into its shared memory.  It stays until every
+// thread of theirs has ended or given up too (a cluster barrier waits for threads that have not exited, and for no others), and
+// then for what those sent last.  For all warps that are left in the CTA, each past its wait for the barrier's phase before.
+__device__ __forceinline__ void stay_for_cluster()
+{
+    cluster_sync_all();
+    let_flights_land();
+}
 __device__ __forceinline__ void umma_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");

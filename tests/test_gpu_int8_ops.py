@@ -675,3 +675,22 @@ def test_codes_are_the_definition_bit_for_bit(q, rows, K, dtype):
     u = u + r.float().cpu().numpy() if r is not None else u
     u = u * gamma.float().cpu().numpy() if gamma is not None else u
     assert np.array_equal(o.codes.t[:, :K].cpu().numpy(), codes_by_definition(u)[0])
+
+
+# ---- waits that run out ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("which", ["QNN_SELFTEST_PRODUCT", "QNN_SELFTEST_SCORES"])
+def test_receivers_that_give_up_stay_for_late_senders(q, which):
+    """A block of a cluster sends nothing and another late, so that the receivers' waits run out: they report it, are still there
+    when the late block's stores arrive, and every later call is as right as before."""
+    scratch = torch.empty(q.QNN_SELFTEST_CLUSTER_BYTES, dtype=torch.uint8, device="cuda")
+    assert q.qnn_device_status() == 0
+    for _ in range(3):
+        q.qnn_selftest_cluster_timeout(getattr(q, which), scratch)
+        assert q.qnn_device_status() == q.QNN_ERR_TIMEOUT
+        assert "wait" in q.qnn_last_error()
+        assert q.qnn_device_status() == 0
+    check_product(q, 16, 300, 4096, torch.float32)
+    z = (torch.randn(3, 20001, generator=gen(8), device="cuda") * 3).bfloat16()
+    check_scores(q, z, torch.tensor([5, 0, 20000], device="cuda"), 8, 20001)
+    assert q.qnn_device_status() == 0

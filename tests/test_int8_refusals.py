@@ -116,3 +116,11 @@ def test_empty_calls_are_ok(q):
     z = _mem()
     q.qnn_token_logprobs(z, 0, 10, 10, None, None)
     q.qnn_token_logprobs_backward(z, 0, 10, 10, None, None, None, None, None, z, 10)
+
+
+def test_selftest_refuses(q):
+    m = _mem(q.QNN_SELFTEST_CLUSTER_BYTES, torch.uint8)
+    refuses(q, q.QNN_ERR_INVALID_ARG, q.qnn_selftest_cluster_timeout, 2, m)
+    refuses(q, q.QNN_ERR_WORKSPACE, q.qnn_selftest_cluster_timeout, q.QNN_SELFTEST_PRODUCT, m[:-1])
+    refuses(q, q.QNN_ERR_WORKSPACE, q.qnn_selftest_cluster_timeout, q.QNN_SELFTEST_SCORES, m[1:])
+    refuses(q, q.QNN_ERR_WORKSPACE, q.qnn_selftest_cluster_timeout, q.QNN_SELFTEST_SCORES, None)
