@@ -565,8 +565,9 @@ QNN_API int qnn_logquant_combine(const int32_t *p, int groups, int64_t M, int64_
  *           stand for, code * scale rounded to values_type -- the operand a
  *           training step uses beside the codes when it passes the gradient
  *           straight through the quantiser.
- *  - A row whose largest magnitude is below 2^-118 gives scale 0 and codes 0;
- *    K = 0 gives scale 0 and touches nothing else.
+ *  - A row whose largest magnitude is below 2^-118 gives scale 0 and codes 0
+ *    (in the norm: the largest |s * gamma|, whatever 1 / sqrt(...) would make
+ *    of it); K = 0 gives scale 0 and touches nothing else.
  *    A row that holds (or computes) an infinity or a NaN, or whose sum of
  *    squares overflows fp32, gives scale NaN and codes 0, so that everything
  *    computed from it is NaN, as it would be without the quantiser.
@@ -582,7 +583,8 @@ QNN_API int qnn_quantize_rows_i8(const void *x, int type, int64_t rows, int64_t 
  *   s = x + residual (fp32),  t[k] = s[k] * gamma[k] / sqrt(mean_k s[k]^2 + eps)
  * residual [rows, ldr] or NULL (s = x); gamma [K] or NULL (all one), both of x's
  * type.  sum_out [rows, ld_sum] or NULL receives s rounded to that type, the next
- * block's residual; it may be x or residual itself (same leading dimension). */
+ * block's residual; it may be x or residual itself (same leading dimension).
+ * eps may be 0: a row whose squares fp32 cannot hold is added up in 64 bits. */
 QNN_API int qnn_rmsnorm_quant_i8(const void *x, const void *residual, int type, int64_t rows, int64_t K, int64_t ldx,
                                  int64_t ldr, const void *gamma, float eps, void *codes, int64_t ldq, float *scale,
                                  void *sum_out, int64_t ld_sum, void *values, int values_type, int64_t ld_values,

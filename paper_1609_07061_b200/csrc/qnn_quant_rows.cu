@@ -49,8 +49,27 @@ struct RowScale {
     float inv, scale;
     uint32_t keep;
 };
-template <int OP>
-__device__ __forceinline__ RowScale row_scale(float ss, uint32_t top_bits, int32_t K, float eps)
+// Below this mean square (plus eps) the fp32 sum may have lost squares to the end of the range, 2^-149; above it what is lost
+// is less than 2^-52 of the sum.
+constexpr float LEAST_MEAN = 1.2621774e-29f;             // 2^-96
+// The sum of squares of such a row times 2^180, added up in 64 bits by every warp of the row for itself.
+template <typename T>
+__device__ __forceinline__ float square_sum_again(const T *x, const T *b, int32_t K)
+{
+    double ss = 0.0;
+#pragma unroll 1
+    for (int32_t k = threadIdx.x & 31; k < K; k += 32) {
+        float s = to_float(x[k]);
+        if (b != nullptr) s += to_float(b[k]);
+        ss = fma((double)s, (double)s, ss);
+    }
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    return (float)(ss * 0x1p180);
+}
+// again(): square_sum_again of the row, only called where eps is below LEAST_MEAN
+template <int OP, class Again>
+__device__ __forceinline__ RowScale row_scale(float ss, uint32_t top_bits, int32_t K, float eps, const Again &again)
 {
     RowScale r;
     const float top = __uint_as_float(top_bits);
@@ -64,7 +83,15 @@ __device__ __forceinline__ RowScale row_scale(float ss, uint32_t top_bits, int32
     } else if (top >= 3.0092655e-36f) {      // 2^-118: below it 127 / top may overflow, and the row counts as zero
         r.inv = 127.0f / top;
         r.scale = top / 127.0f;
-        if (OP == ROW_NORM) r.scale *= 1.0f / sqrtf(ss / (float)K + eps);
+        if (OP == ROW_NORM) {
+            const float mean = ss / (float)K + eps;
+            if (mean >= LEAST_MEAN) {
+                r.scale *= 1.0f / sqrtf(mean);
+            } else {                                     // 2^90 times the root; whichever factor comes first stays in range
+                const float root = sqrtf(again() / (float)K + eps * 0x1p90f * 0x1p90f);
+                r.scale = top < 1.0f ? r.scale * 0x1p90f / root : r.scale / root * 0x1p90f;
+            }
+        }
     }
     return r;
 }
@@ -160,6 +187,21 @@ __device__ __forceinline__ void to_codes(const float (&t)[W], float inv, float o
     } else {
 #pragma unroll
         for (int i = 0; i < W; i += 2) unpair(fma2(mul2(pair(t[i], t[i + 1]), pair(inv, inv)), pair(one, one), pair(MAGIC, MAGIC)), f[i], f[i + 1]);
+    }
+}
+// the same with single sums: an instruction more for two elements, four registers less
+template <int W>
+__device__ __forceinline__ void to_codes_lean(const float (&t)[W], float inv, float (&f)[W])
+{
+    if constexpr (W == 1) {
+        f[0] = __fadd_rn(__fmul_rn(t[0], inv), MAGIC);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; i += 2) {
+            unpair(mul2(pair(t[i], t[i + 1]), pair(inv, inv)), f[i], f[i + 1]);
+            f[i] = __fadd_rn(f[i], MAGIC);
+            f[i + 1] = __fadd_rn(f[i + 1], MAGIC);
+        }
     }
 }
 template <int W>
@@ -268,7 +310,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_kernel(cons
         join_warps<OP>(sh_ss, sh_top, sub * (tpr >> 5), tpr >> 5, ss, top);
     }
     if (!live) return;
-    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
+    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps, [&] { return square_sum_again<T>(xr, br, p.K); });
     if (t0 == 0) p.scale[row] = r.scale;
     uint8_t *cr = p.codes + row * p.ldq;
 #pragma unroll
@@ -535,7 +577,7 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_ragged_kern
         if (keep_sum && w > 0 && first < K) sums.release(first, sh_sum[warp - 1]);
     }
     if (!live) return;
-    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
+    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps, [&] { return square_sum_again<T>(xr.row, br.row, p.K); });
     if (w == 0 && lane == 0) p.scale[row] = r.scale;
     uint8_t *cr = p.codes + row * p.ldq;
     auto finish = [&](auto type) {
@@ -571,8 +613,19 @@ __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_ragged_kern
 
 // Rows longer than the registers of a block hold: two passes over the row, the second mostly from L2.  sum_out may be x
 // or residual, so the first pass writes nothing and the second writes each element after reading it.
-template <int OP, typename T, int W>
-__global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
+// AGAIN: rows of a norm may need their sum of squares a second time (left to where eps allows it: the path costs registers).
+// What is read comes from blocks that share an SM; where the compiler would take the registers of one of them, it is held to as
+// many blocks as fit otherwise (2000 rows: norm 33000 bf16 122 us with two blocks, 172 with one; norm 11010 fp32 79.5 / 88; gate
+// 33000 fp32 150 / 179; plain 33000 bf16 46 / 54).
+template <typename T, int W>
+constexpr int long_blocks(int op)
+{
+    if (W == 8 && op == (sizeof(T) == 4 ? ROW_GATE : ROW_NORM)) return 2;
+    if (op == ROW_NORM ? W == 2 && sizeof(T) == 4 : op == ROW_PLAIN && W == 8 && sizeof(T) == 2) return 3;
+    return 0;                                            // (no such demand)
+}
+template <int OP, typename T, int W, bool AGAIN>
+__global__ void __launch_bounds__(512, (long_blocks<T, W>(OP))) row_quant_long_kernel(const RowArgs p)
 {
     __shared__ float sh_ss[16];
     __shared__ uint32_t sh_top[16];
@@ -584,8 +637,9 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     const int64_t step = (int64_t)blockDim.x * W;
     f32x2 ss2 = 0ull;
     float topf = 0.0f;
-    // CH pieces a round, their loads in flight together
-    constexpr int CH = 2;
+    // CH pieces a round, their loads in flight together (narrow ones: gate 2000 x 28002 bf16 in pairs 113 us with four, 153 with two;
+    // the norm, with gamma's besides, 78 and 70)
+    constexpr int CH = W < 8 && OP != ROW_NORM ? 4 : 2;
     for (int64_t k = (int64_t)threadIdx.x * W; k < p.K; k += CH * step) {
         Piece<T, W> xv[CH], bv[CH];
 #pragma unroll
@@ -616,7 +670,14 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
     __syncthreads();
     griddep_launch_dependents();
     join_warps<OP>(sh_ss, sh_top, 0, (int)(blockDim.x >> 5), ss, top);
-    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps);
+    const RowScale r = row_scale<OP>(ss, top, p.K, p.eps, [&] {
+        float again = ss;
+        if constexpr (AGAIN) {
+            again = square_sum_again<T>(xr, br, p.K);
+            __syncthreads();                             // (the block is one row) nobody writes the sums over x before all have read it
+        }
+        return again;
+    });
     if (threadIdx.x == 0) p.scale[row] = r.scale;
     uint8_t *cr = p.codes + row * p.ldq;
     for (int64_t k = (int64_t)threadIdx.x * W; k < p.KP; k += CH * step) {
@@ -642,7 +703,8 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
                                  [&](Piece<T, W> &gv) { load_piece<T, W>(static_cast<const T *>(p.gamma) + k0, gv); });
                 if (OP == ROW_NORM && p.sum != nullptr) store_floats<T, W>(static_cast<T *>(p.sum) + row * p.ld_sum + k0, s);
             }
-            to_codes<W>(t, r.inv, p.one, f);
+            if constexpr (OP == ROW_GATE) to_codes<W>(t, r.inv, p.one, f);   // (gate 2000 x 28002 bf16 113 us, lean 132; plain 33002 114, 89)
+            else to_codes_lean<W>(t, r.inv, f);
             store_codes<W>(cr + k0, f, r.keep);
             if (p.values != nullptr && k0 < p.K) {
                 to_values<W>(f, r.scale);
@@ -655,14 +717,20 @@ __global__ void __launch_bounds__(512) row_quant_long_kernel(const RowArgs p)
 constexpr int MAX_TPR = 512;
 
 template <int OP, typename T, int W>
-int launch_rows(RowArgs p, const char *what, cudaStream_t st)
+int launch_rows(RowArgs p, const char *what, cudaStream_t st, bool two_passes = false)
 {
     // (narrow accesses: more instructions an element, so long rows take the rolled loops of the other kernel)
     constexpr int MAX_NV = W == 8 ? 8 : 2;
     constexpr int64_t MAX_GROUPS = W == 8 ? (int64_t)MAX_TPR * MAX_NV : W == 2 ? 1024 : 256;
     const int64_t groups = ceil_div(p.KP, 8);            // a row in units of eight elements
-    if (groups > MAX_GROUPS) {
-        QNN_CUDA(launch_pdl(row_quant_long_kernel<OP, T, W>, dim3((unsigned)p.rows), dim3(512), 0, st, p));
+    if (groups > MAX_GROUPS || two_passes) {
+        if constexpr (OP == ROW_NORM) {
+            if (p.eps < LEAST_MEAN) {
+                QNN_CUDA(launch_pdl(row_quant_long_kernel<OP, T, W, true>, dim3((unsigned)p.rows), dim3(512), 0, st, p));
+                return check_launch(what);
+            }
+        }
+        QNN_CUDA(launch_pdl(row_quant_long_kernel<OP, T, W, false>, dim3((unsigned)p.rows), dim3(512), 0, st, p));
         return check_launch(what);
     }
     // Groups a thread.  Few rows: one, for latency.  Many rows: two while that gives blocks of at most 128 threads; small blocks
@@ -728,6 +796,13 @@ int launch_rows_w(const RowArgs &p, const char *what, cudaStream_t st)
         return ok(p.x, p.ldx, sizeof(T)) && ok(p.b, p.ldb, sizeof(T)) && ok(p.gamma, 0, sizeof(T)) && ok(p.sum, p.ld_sum, sizeof(T)) &&
                ok(p.values, p.ld_values, vs);
     };
+    if constexpr (OP == ROW_NORM) {
+        // Without an eps worth the name a row may have to be read once more, and is gone by then if the sums overwrite it as they
+        // are computed: the two passes write them last.  (8192 x 4096 bf16 in place with eps 0: 88 us; not in place 50.)
+        if (p.eps < LEAST_MEAN && p.sum != nullptr && (p.sum == p.x || p.sum == p.b))
+            return fits(8) ? launch_rows<OP, T, 8>(p, what, st, true) : fits(2) ? launch_rows<OP, T, 2>(p, what, st, true)
+                                                                               : launch_rows<OP, T, 1>(p, what, st, true);
+    }
     if (fits(8)) return launch_rows<OP, T, 8>(p, what, st);
     // Rows that end inside 16 bytes: in pairs where all tensors lie alike and a block's registers hold the row (bf16 norm 5000 x
     // 4098 51 us, shifted units 70; gate 36 and 51), and for the norm of many longer rows in pairs too, in two passes (2000 x

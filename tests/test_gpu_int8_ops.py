@@ -694,3 +694,41 @@ def test_receivers_that_give_up_stay_for_late_senders(q, which):
     z = (torch.randn(3, 20001, generator=gen(8), device="cuda") * 3).bfloat16()
     check_scores(q, z, torch.tensor([5, 0, 20000], device="cuda"), 8, 20001)
     assert q.qnn_device_status() == 0
+
+
+# ---- norms of tiny rows ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,K", [(9, 1), (9, 96), (40, 200), (9, 1031), (700, 4096), (9, 4097), (9, 16386), (9, 40000)])
+def test_rmsnorm_of_rows_whose_squares_underflow(q, rows, K, dtype):
+    """eps = 0, or as small as the squares: the sum of squares is below what fp32 holds, the norm is as usual.  1 / rms of a
+    64-bit sum rounds once; max / 127 and the product twice more, so scales within 4 U of the exact ones (elsewhere 2e-5)."""
+    g = gen(rows + K)
+    size = torch.tensor([1e-30, 3e-25, 1e-22, 2e-21, 3e-20, 1e-17, 1e-15, 1.0, 1e-33], device="cuda").repeat(rows // 9 + 1)[:rows]
+    x0 = torch.randn(rows, K, generator=g, device="cuda")
+    x0[:, 0] = 1.0
+    x0 = (x0 * size[:, None]).to(dtype)
+    r0 = (torch.randn(rows, K, generator=g, device="cuda") * size[:, None]).to(dtype)
+    gamma = (1 + 0.3 * torch.randn(K, generator=g, device="cuda")).to(dtype)
+    for eps in (0.0, 1e-40, 1e-30):
+        for over in (None, "apart", "x", "residual"):
+            x, r = x0.clone(), r0.clone() if over else None
+            s64 = x0.float() + r0.float() if over else x0.float()
+            want_sum = s64.to(dtype)
+            s64 = s64.double()
+            t64 = s64 * gamma.double() / torch.sqrt((s64 * s64).mean(1, keepdim=True) + float(np.float32(eps)))
+            into = {None: None, "apart": torch.empty_like(x), "x": x, "residual": r}[over]
+            o = Quantised(rows, K, values=torch.float32)
+            q.qnn_rmsnorm_quant_i8(x, r, rows, K, K, K, gamma, eps, o.codes.t, o.ldq, o.scale.t, sum_out=into, ld_sum=K,
+                                   values=o.values.t, ld_values=K)
+            if into is not None:
+                assert torch.equal(into, want_sum)
+            assert o.scale.t.isfinite().all() and o.values.t.isfinite().all()
+            # (one element with a residual may come close to nothing: rows below 2^-118 count as zero)
+            some = (s64 * gamma.double()).abs().amax(1) > 2.0 ** -117
+            top = t64.abs().amax(1)[some] / 127
+            assert ((o.scale.t.double()[some] - top).abs() <= 2e-5 * top).all()
+            tiny = (s64 * s64).mean(1)[some] + eps < 2.0 ** -98
+            assert ((o.scale.t.double()[some] - top).abs()[tiny] <= 4 * U * top[tiny]).all()
+            off = o.codes.t[:, :K].double()[some] - t64[some] / top[:, None]
+            assert off.abs().max().item() <= 0.5 + 3e-3
