@@ -591,7 +591,8 @@ QNN_API int qnn_rmsnorm_quant_i8(const void *x, const void *residual, int type, 
                                  void *stream);
 
 /* Gated activation: t = gate / (1 + exp(-gate)) * up.  gate [rows, ldg] and up
- * [rows, ldu] may be the two halves of one product's output. */
+ * [rows, ldu] may be the two halves of one product's output.  exp in fp32: gates
+ * below -88.72, where it overflows, give t = 0 (and gate = -inf gives NaN). */
 QNN_API int qnn_silu_mul_quant_i8(const void *gate, const void *up, int type, int64_t rows, int64_t K, int64_t ldg,
                                   int64_t ldu, void *codes, int64_t ldq, float *scale, void *values, int values_type,
                                   int64_t ld_values, void *stream);

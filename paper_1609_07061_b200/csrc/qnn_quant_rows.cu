@@ -41,8 +41,10 @@ constexpr float MAGIC = 12582912.0f;
 // two to the power, and reciprocal, on the special-function unit; results below the normal range are 0
 __device__ __forceinline__ float exp2_sfu(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float rcp_sfu(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-// a / (1 + e^-a): below a = -127 or so the sum is infinite and its reciprocal 0, the limit (but -inf gives -inf * 0, a NaN)
-__device__ __forceinline__ float silu(float a) { return a * rcp_sfu(1.0f + exp2_sfu(a * -1.4426950408889634f)); }
+// a / (1 + e^-a).  The reciprocal is taken of a quarter of the sum, which stays below 2^126 as long as e^-a is finite (a > -88.72):
+// of the sum itself it would be 0 from a = -87.3 on, where 1e-36 is left.  Below -88.72 the sum is infinite and its reciprocal 0, as
+// in the formula (but -inf gives -inf * 0, a NaN).
+__device__ __forceinline__ float silu(float a) { return a * (0.25f * rcp_sfu(fmaf(0.25f, exp2_sfu(a * -1.4426950408889634f), 0.25f))); }
 
 // what the reduction leaves a thread with: the factor that turns t into codes, the scale, and a mask for the codes
 struct RowScale {
@@ -142,11 +144,12 @@ __device__ __forceinline__ void row_op(const RowArgs &p, const Piece<T, W> &xv, 
         } else {
 #pragma unroll
             for (int i = 0; i < W; i += 2) {             // the same on pairs
+                const f32x2 quarter = pair(0.25f, 0.25f);
                 const f32x2 a2 = pair(x[i], x[i + 1]);
                 float e0, e1, d0, d1;
                 unpair(mul2(a2, pair(-1.4426950408889634f, -1.4426950408889634f)), e0, e1);
-                unpair(add2(pair(exp2_sfu(e0), exp2_sfu(e1)), pair(1.0f, 1.0f)), d0, d1);
-                unpair(mul2(mul2(a2, pair(rcp_sfu(d0), rcp_sfu(d1))), pair(b[i], b[i + 1])), t[i], t[i + 1]);
+                unpair(fma2(quarter, pair(exp2_sfu(e0), exp2_sfu(e1)), quarter), d0, d1);
+                unpair(mul2(mul2(a2, mul2(quarter, pair(rcp_sfu(d0), rcp_sfu(d1)))), pair(b[i], b[i + 1])), t[i], t[i + 1]);
             }
         }
     } else {

@@ -732,3 +732,28 @@ def test_rmsnorm_of_rows_whose_squares_underflow(q, rows, K, dtype):
             assert ((o.scale.t.double()[some] - top).abs()[tiny] <= 4 * U * top[tiny]).all()
             off = o.codes.t[:, :K].double()[some] - t64[some] / top[:, None]
             assert off.abs().max().item() <= 0.5 + 3e-3
+
+
+# ---- gates far below zero ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K", [1, 96, 1030, 1031, 4096, 16386, 20001])
+def test_silu_down_to_the_end_of_exp(q, K, dtype):
+    """Gates of -80 to -88.7, where 1 + exp(-gate) reaches the end of fp32, with factors that keep the product in range; tolerances
+    as everywhere (exp is off by (|gate| + 8) U).  Below -88.72 exp overflows, and the gate is 0 whatever it multiplies."""
+    big = min(torch.finfo(dtype).max / 8, 1e34)
+    gate = torch.empty(6, K, device="cuda")
+    for r, (lo, hi) in enumerate([(-88.5, -80.0), (-88.5, -87.0), (-88.0, -88.0), (-87.5, -86.9), (-200.0, -89.0), (-40.0, 3.0)]):
+        gate[r] = torch.linspace(hi, lo, K, device="cuda")
+    gate = gate.to(dtype)
+    up = (torch.rand(6, K, generator=gen(K), device="cuda") * 0.5 + 0.5).to(dtype)
+    up[:5] = (up[:5].float() * big).to(dtype)
+    o = Quantised(6, K, values=torch.float32)
+    q.qnn_silu_mul_quant_i8(gate, up, 6, K, K, K, o.codes.t, o.ldq, o.scale.t, values=o.values.t, ld_values=K)
+    assert o.scale.t[4].item() == 0.0 and (o.codes.t[4, :K] == 0).all() and (o.values.t[4] == 0).all()
+    a = gate.double()
+    t64 = a / (1 + torch.exp(-a)) * up.double()
+    top = t64.abs().amax(1)
+    for r in (0, 1, 2, 3, 5):
+        assert abs(o.scale.t[r].item() * 127 / top[r].item() - 1) < 2e-5, r
+        assert (o.codes.t[r, :K].double() - t64[r] * 127 / top[r]).abs().max().item() <= 0.5 + 3e-3, r
