@@ -623,8 +623,70 @@ def qnn_xnor_gemm_noalloc(a, lda, b, ldb, M, N, K, out, ldo):
 
 
 # The 8-bit language-model calls are made once per layer and token: they go through a CPython module (_qnn_calls, built next
-# to the library) that checks the tensors' types and converts the arguments in nanoseconds; ctypes needs 2 us for as many.
-from . import _qnn_calls  # noqa: E402  (after the library's own check above)
+# to the library) that checks the tensors' types and converts the arguments in nanoseconds; ctypes needs some 2 us for as many.
+# Where that module could not be built (no Python headers), the same calls go through ctypes.
+try:
+    from . import _qnn_calls  # (after the library's own check above)
+except ImportError:
+    class _qnn_calls:
+        """The module's functions through ctypes: same names, arguments and refusals."""
+
+        @staticmethod
+        def _real(t, where):
+            if t is None:
+                return QNN_TYPE_F32
+            kinds = {torch.float32: QNN_TYPE_F32, torch.bfloat16: QNN_TYPE_BF16, torch.float16: QNN_TYPE_F16}
+            if t.dtype not in kinds:
+                raise TypeError(f"{where}: {t.dtype} where float32, bfloat16 or float16 is needed")
+            return kinds[t.dtype]
+
+        @staticmethod
+        def _need(t, dtype, where):
+            if t is not None and t.dtype != dtype:
+                raise TypeError(f"{where}: {t.dtype} where {dtype} is needed")
+            return _p(t)
+
+        @classmethod
+        def qnn_quantize_rows_i8(cls, x, rows, K, ldx, codes, ldq, scale, values, ldv, stream):
+            w = "qnn_quantize_rows_i8"
+            return _lib.qnn_quantize_rows_i8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(codes, torch.int8, w), ldq,
+                                             cls._need(scale, torch.float32, w), _p(values), cls._real(values, w), ldv, stream)
+
+        @classmethod
+        def qnn_rmsnorm_quant_i8(cls, x, r, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, total, ld_sum, values, ldv, stream):
+            w, dt = "qnn_rmsnorm_quant_i8", torch.float32 if x is None else x.dtype
+            return _lib.qnn_rmsnorm_quant_i8(_p(x), cls._need(r, dt, w), cls._real(x, w), rows, K, ldx, ldr, cls._need(gamma, dt, w), eps,
+                                             cls._need(codes, torch.int8, w), ldq, cls._need(scale, torch.float32, w),
+                                             cls._need(total, dt, w), ld_sum, _p(values), cls._real(values, w), ldv, stream)
+
+        @classmethod
+        def qnn_silu_mul_quant_i8(cls, gate, up, rows, K, ldg, ldu, codes, ldq, scale, values, ldv, stream):
+            w, dt = "qnn_silu_mul_quant_i8", torch.float32 if gate is None else gate.dtype
+            return _lib.qnn_silu_mul_quant_i8(_p(gate), cls._need(up, dt, w), cls._real(gate, w), rows, K, ldg, ldu,
+                                              cls._need(codes, torch.int8, w), ldq, cls._need(scale, torch.float32, w), _p(values),
+                                              cls._real(values, w), ldv, stream)
+
+        @classmethod
+        def qnn_gemm_i8_scaled(cls, a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, stream):
+            w, f, i = "qnn_gemm_i8_scaled", torch.float32, torch.int8
+            return _lib.qnn_gemm_i8_scaled(cls._need(a, i, w), lda, cls._need(a_scale, f, w), cls._need(b, i, w), ldb,
+                                           cls._need(b_scale, f, w), cls._need(bias, f, w), M, N, K, _p(out), cls._real(out, w), ldo, stream)
+
+        @classmethod
+        def qnn_token_logprobs(cls, z, T, V, ldl, ids, logprob, entropy, lse, topk, top_logprob, top_ids, stream):
+            w, f = "qnn_token_logprobs", torch.float32
+            if not -2 ** 31 <= topk < 2 ** 31:
+                raise OverflowError("argument does not fit a C int")
+            return _lib.qnn_token_logprobs(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(logprob, f, w),
+                                           cls._need(entropy, f, w), cls._need(lse, f, w), topk, cls._need(top_logprob, f, w),
+                                           cls._need(top_ids, torch.int64, w), stream)
+
+        @classmethod
+        def qnn_token_logprobs_backward(cls, z, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d, ldd, stream):
+            w, f = "qnn_token_logprobs_backward", torch.float32
+            return _lib.qnn_token_logprobs_backward(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(lse, f, w),
+                                                    cls._need(entropy, f, w), cls._need(g_logprob, f, w), cls._need(g_entropy, f, w),
+                                                    cls._need(d, f if z is None else z.dtype, w), ldd, stream)
 
 
 def qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values=None, ld_values=0):
@@ -655,6 +717,58 @@ def qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, M, N, K, out, ldo, bias
     s = _qnn_calls.qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, _stream())
     if s:
         raise QnnError(s, "qnn_gemm_i8_scaled")
+
+
+def qnn_token_logprobs(cls, z, T, V, ldl, ids, logprob, entropy, lse, topk, top_logprob, top_ids, stream):
+            w, f = "qnn_token_logprobs", torch.float32
+            if not -2 ** 31 <= topk < 2 ** 31:
+                raise OverflowError("argument does not fit a C int")
+            return _lib.qnn_token_logprobs(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(logprob, f, w),
+                                           cls._need(entropy, f, w), cls._need(lse, f, w), topk, cls._need(top_logprob, f, w),
+                                           cls._need(top_ids, torch.int64, w), stream)
+
+        @classmethod
+        def qnn_token_logprobs_backward(cls, z, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d, ldd, stream):
+            w, f = "qnn_token_logprobs_backward", torch.float32
+            return _lib.qnn_token_logprobs_backward(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(lse, f, w),
+                                                    cls._need(entropy, f, w), cls._need(g_logprob, f, w), cls._need(g_entropy, f, w),
+                                                    cls._need(d, f if z is None else z.dtype, w), ldd, stream)
+
+
+def qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values=None, ld_values=0):
+    """Rows of x -> int8 codes and one fp32 scale a row (weights once, or activations); values: what the codes stand for."""
+    s = _qnn_calls.qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values, ld_values, _stream())
+    if s:
+        raise QnnError(s, "qnn_quantize_rows_i8")
+
+
+def qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out=None, ld_sum=0, values=None,
+                         ld_values=0):
+    """Root-mean-square norm of x + residual, scaled by gamma, as int8 codes and one scale a row; sum_out: x + residual."""
+    s = _qnn_calls.qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out, ld_sum, values,
+                                        ld_values, _stream())
+    if s:
+        raise QnnError(s, "qnn_rmsnorm_quant_i8")
+
+
+def qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values=None, ld_values=0):
+    """gate / (1 + exp(-gate)) * up as int8 codes and one scale a row."""
+    s = _qnn_calls.qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values, ld_values, _stream())
+    if s:
+        raise QnnError(s, "qnn_silu_mul_quant_i8")
+
+
+def qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, M, N, K, out, ldo, bias=None):
+    """out[m, n] = sum_k a[m, k] b[n, k] * a_scale[m] * b_scale[n] + bias[n], in the type of `out`."""
+    s = _qnn_calls.qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, _stream())
+    if s:
+        raise QnnError(s, "qnn_gemm_i8_scaled")
+
+
+def qnn_gemm_i8_scaled_kernel(M, N, K):
+    """(kind, columns, split) of the kernel that a product of this size runs on: QNN_I8S_*, see qnn.h; (0, 0, 0) for none."""
+    k = _lib.qnn_gemm_i8_scaled_kernel(M, N, K)
+    return k & 15, k >> 4 & 0xfff, k >> 16
 
 
 def qnn_token_logprobs(logits, T, V, ldl, ids, logprob, entropy=None, lse=None, topk=0, top_logprob=None, top_ids=None):

@@ -13,7 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqnn.so")
-CALLS = os.path.join(HERE, "_qnn_calls.so")
+# (the interpreter's own suffix: another Python does not load a module built for this one)
+CALLS = os.path.join(HERE, "_qnn_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -34,6 +35,30 @@ def _stale(target: str, deps) -> bool:
         return True
     t = os.path.getmtime(target)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def build_calls(force: bool = False) -> bool:
+    """The CPython module that marshals the per-token calls; it finds libqnn.so next to itself.  A machine without Python's headers
+    does without: the binding then makes the same calls through ctypes, some microseconds slower each."""
+    untagged = os.path.join(HERE, "_qnn_calls.so")           # any Python would load it
+    if untagged != CALLS and os.path.exists(untagged):
+        os.remove(untagged)
+    src = os.path.join(CSRC, "qnn_pycalls.c")
+    if not force and not _stale(CALLS, [src, LIB]):
+        return True
+    cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
+           src, "-o", CALLS, "-L", HERE, "-l:libqnn.so", "-Wl,-rpath,$ORIGIN"]
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        failed = r.stderr if r.returncode != 0 else None
+    except OSError as e:
+        failed = str(e)
+    if failed is None:
+        return True
+    if os.path.exists(CALLS):
+        os.remove(CALLS)                                     # an older one may not match the library any more
+    sys.stderr.write(f"{os.path.basename(CALLS)} was not built, the per-token calls go through ctypes:\n{failed}\n")
+    return False
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -62,14 +87,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
-    # the CPython module that marshals the per-token calls; it finds libqnn.so next to itself
-    src = os.path.join(CSRC, "qnn_pycalls.c")
-    if force or _stale(CALLS, [src, LIB]):
-        cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
-               src, "-o", CALLS, "-L", HERE, "-l:libqnn.so", "-Wl,-rpath,$ORIGIN"]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"gcc failed for {src}:\n{r.stdout}\n{r.stderr}")
+    build_calls(force)
     return LIB
 
 
