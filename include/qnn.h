@@ -612,6 +612,19 @@ QNN_API int qnn_gemm_i8_scaled(const void *a, int64_t lda, const float *a_scale,
                                const float *b_scale, const float *bias, int64_t M, int64_t N, int64_t K, void *out,
                                int out_type, int64_t ldo, void *stream);
 
+/* Which kernel a product of this size runs on (for reports and tests, as
+ * qnn_select_algo): kind | columns << 4 | split << 16, or 0 where none of them
+ * does (nothing to compute, K = 0, sizes that are refused).
+ *   QNN_I8S_TOKENS  integer units; columns: tokens, split: rows of weights a warp
+ *   QNN_I8S_NARROW  tensor cores, weights as the tile's rows; columns: tokens of a
+ *                   tile, split: thread blocks that share K
+ *   QNN_I8S_WIDE    tensor cores, tokens as the tile's rows; columns: channels of a
+ *                   tile, split: thread blocks that share a tile */
+#define QNN_I8S_TOKENS 1
+#define QNN_I8S_NARROW 2
+#define QNN_I8S_WIDE 3
+QNN_API int qnn_gemm_i8_scaled_kernel(int64_t M, int64_t N, int64_t K);
+
 /* Scores of given tokens from logits z [T, ldl] of `type`, one pass over them:
  *   lse[t]       = log sum_v exp(z[t,v])
  *   logprob[t]   = z[t, ids[t]] - lse[t]

@@ -26,6 +26,7 @@ QNN_OP_XNOR_GEMM, QNN_OP_BITPLANE_GEMM, QNN_OP_CONV2D, QNN_OP_MLP = 1, 2, 3, 4
 QNN_LAYER_CONV_U8, QNN_LAYER_CONV, QNN_LAYER_FC = 1, 2, 3
 QNN_NOALLOC_SCRATCH_BYTES = 8 << 20
 QNN_TYPE_F32, QNN_TYPE_BF16, QNN_TYPE_F16 = 0, 1, 2
+QNN_I8S_TOKENS, QNN_I8S_NARROW, QNN_I8S_WIDE = 1, 2, 3
 QNN_SELFTEST_PRODUCT, QNN_SELFTEST_SCORES = 0, 1
 QNN_SELFTEST_CLUSTER_BYTES = 128 << 10
 
@@ -133,6 +134,7 @@ _SIGS = {
     "qnn_rmsnorm_quant_i8": (i32, [vp, vp, i32, i64, i64, i64, i64, vp, f32, vp, i64, vp, vp, i64, vp, i32, i64, vp]),
     "qnn_silu_mul_quant_i8": (i32, [vp, vp, i32, i64, i64, i64, i64, vp, i64, vp, vp, i32, i64, vp]),
     "qnn_gemm_i8_scaled": (i32, [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp]),
+    "qnn_gemm_i8_scaled_kernel": (i32, [i64, i64, i64]),
     "qnn_token_logprobs": (i32, [vp, i32, i64, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp]),
     "qnn_token_logprobs_backward": (i32, [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]),
     "qnn_workspace_bytes": (sz, [i32, i64, i64, i64, i32, i32, i32]),
@@ -674,52 +676,6 @@ except ImportError:
 
         @classmethod
         def qnn_token_logprobs(cls, z, T, V, ldl, ids, logprob, entropy, lse, topk, top_logprob, top_ids, stream):
-            w, f = "qnn_token_logprobs", torch.float32
-            if not -2 ** 31 <= topk < 2 ** 31:
-                raise OverflowError("argument does not fit a C int")
-            return _lib.qnn_token_logprobs(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(logprob, f, w),
-                                           cls._need(entropy, f, w), cls._need(lse, f, w), topk, cls._need(top_logprob, f, w),
-                                           cls._need(top_ids, torch.int64, w), stream)
-
-        @classmethod
-        def qnn_token_logprobs_backward(cls, z, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d, ldd, stream):
-            w, f = "qnn_token_logprobs_backward", torch.float32
-            return _lib.qnn_token_logprobs_backward(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(lse, f, w),
-                                                    cls._need(entropy, f, w), cls._need(g_logprob, f, w), cls._need(g_entropy, f, w),
-                                                    cls._need(d, f if z is None else z.dtype, w), ldd, stream)
-
-
-def qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values=None, ld_values=0):
-    """Rows of x -> int8 codes and one fp32 scale a row (weights once, or activations); values: what the codes stand for."""
-    s = _qnn_calls.qnn_quantize_rows_i8(x, rows, K, ldx, codes, ldq, scale, values, ld_values, _stream())
-    if s:
-        raise QnnError(s, "qnn_quantize_rows_i8")
-
-
-def qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out=None, ld_sum=0, values=None,
-                         ld_values=0):
-    """Root-mean-square norm of x + residual, scaled by gamma, as int8 codes and one scale a row; sum_out: x + residual."""
-    s = _qnn_calls.qnn_rmsnorm_quant_i8(x, residual, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, sum_out, ld_sum, values,
-                                        ld_values, _stream())
-    if s:
-        raise QnnError(s, "qnn_rmsnorm_quant_i8")
-
-
-def qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values=None, ld_values=0):
-    """gate / (1 + exp(-gate)) * up as int8 codes and one scale a row."""
-    s = _qnn_calls.qnn_silu_mul_quant_i8(gate, up, rows, K, ldg, ldu, codes, ldq, scale, values, ld_values, _stream())
-    if s:
-        raise QnnError(s, "qnn_silu_mul_quant_i8")
-
-
-def qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, M, N, K, out, ldo, bias=None):
-    """out[m, n] = sum_k a[m, k] b[n, k] * a_scale[m] * b_scale[n] + bias[n], in the type of `out`."""
-    s = _qnn_calls.qnn_gemm_i8_scaled(a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, _stream())
-    if s:
-        raise QnnError(s, "qnn_gemm_i8_scaled")
-
-
-def qnn_token_logprobs(cls, z, T, V, ldl, ids, logprob, entropy, lse, topk, top_logprob, top_ids, stream):
             w, f = "qnn_token_logprobs", torch.float32
             if not -2 ** 31 <= topk < 2 ** 31:
                 raise OverflowError("argument does not fit a C int")

@@ -899,25 +899,26 @@ int launch_gemv(const I8sCall &c, const I8sParams &p, cudaStream_t st)
     return check_launch("qnn_gemm_i8_scaled");
 }
 
-template <typename TOUT>
-int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
+// The kernel that a product runs on.
+struct I8sChoice {
+    int kind;                        // QNN_I8S_*; 0: no kernel of these (K = 0)
+    int cols;                        // tokens of a thread / columns of a tile
+    int split;                       // rows of weights a warp / CTAs that share K / CTAs that share a tile
+};
+I8sChoice choose_i8s(int64_t M, int64_t N, int64_t K)
 {
-    if (c.K == 0) {
-        const int64_t need = ceil_div(p.M * p.N, 256), cap = (int64_t)sm_count() * 32;
-        QNN_CUDA(launch_pdl(bias_rows_kernel<TOUT>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0, st, p.M, p.N, p.bias,
-                            static_cast<TOUT *>(p.out), p.ldo));
-        return check_launch("qnn_gemm_i8_scaled");
-    }
+    if (K == 0) return {0, 0, 0};
+    const int32_t num_kb = (int32_t)ceil_div(K, BKB);
     // A handful of tokens: the weights go through the integer units.  One token always (4096 x 4096: 2.8 us against 4.9 us on the
     // tensor cores, 28672 x 4096: 20.9 against 21.4; rows of at most 1024 codes four to a warp: 131072 x 1024 22.7 against
     // 30.5 us two to a warp).  Two to four tokens while the weights are at most 32 MB (two: 4096 x 4096 3.2 against 4.9, but
     // 131072 x 1024 34.4 against 29.2; four: 4096 x 4096 3.5 against 4.9, 11008 x 2048 4.9 against 5.7, but 16384 x 4096 20.3
     // against 14.8), three and four not for the shortest rows (16384 x 512: 4.8 against 4.0).  Eight tokens: 5.9 us for 4096 x
     // 4096.
-    if (p.M == 1) return c.K <= 1024 ? launch_gemv<1, 4, 1, TOUT>(c, p, st) : launch_gemv<1, 2, 4, TOUT>(c, p, st);
-    if (p.M <= 4 && p.N * c.K <= (int64_t)32 << 20) {
-        if (p.M == 2) return launch_gemv<2, 4, 1, TOUT>(c, p, st);
-        if (c.K >= 1024) return launch_gemv<4, 4, 4, TOUT>(c, p, st);
+    if (M == 1) return {QNN_I8S_TOKENS, 1, K <= 1024 ? 4 : 2};
+    if (M <= 4 && N * K <= (int64_t)32 << 20) {
+        if (M == 2) return {QNN_I8S_TOKENS, 2, 4};
+        if (K >= 1024) return {QNN_I8S_TOKENS, 4, 4};
     }
 
     // On the tensor cores the time of a launch is, within about 15 % over M = 3 .. 4096, N = 128 .. 131072, K = 128 .. 16384,
@@ -936,8 +937,8 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
     for (int i = 0; i < 5; ++i) {
         const int workers = wide[i].rows == 128 ? sms : pairs;
         if (workers < 1) continue;
-        const int64_t tiles = ceil_div(p.M, wide[i].rows) * ceil_div(p.N, wide[i].cols);
-        const float t = wide[i].start + (float)ceil_div(tiles, workers) * (wide[i].block * (float)p.num_kb + wide[i].hand);
+        const int64_t tiles = ceil_div(M, wide[i].rows) * ceil_div(N, wide[i].cols);
+        const float t = wide[i].start + (float)ceil_div(tiles, workers) * (wide[i].block * (float)num_kb + wide[i].hand);
         if (best < 0 || t < cost) { best = i; cost = t; }
     }
     {
@@ -948,35 +949,53 @@ int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
         struct Narrow { int cols; float start, block, stream, hand; };
         static const Narrow narrow[] = {{16, 3.0f, 0.28f, 0.34f, 0.3f}, {32, 3.5f, 0.31f, 0.28f, 0.3f}, {64, 4.0f, 0.22f, 0.38f, 0.3f},
                                         {128, 5.0f, 0.31f, 0.46f, 0.6f}};
-        const int i = p.M <= 16 ? 0 : p.M <= 32 ? 1 : p.M <= 64 ? 2 : 3;
-        const int64_t tiles = ceil_div(p.N, BM) * ceil_div(p.M, narrow[i].cols);
+        const int i = M <= 16 ? 0 : M <= 32 ? 1 : M <= 64 ? 2 : 3;
+        const int64_t tiles = ceil_div(N, BM) * ceil_div(M, narrow[i].cols);
         int split = 1;
-        while (split < 8 && p.num_kb / (split * 2) >= 2 &&
+        while (split < 8 && num_kb / (split * 2) >= 2 &&
                (i == 3 ? tiles <= narrow_clusters(split * 2) : tiles * split * 2 <= (int64_t)sms * 5 / 4)) split *= 2;
         const int64_t waves = i == 3 ? ceil_div(tiles, narrow_clusters(split)) : ceil_div(tiles * split, 2 * sms);
         const int64_t ctas = tiles * split;
         const float an_sm = (float)ctas / (float)sms * narrow[i].stream;
         const float t = (float)waves * narrow[i].start +
-                        (float)ceil_div(p.num_kb, split) * (an_sm > narrow[i].block ? an_sm : narrow[i].block) + (split > 1 ? narrow[i].hand : 0.0f);
-        if (p.M <= 128) {
-            const float stream = 4.0f + 1.35f * (float)(p.N * c.K) * 1e-6f / 6.5f;   // (6.5 MB a us)
+                        (float)ceil_div(num_kb, split) * (an_sm > narrow[i].block ? an_sm : narrow[i].block) + (split > 1 ? narrow[i].hand : 0.0f);
+        if (M <= 128) {
+            const float stream = 4.0f + 1.35f * (float)(N * K) * 1e-6f / 6.5f;   // (6.5 MB a us)
             if (cost < stream) cost = stream;
         }
-        if (t < cost) {
-            switch (i) {
-                case 0: return launch_narrow<16, TOUT>(c, p, split, st);
-                case 1: return launch_narrow<32, TOUT>(c, p, split, st);
-                case 2: return launch_narrow<64, TOUT>(c, p, split, st);
-                default: return launch_narrow<128, TOUT>(c, p, split, st);
-            }
-        }
+        if (t < cost) return {QNN_I8S_NARROW, narrow[i].cols, split};
     }
-    switch (best) {
-        case 0: return launch_wide<64, 1, TOUT>(c, p, sms, st);
-        case 1: return launch_wide<128, 1, TOUT>(c, p, sms, st);
-        case 2: return launch_wide<128, 2, TOUT>(c, p, pairs, st);
-        case 3: return launch_wide<192, 2, TOUT>(c, p, pairs, st);
-        default: return launch_wide<256, 2, TOUT>(c, p, pairs, st);
+    return {QNN_I8S_WIDE, wide[best].cols, wide[best].rows / BM};
+}
+
+template <typename TOUT>
+int run_i8s(const I8sCall &c, const I8sParams &p, cudaStream_t st)
+{
+    const I8sChoice k = choose_i8s(p.M, p.N, c.K);
+    switch (k.kind) {
+        case QNN_I8S_TOKENS:
+            if (k.cols == 1) return k.split == 4 ? launch_gemv<1, 4, 1, TOUT>(c, p, st) : launch_gemv<1, 2, 4, TOUT>(c, p, st);
+            return k.cols == 2 ? launch_gemv<2, 4, 1, TOUT>(c, p, st) : launch_gemv<4, 4, 4, TOUT>(c, p, st);
+        case QNN_I8S_NARROW:
+            switch (k.cols) {
+                case 16: return launch_narrow<16, TOUT>(c, p, k.split, st);
+                case 32: return launch_narrow<32, TOUT>(c, p, k.split, st);
+                case 64: return launch_narrow<64, TOUT>(c, p, k.split, st);
+                default: return launch_narrow<128, TOUT>(c, p, k.split, st);
+            }
+        case QNN_I8S_WIDE:
+            if (k.split == 1) return k.cols == 64 ? launch_wide<64, 1, TOUT>(c, p, sm_count(), st) : launch_wide<128, 1, TOUT>(c, p, sm_count(), st);
+            switch (k.cols) {
+                case 128: return launch_wide<128, 2, TOUT>(c, p, pairs_resident(), st);
+                case 192: return launch_wide<192, 2, TOUT>(c, p, pairs_resident(), st);
+                default: return launch_wide<256, 2, TOUT>(c, p, pairs_resident(), st);
+            }
+        default: {
+            const int64_t need = ceil_div(p.M * p.N, 256), cap = (int64_t)sm_count() * 32;
+            QNN_CUDA(launch_pdl(bias_rows_kernel<TOUT>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0, st, p.M, p.N, p.bias,
+                                static_cast<TOUT *>(p.out), p.ldo));
+            return check_launch("qnn_gemm_i8_scaled");
+        }
     }
 }
 
@@ -1004,6 +1023,13 @@ int gemm_i8s_status(int *code)
 }  // namespace qnn
 
 using namespace qnn;
+
+extern "C" int qnn_gemm_i8_scaled_kernel(int64_t M, int64_t N, int64_t K)
+{
+    if (M <= 0 || N <= 0 || K < 0 || M > (int64_t)1 << 30 || N > (int64_t)1 << 30 || K >= (int64_t)1 << 17) return 0;
+    const I8sChoice k = choose_i8s(M, N, K);
+    return k.kind | k.cols << 4 | k.split << 16;
+}
 
 extern "C" int qnn_gemm_i8_scaled(const void *a, int64_t lda, const float *a_scale, const void *b, int64_t ldb, const float *b_scale,
                                   const float *bias, int64_t M, int64_t N, int64_t K, void *out, int out_type, int64_t ldo, void *stream)

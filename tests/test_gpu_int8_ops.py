@@ -757,3 +757,35 @@ def test_silu_down_to_the_end_of_exp(q, K, dtype):
     for r in (0, 1, 2, 3, 5):
         assert abs(o.scale.t[r].item() * 127 / top[r].item() - 1) < 2e-5, r
         assert (o.codes.t[r, :K].double() - t64[r] * 127 / top[r]).abs().max().item() <= 0.5 + 3e-3, r
+
+
+# ---- every kernel instance -----------------------------------------------------------------------------------------------------
+
+# odd remainders of tiles, of K blocks and of the shares of K
+INSTANCES = [(1, 301, 700), (1, 301, 4001), (2, 1030, 333), (3, 30, 1044), (3, 1728, 4416), (4, 143, 12138),
+             (8, 112, 20), (3, 113, 426), (5, 2058, 1060), (6, 489, 2288),
+             (30, 2694, 30), (19, 9673, 2880), (19, 295, 1353), (27, 99, 1985),
+             (47, 14336, 1366), (41, 10112, 5760), (48, 11008, 2048), (45, 389, 1307), (64, 4096, 4096), (43, 102, 2361),
+             (109, 15538, 4352), (100, 16384, 4096), (160, 3392, 14144), (65, 4245, 5562), (90, 2684, 2520), (107, 153, 5154),
+             (169, 75, 41), (65, 745, 245), (46, 9502, 630), (524, 3149, 1129), (900, 1856, 2752), (133, 4738, 2528),
+             (153, 10338, 682), (1846, 1431, 1315), (701, 4096, 4096), (1442, 2465, 1947), (134, 16473, 1322), (10000, 4096, 4096)]
+
+
+def test_instances_are_all_of_them(q):
+    """The products below run on every kernel that the choice by cost can reach, with rows that leave as bulk stores or 16-byte
+    stores, and with rows that leave element by element."""
+    every = {(q.QNN_I8S_TOKENS, c, r) for c, r in ((1, 4), (1, 2), (2, 4), (4, 4))}
+    every |= {(q.QNN_I8S_NARROW, c, s) for c in (16, 32, 64, 128) for s in (1, 2, 4, 8)}
+    every |= {(q.QNN_I8S_WIDE, c, s) for c, s in ((64, 1), (128, 1), (128, 2), (192, 2), (256, 2))}
+    for round_to in (lambda N: N // 8 * 8, lambda N: N | 1):
+        reached = {q.qnn_gemm_i8_scaled_kernel(M, round_to(N), K) for M, N, K in INSTANCES}
+        assert reached == every, (every - reached, reached - every)
+    assert q.qnn_gemm_i8_scaled_kernel(5, 5, 0) == q.qnn_gemm_i8_scaled_kernel(0, 5, 5) == (0, 0, 0)
+
+
+@pytest.mark.parametrize("M,N,K", INSTANCES)
+def test_product_instances(q, M, N, K):
+    for n, dtypes in ((N // 8 * 8, TYPES), (N | 1, TYPES[:2])):
+        for dtype in dtypes:
+            check_product(q, M, n, K, dtype, bias=dtype != torch.float16, seed=1)
+    assert q.qnn_device_status() == 0
