@@ -789,3 +789,140 @@ def test_product_instances(q, M, N, K):
         for dtype in dtypes:
             check_product(q, M, n, K, dtype, bias=dtype != torch.float16, seed=1)
     assert q.qnn_device_status() == 0
+
+
+# ---- scores: nothing lost, nothing counted twice --------------------------------------------------------------------------------
+
+LONG_SCORES = [(5, 40), (130, 1000), (2000, 2560), (300, 5003), (1100, 8001), (700, 16384), (64, 32000), (33, 50021), (200, 65536), (1, 70001),
+               (4, 128001), (40, 128000), (3, 300001)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", LONG_SCORES)
+def test_scores_count_every_logit(q, T, V, dtype):
+    """Equal logits: every e^(z - m) is 1 and the sum is the whole number V, exactly, in any order; what is left is one logarithm
+    (2 units of its value) and one rounding.  A logit more or less moves it by 1 / V, 30 times that at V = 300001."""
+    for value, ld, off in ((0.0, V, 0), (1.5, V + 3, 1)):
+        z = torch.full((off + T * ld,), float("nan"), dtype=dtype, device="cuda")[off:].view(T, ld)[:, :V]
+        z.fill_(value)
+        ids = torch.randint(0, V, (T,), generator=gen(V), device="cuda")
+        lp, h, lse, _, _ = run_scores(q, z, ids, 0, ld)
+        log = float(np.log(np.float64(V)))
+        assert ((lse.double() - (value + log)).abs() <= 4 * U * (value + log)).all()
+        assert ((h.double() - log).abs() <= 4 * U * log).all()
+        assert ((lp.double() + log).abs() <= 4 * U * log).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(40, 40), (1031, 1031), (5003, 5003), (600, 50021), (5, 131077), (3, 300001), (64, 131077)])
+def test_scores_find_every_place(q, T, V, dtype):
+    """One logit left among masked ones, in another place in every row (in every place, where there are as many rows): e^0 is the
+    whole sum, so every number is exact, and it is the best alternative."""
+    g = gen(T + V)
+    at = torch.arange(T, device="cuda") if T == V else torch.randint(0, V, (T,), generator=g, device="cuda")
+    if T < V:                                            # the ends, and both sides of where a row is cut in two, four or eight
+        edges = [0, V - 1, V // 2, V // 2 + 7, V // 8, V // 4 - 1, V - 9]
+        at[:min(T, 7)] = torch.tensor(edges[:min(T, 7)], device="cuda")
+    for value in (0.0, -7.5):
+        z = torch.full((T, V), float("-inf"), device="cuda", dtype=dtype)
+        z.scatter_(1, at[:, None], value)
+        lp, h, lse, tl, ti = run_scores(q, z, at, 1, V)
+        assert (lse == value).all() and (lp == 0).all() and (h == 0).all() and (tl == 0).all()
+        assert torch.equal(ti[:, 0], at)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", LONG_SCORES)
+def test_scores_of_rising_and_falling_rows(q, T, V, dtype):
+    """Rows that rise, so that the running maximum moves in every step and all that was added is rescaled (by a factor off by
+    8 units), rows that fall, and rows that are mostly low with a high end.  A thread adds at most V / (2 * threads) terms in
+    turn, exp is off by (3 |z - m| + 4) units and counts by its probability."""
+    ramp = torch.linspace(-3.0, 0.0, V, device="cuda")
+    late = torch.where(torch.arange(V, device="cuda") >= V - max(1, V // 50), 0.0, -2.0)
+    z = torch.stack([(ramp, ramp.flip(0), late, late.flip(0))[t % 4] for t in range(min(T, 8))]).to(dtype)
+    z = z.repeat((T + z.shape[0] - 1) // z.shape[0], 1)[:T].contiguous()
+    ids = torch.randint(0, V, (T,), generator=gen(V), device="cuda")
+    lp, h, lse, _, _ = run_scores(q, z, ids, 0, V)
+    z64 = z.double()
+    logp = torch.log_softmax(z64, 1)
+    h64 = -(logp.exp() * logp).sum(1)
+    lse64 = torch.logsumexp(z64, 1)
+    threads = 64 if V <= 8192 else 128 if V <= 65536 else 256
+    steps = V / (threads * (16 if dtype == torch.float32 else 32))      # rounds, and so rescales
+    tol = U * (V / (2 * threads) + 8 * steps + 24 + 13 + 3 * lse64)
+    assert ((lse.double() - lse64).abs() <= tol).all()
+    assert ((lp.double() - logp.gather(1, ids[:, None])[:, 0]).abs() <= tol + 3 * U).all()
+    assert ((h.double() - h64).abs() <= tol * (1 + 2 * 3.0) + 3 * U * h64).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(500, 2000), (200, 32000), (100, 128000)])
+def test_scores_errors_are_roundings(q, T, V, dtype):
+    """Over many rows of random logits: the errors of hundreds of partial sums average out, so the root mean square is that of the
+    last operations -- a logarithm, a sum, exp's own bias -- and not of the terms' number."""
+    z = (torch.randn(T, V, generator=gen(T), device="cuda") * 3).to(dtype)
+    ids = torch.randint(0, V, (T,), generator=gen(V), device="cuda")
+    lp, h, lse, _, _ = run_scores(q, z, ids, 0, V)
+    logp = torch.log_softmax(z.double(), 1)
+    lse64, h64 = torch.logsumexp(z.double(), 1), -(logp.exp() * logp).sum(1)
+
+    def rms(x):
+        return x.square().mean().sqrt().item()
+    assert rms(lse.double() - lse64) <= U * (lse64.mean().item() + 8)
+    assert rms(lp.double() - logp.gather(1, ids[:, None])[:, 0]) <= U * (-lp.double().mean().item() + 2 * lse64.mean().item() + 8)
+    assert rms(h.double() - h64) <= U * (2 * h64.mean().item() + 2 * lse64.mean().item() + 16)
+
+
+# ---- gradients of batches long enough for several rounds a block ----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("T,V", [(400, 60001), (600, 60001), (1000, 60001), (300, 262147)])
+def test_scores_gradient_of_long_batches(q, T, V, dtype):
+    """16-bit batches of 20 to 80 million logits (two to four rounds a block), a token in every round: the fp32 gradient rounded
+    once, bit for bit, and that within its tolerance of 64 bits."""
+    g = gen(T + V)
+    z = (torch.randn(T, V, generator=g, device="cuda") * 2.5).to(dtype)
+    ids = (torch.arange(T, device="cuda") * (V // T) + torch.randint(0, V // T, (T,), generator=g, device="cuda"))
+    lp, h, lse = (torch.empty(T, device="cuda") for _ in range(3))
+    q.qnn_token_logprobs(z, T, V, V, ids, lp, entropy=h, lse=lse)
+    gl, gh = torch.randn(T, generator=g, device="cuda"), torch.randn(T, generator=g, device="cuda") * 0.1
+    d = Guarded((T, V), dtype)
+    q.qnn_token_logprobs_backward(z, T, V, V, ids, lse, h, gl, gh, d.t, V)
+    d.check()
+    full = torch.empty(T, V, device="cuda")
+    zf = z.float()
+    q.qnn_token_logprobs_backward(zf, T, V, V, ids, lse, h, gl, gh, full, V)
+    assert torch.equal(d.t, full.to(dtype))
+    for rows in range(0, T, 100):
+        s = slice(rows, rows + 100)
+        x = zf[s].double() - lse[s].double()[:, None]
+        p = x.exp()
+        want = -p * (gl[s].double()[:, None] + gh[s].double()[:, None] * (x + h[s].double()[:, None]))
+        want.scatter_add_(1, ids[s][:, None], gl[s].double()[:, None])
+        # exp is off by (3 |x| + 4) units, the factor by 3 of its terms, the token's sum by one of its own
+        terms = p * (gl[s].double().abs()[:, None] + gh[s].double().abs()[:, None] * (x.abs() + h[s].double()[:, None]))
+        tol = U * terms * (3 * x.abs() + 10) + 2 * U * want.abs() + 1e-37
+        assert ((full[s].double() - want).abs() <= tol).all()
+
+
+# ---- scales ------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,K", [(1, 4096), (3, 1), (400, 1000), (33, 4097), (700, 4096), (5, 11010), (5, 16386), (3, 20001), (9, 33000)])
+def test_scales_of_norm_and_gate(q, rows, K, dtype):
+    """The norm: a thread adds at most K / 1024 + 32 squares in turn and a tree 12 sums, of which the root halves the error; s * gamma,
+    max / 127, the root, its reciprocal and the product round once each (the root and the reciprocal within two units).  The gate:
+    exp within (3 |a| + 4) units, the reciprocal within 2, three products, one division."""
+    g = gen(rows + K)
+    x, r = ((torch.randn(rows, K, generator=g, device="cuda") * 2).to(dtype) for _ in range(2))
+    gamma = (1 + 0.3 * torch.randn(K, generator=g, device="cuda")).to(dtype)
+    o = Quantised(rows, K)
+    q.qnn_rmsnorm_quant_i8(x, r, rows, K, K, K, gamma, 1e-6, o.codes.t, o.ldq, o.scale.t)
+    s64 = (x.float() + r.float()).double()
+    want = (s64 * gamma.double()).abs().amax(1) / 127 / torch.sqrt((s64 * s64).mean(1) + float(np.float32(1e-6)))
+    assert ((o.scale.t.double() - want).abs() <= U * ((K / 1024 + 32 + 12) / 2 + 8) * want).all()
+    o = Quantised(rows, K)
+    q.qnn_silu_mul_quant_i8(x, r, rows, K, K, K, o.codes.t, o.ldq, o.scale.t)
+    a = x.double()
+    want = (a / (1 + torch.exp(-a)) * r.double()).abs().amax(1) / 127
+    assert ((o.scale.t.double() - want).abs() <= U * (3 * a.abs().amax(1) + 4 + 2 + 4) * want).all()
