@@ -650,7 +650,8 @@ QNN_API int qnn_token_logprobs(const void *logits, int type, int64_t T, int64_t 
  * g_logprob (with ids) or g_entropy (with entropy) may be NULL: no such gradient.
  * d_logits [T, ldd] of the logits' type, rounded once; it may be logits itself
  * (ldd = ldl).  Masked entries and rows with nothing left get 0.  The top
- * alternatives carry no gradient. */
+ * alternatives carry no gradient.  p is exp(z - lse) of an fp32 lse: where all
+ * logits are far from 0, |lse| 2^-24 is the relative error of every p. */
 QNN_API int qnn_token_logprobs_backward(const void *logits, int type, int64_t T, int64_t V, int64_t ldl,
                                         const int64_t *ids, const float *lse, const float *entropy,
                                         const float *g_logprob, const float *g_entropy, void *d_logits, int64_t ldd,

@@ -5,12 +5,13 @@
 // Three kernels:
 //  - wide: persistent; tokens are the tile's 128 (a CTA pair: 256) rows, channels its columns.  Warp 0 loads by TMA, warp 1
 //    multiplies into one of two accumulator stages in tensor memory, the other warps scale and store the previous tile.  Bound
-//    by the tensor cores: 10000 x 4096 x 4096 in 110 us, 3050 T operations/s, their pipe busy 79 % of the time (nine waves of
+//    by the tensor cores: 10000 x 4096 x 4096 in 110 to 113 us, 3000 T operations/s, their pipe busy 79 % of the time (nine waves of
 //    tiles for 8.65; repeated for seconds the power limit holds it at 128 us).
 //  - narrow, for few tokens: bound by the bytes of the weights and by latency, so weights are the tile's 128 rows and the tokens
 //    its 16..128 columns; K is cut among the CTAs of a cluster, whose int32 partial sums meet in shared memory.  16 x 131072 x
-//    4096: 85 us, 6.3 TB/s of weights; 100 x 4096 x 4096: 7.7 us.
-//  - integer units, for one to four tokens: 1 x 4096 x 4096 in 2.8 us (6.1 TB/s of weights, launch and all).
+//    4096: 88 us, 6.1 TB/s of weights; 100 x 4096 x 4096: 8.8 us, 7.6 where L2 still holds the weights.
+//  - integer units, for one to four tokens: 1 x 4096 x 4096 in 5.2 us (3.2 TB/s of weights, launch and all), 2.9 where L2 still holds
+//    them; 1 x 128000 x 4096 in 76 us (6.9 TB/s).
 // All device-side waits are bounded.
 #include <cuda.h>
 #include <atomic>
@@ -579,7 +580,7 @@ gemm_i8s_narrow_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
 
 // ---- a handful of tokens ---------------------------------------------------------------------------------------
 //
-// Bound by reading the weights once, and at 2.6 us of it (16.8 MB) by latency: a launch, one round of loads, a sum.  So no
+// Bound by reading the weights once, and at 2.6 us of it (16.8 MB at the copy rate) by latency: a launch, one round of loads, a sum.  So no
 // shared-memory staging and no tensor memory: a warp reads GEMV_R rows of weights 16 bytes a lane, multiplies by the tokens'
 // codes (which stay in L1) four at a time on the integer units (dp4a), and sums over its lanes.  K may be cut among the warps
 // of a block, whose partial sums meet in shared memory.
@@ -914,17 +915,20 @@ I8sChoice choose_i8s(int64_t M, int64_t N, int64_t K)
     // 30.5 us two to a warp).  Two to four tokens while the weights are at most 32 MB (two: 4096 x 4096 3.2 against 4.9, but
     // 131072 x 1024 34.4 against 29.2; four: 4096 x 4096 3.5 against 4.9, 11008 x 2048 4.9 against 5.7, but 16384 x 4096 20.3
     // against 14.8), three and four not for the shortest rows (16384 x 512: 4.8 against 4.0).  Eight tokens: 5.9 us for 4096 x
-    // 4096.
+    // 4096.  (Weights of up to 32 MB in L2; 4096 x 4096 from HBM: one token 5.2 us, two 5.9, four 6.1, eight on the tensor cores 5.9.)
     if (M == 1) return {QNN_I8S_TOKENS, 1, K <= 1024 ? 4 : 2};
     if (M <= 4 && N * K <= (int64_t)32 << 20) {
         if (M == 2) return {QNN_I8S_TOKENS, 2, 4};
         if (K >= 1024) return {QNN_I8S_TOKENS, 4, 4};
     }
 
-    // On the tensor cores the time of a launch is, within about 15 % over M = 3 .. 4096, N = 128 .. 131072, K = 128 .. 16384,
+    // On the tensor cores the time of a launch is roughly, over M = 3 .. 4096, N = 128 .. 131072, K = 128 .. 16384,
     //   wide    start + waves * (K blocks * block + hand-over)
     //   narrow  waves * start + (K blocks of a CTA) * max(block, CTAs an SM * stream) + hand-over      (us, fitted to sweeps)
-    // with the constants below; the cheapest configuration runs.  100 x 4096 x 4096: narrow 7.8, wide 64 columns 9.2;
+    // with the constants below; the cheapest configuration runs.  Of 300 random sizes, measured over predicted: narrow 0.8 to 1.3
+    // (median 0.99, 5 to 95 %), wide 1.0 to 2.1 (median 1.14, the largest 3.1: a K block or two and large results, whose stores the
+    // model does not have -- 273 x 102905 x 211 takes 36 to 50 us and is taken for 16).  It ranks the configurations, and does no more.
+    // (Figures here and below: weights of up to 32 MB in L2.)  100 x 4096 x 4096: narrow 7.6, wide 64 columns 9.2;
     // 100 x 11008 x 2048: narrow 9.8, wide 128 columns 7.7; 16 x 131072 x 4096: narrow 85, wide 116 .. 200; 701 x 2047 x 1111:
     // wide 64 columns 8.2, 128 columns 6.6, pairs of 256 columns 9.2; 701 x 4096 x 4096: 22.8, 19.8, and pairs of 128 / 192 / 256
     // columns 18.1 / 13.2 / 15.1.

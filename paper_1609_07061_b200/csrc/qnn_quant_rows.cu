@@ -11,7 +11,8 @@
 // row that stays in registers is read once and written once.
 //
 // Bound by HBM: 16-bit x and residual in, 16-bit sum, 8-bit codes and their 16-bit values out is 9 bytes an element; norm
-// 8192 x 4096 bf16 49 us (6.2 TB/s), gate 4096 x 12288 f16 54 us (6.5 TB/s), one row of 4096 1.9 us.
+// 8192 x 4096 bf16 49 us (6.2 TB/s), gate 4096 x 12288 f16 53 us (6.6 TB/s; kept up for seconds, the power limit: 59), plain
+// 8192 x 4096 fp32 25 us (6.6 TB/s), one row of 4096 2.1 us.
 #include "qnn_types.cuh"
 
 namespace qnn {
@@ -502,9 +503,10 @@ struct RunStore {
 
 // A row of any alignment in registers: a warp owns a run of P * 256 elements, lane by lane eight, and the real tensors move in
 // aligned units of 16 bytes whatever their offsets, which may differ from tensor to tensor.  A unit's elements are shifted
-// into place by selects and byte permutes (15 a unit and direction), so what bounds it is instructions: 3000 x 11009 bf16, norm 116 us
-// (2.0 TB/s), gate 71 us (3.3 TB/s); element by element 148 and 119.  The register limits let two blocks of 350 threads
-// run on an SM (gate 3000 x 11009 116 us without them).
+// into place by selects and byte permutes (15 a unit and direction, 37 instructions an element where whole vectors take 23).  Half
+// the issue slots are used and loads are the first thing waited for: registers hold what is in flight, and their number lets two
+// blocks of 350 threads run on an SM (gate 3000 x 11009 116 us without the limits).  3000 x 11009 bf16: norm 112 us (2.7 TB/s), gate
+// 71 us (3.3 TB/s); element by element 148 and 119.
 template <int OP, typename T, int P, int MAXREG = P == 4 ? 80 : 64>
 __global__ void __launch_bounds__(512) __maxnreg__(MAXREG) row_quant_ragged_kernel(const RowArgs p)
 {
@@ -752,9 +754,9 @@ int launch_rows(RowArgs p, const char *what, cudaStream_t st, bool two_passes = 
         case 2: QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 2>, grid, block, 0, st, p)); break;
         case 4:
             if constexpr (OP == ROW_GATE && W == 8 && sizeof(T) == 2) {
-                // 64 registers a thread let 1024 threads of an SM run: two blocks of 384, a quarter of them idle.  56 let three
-                // run, at the price of a few spills (4096 x 12288 f16: 56.7 against 60.9 us; 8192 wide, where four blocks of
-                // 256 fit anyway, 38.1 against 36.4).
+                // 64 registers a thread let 1024 threads of an SM run: two blocks of 352 or 384 (K of 10241 to 12288), a quarter or
+                // more of them idle.  56 let three run, at the price of a few spills (4096 x 12288 f16: 52.9 against 58.8 us, 4096 x
+                // 10496 bf16 49 against 56).  Other blocks fill at least 820 of the 1024.
                 if (1024 / block.x * block.x < 820) {
                     QNN_CUDA(launch_pdl(row_quant_kernel<OP, T, W, 4, 56>, grid, block, 0, st, p));
                     break;
@@ -808,10 +810,10 @@ int launch_rows_w(const RowArgs &p, const char *what, cudaStream_t st)
     }
     if (fits(8)) return launch_rows<OP, T, 8>(p, what, st);
     // Rows that end inside 16 bytes: in pairs where all tensors lie alike and a block's registers hold the row (bf16 norm 5000 x
-    // 4098 51 us, shifted units 70; gate 36 and 51), and for the norm of many longer rows in pairs too, in two passes (2000 x
-    // 11010 66 and 76); else shifted units (2000 x 11010 gate 47 us, 66 in pairs; 64 x 11009 norm 6.9, 13; 5000 x 4097 norm 70, by
-    // single elements 97, gate 51, 84; 1 x 4097 norm 3.6, 6.0).  Single elements are left to the shortest rows and those that
-    // no block holds.
+    // 4098 51 us, shifted units 68; gate 39 and 49), and for the norm of many longer rows in pairs too, in two passes (2000 x
+    // 11010 70 and 74); else shifted units (2000 x 11010 gate 47.5 us, 51.5 in pairs; 64 x 11010 norm 8.1, 10; 5000 x 4097 norm 70,
+    // by single elements 97, gate 50, 84; 1 x 4097 norm 3.7, 6.0).  Single elements are left to the shortest rows and those that
+    // no block holds (gate 2000 x 28001 200 us, in pairs 2000 x 28002 116).
     const bool pairs = fits(2), held = p.KP <= 8 * 4 * MAX_TPR;
     if (pairs && (p.KP <= 8192 || !held || (OP == ROW_NORM && p.rows > 2 * (int64_t)sm_count()))) return launch_rows<OP, T, 2>(p, what, st);
     if (held && p.KP >= 256) return launch_ragged<OP, T>(p, what, st);
