@@ -396,6 +396,10 @@ __global__ void __launch_bounds__(THREADS + 32, RESIDENT) scores_kernel(const Sc
                 if (j * THREADS + tid < n) w[j] = sh.ring[stage][j * THREADS + tid];
             }
         }
+        // The stage is handed back to a bulk copy, which is of the asynchronous proxy: without this fence it may overtake the reads
+        // above.  (It did, where other rows on the SM kept its memory pipe busy with their alternatives: 232 x 171761 fp32 with 32
+        // of them, sums of some rows off by 1e-4 to 1e-2.  With it 2048 x 131072 bf16 takes 94.7 us for 94.3, 4 x 128000 6.3 for 6.2.)
+        fence_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.empty[stage]));
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }

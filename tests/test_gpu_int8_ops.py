@@ -926,3 +926,21 @@ def test_scales_of_norm_and_gate(q, rows, K, dtype):
     a = x.double()
     want = (a / (1 + torch.exp(-a)) * r.double()).abs().amax(1) / 127
     assert ((o.scale.t.double() - want).abs() <= U * (3 * a.abs().amax(1) + 4 + 2 + 4) * want).all()
+
+
+# ---- scores while other rows keep the SM busy ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V,topk", [(232, 171761, 32), (453, 88169, 32), (710, 56298, 32), (345, 115791, 20), (1500, 9001, 32), (30, 300001, 32)])
+def test_scores_stand_beside_rows_that_look_for_alternatives(q, T, V, topk, dtype):
+    """Rows stream while others on the same SM read theirs again for many alternatives: whatever that does to the timing of their
+    copies, every call gives the same bits, and those within the roundings of random rows."""
+    ld = V + 3
+    z = strided(T, V, ld, dtype, 1, gen(T + V), 3.0)
+    ids = torch.randint(0, V, (T,), generator=gen(V), device="cuda")
+    check_scores(q, z, ids, topk, ld)
+    first = run_scores(q, z, ids, topk, ld)
+    lse64 = torch.logsumexp(z.double(), 1)
+    assert (first[2].double() - lse64).abs().max().item() <= 40 * U * (1 + lse64.max().item())
+    for _ in range(30):
+        assert all(torch.equal(a, b) for a, b in zip(run_scores(q, z, ids, topk, ld), first))
