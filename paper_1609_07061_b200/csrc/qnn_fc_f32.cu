@@ -267,6 +267,7 @@ fc_sign_f32_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 for (int j = 0; j < KPT; ++j) t[j] = *reinterpret_cast<const float4 *>(wt + (kq * KPT + j) * FC_BN + 4 * n4);
                 uint32_t wv[4];
                 convert(t, kb, wv);
+                fence_async_shared();                                // the refill is of the asynchronous proxy: it must not overtake the reads
                 __syncwarp();                                        // every lane holds its values in registers: the tile may be refilled
                 if (lane == 0) mbar_arrive(wempty_bar(ws));
                 if (++ws == FC_W_STAGES) { ws = 0; wphase ^= 1u; }

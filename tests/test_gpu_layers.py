@@ -426,6 +426,30 @@ def test_fc_sign_f32_weights_read_once(q, M, K, N, ldx, ldw):
     assert e.value.status == q.QNN_ERR_WORKSPACE
 
 
+def test_fc_sign_f32_beside_calls_that_keep_memory_busy(q):
+    """Weight tiles are refilled while they are being read into registers, with another stream's calls on the same SMs: every
+    call gives the exact sums."""
+    M, K, N = 128, 4096, 4096
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x, w = torch.randn(M, K, generator=g, device="cuda"), torch.randn(K, N, generator=g, device="cuda")
+    want = (torch.where(x >= 0, 1.0, -1.0).double() @ torch.where(w >= 0, 1.0, -1.0).double()).int()
+    ws = torch.empty(q.qnn_fc_sign_f32_workspace_bytes(M, K), dtype=torch.uint8, device="cuda")
+    rows = torch.randn(2048, 11009, generator=g, device="cuda")
+    codes, scale = torch.empty(2048, 11136, dtype=torch.int8, device="cuda"), torch.empty(2048, device="cuda")
+    outs = [torch.zeros(M, N, dtype=torch.int32, device="cuda") for _ in range(20)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            q.qnn_quantize_rows_i8(rows, 2048, 11009, 11009, codes, 11136, scale)
+    for o in outs:
+        q.qnn_fc_sign_f32(x, M, K, K, w, N, N, o, N, ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    assert q.qnn_device_status() == 0
+
+
 @pytest.mark.parametrize("M,dims,chunks", [(2100, (784, 1024, 1024, 10), 3), (300, (784, 512, 256, 10), 1), (5000, (784, 1024, 1024, 10), 4)])
 def test_mlp_graph_from_host_buffers(q, M, dims, chunks):
     """The end-to-end pass (pinned host input -> scores in pinned host memory) as one CUDA graph: every replay, also
