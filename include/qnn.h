@@ -658,6 +658,104 @@ QNN_API int qnn_token_logprobs_backward(const void *logits, int type, int64_t T,
                                         void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* 8-bit floating point with a scale for each block of 128                    */
+/* ------------------------------------------------------------------------- */
+
+/* Finer scales than one a row: a layer can be trained in them.  A code is an
+ * e4m3 or e5m2 number (largest 448 and 57344); the byte s of its block scales it
+ * by 2^(s - 127), 255 meaning NaN.  Blocks are 128 elements along what a product
+ * adds up over:
+ *   activations  128 elements of a row            scale [rows, ld_scale]: byte k / 128
+ *   weights      128 x 128 of the matrix          scale [ceil(N / 128), ld_scale]: byte k / 128
+ *   columns      128 rows of a group, one column  scale [blocks, ld_scale]: byte of the column
+ * Weights serve both directions from one copy, their blocks being square.  The
+ * last kind are the operands of a weight gradient, which adds up over rows.
+ *
+ * Groups: `groups` matrices of weights (experts), and rows sorted by group.
+ * offsets int64 [groups + 1] on the device: group g has the rows offsets[g] ..
+ * offsets[g + 1] - 1, possibly none.  Rows before the first and behind the last
+ * offset belong to no group.  Offsets that fall or leave 0 .. M are taken as the
+ * largest before them, held to 0 .. M.  At most QNN_F8_MAX_GROUPS groups.
+ *
+ * Codes and scales are 16-byte aligned, their leading dimensions multiples of 16
+ * (for codes, whole 128-byte lines recommended).  No call needs a workspace, and
+ * every one may be captured in a CUDA graph. */
+#define QNN_F8_E4M3 0
+#define QNN_F8_E5M2 1
+#define QNN_F8_MAX_GROUPS 1024
+
+/* Rules shared by the three calls that quantise:
+ *   2^(s - 127) is the least power of two (not below 2^-127) at which the block's
+ *   largest magnitude is at most the largest code; code = x * 2^(127 - s) rounded
+ *   to nearest, ties to even.
+ *  - A block of zeros has s = 0 and codes 0.  A block that holds an infinity or a
+ *    NaN has s = 255 and codes 0: whatever is computed from it is NaN.
+ *  - x       device, [rows, ldx] of `type` (QNN_TYPE_*), aligned to its elements
+ *  - codes   device, [rows, ldq] of code_type; elements K .. roundup(K, 16) of
+ *            every row are written as 0, bytes beyond that are left untouched
+ *  - values  device, [rows, ld_values] of values_type, or NULL: what the codes
+ *            stand for, code * 2^(s - 127) rounded to values_type
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (a size above 2^30; tiles and columns:
+ * 65536 blocks of 128 rows and more), CUDA. */
+
+/* Blocks of 128 elements of a row.  index int64 [rows] or NULL: row r of the
+ * result is row index[r] of x (src_rows rows), e.g. tokens in the order of their
+ * experts; an index outside 0 .. src_rows - 1 gives a row of zeros. */
+QNN_API int qnn_quantize_blocks_f8(const void *x, int type, int64_t rows, int64_t K, int64_t ldx, const int64_t *index,
+                                   int64_t src_rows, void *codes, int code_type, int64_t ldq, void *scale, int64_t ld_scale,
+                                   void *values, int values_type, int64_t ld_values, void *stream);
+
+/* Blocks of 128 x 128: weights [rows, K]. */
+QNN_API int qnn_quantize_tiles_f8(const void *w, int type, int64_t rows, int64_t K, int64_t ldw, void *codes, int code_type,
+                                  int64_t ldq, void *scale, int64_t ld_scale, void *values, int values_type,
+                                  int64_t ld_values, void *stream);
+
+/* Blocks of 128 rows of a column, within groups: the rows of group g become rows
+ * 128 * (blocks of the groups before) and following of codes and values, filled up
+ * with zeros to whole blocks.  offsets may be NULL for a single group of all rows.
+ * codes, values: at least 128 * (rows / 128 + groups) rows, scale as many / 128;
+ * blocks behind the last group's are left untouched. */
+QNN_API int qnn_quantize_columns_f8(const void *x, int type, int64_t rows, int64_t K, int64_t ldx, const int64_t *offsets,
+                                    int64_t groups, void *codes, int code_type, int64_t ldq, void *scale, int64_t ld_scale,
+                                    void *values, int values_type, int64_t ld_values, void *stream);
+
+/* out[m,n] = sum_k A[m,k] B[n,k] + bias[n], A and B what codes and scales stand for,
+ * added up in fp32 and rounded once to out_type.
+ *   a, a_scale  codes [M, lda] of a_type, scales [M, ld_as] (activations)
+ *   b, b_scale  b_transposed = 0: codes [N, ldb], scales [ceil(N / 128), ld_bs]
+ *               b_transposed = 1: codes [K, ldb] with N elements a row, scales
+ *               [ceil(K / 128), ld_bs]: the input gradient, from the same weights as
+ *               the product they belong to
+ *   bias        device, fp32 [N] or NULL
+ *   out         device, [M, ldo] of out_type (QNN_TYPE_*); 16-byte aligned rows run
+ *               fastest
+ * K = 0 gives the bias.  Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (a size above
+ * 2^30), CUDA. */
+QNN_API int qnn_gemm_f8(const void *a, int a_type, int64_t lda, const void *a_scale, int64_t ld_as, const void *b, int b_type,
+                        int64_t ldb, const void *b_scale, int64_t ld_bs, int b_transposed, const float *bias, int64_t M,
+                        int64_t N, int64_t K, void *out, int out_type, int64_t ldo, void *stream);
+
+/* The same with a matrix of weights for each group of rows: b [groups][N or K][ldb],
+ * b_scale [groups][ceil(.. / 128)][ld_bs], bias [groups][N], one after the other.
+ * M is the number of rows of a and out; rows that belong to no group are left as
+ * they were. */
+QNN_API int qnn_gemm_f8_grouped(const void *a, int a_type, int64_t lda, const void *a_scale, int64_t ld_as, const void *b,
+                                int b_type, int64_t ldb, const void *b_scale, int64_t ld_bs, int b_transposed,
+                                const float *bias, const int64_t *offsets, int64_t groups, int64_t M, int64_t N, int64_t K,
+                                void *out, int out_type, int64_t ldo, void *stream);
+
+/* Weight gradient of each group: dw[g][n,k] = sum over the group's rows m of
+ * DY[m,n] X[m,k]; 0 for a group without rows.
+ *   dy, x       codes and scales as qnn_quantize_columns_f8 writes them for the same
+ *               offsets, with N and K elements a row; M is the number of rows that
+ *               call was given.  offsets may be NULL for a single group of all rows.
+ *   dw          device, [groups][N][ld_dw] of dw_type */
+QNN_API int qnn_gemm_f8_wgrad(const void *dy, int dy_type, int64_t ld_dy, const void *dy_scale, int64_t ld_dys, const void *x,
+                              int x_type, int64_t ldx, const void *x_scale, int64_t ld_xs, const int64_t *offsets,
+                              int64_t groups, int64_t M, int64_t N, int64_t K, void *dw, int dw_type, int64_t ld_dw,
+                              void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* The ConvNet of Table 7                                                     */
 /* ------------------------------------------------------------------------- */
 

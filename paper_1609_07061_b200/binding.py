@@ -29,6 +29,7 @@ QNN_TYPE_F32, QNN_TYPE_BF16, QNN_TYPE_F16 = 0, 1, 2
 QNN_I8S_TOKENS, QNN_I8S_NARROW, QNN_I8S_WIDE = 1, 2, 3
 QNN_SELFTEST_PRODUCT, QNN_SELFTEST_SCORES = 0, 1
 QNN_SELFTEST_CLUSTER_BYTES = 128 << 10
+QNN_F8_E4M3, QNN_F8_E5M2, QNN_F8_MAX_GROUPS = 0, 1, 1024
 
 
 class QnnError(RuntimeError):
@@ -137,6 +138,12 @@ _SIGS = {
     "qnn_gemm_i8_scaled_kernel": (i32, [i64, i64, i64]),
     "qnn_token_logprobs": (i32, [vp, i32, i64, i64, i64, vp, vp, vp, vp, i32, vp, vp, vp]),
     "qnn_token_logprobs_backward": (i32, [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]),
+    "qnn_quantize_blocks_f8": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, i32, i64, vp, i64, vp, i32, i64, vp]),
+    "qnn_quantize_tiles_f8": (i32, [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp, i32, i64, vp]),
+    "qnn_quantize_columns_f8": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, i32, i64, vp, i64, vp, i32, i64, vp]),
+    "qnn_gemm_f8": (i32, [vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, i32, vp, i64, i64, i64, vp, i32, i64, vp]),
+    "qnn_gemm_f8_grouped": (i32, [vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, i32, vp, vp, i64, i64, i64, i64, vp, i32, i64, vp]),
+    "qnn_gemm_f8_wgrad": (i32, [vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp]),
     "qnn_workspace_bytes": (sz, [i32, i64, i64, i64, i32, i32, i32]),
     "qnn_select_algo": (i32, [i64, i64, i64, i32, i32, i32, i32]),
     "qnn_device_status": (i32, [vp]),
@@ -674,6 +681,69 @@ except ImportError:
             return _lib.qnn_gemm_i8_scaled(cls._need(a, i, w), lda, cls._need(a_scale, f, w), cls._need(b, i, w), ldb,
                                            cls._need(b_scale, f, w), cls._need(bias, f, w), M, N, K, _p(out), cls._real(out, w), ldo, stream)
 
+        @staticmethod
+        def _f8(t, where):
+            kinds = {torch.float8_e4m3fn: QNN_F8_E4M3, torch.float8_e5m2: QNN_F8_E5M2}
+            if t is not None and t.dtype not in kinds:
+                raise TypeError(f"{where}: {t.dtype} where float8_e4m3fn or float8_e5m2 is needed")
+            return QNN_F8_E4M3 if t is None else kinds[t.dtype]
+
+        @staticmethod
+        def _scale8(t, where):
+            if t is not None and t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+                raise TypeError(f"{where}: {t.dtype} where uint8 or float8_e8m0fnu is needed")
+            return _p(t)
+
+        @staticmethod
+        def _here(device, where, *tensors):
+            for t in tensors:
+                if t is not None and t.get_device() != device:
+                    raise ValueError(f"{where}: a tensor on another device than the current one")
+
+        @classmethod
+        def qnn_quantize_blocks_f8(cls, x, rows, K, ldx, index, src_rows, codes, ldq, scale, lds, values, ldv, device, stream):
+            w = "qnn_quantize_blocks_f8"
+            cls._here(device, w, x, index, codes, scale, values)
+            return _lib.qnn_quantize_blocks_f8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(index, torch.int64, w), src_rows, _p(codes),
+                                               cls._f8(codes, w), ldq, cls._scale8(scale, w), lds, _p(values), cls._real(values, w), ldv, stream)
+
+        @classmethod
+        def qnn_quantize_tiles_f8(cls, x, rows, K, ldx, codes, ldq, scale, lds, values, ldv, device, stream):
+            w = "qnn_quantize_tiles_f8"
+            cls._here(device, w, x, codes, scale, values)
+            return _lib.qnn_quantize_tiles_f8(_p(x), cls._real(x, w), rows, K, ldx, _p(codes), cls._f8(codes, w), ldq, cls._scale8(scale, w),
+                                              lds, _p(values), cls._real(values, w), ldv, stream)
+
+        @classmethod
+        def qnn_quantize_columns_f8(cls, x, rows, K, ldx, offsets, groups, codes, ldq, scale, lds, values, ldv, device, stream):
+            w = "qnn_quantize_columns_f8"
+            cls._here(device, w, x, offsets, codes, scale, values)
+            return _lib.qnn_quantize_columns_f8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(offsets, torch.int64, w), groups, _p(codes),
+                                                cls._f8(codes, w), ldq, cls._scale8(scale, w), lds, _p(values), cls._real(values, w), ldv, stream)
+
+        @classmethod
+        def qnn_gemm_f8(cls, a, lda, a_s, ld_as, b, ldb, b_s, ld_bs, across, bias, M, N, K, out, ldo, device, stream):
+            w = "qnn_gemm_f8"
+            cls._here(device, w, a, a_s, b, b_s, bias, out)
+            return _lib.qnn_gemm_f8(_p(a), cls._f8(a, w), lda, cls._scale8(a_s, w), ld_as, _p(b), cls._f8(b, w), ldb, cls._scale8(b_s, w),
+                                    ld_bs, across, cls._need(bias, torch.float32, w), M, N, K, _p(out), cls._real(out, w), ldo, stream)
+
+        @classmethod
+        def qnn_gemm_f8_grouped(cls, a, lda, a_s, ld_as, b, ldb, b_s, ld_bs, across, bias, offsets, groups, M, N, K, out, ldo, device, stream):
+            w = "qnn_gemm_f8_grouped"
+            cls._here(device, w, a, a_s, b, b_s, bias, offsets, out)
+            return _lib.qnn_gemm_f8_grouped(_p(a), cls._f8(a, w), lda, cls._scale8(a_s, w), ld_as, _p(b), cls._f8(b, w), ldb,
+                                            cls._scale8(b_s, w), ld_bs, across, cls._need(bias, torch.float32, w),
+                                            cls._need(offsets, torch.int64, w), groups, M, N, K, _p(out), cls._real(out, w), ldo, stream)
+
+        @classmethod
+        def qnn_gemm_f8_wgrad(cls, dy, ld_dy, dy_s, ld_dys, x, ldx, x_s, ld_xs, offsets, groups, M, N, K, dw, ld_dw, device, stream):
+            w = "qnn_gemm_f8_wgrad"
+            cls._here(device, w, dy, dy_s, x, x_s, offsets, dw)
+            return _lib.qnn_gemm_f8_wgrad(_p(dy), cls._f8(dy, w), ld_dy, cls._scale8(dy_s, w), ld_dys, _p(x), cls._f8(x, w), ldx,
+                                          cls._scale8(x_s, w), ld_xs, cls._need(offsets, torch.int64, w), groups, M, N, K, _p(dw),
+                                          cls._real(dw, w), ld_dw, stream)
+
         @classmethod
         def qnn_token_logprobs(cls, z, T, V, ldl, ids, logprob, entropy, lse, topk, top_logprob, top_ids, stream):
             w, f = "qnn_token_logprobs", torch.float32
@@ -725,6 +795,61 @@ def qnn_gemm_i8_scaled_kernel(M, N, K):
     """(kind, columns, split) of the kernel that a product of this size runs on: QNN_I8S_*, see qnn.h; (0, 0, 0) for none."""
     k = _lib.qnn_gemm_i8_scaled_kernel(M, N, K)
     return k & 15, k >> 4 & 0xfff, k >> 16
+
+
+# 8-bit floating point with block scales.  codes: float8_e4m3fn or float8_e5m2; scales: uint8 or float8_e8m0fnu; every tensor on the
+# current device.
+
+def _here():
+    """The current device's index, and its current stream's handle."""
+    if _initialized():
+        d = _device()
+        return d, _raw_stream(d)
+    return (torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream) if torch.cuda.is_available() else (-1, None)
+
+
+def qnn_quantize_blocks_f8(x, rows, K, ldx, codes, ldq, scale, ld_scale, index=None, src_rows=0, values=None, ld_values=0):
+    """Rows of x (or rows index[r] of its src_rows rows) -> 8-bit floating-point codes and a scale byte for each block of 128."""
+    s = _qnn_calls.qnn_quantize_blocks_f8(x, rows, K, ldx, index, src_rows, codes, ldq, scale, ld_scale, values, ld_values, *_here())
+    if s:
+        raise QnnError(s, "qnn_quantize_blocks_f8")
+
+
+def qnn_quantize_tiles_f8(w, rows, K, ldw, codes, ldq, scale, ld_scale, values=None, ld_values=0):
+    """Weights [rows, K] -> 8-bit floating-point codes and a scale byte for each 128 x 128."""
+    s = _qnn_calls.qnn_quantize_tiles_f8(w, rows, K, ldw, codes, ldq, scale, ld_scale, values, ld_values, *_here())
+    if s:
+        raise QnnError(s, "qnn_quantize_tiles_f8")
+
+
+def qnn_quantize_columns_f8(x, rows, K, ldx, offsets, groups, codes, ldq, scale, ld_scale, values=None, ld_values=0):
+    """Columns of x in blocks of 128 rows of one group -> operands of qnn_gemm_f8_wgrad, groups filled up to whole blocks."""
+    s = _qnn_calls.qnn_quantize_columns_f8(x, rows, K, ldx, offsets, groups, codes, ldq, scale, ld_scale, values, ld_values, *_here())
+    if s:
+        raise QnnError(s, "qnn_quantize_columns_f8")
+
+
+def qnn_gemm_f8(a, lda, a_scale, ld_as, b, ldb, b_scale, ld_bs, M, N, K, out, ldo, bias=None, b_transposed=False):
+    """out[m, n] = sum_k A[m, k] B[n, k] (b_transposed: B[k, n]) + bias[n], in the type of `out`."""
+    s = _qnn_calls.qnn_gemm_f8(a, lda, a_scale, ld_as, b, ldb, b_scale, ld_bs, int(b_transposed), bias, M, N, K, out, ldo, *_here())
+    if s:
+        raise QnnError(s, "qnn_gemm_f8")
+
+
+def qnn_gemm_f8_grouped(a, lda, a_scale, ld_as, b, ldb, b_scale, ld_bs, offsets, groups, M, N, K, out, ldo, bias=None,
+                        b_transposed=False):
+    """The product with a matrix of b for each group of rows: offsets[g] .. offsets[g + 1]."""
+    s = _qnn_calls.qnn_gemm_f8_grouped(a, lda, a_scale, ld_as, b, ldb, b_scale, ld_bs, int(b_transposed), bias, offsets, groups, M, N, K,
+                                       out, ldo, *_here())
+    if s:
+        raise QnnError(s, "qnn_gemm_f8_grouped")
+
+
+def qnn_gemm_f8_wgrad(dy, ld_dy, dy_scale, ld_dys, x, ldx, x_scale, ld_xs, offsets, groups, M, N, K, dw, ld_dw):
+    """dw[g][n, k] = sum over the rows m of group g of DY[m, n] X[m, k], from what qnn_quantize_columns_f8 wrote."""
+    s = _qnn_calls.qnn_gemm_f8_wgrad(dy, ld_dy, dy_scale, ld_dys, x, ldx, x_scale, ld_xs, offsets, groups, M, N, K, dw, ld_dw, *_here())
+    if s:
+        raise QnnError(s, "qnn_gemm_f8_wgrad")
 
 
 def qnn_token_logprobs(logits, T, V, ldl, ids, logprob, entropy=None, lse=None, topk=0, top_logprob=None, top_ids=None):

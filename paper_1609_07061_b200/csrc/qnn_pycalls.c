@@ -8,8 +8,9 @@
 #include <Python.h>
 #include "qnn.h"
 
-static PyObject *s_dtype, *s_data_ptr;                   /* attribute names */
+static PyObject *s_dtype, *s_data_ptr, *s_get_device;    /* attribute names */
 static PyObject *t_f32, *t_bf16, *t_f16, *t_i8, *t_i64;  /* torch's type objects: one of each exists */
+static PyObject *t_e4m3, *t_e5m2, *t_u8, *t_e8m0;
 
 static void *ptr(PyObject *o) { return o == Py_None ? NULL : PyLong_AsVoidPtr(o); }
 /* pointer of a tensor of any type; None gives NULL */
@@ -51,6 +52,50 @@ static PyObject *real(PyObject *t, int *type, const char *where)
     else if (d == t_f16) *type = QNN_TYPE_F16;
     else if (d != t_f32) PyErr_Format(PyExc_TypeError, "%s: %S where float32, bfloat16 or float16 is needed", where, d);
     return d;
+}
+/* pointer of a tensor of 8-bit floating-point codes and its QNN_F8_*; None gives NULL */
+static void *f8(PyObject *t, int *type, const char *where)
+{
+    PyObject *d;
+    *type = QNN_F8_E4M3;
+    if (t == Py_None || PyErr_Occurred()) return NULL;
+    d = PyObject_GetAttr(t, s_dtype);
+    if (d == NULL) return NULL;
+    Py_DECREF(d);
+    if (d == t_e5m2) *type = QNN_F8_E5M2;
+    else if (d != t_e4m3) {
+        PyErr_Format(PyExc_TypeError, "%s: %S where float8_e4m3fn or float8_e5m2 is needed", where, d);
+        return NULL;
+    }
+    return any(t);
+}
+/* pointer of a tensor of scale bytes */
+static void *scale8(PyObject *t, const char *where)
+{
+    PyObject *d;
+    if (t == Py_None || PyErr_Occurred()) return NULL;
+    d = PyObject_GetAttr(t, s_dtype);
+    if (d == NULL) return NULL;
+    Py_DECREF(d);
+    if (d != t_u8 && d != t_e8m0) {
+        PyErr_Format(PyExc_TypeError, "%s: %S where uint8 or float8_e8m0fnu is needed", where, d);
+        return NULL;
+    }
+    return any(t);
+}
+/* every tensor among the n arguments must be on the current device, whose index is `device` */
+static void here(PyObject *const *a, Py_ssize_t n, PyObject *device, const char *where)
+{
+    const long dev = PyLong_AsLong(device);
+    Py_ssize_t i;
+    for (i = 0; i < n && !PyErr_Occurred(); ++i) {
+        PyObject *v;
+        if (a[i] == Py_None || PyLong_Check(a[i])) continue;
+        v = PyObject_CallMethodNoArgs(a[i], s_get_device);
+        if (v == NULL) return;
+        if (PyLong_AsLong(v) != dev) PyErr_Format(PyExc_ValueError, "%s: a tensor on another device than the current one", where);
+        Py_DECREF(v);
+    }
 }
 static int64_t i64(PyObject *o) { return (int64_t)PyLong_AsLongLong(o); }
 static int i32(PyObject *o)
@@ -112,6 +157,51 @@ ENTRY(qnn_gemm_i8_scaled, 13,
       int64_t M = i64(a[7]) COMMA N = i64(a[8]) COMMA K = i64(a[9]); void *out = any(a[10]); int64_t ldo = i64(a[11]); void *stream = ptr(a[12]),
       qnn_gemm_i8_scaled(x, lda, sa, wt, ldb, sb, bias, M, N, K, out, type, ldo, stream))
 
+ENTRY(qnn_quantize_blocks_f8, 14,
+      const char *w = "qnn_quantize_blocks_f8"; int type COMMA vtype COMMA ctype; here(a, 12, a[12], w); real(a[0], &type, w);
+      void *x = any(a[0]); int64_t rows = i64(a[1]) COMMA K = i64(a[2]) COMMA ldx = i64(a[3]); void *index = need(a[4], t_i64, w);
+      int64_t src = i64(a[5]); void *codes = f8(a[6], &ctype, w); int64_t ldq = i64(a[7]); void *scale = scale8(a[8], w);
+      int64_t lds = i64(a[9]); real(a[10], &vtype, w); void *values = any(a[10]); int64_t ldv = i64(a[11]); void *stream = ptr(a[13]),
+      qnn_quantize_blocks_f8(x, type, rows, K, ldx, index, src, codes, ctype, ldq, scale, lds, values, vtype, ldv, stream))
+
+ENTRY(qnn_quantize_tiles_f8, 12,
+      const char *w = "qnn_quantize_tiles_f8"; int type COMMA vtype COMMA ctype; here(a, 10, a[10], w); real(a[0], &type, w);
+      void *x = any(a[0]); int64_t rows = i64(a[1]) COMMA K = i64(a[2]) COMMA ldx = i64(a[3]); void *codes = f8(a[4], &ctype, w);
+      int64_t ldq = i64(a[5]); void *scale = scale8(a[6], w); int64_t lds = i64(a[7]); real(a[8], &vtype, w);
+      void *values = any(a[8]); int64_t ldv = i64(a[9]); void *stream = ptr(a[11]),
+      qnn_quantize_tiles_f8(x, type, rows, K, ldx, codes, ctype, ldq, scale, lds, values, vtype, ldv, stream))
+
+ENTRY(qnn_quantize_columns_f8, 14,
+      const char *w = "qnn_quantize_columns_f8"; int type COMMA vtype COMMA ctype; here(a, 12, a[12], w); real(a[0], &type, w);
+      void *x = any(a[0]); int64_t rows = i64(a[1]) COMMA K = i64(a[2]) COMMA ldx = i64(a[3]); void *offsets = need(a[4], t_i64, w);
+      int64_t groups = i64(a[5]); void *codes = f8(a[6], &ctype, w); int64_t ldq = i64(a[7]); void *scale = scale8(a[8], w);
+      int64_t lds = i64(a[9]); real(a[10], &vtype, w); void *values = any(a[10]); int64_t ldv = i64(a[11]); void *stream = ptr(a[13]),
+      qnn_quantize_columns_f8(x, type, rows, K, ldx, offsets, groups, codes, ctype, ldq, scale, lds, values, vtype, ldv, stream))
+
+ENTRY(qnn_gemm_f8, 17,
+      const char *w = "qnn_gemm_f8"; int type COMMA at COMMA bt; here(a, 15, a[15], w); real(a[13], &type, w);
+      void *x = f8(a[0], &at, w); int64_t lda = i64(a[1]); void *sa = scale8(a[2], w); int64_t ldsa = i64(a[3]);
+      void *wt = f8(a[4], &bt, w); int64_t ldb = i64(a[5]); void *sb = scale8(a[6], w); int64_t ldsb = i64(a[7]); int across = i32(a[8]);
+      void *bias = need(a[9], t_f32, w); int64_t M = i64(a[10]) COMMA N = i64(a[11]) COMMA K = i64(a[12]);
+      void *out = any(a[13]); int64_t ldo = i64(a[14]); void *stream = ptr(a[16]),
+      qnn_gemm_f8(x, at, lda, sa, ldsa, wt, bt, ldb, sb, ldsb, across, bias, M, N, K, out, type, ldo, stream))
+
+ENTRY(qnn_gemm_f8_grouped, 19,
+      const char *w = "qnn_gemm_f8_grouped"; int type COMMA at COMMA bt; here(a, 17, a[17], w); real(a[15], &type, w);
+      void *x = f8(a[0], &at, w); int64_t lda = i64(a[1]); void *sa = scale8(a[2], w); int64_t ldsa = i64(a[3]);
+      void *wt = f8(a[4], &bt, w); int64_t ldb = i64(a[5]); void *sb = scale8(a[6], w); int64_t ldsb = i64(a[7]); int across = i32(a[8]);
+      void *bias = need(a[9], t_f32, w); void *offsets = need(a[10], t_i64, w); int64_t groups = i64(a[11]);
+      int64_t M = i64(a[12]) COMMA N = i64(a[13]) COMMA K = i64(a[14]); void *out = any(a[15]); int64_t ldo = i64(a[16]); void *stream = ptr(a[18]),
+      qnn_gemm_f8_grouped(x, at, lda, sa, ldsa, wt, bt, ldb, sb, ldsb, across, bias, offsets, groups, M, N, K, out, type, ldo, stream))
+
+ENTRY(qnn_gemm_f8_wgrad, 17,
+      const char *w = "qnn_gemm_f8_wgrad"; int type COMMA at COMMA bt; here(a, 15, a[15], w); real(a[13], &type, w);
+      void *dy = f8(a[0], &at, w); int64_t ldy = i64(a[1]); void *sy = scale8(a[2], w); int64_t ldsy = i64(a[3]);
+      void *x = f8(a[4], &bt, w); int64_t ldx = i64(a[5]); void *sx = scale8(a[6], w); int64_t ldsx = i64(a[7]);
+      void *offsets = need(a[8], t_i64, w); int64_t groups = i64(a[9]) COMMA M = i64(a[10]) COMMA N = i64(a[11]) COMMA K = i64(a[12]);
+      void *dw = any(a[13]); int64_t ldd = i64(a[14]); void *stream = ptr(a[16]),
+      qnn_gemm_f8_wgrad(dy, at, ldy, sy, ldsy, x, bt, ldx, sx, ldsx, offsets, groups, M, N, K, dw, type, ldd, stream))
+
 ENTRY(qnn_token_logprobs, 12,
       const char *w = "qnn_token_logprobs"; int type; real(a[0], &type, w);
       void *z = any(a[0]); int64_t T = i64(a[1]) COMMA V = i64(a[2]) COMMA ldl = i64(a[3]); void *ids = need(a[4], t_i64, w);
@@ -128,7 +218,9 @@ ENTRY(qnn_token_logprobs_backward, 12,
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, "status of the C call of this name"}
 static PyMethodDef methods[] = {METHOD(qnn_quantize_rows_i8), METHOD(qnn_rmsnorm_quant_i8), METHOD(qnn_silu_mul_quant_i8),
-                                METHOD(qnn_gemm_i8_scaled), METHOD(qnn_token_logprobs), METHOD(qnn_token_logprobs_backward),
+                                METHOD(qnn_gemm_i8_scaled), METHOD(qnn_quantize_blocks_f8), METHOD(qnn_quantize_tiles_f8),
+                                METHOD(qnn_quantize_columns_f8), METHOD(qnn_gemm_f8), METHOD(qnn_gemm_f8_grouped), METHOD(qnn_gemm_f8_wgrad),
+                                METHOD(qnn_token_logprobs), METHOD(qnn_token_logprobs_backward),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qnn_calls", "Argument marshalling of libqnn.so calls.", -1, methods,
                                     NULL, NULL, NULL, NULL};
@@ -143,7 +235,13 @@ PyMODINIT_FUNC PyInit__qnn_calls(void)
     t_f16 = PyObject_GetAttrString(torch, "float16");
     t_i8 = PyObject_GetAttrString(torch, "int8");
     t_i64 = PyObject_GetAttrString(torch, "int64");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    t_e4m3 = PyObject_GetAttrString(torch, "float8_e4m3fn");
+    t_e5m2 = PyObject_GetAttrString(torch, "float8_e5m2");
+    t_u8 = PyObject_GetAttrString(torch, "uint8");
+    t_e8m0 = PyObject_GetAttrString(torch, "float8_e8m0fnu");
     Py_DECREF(torch);
+    if (!s_get_device || !t_e4m3 || !t_e5m2 || !t_u8 || !t_e8m0) return NULL;
     if (!s_dtype || !s_data_ptr || !t_f32 || !t_bf16 || !t_f16 || !t_i8 || !t_i64) return NULL;
     return PyModule_Create(&module);
 }
