@@ -22,7 +22,7 @@ struct F8Source {
     int e5m2;
     int vec_values;                              // the values' rows may be written in 16-byte pieces
     const int64_t *offsets; int32_t groups;      // columns
-    int32_t log_seg, segs;                       // rows: blocks of a warp's part of a row (log2), parts a row
+    int32_t log_seg, parts;                      // rows: blocks of a warp's part of a row (log2), thread blocks a row
 };
 
 // scale byte of a block from the bits of its largest magnitude; an infinity or a NaN gives 255
@@ -43,118 +43,253 @@ __device__ __forceinline__ uint32_t codes2(float lo, float hi, int e5m2)
     else asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ float2 decode2(uint32_t c, int e5m2)
+__device__ __forceinline__ f32x2 decode2(uint32_t c, int e5m2)
 {
     uint32_t h;
     if (e5m2) asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
     else asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
-    return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    return pair(f.x, f.y);
 }
-// Eight values of a block with scale byte s: their codes, two a register.  (0 times an infinity is a NaN: such blocks' codes are set.)
-__device__ __forceinline__ uint2 encode8(const float (&f)[8], uint32_t s, int e5m2)
+
+// ---- eight elements of a row, as they lie in memory --------------------------------------------------------------
+
+// 16 lanes next to each other read 16 x 8 elements of a row.  VEC: rows start on 16 bytes.  Otherwise all of a row's pieces start at the
+// same offset into 16 bytes: each lane reads the aligned unit its piece starts in, takes the next one from the next lane, and shifts the
+// two into place.  A unit is read only if it holds an element of the row.  Lanes whose row is not there (row == nullptr) get zeros.
+// All lanes of the warp call it.
+template <typename T>
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+};
+__device__ __forceinline__ void put4(uint32_t *w, uint4 v) { w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+template <typename T>
+__device__ __forceinline__ void clear_from(Eight<T> &v, int n)       // elements n, n + 1, ... become 0
 {
-    const float inv = scale_inverse(s);
-    uint2 q;
-    q.x = codes2(f[0] * inv, f[1] * inv, e5m2) | codes2(f[2] * inv, f[3] * inv, e5m2) << 16;
-    q.y = codes2(f[4] * inv, f[5] * inv, e5m2) | codes2(f[6] * inv, f[7] * inv, e5m2) << 16;
-    return s == 255u ? make_uint2(0u, 0u) : q;
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+        if constexpr (sizeof(T) == 4) v.w[i] = i < n ? v.w[i] : 0u;
+        else v.w[i] = 2 * i + 1 < n ? v.w[i] : 2 * i < n ? v.w[i] & 0xffffu : 0u;
+    }
 }
-__device__ __forceinline__ void decode8(uint2 q, float scale, int e5m2, float (&f)[8])
+template <typename T, bool VEC>
+__device__ __forceinline__ Eight<T> read8(const T *row, int32_t k, int32_t K)
+{
+    constexpr int W = 2 * (int)sizeof(T), U = W / 4;                 // words and 16-byte units of a piece
+    const int left = row == nullptr ? 0 : K - k;                     // elements from here on
+    Eight<T> v;
+    if constexpr (VEC) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            put4(v.w + 4 * u, left > u * 16 / (int)sizeof(T) ? __ldg(reinterpret_cast<const uint4 *>(row + k) + u) : make_uint4(0, 0, 0, 0));
+    } else {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row + (left > 0 ? k : 0));
+        const int off = (int)(at & 15);
+        const uint4 *unit = reinterpret_cast<const uint4 *>(at - off);
+        const int have = (16 - off) / (int)sizeof(T);                // elements of the piece in its first unit
+        uint32_t x[W + 4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            put4(x + 4 * u, left > (u == 0 ? 0 : have + (u - 1) * 16 / (int)sizeof(T)) ? __ldg(unit + u) : make_uint4(0, 0, 0, 0));
+        // the unit after these: the next lane's first one, where that lane has read it
+        const uint4 f = make_uint4(__shfl_down_sync(0xffffffffu, x[0], 1, 16), __shfl_down_sync(0xffffffffu, x[1], 1, 16),
+                                   __shfl_down_sync(0xffffffffu, x[2], 1, 16), __shfl_down_sync(0xffffffffu, x[3], 1, 16));
+        put4(x + W, f);
+        if (((threadIdx.x & 15) == 15 || left <= 8) && left > have + (U - 1) * 16 / (int)sizeof(T) && off != 0) put4(x + W, __ldg(unit + U));
+        const bool two = off & 8, one = off & 4;
+#pragma unroll
+        for (int i = 0; i < W + 2; ++i) x[i] = two ? x[i + 2] : x[i];
+#pragma unroll
+        for (int i = 0; i < W + 1; ++i) x[i] = one ? x[i + 1] : x[i];
+#pragma unroll
+        for (int i = 0; i < W; ++i) v.w[i] = sizeof(T) == 4 ? x[i] : __funnelshift_r(x[i], x[i + 1], 8 * (off & 2));
+    }
+    if (left < 8) clear_from(v, left);
+    return v;
+}
+__device__ __forceinline__ void floats_of(const Eight<float> &v, f32x2 (&f)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(v.w[2 * i]), __uint_as_float(v.w[2 * i + 1]));
+}
+template <typename T>
+__device__ __forceinline__ void floats_of(const Eight<T> &v, f32x2 (&f)[4])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 d = decode2((i < 2 ? q.x : q.y) >> (16 * (i & 1)) & 0xffffu, e5m2);
-        f[2 * i] = d.x * scale; f[2 * i + 1] = d.y * scale;
+        float lo, hi;
+        unpack2(v.w[i], lo, hi, T());
+        f[i] = pair(lo, hi);
     }
 }
-template <typename V>
-__device__ __forceinline__ void put_values(V *v, const float (&f)[8], int n, int vec)
+// Magnitudes: an infinity or a NaN is larger than every number, as bits are.  16-bit types are compared two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t mag(uint32_t w) { return w & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu); }
+template <typename T>
+__device__ __forceinline__ uint32_t mag_max(uint32_t a, uint32_t b)
 {
-    if (vec && n >= 8) store_floats<V, 8>(v, f);
-    else
+    if constexpr (sizeof(T) == 4) return max(a, b);
+    else return __vmaxu2(a, b);
+}
+// bits of the larger magnitude of a word, as fp32
+__device__ __forceinline__ uint32_t mag_bits(uint32_t w, float) { return w; }
+__device__ __forceinline__ uint32_t mag_bits(uint32_t w, __nv_bfloat16) { return max(w >> 16, w & 0xffffu) << 16; }
+__device__ __forceinline__ uint32_t mag_bits(uint32_t w, __half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)max(w >> 16, w & 0xffffu)))); }
+template <typename T>
+__device__ __forceinline__ uint32_t mag8(const Eight<T> &v)
+{
+    uint32_t t = mag<T>(v.w[0]);
+#pragma unroll
+    for (int i = 1; i < 2 * (int)sizeof(T); ++i) t = mag_max<T>(t, mag<T>(v.w[i]));
+    return t;
+}
+
+// ---- what the codes stand for ------------------------------------------------------------------------------------
+
+// Eight values of a row from k on: 16 lanes next to each other hold 16 x 8, all lanes of the warp call it (`on`: those with a row).
+// Where rows do not start on 16 bytes, each lane writes the aligned unit that its piece starts in, with the end of the lane's before;
+// the ends of the 128 go element by element.
+template <typename V>
+__device__ __forceinline__ void put_values(V *row, int32_t k, int32_t K, const f32x2 (&f)[4], bool vec, bool on)
+{
+    constexpr int W = 2 * (int)sizeof(V), U = W / 4, PER = 16 / (int)sizeof(V);       // words, units; elements of a unit
+    uint32_t w[W];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        unpair(f[i], lo, hi);
+        if constexpr (sizeof(V) == 4) { w[2 * i] = __float_as_uint(lo); w[2 * i + 1] = __float_as_uint(hi); }
+        else w[i] = pack2(lo, hi, V());
+    }
+    const int left = on ? K - k : 0;
+    V *at = row + (on ? k : 0);
+    if (vec) {                                                       // (uniform)
+        if (left >= 8) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) *(reinterpret_cast<uint4 *>(at) + u) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < n) from_float(f[i], v[i]);
+            if (i < left) {
+                if constexpr (sizeof(V) == 4) reinterpret_cast<uint32_t *>(at)[i] = w[i];
+                else reinterpret_cast<uint16_t *>(at)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            }
+        return;
+    }
+    const int off = (int)(reinterpret_cast<uintptr_t>(at) & 15), behind = off / (int)sizeof(V), lane16 = threadIdx.x & 15;
+    // x: the last unit of the lane's before, then this lane's; t: the same moved so that t[4 + i] starts at word i of the first unit
+    uint32_t x[W + 4], t[W + 4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __shfl_up_sync(0xffffffffu, w[W - 4 + i], 1, 16);
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[4 + i] = w[i];
+#pragma unroll
+    for (int i = W + 3; i >= 2; --i) x[i] = off & 8 ? x[i - 2] : x[i];
+#pragma unroll
+    for (int i = W + 3; i >= 3; --i) t[i] = off & 4 ? x[i - 1] : x[i];
+    bool whole[U];                                                   // all elements of the unit are this lane's or the one's before
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        whole[u] = left > 0 && (u + 1) * PER - behind <= left && (u > 0 || behind == 0 || lane16 > 0);
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = sizeof(V) == 2 && (off & 2) ? __funnelshift_r(t[3 + 4 * u + i], t[4 + 4 * u + i], 16) : t[4 + 4 * u + i];
+        if (whole[u]) *reinterpret_cast<uint4 *>(at - behind + u * PER) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    const bool next_whole = lane16 < 15 && PER - behind <= left - 8; // the next lane's first unit, which holds this lane's last elements
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int u = (i + behind) / PER;
+        if (i < left && !(u == 0 ? whole[0] : u < U ? whole[U - 1] : next_whole)) {
+            if constexpr (sizeof(V) == 4) reinterpret_cast<uint32_t *>(at)[i] = w[i];
+            else reinterpret_cast<uint16_t *>(at)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        }
+    }
 }
-// what the codes stand for: n elements of a row from (row, k) on
-__device__ __forceinline__ void write_values(const F8Source &p, int64_t row, int32_t k, const float (&f)[8], int n)
+// (all lanes of the warp)
+__device__ __forceinline__ void write_values(const F8Source &p, int64_t row, int32_t k, const f32x2 (&f)[4], bool on)
 {
-    const int64_t at = row * p.ld_values + k;
+    const int64_t at = row * p.ld_values;
     switch (p.values_type) {
-        case QNN_TYPE_F32: put_values(static_cast<float *>(p.values) + at, f, n, p.vec_values); break;
-        case QNN_TYPE_BF16: put_values(static_cast<__nv_bfloat16 *>(p.values) + at, f, n, p.vec_values); break;
-        default: put_values(static_cast<__half *>(p.values) + at, f, n, p.vec_values); break;
+        case QNN_TYPE_F32: put_values(static_cast<float *>(p.values) + at, k, p.K, f, p.vec_values != 0, on); break;
+        case QNN_TYPE_BF16: put_values(static_cast<__nv_bfloat16 *>(p.values) + at, k, p.K, f, p.vec_values != 0, on); break;
+        default: put_values(static_cast<__half *>(p.values) + at, k, p.K, f, p.vec_values != 0, on); break;
     }
 }
-// eight elements of a row from k on, 0 where it has ended (or is not there)
-template <typename T, bool VEC>
-__device__ __forceinline__ void read8(const T *row, int32_t k, int32_t K, float (&f)[8])
+__device__ __forceinline__ uint2 encode8(const f32x2 (&f)[4], const f32x2 (&inv)[4], int e5m2)
 {
-    if (row != nullptr && VEC && k + 8 <= K) {
-        Piece<T, 8> v;
-        load_piece<T, 8>(row + k, v);
-        piece_to_floats<T, 8>(v, f);
-    } else {
+    uint32_t c[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = row != nullptr && k + i < K ? to_float(row[k + i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        unpair(mul2(f[i], inv[i]), lo, hi);
+        c[i] = codes2(lo, hi, e5m2);
     }
+    return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
 }
-__device__ __forceinline__ uint32_t magnitude(float f) { return __float_as_uint(f) & 0x7fffffffu; }
-__device__ __forceinline__ uint32_t top8(const float (&f)[8])
+__device__ __forceinline__ void decode8(uint2 q, const f32x2 (&scale)[4], int e5m2, f32x2 (&f)[4])
 {
-    uint32_t t = magnitude(f[0]);
 #pragma unroll
-    for (int i = 1; i < 8; ++i) t = max(t, magnitude(f[i]));
-    return t;
+    for (int i = 0; i < 4; ++i) f[i] = mul2(decode2((i < 2 ? q.x : q.y) >> (16 * (i & 1)) & 0xffffu, e5m2), scale[i]);
 }
 
 // ---- blocks of a row ---------------------------------------------------------------------------------------------
 
-constexpr int ROW_UNITS = 4;                     // blocks a half warp has in flight
-
-// A warp takes eight blocks: 2^log_seg next to each other of each of 8 / 2^log_seg rows; 16 lanes hold a block, eight elements each.
-template <typename T, bool VEC>
+// 16 lanes hold a block, eight elements each; a warp takes eight blocks, 2^log_seg next to each other of each of 8 / 2^log_seg rows (WIDE:
+// all eight of one row), four in flight a lane.
+template <typename T, bool VEC, bool WIDE>
 __global__ void __launch_bounds__(128)
 quant_rows_f8_kernel(const F8Source p)
 {
     const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int64_t rg = w / p.segs;
-    const int32_t seg = (int32_t)(w - rg * p.segs);
+    const uint32_t rb = blockIdx.x / (uint32_t)p.parts, part = blockIdx.x - rb * (uint32_t)p.parts;
+    const int64_t rg = (int64_t)rb * blockDim.y + threadIdx.y;
+    const int32_t seg = (int32_t)(part * (blockDim.x >> 5) + (threadIdx.x >> 5));
+    const int log_seg = WIDE ? 3 : p.log_seg;
+    const int64_t row0 = rg << (3 - log_seg);
     const int32_t K16 = (p.K + 15) & ~15;
-    griddep_wait();
-    float f[ROW_UNITS][8];
-#pragma unroll
-    for (int u = 0; u < ROW_UNITS; ++u) {
-        const int j = 2 * u + half;
-        const int64_t row = (rg << (3 - p.log_seg)) + (j >> p.log_seg);
-        const int32_t k = (((seg << p.log_seg) + (j & ((1 << p.log_seg) - 1))) << 7) + 8 * l16;
-        const T *src = nullptr;
-        if (row < p.rows && k < p.K) {
-            int64_t from = row;
-            if (p.index) from = __ldg(p.index + row);
-            if (from >= 0 && (!p.index || from < p.src_rows)) src = static_cast<const T *>(p.x) + from * p.ldx;
+    auto row_of = [&](int u) { return WIDE ? row0 : row0 + ((2 * u + half) >> log_seg); };
+    auto blk_of = [&](int u) { return (seg << log_seg) + ((2 * u + half) & ((1 << log_seg) - 1)); };
+    auto source = [&](int64_t row) -> const T * {
+        if (row >= p.rows) return nullptr;
+        int64_t from = row;
+        if (p.index) {
+            from = __ldg(p.index + row);
+            if (from < 0 || from >= p.src_rows) return nullptr;
         }
-        read8<T, VEC>(src, k, p.K, f[u]);
-    }
+        return static_cast<const T *>(p.x) + from * p.ldx;
+    };
+    griddep_wait();
+    Eight<T> v[4];
+    const T *src = WIDE ? source(row0) : nullptr;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = read8<T, VEC>(WIDE ? src : source(row_of(u)), (blk_of(u) << 7) + 8 * l16, p.K);
     griddep_launch_dependents();
 #pragma unroll
-    for (int u = 0; u < ROW_UNITS; ++u) {
-        const int j = 2 * u + half;
-        const int64_t row = (rg << (3 - p.log_seg)) + (j >> p.log_seg);
-        const int32_t blk = (seg << p.log_seg) + (j & ((1 << p.log_seg) - 1)), k = (blk << 7) + 8 * l16;
-        uint32_t top = top8(f[u]);
+    for (int u = 0; u < 4; ++u) {
+        const int64_t row = row_of(u);
+        const int32_t blk = blk_of(u), k = (blk << 7) + 8 * l16;
+        uint32_t top = mag8(v[u]);
 #pragma unroll
-        for (int d = 8; d > 0; d /= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-        if (row >= p.rows || k >= K16) continue;
-        const uint32_t s = scale_byte(top, p.e5m2);
-        const uint2 q = encode8(f[u], s, p.e5m2);
-        *reinterpret_cast<uint2 *>(p.codes + row * p.ldq + k) = q;
-        if (l16 == 0) p.scale[row * p.ld_scale + blk] = (uint8_t)s;
-        if (p.values && k < p.K) {
-            float v[8];
-            decode8(q, scale_value(s), p.e5m2, v);
-            write_values(p, row, k, v, p.K - k);
+        for (int d = 8; d > 0; d /= 2) top = mag_max<T>(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const uint32_t s = scale_byte(mag_bits(top, T()), p.e5m2);
+        f32x2 f[4], by[4];
+        floats_of(v[u], f);
+        const float inv = scale_inverse(s), val = scale_value(s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) by[i] = pair(inv, inv);
+        uint2 q = encode8(f, by, p.e5m2);
+        if (s == 255u) q = make_uint2(0u, 0u);           // (0 times an infinity is a NaN)
+        if (row < p.rows && k < K16) {
+            *reinterpret_cast<uint2 *>(p.codes + row * p.ldq + k) = q;
+            if (l16 == 0) p.scale[row * p.ld_scale + blk] = (uint8_t)s;
+        }
+        if (p.values) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) by[i] = pair(val, val);
+            decode8(q, by, p.e5m2, f);
+            write_values(p, row, k, f, row < p.rows && k < p.K);
         }
     }
 }
@@ -207,17 +342,18 @@ __device__ __forceinline__ void find_block(const int64_t *offsets, int32_t group
 
 constexpr int TILE_THREADS = 256;
 
-// 128 rows x 128 columns a block: 16 lanes hold a row's 128 columns, eight each, and a thread every sixteenth row.
+// 128 rows x 128 columns at a time: 16 lanes hold a row's 128 columns, eight each, and a thread every sixteenth row.  Elements stay as they
+// lie in memory until they are encoded, so that four blocks (of 16-bit types) fit an SM: one's loads go on while the others join and write.
 template <typename T, bool VEC, bool COLUMNS>
-__global__ void __launch_bounds__(TILE_THREADS)
+__global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 2 : 4)
 quant_tiles_f8_kernel(const F8Source p)
 {
-    __shared__ uint32_t tops[8][128];
+    constexpr int W = 2 * (int)sizeof(T);
+    __shared__ uint4 tops[8][8 * sizeof(T)];             // of 128 columns, a row a warp
     __shared__ __align__(8) uint8_t bytes[128];
     __shared__ int64_t where[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, l16 = tid & 15, r16 = tid >> 4;
-    const int32_t tile = blockIdx.x, blk = blockIdx.y;
-    const int32_t k = tile * 128 + 8 * l16;
+    const int32_t blk = blockIdx.y, tiles = (p.K + 127) / 128;
     const int32_t K16 = (p.K + 15) & ~15;
     griddep_wait();
     int64_t row0 = (int64_t)blk * 128, left = p.rows - row0;
@@ -232,77 +368,83 @@ quant_tiles_f8_kernel(const F8Source p)
     }
     const int rows = left < 128 ? (int)left : 128;
     const T *src = static_cast<const T *>(p.x) + row0 * p.ldx;
-    float f[8][8];
+    for (int32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int32_t k = tile * 128 + 8 * l16;
+        Eight<T> v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = i * 16 + r16;
-        read8<T, VEC>(r < rows ? src + (int64_t)r * p.ldx : nullptr, k, p.K, f[i]);
-    }
-    griddep_launch_dependents();
-    uint32_t s[8];
-    if (COLUMNS) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            uint32_t t = magnitude(f[0][c]);
-#pragma unroll
-            for (int i = 1; i < 8; ++i) t = max(t, magnitude(f[i][c]));
-            t = max(t, __shfl_xor_sync(0xffffffffu, t, 16));
-            s[c] = t;
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 16 + r16;
+            v[i] = read8<T, VEC>(r < rows ? src + (int64_t)r * p.ldx : nullptr, k, p.K);
         }
-        if (lane < 16) {
-            *reinterpret_cast<uint4 *>(&tops[warp][8 * l16]) = make_uint4(s[0], s[1], s[2], s[3]);
-            *reinterpret_cast<uint4 *>(&tops[warp][8 * l16 + 4]) = make_uint4(s[4], s[5], s[6], s[7]);
-        }
-        __syncthreads();
-        if (tid < 128) {
-            uint32_t t = tops[0][tid];
+        if (tile + (int32_t)gridDim.x >= tiles) griddep_launch_dependents();
+        uint32_t s8[2];                                  // this thread's columns' scale bytes
+        if (COLUMNS) {
+            uint32_t m[W];
 #pragma unroll
-            for (int w = 1; w < 8; ++w) t = max(t, tops[w][tid]);
+            for (int c = 0; c < W; ++c) {
+                uint32_t t = mag<T>(v[0].w[c]);
+#pragma unroll
+                for (int i = 1; i < 8; ++i) t = mag_max<T>(t, mag<T>(v[i].w[c]));
+                m[c] = mag_max<T>(t, __shfl_xor_sync(0xffffffffu, t, 16));
+            }
+            if (lane < 16)
+#pragma unroll
+                for (int u = 0; u < W / 4; ++u) tops[warp][l16 * (W / 4) + u] = make_uint4(m[4 * u], m[4 * u + 1], m[4 * u + 2], m[4 * u + 3]);
+            __syncthreads();
+            if (tid < 128) {
+                uint32_t t = 0;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    if constexpr (sizeof(T) == 4) t = max(t, reinterpret_cast<const uint32_t *>(tops[w])[tid]);
+                    else t = max(t, (uint32_t)reinterpret_cast<const uint16_t *>(tops[w])[tid]);
+                }
+                const uint32_t b = scale_byte(mag_bits(t, T()), p.e5m2);
+                bytes[tid] = (uint8_t)b;
+                if (tile * 128 + tid < p.K) p.scale[(int64_t)blk * p.ld_scale + tile * 128 + tid] = (uint8_t)b;
+            }
+            __syncthreads();
+            const uint2 b8 = *reinterpret_cast<const uint2 *>(&bytes[8 * l16]);
+            s8[0] = b8.x; s8[1] = b8.y;
+        } else {
+            uint32_t t = mag8(v[0]);
+#pragma unroll
+            for (int i = 1; i < 8; ++i) t = mag_max<T>(t, mag8(v[i]));
+            t = __reduce_max_sync(0xffffffffu, mag_bits(t, T()));
+            uint32_t *part = reinterpret_cast<uint32_t *>(tops[tile / (int32_t)gridDim.x & 1]);
+            if (lane == 0) part[warp] = t;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < 8; ++w) t = max(t, part[w]);
             const uint32_t b = scale_byte(t, p.e5m2);
-            bytes[tid] = (uint8_t)b;
-            if (tile * 128 + tid < p.K) p.scale[(int64_t)blk * p.ld_scale + tile * 128 + tid] = (uint8_t)b;
+            if (tid == 0) p.scale[(int64_t)blk * p.ld_scale + tile] = (uint8_t)b;
+            s8[0] = s8[1] = b * 0x01010101u;
         }
-        __syncthreads();
-        const uint2 b8 = *reinterpret_cast<const uint2 *>(&bytes[8 * l16]);
+        f32x2 inv[4], val[4];
+        uint2 keep = make_uint2(0u, 0u);                 // codes of columns with a NaN scale are 0
 #pragma unroll
-        for (int c = 0; c < 8; ++c) s[c] = (c < 4 ? b8.x : b8.y) >> (8 * (c & 3)) & 0xffu;
-    } else {
-        uint32_t t = top8(f[0]);
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t a = s8[c / 2] >> (16 * (c & 1)) & 0xffu, b = s8[c / 2] >> (16 * (c & 1) + 8) & 0xffu;
+            inv[c] = pair(scale_inverse(a), scale_inverse(b));
+            val[c] = pair(scale_value(a), scale_value(b));
+            const uint32_t both = ((a != 255u ? 0xffu : 0u) | (b != 255u ? 0xff00u : 0u)) << (16 * (c & 1));
+            if (c < 2) keep.x |= both;
+            else keep.y |= both;
+        }
+        // (columns: the rows that fill a group up to whole blocks are written too, as zeros)
+        const int64_t out0 = (int64_t)blk * 128;
 #pragma unroll
-        for (int i = 1; i < 8; ++i) t = max(t, top8(f[i]));
-        t = __reduce_max_sync(0xffffffffu, t);
-        if (lane == 0) tops[0][warp] = t;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 8; ++w) t = max(t, tops[0][w]);
-        const uint32_t b = scale_byte(t, p.e5m2);
-        if (tid == 0) p.scale[(int64_t)blk * p.ld_scale + tile] = (uint8_t)b;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) s[c] = b;
-    }
-    if (k >= K16) return;
-    float inv[8], val[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) { inv[c] = scale_inverse(s[c]); val[c] = scale_value(s[c]); }
-    // (columns: the rows that fill a group up to whole blocks are written too, as zeros)
-    const int64_t out0 = (int64_t)blk * 128;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = i * 16 + r16;
-        if (!COLUMNS && r >= rows) continue;
-        float g[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) g[c] = s[c] == 255u ? 0.0f : f[i][c] * inv[c];
-        uint2 q;
-        q.x = codes2(g[0], g[1], p.e5m2) | codes2(g[2], g[3], p.e5m2) << 16;
-        q.y = codes2(g[4], g[5], p.e5m2) | codes2(g[6], g[7], p.e5m2) << 16;
-        *reinterpret_cast<uint2 *>(p.codes + (out0 + r) * p.ldq + k) = q;
-        if (p.values && k < p.K) {
-            float v[8];
-            decode8(q, 1.0f, p.e5m2, v);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] *= val[c];
-            write_values(p, out0 + r, k, v, p.K - k);
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 16 + r16;
+            const bool there = (COLUMNS || r < rows) && k < K16;
+            f32x2 f[4];
+            floats_of(v[i], f);
+            uint2 q = encode8(f, inv, p.e5m2);
+            q.x &= keep.x; q.y &= keep.y;
+            if (there) *reinterpret_cast<uint2 *>(p.codes + (out0 + r) * p.ldq + k) = q;
+            if (p.values) {
+                decode8(q, val, p.e5m2, f);
+                write_values(p, out0 + r, k, f, there && k < p.K);
+            }
         }
     }
 }
@@ -317,17 +459,26 @@ int launch_quant(F8Source p, const char *what, cudaStream_t st)
     const bool vec = aligned(p.x, 16) && (p.ldx * (int64_t)sizeof(T)) % 16 == 0;
     const int64_t nblk = ceil_div(p.K, 128);
     if (HOW == BY_ROWS) {
-        p.log_seg = nblk >= 8 ? 3 : nblk > 2 ? 2 : nblk > 1 ? 1 : 0;
-        p.segs = (int32_t)ceil_div(nblk, 1 << p.log_seg);
-        const int64_t warps = ceil_div(p.rows, 8 >> p.log_seg) * p.segs, blocks = ceil_div(warps, 4);
+        p.log_seg = nblk > 4 ? 3 : nblk > 2 ? 2 : nblk > 1 ? 1 : 0;
+        const int64_t segs = ceil_div(nblk, 1 << p.log_seg);
+        const int wide = segs >= 4 ? 4 : segs == 2 ? 2 : 1;          // warps along a row
+        p.parts = (int32_t)ceil_div(segs, wide);
+        const int64_t blocks = ceil_div(ceil_div(p.rows, 8 >> p.log_seg), 4 / wide) * p.parts;
         QNN_REQUIRE(blocks < (int64_t)1 << 31, QNN_ERR_UNSUPPORTED, "%s: too many blocks", what);
-        const dim3 grid((unsigned)blocks);
-        if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true>, grid, dim3(128), 0, st, p));
-        else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false>, grid, dim3(128), 0, st, p));
+        const dim3 grid((unsigned)blocks), block(32 * (unsigned)wide, 4 / (unsigned)wide);
+        if (p.log_seg == 3) {
+            if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true, true>, grid, block, 0, st, p));
+            else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false, true>, grid, block, 0, st, p));
+        } else {
+            if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true, false>, grid, block, 0, st, p));
+            else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false, false>, grid, block, 0, st, p));
+        }
     } else {
         const int64_t blocks = HOW == BY_COLUMNS ? p.rows / 128 + p.groups : ceil_div(p.rows, 128);
         QNN_REQUIRE(blocks < 65536, QNN_ERR_UNSUPPORTED, "%s: 65536 blocks of 128 rows and more", what);
-        const dim3 grid((unsigned)nblk, (unsigned)blocks);
+        // columns: a block's rows are looked up once for up to four tiles, while there are several thread blocks for every SM
+        const int64_t tiles = HOW == BY_COLUMNS && nblk * blocks > 16 * (int64_t)sm_count() ? ceil_div(nblk, 4) : nblk;
+        const dim3 grid((unsigned)tiles, (unsigned)blocks);
         if (vec) QNN_CUDA(launch_pdl(quant_tiles_f8_kernel<T, true, HOW == BY_COLUMNS>, grid, dim3(TILE_THREADS), 0, st, p));
         else QNN_CUDA(launch_pdl(quant_tiles_f8_kernel<T, false, HOW == BY_COLUMNS>, grid, dim3(TILE_THREADS), 0, st, p));
     }
