@@ -6,6 +6,7 @@
 //
 // All of it is bound by memory: every element is read once into registers, the blocks' maxima are joined across lanes (rows: 16 lanes
 // hold a block) or through shared memory (tiles, columns), and codes, scales and values are written from the registers.
+#include <type_traits>
 #include "qnn_types.cuh"
 
 namespace qnn {
@@ -19,16 +20,16 @@ struct F8Source {
     uint8_t *codes; int64_t ldq;
     uint8_t *scale; int64_t ld_scale;
     void *values; int values_type; int64_t ld_values;
-    int e5m2;
     int vec_values;                              // the values' rows may be written in 16-byte pieces
     const int64_t *offsets; int32_t groups;      // columns
-    int32_t log_seg, parts;                      // rows: blocks of a warp's part of a row (log2), thread blocks a row
+    int32_t log_seg, segs;                       // rows: blocks of a warp's part of a row (log2), parts a row
 };
 
 // scale byte of a block from the bits of its largest magnitude; an infinity or a NaN gives 255
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top, int e5m2)
+template <bool E5>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top)
 {
-    const int e = (int)(top >> 23), low = e5m2 ? 15 : 8;
+    const int e = (int)(top >> 23), low = E5 ? 15 : 8;
     const int s = e - low + ((top & 0x7fffffu) > MANT_MOST ? 1 : 0);
     return e == 255 ? 255u : s < 0 ? 0u : (uint32_t)s;
 }
@@ -36,17 +37,19 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top, int e5m2)
 __device__ __forceinline__ float scale_inverse(uint32_t s) { return s == 255u ? 0.0f : __uint_as_float((254u - s) << 23); }
 __device__ __forceinline__ float scale_value(uint32_t s) { return s == 255u ? __uint_as_float(0x7fffffffu) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23); }
 
-__device__ __forceinline__ uint32_t codes2(float lo, float hi, int e5m2)
+template <bool E5>
+__device__ __forceinline__ uint32_t codes2(float lo, float hi)
 {
     uint16_t r;
-    if (e5m2) asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    if constexpr (E5) asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     else asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ f32x2 decode2(uint32_t c, int e5m2)
+template <bool E5>
+__device__ __forceinline__ f32x2 decode2(uint32_t c)
 {
     uint32_t h;
-    if (e5m2) asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
+    if constexpr (E5) asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
     else asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
     return pair(f.x, f.y);
@@ -207,47 +210,174 @@ __device__ __forceinline__ void put_values(V *row, int32_t k, int32_t K, const f
         }
     }
 }
-// (all lanes of the warp)
-__device__ __forceinline__ void write_values(const F8Source &p, int64_t row, int32_t k, const f32x2 (&f)[4], bool on)
+// The values' type as an argument of f: one copy of its code for each, one branch a thread.
+struct Nothing {};
+template <typename F>
+__device__ __forceinline__ void with_values(const F8Source &p, F f)
 {
-    const int64_t at = row * p.ld_values;
-    switch (p.values_type) {
-        case QNN_TYPE_F32: put_values(static_cast<float *>(p.values) + at, k, p.K, f, p.vec_values != 0, on); break;
-        case QNN_TYPE_BF16: put_values(static_cast<__nv_bfloat16 *>(p.values) + at, k, p.K, f, p.vec_values != 0, on); break;
-        default: put_values(static_cast<__half *>(p.values) + at, k, p.K, f, p.vec_values != 0, on); break;
-    }
+    if (p.values == nullptr) f(Nothing());
+    else if (p.values_type == QNN_TYPE_F32) f(float());
+    else if (p.values_type == QNN_TYPE_BF16) f(__nv_bfloat16());
+    else f(__half());
 }
-__device__ __forceinline__ uint2 encode8(const f32x2 (&f)[4], const f32x2 (&inv)[4], int e5m2)
+template <bool E5>
+__device__ __forceinline__ uint2 encode8(const f32x2 (&f)[4], const f32x2 (&inv)[4])
 {
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float lo, hi;
         unpair(mul2(f[i], inv[i]), lo, hi);
-        c[i] = codes2(lo, hi, e5m2);
+        c[i] = codes2<E5>(lo, hi);
     }
     return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
 }
-__device__ __forceinline__ void decode8(uint2 q, const f32x2 (&scale)[4], int e5m2, f32x2 (&f)[4])
+template <bool E5>
+__device__ __forceinline__ void decode8(uint2 q, const f32x2 (&scale)[4], f32x2 (&f)[4])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = mul2(decode2((i < 2 ? q.x : q.y) >> (16 * (i & 1)) & 0xffffu, e5m2), scale[i]);
+    for (int i = 0; i < 4; ++i) f[i] = mul2(decode2<E5>((i < 2 ? q.x : q.y) >> (16 * (i & 1))), scale[i]);
+}
+
+// ---- 1024 elements of a row: four times 256, a warp's lanes next to each other ------------------------------------
+
+// words A and following of x, moved down by another `bits` (0 or 16)
+template <typename T, int A>
+__device__ __forceinline__ void shift_down(const uint32_t *x, int bits, Eight<T> &v)
+{
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) v.w[i] = sizeof(T) == 4 ? x[i + A] : __funnelshift_r(x[i + A], x[i + A + 1], bits);
+}
+// As read8, k the first of this lane's elements; the offset into 16 bytes is the warp's.
+template <typename T, bool VEC>
+__device__ __forceinline__ void read_segment(const T *row, int32_t k, int32_t K, Eight<T> (&v)[4])
+{
+    constexpr int W = 2 * (int)sizeof(T), U = W / 4, PER = 16 / (int)sizeof(T);
+    const int left = row == nullptr ? 0 : K - k, lane = threadIdx.x & 31;
+    if constexpr (VEC) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                put4(v[u].w + 4 * i, left > 256 * u + i * PER ? __ldg(reinterpret_cast<const uint4 *>(row + k + 256 * u) + i) : make_uint4(0, 0, 0, 0));
+    } else {
+        const int off = (int)(reinterpret_cast<uintptr_t>(row) & 15), have = (16 - off) / (int)sizeof(T);
+        const T *at = row + (row == nullptr ? 0 : k - off / (int)sizeof(T));       // (16-byte aligned)
+        uint32_t x[4][W + 4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                put4(x[u] + 4 * i, left > 256 * u + (i == 0 ? 0 : have + (i - 1) * PER) ? __ldg(reinterpret_cast<const uint4 *>(at + 256 * u) + i) : make_uint4(0, 0, 0, 0));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            // the unit after these: the next lane's first one, or the first lane's of the next 256
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t next = __shfl_down_sync(0xffffffffu, x[u][i], 1), first = u < 3 ? __shfl_sync(0xffffffffu, x[u < 3 ? u + 1 : 3][i], 0) : 0u;
+                x[u][W + i] = lane == 31 ? first : next;
+            }
+            const int l = left - 256 * u;
+            if (((lane == 31 && u == 3) || l <= 8) && l > have + (U - 1) * PER && off != 0) put4(x[u] + W, __ldg(reinterpret_cast<const uint4 *>(at + 256 * u) + U));
+        }
+        const int bits = 8 * (off & 2);
+        switch (off >> 2) {
+            case 0:
+#pragma unroll
+                for (int u = 0; u < 4; ++u) shift_down<T, 0>(x[u], bits, v[u]);
+                break;
+            case 1:
+#pragma unroll
+                for (int u = 0; u < 4; ++u) shift_down<T, 1>(x[u], bits, v[u]);
+                break;
+            case 2:
+#pragma unroll
+                for (int u = 0; u < 4; ++u) shift_down<T, 2>(x[u], bits, v[u]);
+                break;
+            default:
+#pragma unroll
+                for (int u = 0; u < 4; ++u) shift_down<T, 3>(x[u], bits, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+        if (left < 256 * u + 8) clear_from(v[u], left - 256 * u);
+}
+
+template <typename V, int A>
+__device__ __forceinline__ void store_shifted(const uint32_t *x, bool half, V *unit, const bool *whole)
+{
+    constexpr int U = (int)sizeof(V) / 2;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = sizeof(V) == 2 ? (half ? __funnelshift_r(A + 1 <= 4 + 4 * u + i ? x[3 + 4 * u + i - A] : 0u, x[4 + 4 * u + i - A], 16) : x[4 + 4 * u + i - A]) : x[4 + 4 * u + i - A];
+        if (whole[u]) *reinterpret_cast<uint4 *>(unit + u * (16 / (int)sizeof(V))) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+}
+// Part u of a row's 1024 values (rows that do not start on 16 bytes): as put_values, the unit that a lane's piece starts in holds the end of
+// the lane's before, or (first lane) of the last lane's of the part before, which `carry` hands on.  row: not null where left > 0.
+template <typename V>
+__device__ __forceinline__ void put_part(V *row, int32_t k, int32_t K, const f32x2 (&f)[4], int u4, uint32_t (&carry)[4])
+{
+    constexpr int W = 2 * (int)sizeof(V), U = W / 4, PER = 16 / (int)sizeof(V);
+    const int lane = threadIdx.x & 31, left = K - k;
+    uint32_t x[W + 4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        unpair(f[i], lo, hi);
+        if constexpr (sizeof(V) == 4) { x[4 + 2 * i] = __float_as_uint(lo); x[5 + 2 * i] = __float_as_uint(hi); }
+        else x[4 + i] = pack2(lo, hi, V());
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t before = __shfl_up_sync(0xffffffffu, x[W + i], 1);
+        x[i] = lane == 0 ? carry[i] : before;
+        carry[i] = __shfl_sync(0xffffffffu, x[W + i], 31);
+    }
+    const int off = (int)(reinterpret_cast<uintptr_t>(row) & 15), behind = off / (int)sizeof(V);
+    V *at = row + k;
+    bool whole[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) whole[u] = left > 0 && (u + 1) * PER - behind <= left && (u > 0 || behind == 0 || lane > 0 || u4 > 0);
+    const bool half = off & 2;
+    switch (off >> 2) {                                  // (the warp's)
+        case 0: store_shifted<V, 0>(x, half, at - behind, whole); break;
+        case 1: store_shifted<V, 1>(x, half, at - behind, whole); break;
+        case 2: store_shifted<V, 2>(x, half, at - behind, whole); break;
+        default: store_shifted<V, 3>(x, half, at - behind, whole);
+    }
+    // the ends: before the first whole unit of the 1024, behind the last one, and where the row ends
+    if (u4 == 0 || u4 == 3 || __any_sync(0xffffffffu, left < 24)) {
+        const bool next_whole = (lane < 31 || u4 < 3) && PER - behind <= left - 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int u = (i + behind) / PER;
+            if (i < left && !(u == 0 ? whole[0] : u < U ? whole[U - 1] : next_whole)) {
+                if constexpr (sizeof(V) == 4) reinterpret_cast<uint32_t *>(at)[i] = x[4 + i];
+                else reinterpret_cast<uint16_t *>(at)[i] = (uint16_t)(x[4 + i / 2] >> (16 * (i & 1)));
+            }
+        }
+    }
 }
 
 // ---- blocks of a row ---------------------------------------------------------------------------------------------
 
 // 16 lanes hold a block, eight elements each; a warp takes eight blocks, 2^log_seg next to each other of each of 8 / 2^log_seg rows (WIDE:
 // all eight of one row), four in flight a lane.
-template <typename T, bool VEC, bool WIDE>
+template <typename T, bool VEC, bool WIDE, bool E5>
 __global__ void __launch_bounds__(128)
 quant_rows_f8_kernel(const F8Source p)
 {
     const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
-    const uint32_t rb = blockIdx.x / (uint32_t)p.parts, part = blockIdx.x - rb * (uint32_t)p.parts;
-    const int64_t rg = (int64_t)rb * blockDim.y + threadIdx.y;
-    const int32_t seg = (int32_t)(part * (blockDim.x >> 5) + (threadIdx.x >> 5));
+    const uint32_t warp = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const uint32_t rg = warp / (uint32_t)p.segs;
+    const int32_t seg = (int32_t)(warp - rg * (uint32_t)p.segs);
     const int log_seg = WIDE ? 3 : p.log_seg;
-    const int64_t row0 = rg << (3 - log_seg);
+    const int64_t row0 = (int64_t)rg << (3 - log_seg);
     const int32_t K16 = (p.K + 15) & ~15;
     auto row_of = [&](int u) { return WIDE ? row0 : row0 + ((2 * u + half) >> log_seg); };
     auto blk_of = [&](int u) { return (seg << log_seg) + ((2 * u + half) & ((1 << log_seg) - 1)); };
@@ -262,36 +392,57 @@ quant_rows_f8_kernel(const F8Source p)
     };
     griddep_wait();
     Eight<T> v[4];
-    const T *src = WIDE ? source(row0) : nullptr;
+    const int32_t k0 = (seg << 10) + 8 * lane;           // (WIDE)
+    if constexpr (WIDE) {
+        read_segment<T, VEC>(source(row0), k0, p.K, v);
+    } else {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = read8<T, VEC>(WIDE ? src : source(row_of(u)), (blk_of(u) << 7) + 8 * l16, p.K);
-    griddep_launch_dependents();
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int64_t row = row_of(u);
-        const int32_t blk = blk_of(u), k = (blk << 7) + 8 * l16;
-        uint32_t top = mag8(v[u]);
-#pragma unroll
-        for (int d = 8; d > 0; d /= 2) top = mag_max<T>(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const uint32_t s = scale_byte(mag_bits(top, T()), p.e5m2);
-        f32x2 f[4], by[4];
-        floats_of(v[u], f);
-        const float inv = scale_inverse(s), val = scale_value(s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) by[i] = pair(inv, inv);
-        uint2 q = encode8(f, by, p.e5m2);
-        if (s == 255u) q = make_uint2(0u, 0u);           // (0 times an infinity is a NaN)
-        if (row < p.rows && k < K16) {
-            *reinterpret_cast<uint2 *>(p.codes + row * p.ldq + k) = q;
-            if (l16 == 0) p.scale[row * p.ld_scale + blk] = (uint8_t)s;
-        }
-        if (p.values) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) by[i] = pair(val, val);
-            decode8(q, by, p.e5m2, f);
-            write_values(p, row, k, f, row < p.rows && k < p.K);
-        }
+        for (int u = 0; u < 4; ++u) v[u] = read8<T, VEC>(source(row_of(u)), (blk_of(u) << 7) + 8 * l16, p.K);
     }
+    griddep_launch_dependents();
+    const bool chained = WIDE && !p.vec_values;
+    auto encode = [&](auto kind) {                       // V: the values' type; nothing: none
+        using V = decltype(kind);
+        constexpr bool VALUES = !std::is_same<V, Nothing>::value;
+        uint32_t carry[4] = {0u, 0u, 0u, 0u};
+        uint8_t *codes = p.codes + row0 * p.ldq + k0, *scale = p.scale + row0 * p.ld_scale + 8 * seg + half;  // (WIDE)
+        V *values = static_cast<V *>(p.values) + (VALUES ? row0 * p.ld_values : 0);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t row = row_of(u);
+            const int32_t k = WIDE ? k0 + 256 * u : (blk_of(u) << 7) + 8 * l16;
+            if (WIDE && (seg << 10) + 256 * u >= p.K) break;         // (the warp's)
+            uint32_t top = mag8(v[u]);
+#pragma unroll
+            for (int d = 8; d > 0; d /= 2) top = mag_max<T>(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const uint32_t s = scale_byte<E5>(mag_bits(top, T()));
+            f32x2 f[4], by[4];
+            floats_of(v[u], f);
+            const float inv = scale_inverse(s), val = scale_value(s);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) by[i] = pair(inv, inv);
+            uint2 q = encode8<E5>(f, by);
+            if (s == 255u) q = make_uint2(0u, 0u);                   // (0 times an infinity is a NaN)
+            const bool there = row < p.rows && k < K16;
+            if (there) {
+                if constexpr (WIDE) {
+                    *reinterpret_cast<uint2 *>(codes + 256 * u) = q;
+                    if (l16 == 0) scale[2 * u] = (uint8_t)s;
+                } else {
+                    *reinterpret_cast<uint2 *>(p.codes + row * p.ldq + k) = q;
+                    if (l16 == 0) p.scale[row * p.ld_scale + blk_of(u)] = (uint8_t)s;
+                }
+            }
+            if constexpr (VALUES) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) by[i] = pair(val, val);
+                decode8<E5>(q, by, f);
+                if (chained) put_part(values, k, row < p.rows ? p.K : 0, f, u, carry);           // (no row: nothing left of it)
+                else put_values(WIDE ? values : static_cast<V *>(p.values) + row * p.ld_values, k, p.K, f, p.vec_values != 0, there && k < p.K);
+            }
+        }
+    };
+    with_values(p, encode);
 }
 
 // ---- tiles of 128 x 128, and blocks of 128 rows of a column ------------------------------------------------------
@@ -344,7 +495,7 @@ constexpr int TILE_THREADS = 256;
 
 // 128 rows x 128 columns at a time: 16 lanes hold a row's 128 columns, eight each, and a thread every sixteenth row.  Elements stay as they
 // lie in memory until they are encoded, so that four blocks (of 16-bit types) fit an SM: one's loads go on while the others join and write.
-template <typename T, bool VEC, bool COLUMNS>
+template <typename T, bool VEC, bool COLUMNS, bool E5>
 __global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 2 : 4)
 quant_tiles_f8_kernel(const F8Source p)
 {
@@ -398,7 +549,7 @@ quant_tiles_f8_kernel(const F8Source p)
                     if constexpr (sizeof(T) == 4) t = max(t, reinterpret_cast<const uint32_t *>(tops[w])[tid]);
                     else t = max(t, (uint32_t)reinterpret_cast<const uint16_t *>(tops[w])[tid]);
                 }
-                const uint32_t b = scale_byte(mag_bits(t, T()), p.e5m2);
+                const uint32_t b = scale_byte<E5>(mag_bits(t, T()));
                 bytes[tid] = (uint8_t)b;
                 if (tile * 128 + tid < p.K) p.scale[(int64_t)blk * p.ld_scale + tile * 128 + tid] = (uint8_t)b;
             }
@@ -415,7 +566,7 @@ quant_tiles_f8_kernel(const F8Source p)
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < 8; ++w) t = max(t, part[w]);
-            const uint32_t b = scale_byte(t, p.e5m2);
+            const uint32_t b = scale_byte<E5>(t);
             if (tid == 0) p.scale[(int64_t)blk * p.ld_scale + tile] = (uint8_t)b;
             s8[0] = s8[1] = b * 0x01010101u;
         }
@@ -431,21 +582,29 @@ quant_tiles_f8_kernel(const F8Source p)
             else keep.y |= both;
         }
         // (columns: the rows that fill a group up to whole blocks are written too, as zeros)
-        const int64_t out0 = (int64_t)blk * 128;
+        auto encode = [&](auto kind) {
+            using V = decltype(kind);
+            constexpr bool VALUES = !std::is_same<V, Nothing>::value;
+            const int64_t out0 = (int64_t)blk * 128 + r16;
+            uint8_t *codes = p.codes + out0 * p.ldq + k;
+            V *values = static_cast<V *>(p.values) + (VALUES ? out0 * p.ld_values : 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = i * 16 + r16;
-            const bool there = (COLUMNS || r < rows) && k < K16;
-            f32x2 f[4];
-            floats_of(v[i], f);
-            uint2 q = encode8(f, inv, p.e5m2);
-            q.x &= keep.x; q.y &= keep.y;
-            if (there) *reinterpret_cast<uint2 *>(p.codes + (out0 + r) * p.ldq + k) = q;
-            if (p.values) {
-                decode8(q, val, p.e5m2, f);
-                write_values(p, out0 + r, k, f, there && k < p.K);
+            for (int i = 0; i < 8; ++i) {
+                const bool there = (COLUMNS || i * 16 + r16 < rows) && k < K16;
+                f32x2 f[4];
+                floats_of(v[i], f);
+                uint2 q = encode8<E5>(f, inv);
+                q.x &= keep.x; q.y &= keep.y;
+                if (there) *reinterpret_cast<uint2 *>(codes) = q;
+                codes += 16 * p.ldq;
+                if constexpr (VALUES) {
+                    decode8<E5>(q, val, f);
+                    put_values(values, k, p.K, f, p.vec_values != 0, there && k < p.K);
+                    values += 16 * p.ld_values;
+                }
             }
-        }
+        };
+        with_values(p, encode);
     }
 }
 
@@ -453,34 +612,30 @@ quant_tiles_f8_kernel(const F8Source p)
 
 enum { BY_ROWS, BY_TILES, BY_COLUMNS };
 
-template <int HOW, typename T>
+template <int HOW, typename T, bool E5>
 int launch_quant(F8Source p, const char *what, cudaStream_t st)
 {
     const bool vec = aligned(p.x, 16) && (p.ldx * (int64_t)sizeof(T)) % 16 == 0;
     const int64_t nblk = ceil_div(p.K, 128);
     if (HOW == BY_ROWS) {
-        p.log_seg = nblk > 4 ? 3 : nblk > 2 ? 2 : nblk > 1 ? 1 : 0;
-        const int64_t segs = ceil_div(nblk, 1 << p.log_seg);
-        const int wide = segs >= 4 ? 4 : segs == 2 ? 2 : 1;          // warps along a row
-        p.parts = (int32_t)ceil_div(segs, wide);
-        const int64_t blocks = ceil_div(ceil_div(p.rows, 8 >> p.log_seg), 4 / wide) * p.parts;
-        QNN_REQUIRE(blocks < (int64_t)1 << 31, QNN_ERR_UNSUPPORTED, "%s: too many blocks", what);
-        const dim3 grid((unsigned)blocks), block(32 * (unsigned)wide, 4 / (unsigned)wide);
+        p.log_seg = nblk > 2 ? 3 : nblk > 1 ? 1 : 0;
+        p.segs = (int32_t)ceil_div(nblk, 1 << p.log_seg);
+        const int64_t warps = ceil_div(p.rows, 8 >> p.log_seg) * p.segs;
+        QNN_REQUIRE(warps < ((int64_t)1 << 32) - 4, QNN_ERR_UNSUPPORTED, "%s: too many blocks", what);
+        const dim3 grid((unsigned)ceil_div(warps, 4)), block(128);
         if (p.log_seg == 3) {
-            if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true, true>, grid, block, 0, st, p));
-            else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false, true>, grid, block, 0, st, p));
+            if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true, true, E5>, grid, block, 0, st, p));
+            else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false, true, E5>, grid, block, 0, st, p));
         } else {
-            if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true, false>, grid, block, 0, st, p));
-            else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false, false>, grid, block, 0, st, p));
+            if (vec) QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, true, false, E5>, grid, block, 0, st, p));
+            else QNN_CUDA(launch_pdl(quant_rows_f8_kernel<T, false, false, E5>, grid, block, 0, st, p));
         }
     } else {
         const int64_t blocks = HOW == BY_COLUMNS ? p.rows / 128 + p.groups : ceil_div(p.rows, 128);
         QNN_REQUIRE(blocks < 65536, QNN_ERR_UNSUPPORTED, "%s: 65536 blocks of 128 rows and more", what);
-        // columns: a block's rows are looked up once for up to four tiles, while there are several thread blocks for every SM
-        const int64_t tiles = HOW == BY_COLUMNS && nblk * blocks > 16 * (int64_t)sm_count() ? ceil_div(nblk, 4) : nblk;
-        const dim3 grid((unsigned)tiles, (unsigned)blocks);
-        if (vec) QNN_CUDA(launch_pdl(quant_tiles_f8_kernel<T, true, HOW == BY_COLUMNS>, grid, dim3(TILE_THREADS), 0, st, p));
-        else QNN_CUDA(launch_pdl(quant_tiles_f8_kernel<T, false, HOW == BY_COLUMNS>, grid, dim3(TILE_THREADS), 0, st, p));
+        const dim3 grid((unsigned)nblk, (unsigned)blocks);
+        if (vec) QNN_CUDA(launch_pdl(quant_tiles_f8_kernel<T, true, HOW == BY_COLUMNS, E5>, grid, dim3(TILE_THREADS), 0, st, p));
+        else QNN_CUDA(launch_pdl(quant_tiles_f8_kernel<T, false, HOW == BY_COLUMNS, E5>, grid, dim3(TILE_THREADS), 0, st, p));
     }
     return check_launch(what);
 }
@@ -515,12 +670,12 @@ int quant_f8(F8Source p, int type, int64_t K, int code_type, const char *what, v
         QNN_REQUIRE(p.offsets || p.groups == 1, QNN_ERR_INVALID_ARG, "%s: offsets are NULL", what);
     }
     p.K = (int32_t)K;
-    p.e5m2 = code_type == QNN_F8_E5M2;
+    const bool e5 = code_type == QNN_F8_E5M2;
     cudaStream_t st = as_stream(stream);
     switch (type) {
-        case QNN_TYPE_F32: return launch_quant<HOW, float>(p, what, st);
-        case QNN_TYPE_BF16: return launch_quant<HOW, __nv_bfloat16>(p, what, st);
-        default: return launch_quant<HOW, __half>(p, what, st);
+        case QNN_TYPE_F32: return e5 ? launch_quant<HOW, float, true>(p, what, st) : launch_quant<HOW, float, false>(p, what, st);
+        case QNN_TYPE_BF16: return e5 ? launch_quant<HOW, __nv_bfloat16, true>(p, what, st) : launch_quant<HOW, __nv_bfloat16, false>(p, what, st);
+        default: return e5 ? launch_quant<HOW, __half, true>(p, what, st) : launch_quant<HOW, __half, false>(p, what, st);
     }
 }
 
