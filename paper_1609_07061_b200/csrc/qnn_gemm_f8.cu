@@ -1,922 +1,76 @@
-// Products of 8-bit floating-point codes (e4m3, e5m2) with a power-of-two scale for each block of 128 along the reduction:
-//   out[m, n]   = sum_k a[m,k] sa[m, k/128] b[g][n,k] sb[g][n/128, k/128] + bias[g][n]        rows m of group g (forward)
-//   out[m, n]   = sum_k a[m,k] sa[m, k/128] b[g][k,n] sb[g][k/128, n/128]                      the same weights read across (input gradient)
-//   dw[g][n, k] = sum_m y[m,n] sy[m/128, n] x[m,k] sx[m/128, k]                                rows m of group g (weight gradient)
-// The dense product is the grouped one with a single group.
-//
-// The tensor cores apply the scales themselves (tcgen05 kind::mxf8f6f4 with block scales: one byte for 32 elements, here the same
-// byte for the four steps of a block), so partial sums never leave tensor memory before a tile is done.
-//
-// One persistent kernel.  The weights (in a weight gradient: the output's rows) are the tile's 128 rows, the tokens its
-// columns: their number is given to the instruction at run time, so a group of 37 rows costs 48 columns and not a tile.  Weights read
-// across, and both operands of a weight gradient, are taken as they lie in memory: the tensor core reads them MN-major.
-// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 2 loads scales, warps 4..11 store the previous tile,
-// warps 12..15 put the scales into tensor memory.  All waits are bounded.
-#include <cuda.h>
-#include <atomic>
-#include "qnn_types.cuh"
-#include "qnn_tc_ptx.cuh"
+// Products of 8-bit floating-point codes: the entry points, the choice of a configuration, and the forward products' kernels (see
+// qnn_gemm_f8.cuh).
+#include "qnn_gemm_f8.cuh"
 
 namespace qnn {
 namespace {
 
-constexpr int MAX_GROUPS = QNN_F8_MAX_GROUPS;
-constexpr int F8_THREADS = 512;
-enum Mode { FORWARD = 0, ACROSS = 1, WGRAD = 2 };
-
-struct F8Params {
-    int64_t M;                       // rows of a (tokens) of all groups; offsets are held to 0..M
-    int32_t N;                       // channels: rows of the tile's operand (forward: n, across: n, weight gradient: n)
-    int32_t C;                       // weight gradient: columns (k)
-    int32_t nkb;                     // blocks of the reduction (forward, across)
-    int32_t groups;
-    const int64_t *offsets;          // [groups + 1] or NULL: one group of all rows
-    const uint8_t *w_scale; int64_t ld_ws, stride_ws;      // scales of the tile's rows
-    const uint8_t *x_scale; int64_t ld_xs;                 // scales of the tile's columns
-    const float *bias;               // [groups, N] or NULL
-    void *out; int64_t ldo;
-    int32_t vec_out;                 // rows of the output may be written in 16-byte pieces
-    int32_t split;                   // CTAs that share the reduction of a tile
-    int32_t has_maps;                // 0: an empty reduction, nothing is loaded
-    int32_t tma_out;                 // whole blocks of the output leave as bulk stores
-    int32_t tiles_c;                 // tiles of channels
-    int32_t nt;                      // columns of a tile at most
-    int32_t step;                    // ... a multiple of this many, but for the last ones
-    int32_t acc1;                    // tensor-memory column of the second accumulator
-    int32_t overlap;                 // 1: its first 32 columns are the first one's last
-    int32_t chunks, chunk;           // weight gradient: tiles of columns, and columns of each
-    int32_t super;                   // chunks of tokens that go through all channels before the next ones
-    uint32_t idesc;                  // without N and the scales' byte
-};
-
-template <int NT, int MODE, int CTAS, typename TOUT>
-struct F8Cfg {
-    static constexpr int A_BYTES = BM * BKB;
-    static constexpr int BROWS = NT / CTAS > 128 ? 256 : NT / CTAS > 64 ? 128 : NT / CTAS > 32 ? 64 : 32;   // rows (columns, MN-major) a CTA loads at most
-    static constexpr int B_BYTES = BROWS * BKB;
-    static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-    static constexpr int STG_BYTES = 8 * 32 * 32 * (int)sizeof(TOUT);   // a block of 32 x 32 results for each storing warp
-    static constexpr int SFB = (NT + 127) / 128;                        // pieces of 128 columns
-    static constexpr int SF_COLS = 4 + 4 * SFB;                         // tensor-memory columns of one word's scales
-    // Tensor memory: two accumulators and two words of scales.  With 256 columns each that is more than there is: the accumulators
-    // then share 32 columns, which are drained first.
-    static constexpr int SF_BASE = NT == 256 ? 512 - 2 * SF_COLS : 2 * NT;
-    static constexpr int TMEM_NEED = SF_BASE + 2 * SF_COLS;
-    static constexpr int TMEM = TMEM_NEED <= 128 ? 128 : TMEM_NEED <= 256 ? 256 : 512;
-    // Scales on their way: 16 blocks' bytes of every column, handed from warp to warp, or (weight gradient) four blocks' of every row and
-    // column, by TMA.
-    static constexpr int Q_BYTES = (MODE == WGRAD ? 4 * (BM + NT) + 127 : 16 * NT + 127) / 128 * 128;
-    static constexpr int QS = MODE == WGRAD ? 6 : 2;
-    static constexpr int TABLE_BYTES = 2 * 4 * (MAX_GROUPS + 8);
-    static constexpr int AUX = STG_BYTES + QS * Q_BYTES + TABLE_BYTES + 256 + 1024;
-    static constexpr int MAXS = (SMEM_LIMIT - AUX) / STAGE_BYTES;
-    static constexpr int STAGES = MAXS > 8 ? 8 : MAXS;
-    static constexpr int STG_OFFSET = STAGES * STAGE_BYTES;
-    static constexpr int Q_OFFSET = STG_OFFSET + STG_BYTES;
-    static constexpr int TABLE_OFFSET = Q_OFFSET + QS * Q_BYTES;
-    static constexpr int BAR_OFFSET = TABLE_OFFSET + TABLE_BYTES;
-    static constexpr int TOTAL = BAR_OFFSET + 256 + 1024;
-    static_assert(TMEM_NEED <= 512 && (2 * STAGES + 2 * QS + 6) * 8 + 16 <= 256 && TOTAL <= SMEM_LIMIT, "configuration");
-    // The scales' warps learn from a stage's barrier that the word before the last one has been used: the products cannot be more than
-    // four blocks past it by then, so the barrier must not come round within five.
-    static_assert(STAGES >= 5, "configuration");
-};
-
-// ---- PTX ---------------------------------------------------------------------------------------------------------
-
-// descriptor of a tile of 128-byte rows, swizzled over 128 bytes, whose ROWS run along the reduction: 8-row groups 1024 bytes apart,
-// the next 128 elements of the other dimension 128 rows further on
-__device__ __forceinline__ uint64_t make_across_desc(uint32_t saddr)
+// Clusters of a kernel that are resident at once, asked once per device (0: none can be launched).  Fewer than the SMs would hold: the
+// GPU's groups of SMs leave some over (of eights, one CTA an SM, 15 fit).
+template <int NT, int CTAS, int SPLIT>
+int clusters_resident()
 {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
-    d |= (uint64_t)((128 * BKB) >> 4) << 16;
-    d |= (uint64_t)((8 * BKB) >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-// One block of the reduction as ONE instruction stream: poll the NEXT stage's full barrier, issue the block's four steps of 32 (A_STEP
-// and B_STEP apart in the descriptors' address field), commit them to this stage's empty barrier (a pair: of both CTAs), and only then
-// read the poll's result, whose latency hides behind the issue.  Returns non-zero when the next stage has landed.
-template <int CTAS, uint32_t A_STEP, uint32_t B_STEP>
-__device__ __forceinline__ uint32_t umma_f8_block(uint32_t next_full_bar, uint32_t next_parity, uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi,
-                                                  uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate, uint32_t sf, uint32_t empty_bar)
-{
-    uint32_t ready;
-#define QNN_F8_BLOCK(GROUP, COMMIT)                                                                                                          \
-    asm volatile("{\n"                                                                                                                      \
-                 ".reg .pred P, Q, T;\n"                                                                                                    \
-                 ".reg .b64 a0, a1, a2, a3, b0, b1, b2, b3;\n"                                                                              \
-                 ".reg .b32 t1, t2, t3, u1, u2, u3, sb;\n"                                                                                  \
-                 ".reg .b16 both;\n"                                                                                                        \
-                 "mov.b16 both, 3;\n"                                                                                                       \
-                 "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"                                                                  \
-                 "setp.ne.b32 P, %9, 0;\n"                                                                                                  \
-                 "setp.eq.b32 T, 0, 0;\n"                                                                                                   \
-                 "add.u32 sb, %10, 4;\n"                                                                                                    \
-                 "add.u32 t1, %4, %12;\n add.u32 t2, t1, %12;\n add.u32 t3, t2, %12;\n"                                                   \
-                 "add.u32 u1, %6, %13;\n add.u32 u2, u1, %13;\n add.u32 u3, u2, %13;\n"                                                   \
-                 "mov.b64 a0, {%4, %5};\n mov.b64 a1, {t1, %5};\n mov.b64 a2, {t2, %5};\n mov.b64 a3, {t3, %5};\n"                       \
-                 "mov.b64 b0, {%6, %7};\n mov.b64 b1, {u1, %7};\n mov.b64 b2, {u2, %7};\n mov.b64 b3, {u3, %7};\n"                       \
-                 "tcgen05.mma.cta_group::" GROUP ".kind::mxf8f6f4.block_scale.scale_vec::1X [%3], a0, b0, %8, [%10], [sb], P;\n"            \
-                 "tcgen05.mma.cta_group::" GROUP ".kind::mxf8f6f4.block_scale.scale_vec::1X [%3], a1, b1, %8, [%10], [sb], T;\n"            \
-                 "tcgen05.mma.cta_group::" GROUP ".kind::mxf8f6f4.block_scale.scale_vec::1X [%3], a2, b2, %8, [%10], [sb], T;\n"            \
-                 "tcgen05.mma.cta_group::" GROUP ".kind::mxf8f6f4.block_scale.scale_vec::1X [%3], a3, b3, %8, [%10], [sb], T;\n"            \
-                 "tcgen05.commit.cta_group::" GROUP ".mbarrier::arrive::one.shared::cluster" COMMIT ";\n"                                   \
-                 "selp.u32 %0, 1, 0, Q;\n"                                                                                                  \
-                 "}\n"                                                                                                                      \
-                 : "=r"(ready)                                                                                                              \
-                 : "r"(next_full_bar), "r"(next_parity), "r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), \
-                   "r"(sf), "r"(empty_bar), "n"(A_STEP), "n"(B_STEP)                                                                        \
-                 : "memory")
-    if (CTAS == 2) QNN_F8_BLOCK("2", ".multicast::cluster.b64 [%11], both");
-    else QNN_F8_BLOCK("1", ".b64 [%11]");
-#undef QNN_F8_BLOCK
-    return ready;
-}
-// this warp's 32 lanes of four / eight tensor-memory columns
-__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t *v)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-template <int CTAS>
-__device__ __forceinline__ void commit(uint32_t bar)
-{
-    if (CTAS == 2) umma_commit_pair(bar);
-    else umma_commit(bar);
-}
-// 32 lanes x 32 columns as fragments of 8 x 8: v[16 h + 4 c + 2 u + e] of lane 4 r + t is lane 16 h + 8 u + r, column 8 c + 2 t + e
-__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, uint32_t (&v)[32])
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        asm volatile(
-            "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
-            "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-            : "=r"(v[16 * h]), "=r"(v[16 * h + 1]), "=r"(v[16 * h + 2]), "=r"(v[16 * h + 3]), "=r"(v[16 * h + 4]), "=r"(v[16 * h + 5]),
-              "=r"(v[16 * h + 6]), "=r"(v[16 * h + 7]), "=r"(v[16 * h + 8]), "=r"(v[16 * h + 9]), "=r"(v[16 * h + 10]), "=r"(v[16 * h + 11]),
-              "=r"(v[16 * h + 12]), "=r"(v[16 * h + 13]), "=r"(v[16 * h + 14]), "=r"(v[16 * h + 15])
-            : "r"(taddr + ((uint32_t)(16 * h) << 16)) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-// four 8 x 8 blocks of 16-bit elements, transposed: lane 8 m + j gives the address of row j (a column of the fragment) of block m
-__device__ __forceinline__ void stmatrix_trans(uint32_t addr, const uint32_t (&o)[4])
-{
-    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
-}
-// arrival on a barrier of the pair's leader (a shared::cluster address) or of this CTA
-template <int CTAS>
-__device__ __forceinline__ void arrive_at_leader(uint32_t bar)
-{
-    if (CTAS == 2) mbar_arrive_cluster(bar);
-    else mbar_arrive(bar);
-}
-template <int CTAS>
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar)
-{
-    if (CTAS == 2)
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-__device__ __forceinline__ float ld_peer_f32(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-// (volatile: issued where it stands, well before its use)
-__device__ __forceinline__ uint4 ldg128(const uint8_t *ptr)
-{
-    uint4 v;
-    asm volatile("ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(ptr));
-    return v;
-}
-__device__ __forceinline__ void expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// One stage of the loading warp in the same way: poll the NEXT stage's empty barrier, announce this stage's bytes (a pair: those of both
-// CTAs, by its leader), issue the load of the tile's rows and the first of its columns.
-template <int CTAS>
-__device__ __forceinline__ uint32_t tma_f8_stage(uint32_t next_empty_bar, uint32_t next_parity, uint32_t full_bar, uint32_t bytes, uint32_t announce,
-                                                 uint32_t dst_a, const CUtensorMap *map_a, int32_t ax, int32_t ay, int32_t az, uint32_t dst_b,
-                                                 const CUtensorMap *map_b, int32_t bx, int32_t by)
-{
-    uint32_t ready;
-#define QNN_F8_STAGE(GROUP)                                                                                                                       \
-    asm volatile("{\n"                                                                                                                          \
-                 ".reg .pred Q, L;\n"                                                                                                           \
-                 "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"                                                                      \
-                 "setp.ne.b32 L, %14, 0;\n"                                                                                                     \
-                 "@L mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%3], %4;\n"                                                              \
-                 "cp.async.bulk.tensor.3d" GROUP ".shared::cluster.global.mbarrier::complete_tx::bytes [%5], [%6, {%7, %8, %9}], [%3];\n"       \
-                 "cp.async.bulk.tensor.2d" GROUP ".shared::cluster.global.mbarrier::complete_tx::bytes [%10], [%11, {%12, %13}], [%3];\n"       \
-                 "selp.u32 %0, 1, 0, Q;\n"                                                                                                      \
-                 "}\n"                                                                                                                          \
-                 : "=r"(ready)                                                                                                                  \
-                 : "r"(next_empty_bar), "r"(next_parity), "r"(full_bar), "r"(bytes), "r"(dst_a), "l"(map_a), "r"(ax), "r"(ay), "r"(az),         \
-                   "r"(dst_b), "l"(map_b), "r"(bx), "r"(by), "r"(announce)                                                                      \
-                 : "memory")
-    if (CTAS == 2) QNN_F8_STAGE(".cta_group::2");
-    else QNN_F8_STAGE("");
-#undef QNN_F8_STAGE
-    return ready;
-}
-
-// ---- tiles -------------------------------------------------------------------------------------------------------
-
-struct F8Tile {
-    int32_t g;                       // group
-    int32_t c0;                      // first channel (of the pair)
-    int32_t m0;                      // first token; weight gradient: first column
-    int32_t cols;                    // columns with a result
-    int32_t n;                       // columns multiplied: rounded up to what the instruction takes
-    int32_t kb0, kb;                 // blocks of the reduction: the first one and how many
-    int32_t blk0;                    // weight gradient: the group's first block of rows
-};
-
-// Walks the tiles of one CTA (pair) in rising order; every role of the CTA walks by itself.
-template <int MODE, int CTAS>
-struct Tiles {
-    const F8Params &p;
-    const int32_t *first, *start;    // [groups + 1] first tile / (forward, across) first row or (weight gradient) first block
-    const int32_t kb0, kb;           // (forward, across) this CTA's part of the reduction
-    int32_t g = 0;
-    __device__ __forceinline__ Tiles(const F8Params &p_, const int32_t *f, const int32_t *s, int32_t k0, int32_t k) : p(p_), first(f), start(s), kb0(k0), kb(k) {}
-    __device__ __forceinline__ int32_t count() const { return first[p.groups]; }
-    __device__ __forceinline__ F8Tile at(int32_t t)
-    {
-        while (t >= first[g + 1]) ++g;
-        F8Tile r;
-        r.g = g;
-        const int32_t i = t - first[g];
-        if (MODE == WGRAD) {
-            const int32_t c = i / p.chunks, ch = i - c * p.chunks;
-            r.c0 = c * BM * CTAS;
-            r.m0 = ch * p.chunk;
-            r.cols = p.C - r.m0 < p.chunk ? p.C - r.m0 : p.chunk;
-            r.blk0 = start[g];
-            r.kb0 = 0;
-            r.kb = start[g + 1] - start[g];
-        } else {
-            const int32_t len = start[g + 1] - start[g];
-            const int32_t chunks = (len + p.nt - 1) / p.nt;
-            const int32_t csize = ((len + chunks - 1) / chunks + p.step - 1) / p.step * p.step;
-            const int32_t sup = i / (p.super * p.tiles_c);
-            const int32_t j = i - sup * p.super * p.tiles_c;
-            const int32_t wide = chunks - sup * p.super < p.super ? chunks - sup * p.super : p.super;
-            const int32_t c = j / wide;
-            const int32_t ch = sup * p.super + (j - c * wide);
-            r.c0 = c * BM * CTAS;
-            r.m0 = start[g] + ch * csize;
-            r.cols = start[g + 1] - r.m0 < csize ? start[g + 1] - r.m0 : csize;
-            r.kb0 = kb0;
-            r.kb = kb;
-            r.blk0 = 0;
-        }
-        constexpr int STEP = MODE == WGRAD ? 16 * CTAS : 16;          // (halves of MN-major columns start on 16 bytes)
-        r.n = (r.cols + STEP - 1) / STEP * STEP;
-        return r;
-    }
-};
-
-// first[], start[] in shared memory from the offsets in global memory, by all threads of the block.  Offsets that fall, or leave
-// 0..M, are held to rise and to stay inside, so that no group reaches rows that are not there.
-template <int MODE>
-__device__ void fill_tables(const F8Params &p, int32_t *first, int32_t *start, int32_t *scratch)
-{
-    constexpr int W = F8_THREADS / 32;
-    constexpr int PER = (MAX_GROUPS + F8_THREADS) / F8_THREADS;         // offsets a thread: groups + 1 of them at most MAX_GROUPS + 1
-    static_assert(PER * F8_THREADS >= MAX_GROUPS + 1, "table");
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t G = p.groups;
-    if (p.offsets == nullptr) {
-        if (tid == 0) {
-            start[0] = first[0] = 0;
-            start[1] = MODE == WGRAD ? (int32_t)((p.M + 127) / 128) : (int32_t)p.M;
-            first[1] = MODE == WGRAD ? p.tiles_c * p.chunks : (int32_t)((p.M + p.nt - 1) / p.nt) * p.tiles_c;
-        }
-        __syncthreads();
-        return;
-    }
-    int32_t o[PER];
-    int32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int g = tid * PER + i;
-        int64_t v = 0;
-        if (g <= G) v = p.offsets ? __ldg(p.offsets + g) : (g == 0 ? 0 : p.M);
-        v = v < 0 ? 0 : v > p.M ? p.M : v;
-        top = (int32_t)v > top ? (int32_t)v : top;
-        o[i] = top;
-    }
-    // running maximum over the threads before
-    int32_t run = top;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const int32_t v = __shfl_up_sync(0xffffffffu, run, d);
-        if (lane >= d && v > run) run = v;
-    }
-    if (lane == 31) scratch[warp] = run;
-    __syncthreads();
-    int32_t before = __shfl_up_sync(0xffffffffu, run, 1);
-    if (lane == 0) before = 0;
-    for (int w = 0; w < warp; ++w) before = scratch[w] > before ? scratch[w] : before;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int g = tid * PER + i;
-        if (g <= G) start[g] = o[i] > before ? o[i] : before;
-    }
-    __syncthreads();
-    // tiles (and blocks) of each group, added up
-    int32_t tl[PER], bl[PER], tsum = 0, bsum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int g = tid * PER + i;
-        const int32_t len = g < G ? start[g + 1] - start[g] : 0;
-        tl[i] = tsum; bl[i] = bsum;
-        bsum += (len + 127) / 128;
-        if (g < G) tsum += MODE == WGRAD ? p.tiles_c * p.chunks : (len + p.nt - 1) / p.nt * p.tiles_c;
-    }
-    int32_t trun = tsum, brun = bsum;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const int32_t v = __shfl_up_sync(0xffffffffu, trun, d), u = __shfl_up_sync(0xffffffffu, brun, d);
-        if (lane >= d) { trun += v; brun += u; }
-    }
-    if (lane == 31) { scratch[W + warp] = trun; scratch[2 * W + warp] = brun; }
-    __syncthreads();
-    trun -= tsum; brun -= bsum;
-    for (int w = 0; w < warp; ++w) { trun += scratch[W + w]; brun += scratch[2 * W + w]; }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int g = tid * PER + i;
-        if (g <= G) {
-            first[g] = trun + tl[i];
-            if (MODE == WGRAD) start[g] = brun + bl[i];
-        }
-    }
-    __syncthreads();
-}
-
-// ---- the kernel --------------------------------------------------------------------------------------------------
-
-// SPLIT: the CTAs of a cluster share one tile, each adds up a part of the reduction, and the sums meet in shared memory.
-template <int NT, int MODE, int CTAS, typename TOUT, bool SPLIT>
-__global__ void __launch_bounds__(F8_THREADS, 1)
-gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_x32,
-               const __grid_constant__ CUtensorMap tmap_sw, const __grid_constant__ CUtensorMap tmap_sx, const __grid_constant__ CUtensorMap tmap_out,
-               const F8Params p)
-{
-    using S = F8Cfg<NT, MODE, CTAS, TOUT>;
-    static_assert(!SPLIT || (CTAS == 1 && MODE != WGRAD && S::STAGES * S::STAGE_BYTES >= NT * BM * 4), "the partial sums reuse the stages");
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw);
-    const uint32_t base = (raw + 1023u) & ~1023u;                      // swizzled tiles need 1024-byte alignment
-    uint8_t *gen = smem_raw + (base - raw);
-    const uint32_t bar0 = base + S::BAR_OFFSET;
-    auto full_bar = [&](int s) { return bar0 + 8u * (uint32_t)s; };
-    auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(S::STAGES + s); };
-    auto sfull_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + s); };
-    auto tfull_bar = [&](int a) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 2 + a); };
-    auto tempty_bar = [&](int a) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 4 + a); };
-    auto qfull_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + s); };
-    auto qempty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + S::QS + s); };
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 6 + 2 * S::QS));
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    int32_t *first = reinterpret_cast<int32_t *>(gen + S::TABLE_OFFSET);
-    int32_t *start = first + MAX_GROUPS + 8;
-
-    const int warp = threadIdx.x >> 5;
-    const int lane = threadIdx.x & 31;
-    // a pair's CTA 0 leads: it owns the full, scales-full and accumulator-empty barriers and issues the products
-    const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
-    const bool leader = rank == 0;
-
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < S::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(sfull_bar(a), 4 * CTAS); mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 8 * CTAS); }
-        for (int s = 0; s < S::QS; ++s) { mbar_init(qfull_bar(s), MODE == WGRAD ? 1 : 4); mbar_init(qempty_bar(s), 4); }
-        *abort_flag = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    }
-    if (warp == 1) tmem_alloc<CTAS>(smem_u32(tmem_slot), S::TMEM);
-    if (warp == 2 && lane < 3 && p.has_maps) {
-        const CUtensorMap *m = lane == 0 ? &tmap_w : lane == 1 ? &tmap_x : &tmap_x32;
-        asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
-    }
-    tc_fence_before();
-    __syncthreads();
-    if (CTAS == 2) cluster_sync_all();                                 // the peer's barriers exist before anything arrives on them
-    tc_fence_after();
-    const uint32_t tmem_base = *tmem_slot;
-    // only now may the next kernel be scheduled: one that shares this SM could take the tensor memory this CTA waits for
-    griddep_launch_dependents();
-    griddep_wait();
-    fill_tables<MODE>(p, first, start, reinterpret_cast<int32_t *>(gen + S::STG_OFFSET));
-
-    // a part of the reduction is whole words of scales
-    const int32_t split = SPLIT ? p.split : 1, part_k = SPLIT ? (int32_t)cluster_ctarank() : 0;
-    const int32_t words = (p.nkb + 3) / 4, kb0 = SPLIT ? words * part_k / split * 4 : 0;
-    const int32_t kb1 = !SPLIT || part_k == split - 1 ? p.nkb : words * (part_k + 1) / split * 4;
-    Tiles<MODE, CTAS> tiles(p, first, start, kb0, kb1 - kb0);
-    const int32_t num_tiles = tiles.count();
-    const int32_t worker = SPLIT ? (int32_t)(blockIdx.x / (uint32_t)split) : (int32_t)(blockIdx.x / CTAS);
-    const int32_t workers = SPLIT ? num_tiles : (int32_t)(gridDim.x / CTAS);           // (SPLIT: a tile a cluster)
-
-    if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0; uint32_t phase = 0;
-            bool ok = true, ready = false;
-            // (shared::cluster addresses)
-            const uint32_t fb0 = CTAS == 2 ? map_to_cta(full_bar(0), 0) : full_bar(0), eb0 = empty_bar(0);
-            uint32_t sa = base, fb = fb0, eb = eb0;
-            for (int32_t t = worker; t < num_tiles && ok; t += workers) {
-                const F8Tile r = tiles.at(t);
-                const int32_t mine = r.n / CTAS;                       // columns this CTA loads
-                const int32_t x0 = r.m0 + (int32_t)rank * mine;
-                const int32_t c0 = r.c0 + (int32_t)rank * BM;
-                // K-major: boxes of 128 rows, the rest in boxes of 32; MN-major: boxes of 128 columns
-                const int32_t n32 = (mine + 31) / 32;
-                const int32_t big = MODE == WGRAD ? (mine + 127) / 128 : S::BROWS >= 128 ? n32 / 4 + (n32 % 4 == 3 ? 1 : 0) : 0;
-                const int32_t small = MODE == WGRAD || n32 <= 4 * big ? 0 : n32 - 4 * big;
-                const int32_t boxes = big + small;
-                const uint32_t bytes = (uint32_t)(S::A_BYTES + big * 128 * BKB + small * 32 * BKB) * CTAS;
-                const CUtensorMap *map0 = big > 0 ? &tmap_x : &tmap_x32;
-                int32_t k = MODE == WGRAD ? r.blk0 * BKB : r.kb0 * BKB;           // along the reduction
-#pragma unroll 1
-                for (int32_t kb = 0; kb < r.kb; ++kb, k += BKB) {
-                    if (!ready && !mbar_wait(eb, phase ^ 1u, abort_flag, 41)) { ok = false; break; }
-                    const bool wrap = stage == S::STAGES - 1;
-                    const uint32_t sa_n = wrap ? base : sa + (uint32_t)S::STAGE_BYTES;
-                    const uint32_t fb_n = wrap ? fb0 : fb + 8u, eb_n = wrap ? eb0 : eb + 8u;
-                    const uint32_t phase_n = wrap ? phase ^ 1u : phase;
-                    const uint32_t sb = sa + S::A_BYTES;
-                    ready = tma_f8_stage<CTAS>(eb_n, phase_n ^ 1u, fb, bytes, (uint32_t)leader, sa, &tmap_w, MODE == FORWARD ? k : c0, MODE == FORWARD ? c0 : k,
-                                               MODE == WGRAD ? 0 : r.g, sb, map0, MODE == WGRAD ? x0 : k, MODE == WGRAD ? k : x0) != 0;
-                    for (int32_t i = 1; i < boxes; ++i) {
-                        const int32_t at = i < big ? i * 128 : big * 128 + (i - big) * 32;
-                        if (MODE == WGRAD) tma_load_2d<CTAS>(sb + (uint32_t)(at * BKB), &tmap_x, x0 + at, k, fb);
-                        else tma_load_2d<CTAS>(sb + (uint32_t)(at * BKB), i < big ? &tmap_x : &tmap_x32, k, x0 + at, fb);
-                    }
-                    stage = wrap ? 0 : stage + 1;
-                    sa = sa_n; fb = fb_n; eb = eb_n; phase = phase_n;
-                }
-            }
-        }
-    } else if (warp == 1) {
-        if (lane == 0 && leader) {
-            int stage = 0; uint32_t phase = 0, word = 0, iter = 0;
-            bool ok = true, ready = false;
-            // a step of 32 along the reduction: 32 bytes of a K-major row, 32 rows of an MN-major tile
-            constexpr uint32_t A_STEP = MODE == FORWARD ? 2 : (32 * BKB) >> 4, B_STEP = MODE == WGRAD ? (32 * BKB) >> 4 : 2;
-            const uint64_t ad = MODE == FORWARD ? make_kmajor_desc<BKB>(base) : make_across_desc(base);
-            const uint64_t bd = MODE == WGRAD ? make_across_desc(base + S::A_BYTES) : make_kmajor_desc<BKB>(base + S::A_BYTES);
-            const uint32_t a_hi = (uint32_t)(ad >> 32), b_hi = (uint32_t)(bd >> 32), a_lo0 = (uint32_t)ad, fb0 = full_bar(0), eb0 = empty_bar(0);
-            const uint32_t b_off = (uint32_t)bd - (uint32_t)ad;
-            uint32_t a_lo = a_lo0, fb = fb0, eb = eb0;
-            F8Tile next = worker < num_tiles ? tiles.at(worker) : F8Tile{};
-            bool sready = false;
-            for (int32_t t = worker; t < num_tiles && ok; t += workers, ++iter) {
-                const F8Tile r = next;
-                const uint32_t as = iter & 1u, aphase = (iter >> 1) & 1u;
-                // the accumulator's last tile has been read; where the two share columns, those of the last tile have
-                if (p.overlap ? iter > 0 && !mbar_wait(tempty_bar(0), iter - 1u & 1u, abort_flag, 42)
-                              : !mbar_wait(tempty_bar(as), aphase ^ 1u, abort_flag, 42)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t d_tmem = tmem_base + (as ? (uint32_t)p.acc1 : 0u);
-                const uint32_t idesc = p.idesc | (uint32_t)(r.n >> 3) << 17;
-                uint32_t sf = 0;
-#pragma unroll 4
-                for (int32_t kb = 0; kb < r.kb; ++kb) {
-                    if ((kb & 3) == 0) {
-                        if (!sready && !mbar_wait(sfull_bar((int)(word & 1u)), word >> 1 & 1u, abort_flag, 43)) { ok = false; break; }
-                        sready = false;
-                        sf = tmem_base + S::SF_BASE + (word & 1u) * S::SF_COLS;
-                        ++word;
-                    }
-                    if (!ready && !mbar_wait(fb, phase, abort_flag, 44)) { ok = false; break; }
-                    tc_fence_after();
-                    const bool wrap = stage == S::STAGES - 1;
-                    const uint32_t a_lo_n = wrap ? a_lo0 : a_lo + (uint32_t)(S::STAGE_BYTES >> 4);
-                    const uint32_t fb_n = wrap ? fb0 : fb + 8u, eb_n = wrap ? eb0 : eb + 8u;
-                    const uint32_t phase_n = wrap ? phase ^ 1u : phase;
-                    // (bits 4..5 and 29..30: which byte of the scales' words)
-                    ready = umma_f8_block<CTAS, A_STEP, B_STEP>(fb_n, phase_n, d_tmem, a_lo, a_hi, a_lo + b_off, b_hi,
-                                                                idesc | (uint32_t)(kb & 3) << 29 | (uint32_t)(kb & 3) << 4, (uint32_t)(kb != 0), sf, eb) != 0;
-                    stage = wrap ? 0 : stage + 1;
-                    a_lo = a_lo_n; fb = fb_n; eb = eb_n; phase = phase_n;
-                    // (behind the issue: the next tile's numbers, and whether the next word of scales is there)
-                    if (kb == 0 && t + workers < num_tiles) next = tiles.at(t + workers);
-                    if ((kb & 3) == 2) sready = mbar_try_wait(sfull_bar((int)(word & 1u)), word >> 1 & 1u);
-                }
-                if (r.kb == 0 && t + workers < num_tiles) next = tiles.at(t + workers);
-                if (ok) commit<CTAS>(tfull_bar(as));                   // accumulator complete
-            }
-        }
-    } else if (warp == 2) {
-        // weight gradient: scales into shared memory, well ahead of their use
-        if (MODE == WGRAD && lane == 0) {
-            int slot = 0; uint32_t phase = 0;
-            bool ok = true;
-            for (int32_t t = worker; t < num_tiles && ok; t += workers) {
-                const F8Tile r = tiles.at(t);
-                for (int32_t kb = 0; kb < r.kb; kb += 4) {
-                    if (!mbar_wait(qempty_bar(slot), phase ^ 1u, abort_flag, 47)) { ok = false; break; }
-                    const uint32_t dst = base + (uint32_t)(S::Q_OFFSET + slot * S::Q_BYTES), fb = qfull_bar(slot);
-                    expect_tx(fb, 4 * (BM + NT));
-                    tma_load_2d<1>(dst, &tmap_sw, r.c0 + (int32_t)rank * BM, r.blk0 + kb, fb);
-                    tma_load_2d<1>(dst + 4 * BM, &tmap_sx, r.m0, r.blk0 + kb, fb);
-                    if (++slot == S::QS) { slot = 0; phase ^= 1u; }
-                }
-            }
-        }
-    } else if (warp >= 12) {
-        // Scales: a word holds four blocks' bytes of a row; word r of a piece of 128 rows goes to lane r % 32 of column r / 32, the same in
-        // each quarter of the lanes, one warp a quarter.  Two words have room.  A word's room is free when the products of the word before
-        // the last one are done: their last stage's barrier tells.
-        const uint32_t tsf = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + S::SF_BASE;
-        const uint32_t sfull0 = CTAS == 2 ? map_to_cta(sfull_bar(0), 0) : sfull_bar(0);
-        uint32_t word = 0;
-        int stage = 0, last1 = 0, last2 = 0;                           // the next block's stage, those of the last blocks of the last two words
-        uint32_t phase = 0, phase1 = 0, phase2 = 0;
-        int slot = 0; uint32_t qphase = 0;
-        bool ok = true;
-        // w: 4 words of the tile's rows, then 4 for each 128 columns
-        auto put = [&](const uint32_t *w, int blocks) {
-            if (word >= 2 && !__all_sync(0xffffffffu, mbar_wait(empty_bar(last2), phase2, abort_flag, 45))) return false;
-            tc_fence_after();
-            const uint32_t dst = tsf + (word & 1u) * S::SF_COLS;
-#pragma unroll
-            for (int i = 0; i <= S::SFB; ++i) tmem_st4(dst + 4u * (uint32_t)i, w + 4 * i);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at_leader<CTAS>(sfull0 + 8u * (word & 1u));
-            ++word;
-            stage += blocks - 1;
-            if (stage >= S::STAGES) { stage -= S::STAGES; phase ^= 1u; }
-            last2 = last1; phase2 = phase1;
-            last1 = stage; phase1 = phase;
-            if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
-            return true;
-        };
-        if constexpr (MODE == WGRAD) {
-            for (int32_t t = worker; t < num_tiles && ok; t += workers) {
-                const F8Tile r = tiles.at(t);
-                for (int32_t kb = 0; kb < r.kb && ok; kb += 4) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(qfull_bar(slot), qphase, abort_flag, 48))) { ok = false; break; }
-                    const uint8_t *qs = gen + S::Q_OFFSET + slot * S::Q_BYTES + lane;
-                    uint32_t w[S::SF_COLS];
-#pragma unroll
-                    for (int i = 0; i < S::SF_COLS; ++i) {
-                        // (bytes of blocks behind the group's, and of rows and columns behind the last, are multiplied with nothing)
-                        const uint8_t *b = i < 4 ? qs + 32 * i : qs + 4 * BM + 32 * (i - 4);
-                        const int pitch = i < 4 ? BM : NT;
-                        w[i] = i < 4 || 32 * (i - 4) < NT ? (uint32_t)b[0] | (uint32_t)b[pitch] << 8 | (uint32_t)b[2 * pitch] << 16 | (uint32_t)b[3 * pitch] << 24 : 0u;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(qempty_bar(slot));
-                    if (++slot == S::QS) { slot = 0; qphase ^= 1u; }
-                    ok = put(w, r.kb - kb < 4 ? r.kb - kb : 4);
-                }
-            }
-        } else if (kb1 > kb0 && worker < num_tiles) {
-            // Sixteen blocks' bytes at a time: each warp fetches a quarter of the columns', the next ones while these are used, and all
-            // four read the others' from shared memory.  (Each fetching all of them costs the pipe that feeds the tensor core an eighth
-            // of its time, and 16-byte boxes by TMA take the loads' turns.)
-            constexpr int R = (NT + 31) / 32, RW = (R + 3) / 4;        // groups of 32 columns, and those of a warp
-            const int w4 = warp & 3;
-            uint4 mine[RW], a;
-            auto fetch = [&](const F8Tile &r, int32_t kb) {
-#pragma unroll
-                for (int i = 0; i < RW; ++i) {
-                    const int32_t row = 32 * (w4 + 4 * i) + lane;
-                    mine[i] = row < r.cols ? ldg128(p.x_scale + (int64_t)(r.m0 + row) * p.ld_xs + kb) : make_uint4(0, 0, 0, 0);
-                }
-                const int32_t ct = (r.c0 + (int32_t)rank * BM) / BM;
-                const bool has_ct = ct * BM < p.N;                     // (a pair's second half may lie beyond the channels)
-                const uint8_t *ws = p.w_scale + (int64_t)r.g * p.stride_ws;
-                a = make_uint4(0, 0, 0, 0);
-                if (MODE == FORWARD) {
-                    if (has_ct) a = ldg128(ws + (int64_t)ct * p.ld_ws + kb);
-                } else {
-                    if (lane < 16 && has_ct && kb + lane < kb1) a.x = ws[(int64_t)(kb + lane) * p.ld_ws + ct];
-                }
-            };
-            int32_t t = worker, kb = kb0 & ~15;                        // (16 bytes lie on 16 bytes)
-            F8Tile r = tiles.at(t);
-            fetch(r, kb);
-            for (bool more = true; more && ok;) {
-                uint4 *qs = reinterpret_cast<uint4 *>(gen + S::Q_OFFSET + slot * S::Q_BYTES) + lane;
-#pragma unroll
-                for (int i = 0; i < RW; ++i)
-                    if (32 * (w4 + 4 * i) + lane < NT) qs[32 * (w4 + 4 * i)] = mine[i];
-                uint32_t aw[4];
-                if (MODE == FORWARD) { aw[0] = a.x; aw[1] = a.y; aw[2] = a.z; aw[3] = a.w; }
-                else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        aw[j] = 0;
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) aw[j] |= __shfl_sync(0xffffffffu, a.x, 4 * j + b) << (8 * b);
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(qfull_bar(slot));
-                if (!__all_sync(0xffffffffu, mbar_wait(qfull_bar(slot), qphase, abort_flag, 48))) break;
-                uint4 x[R];
-#pragma unroll
-                for (int i = 0; i < R; ++i) x[i] = 32 * i + lane < NT ? qs[32 * i] : make_uint4(0, 0, 0, 0);
-                // (two slots: before a warp writes this one again, all have passed the other's barrier, and so have read this one)
-                if (++slot == 2) { slot = 0; qphase ^= 1u; }
-                const int32_t skip = kb < kb0 ? kb0 - kb : 0, blocks = kb1 - kb;
-                kb += 16;
-                if (kb >= kb1) {
-                    t += workers; kb = kb0 & ~15;
-                    if ((more = t < num_tiles)) r = tiles.at(t);
-                }
-                if (more) fetch(r, kb);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int left = blocks - 4 * j;
-                    if (left <= 0 || !ok) break;
-                    if (4 * j < skip) continue;
-                    uint32_t w[S::SF_COLS];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = aw[j];
-#pragma unroll
-                    for (int i = 0; i < 4 * S::SFB; ++i) w[4 + i] = i < R ? (j == 0 ? x[i < R ? i : 0].x : j == 1 ? x[i < R ? i : 0].y : j == 2 ? x[i < R ? i : 0].z : x[i < R ? i : 0].w) : 0u;
-                    ok = put(w, left < 4 ? left : 4);
-                }
-            }
-        }
-    } else if (warp >= 4) {
-        const int q = warp & 3, part = (warp - 4) >> 2;                // tensor-memory lane quarter this warp may read; even or odd blocks of columns
-        uint8_t *stg = gen + S::STG_OFFSET + (warp - 4) * 32 * 32 * (int)sizeof(TOUT);
-        constexpr int EPV = 16 / (int)sizeof(TOUT);                    // elements of a 16-byte piece
-        constexpr int PIECES = 32 / EPV;                               // pieces of a staged row
-        constexpr int PITCH = 32 * (int)sizeof(TOUT);
-        // 16-byte pieces of a staged row change places with the row, so that rows written by 32 lanes at once meet in no bank
-        auto swz = [](int row, int piece) { return sizeof(TOUT) == 4 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3); };
-        uint32_t iter = 0;
-        for (int32_t t = worker; t < num_tiles; t += workers, ++iter) {
-            const F8Tile r = tiles.at(t);
-            const uint32_t as = iter & 1u, aphase = (iter >> 1) & 1u;
-            const int32_t ch = r.c0 + (int32_t)rank * BM + q * 32;     // the channel of the warp's first row of tensor memory
-            const float bias = MODE != WGRAD && p.bias && ch + lane < p.N ? __ldg(p.bias + (int64_t)r.g * p.N + ch + lane) : 0.0f;
-            // the tensor-memory loads below are warp-collective: leave the loop only as a whole warp
-            if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(as), aphase, abort_flag, 46))) break;
-            tc_fence_after();
-            const uint32_t tacc = tmem_base + ((uint32_t)(q * 32) << 16) + (as ? (uint32_t)p.acc1 : 0u);
-            const int32_t nblk = ch < p.N ? (r.cols + 31) / 32 : 0;    // (warp-uniform)
-            // Blocks of columns in rising order; the first accumulator's, if its last block is shared, in falling order.
-            const bool falling = p.overlap && as == 0;
-            bool shared = p.overlap != 0;                              // not yet handed back
-            auto staged_block_read = [&]() {                           // the block before has left shared memory
-                if (lane == 0) bulk_wait_read<0>();
-                __syncwarp();
-            };
-            auto hand_back = [&](uint32_t bar) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_at_leader<CTAS>(CTAS == 2 ? map_to_cta(bar, 0) : bar);
-            };
-            const int32_t last = (nblk - 1) | 1;
-            for (int32_t i = part; i <= last; i += 2) {
-                const int32_t b = falling ? last - i : i;
-                if (b >= nblk) continue;
-                uint32_t v[32];
-                if constexpr (SPLIT) {
-                    // this CTA's sums over the operand stages, which nothing reads any more: channels next to each other
-                    tmem_ld32(tacc + (uint32_t)(b * 32), v);
-                    float *sums = reinterpret_cast<float *>(gen) + b * 32 * BM + q * 32 + lane;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (b * 32 + j < NT) sums[j * BM] = __uint_as_float(v[j]);
-                    continue;
-                }
-                if constexpr (MODE != WGRAD && sizeof(TOUT) == 2) {
-                    // Channels along lanes become channels along a row: blocks of 8 x 8 in fragments (lane 4 c + t: channel c, columns 2 t
-                    // and 2 t + 1), stored transposed.
-                    if (r.kb > 0) tmem_ld_frag(tacc + (uint32_t)(b * 32), v);
-                    if (shared) { hand_back(tempty_bar(0)); shared = false; }
-                    float bi[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) bi[i] = __shfl_sync(0xffffffffu, bias, 8 * i + (lane >> 2));
-                    staged_block_read();
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {                      // columns 8 c .. 8 c + 7
-                        uint32_t o[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {                  // channels 8 i .. 8 i + 7
-                            const int at = (i >> 1) * 16 + 4 * c + 2 * (i & 1);
-                            o[i] = r.kb > 0 ? pack2(__uint_as_float(v[at]) + bi[i], __uint_as_float(v[at + 1]) + bi[i], TOUT()) : pack2(bi[i], bi[i], TOUT());
-                        }
-                        const int row = 8 * c + (lane & 7);
-                        stmatrix_trans(smem_u32(stg + row * PITCH + swz(row, lane >> 3) * 16), o);
-                    }
-                } else {
-                    if (r.kb > 0) tmem_ld32(tacc + (uint32_t)(b * 32), v);
-                    if (shared) { hand_back(tempty_bar(0)); shared = false; }
-                    float f[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = r.kb > 0 ? __uint_as_float(v[j]) + bias : bias;
-                    staged_block_read();
-                    if (MODE == WGRAD) {
-                        // lanes are rows of the output
-#pragma unroll
-                        for (int c = 0; c < PIECES; ++c) {
-                            uint4 o;
-                            if constexpr (sizeof(TOUT) == 4)
-                                o = make_uint4(__float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]), __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
-                            else
-                                o = make_uint4(pack2(f[8 * c], f[8 * c + 1], TOUT()), pack2(f[8 * c + 2], f[8 * c + 3], TOUT()),
-                                               pack2(f[8 * c + 4], f[8 * c + 5], TOUT()), pack2(f[8 * c + 6], f[8 * c + 7], TOUT()));
-                            *reinterpret_cast<uint4 *>(stg + lane * PITCH + swz(lane, c) * 16) = o;
-                        }
-                    } else {
-                        // lanes are channels, next to each other in the output's rows
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) *reinterpret_cast<float *>(stg + j * PITCH + swz(j, lane / 4) * 16 + (lane % 4) * 4) = f[j];
-                    }
-                }
-                // the staged block: `rows` rows of `cols` elements at dst
-                const int32_t rows_left = MODE == WGRAD ? p.N - ch : r.cols - b * 32, cols_left = MODE == WGRAD ? r.cols - b * 32 : p.N - ch;
-                const int rows = rows_left < 32 ? rows_left : 32, cols = cols_left < 32 ? cols_left : 32;
-                TOUT *dst = static_cast<TOUT *>(p.out) + (MODE == WGRAD ? ((int64_t)r.g * p.N + ch) * p.ldo + r.m0 + b * 32
-                                                                        : (int64_t)(r.m0 + b * 32) * p.ldo + ch);
-                // A bulk store writes the whole block, but for what lies behind the matrix.
-                if (p.tma_out && (MODE == WGRAD ? cols == 32 || r.m0 + b * 32 + cols == p.C : rows == 32 || r.m0 + b * 32 + rows == p.M)) {
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (MODE == WGRAD) tma_store_3d(&tmap_out, r.m0 + b * 32, ch, r.g, smem_u32(stg));
-                        else tma_store_3d(&tmap_out, ch, r.m0 + b * 32, 0, smem_u32(stg));
-                        bulk_commit();
-                    }
-                    continue;
-                }
-                __syncwarp();
-                if (p.vec_out && cols == 32) {
-#pragma unroll
-                    for (int i = 0; i < PIECES; ++i) {
-                        const int row = i * (32 / PIECES) + lane / PIECES, c = lane % PIECES;
-                        const uint4 o = *reinterpret_cast<const uint4 *>(stg + row * PITCH + swz(row, c) * 16);
-                        if (row < rows) *reinterpret_cast<uint4 *>(dst + (int64_t)row * p.ldo + c * EPV) = o;
-                    }
-                } else {
-                    // rows of any alignment: lanes along the row, element by element
-                    TOUT *d = dst + lane;
-#pragma unroll
-                    for (int r0 = 0; r0 < 32; r0 += 8) {
-                        TOUT o[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            o[i] = *reinterpret_cast<const TOUT *>(stg + (r0 + i) * PITCH + swz(r0 + i, lane / EPV) * 16 + (lane % EPV) * (int)sizeof(TOUT));
-#pragma unroll
-                        for (int i = 0; i < 8; ++i, d += p.ldo)
-                            if (r0 + i < rows && lane < cols) *d = o[i];
-                    }
-                }
-            }
-            // all reads of this accumulator are done (where columns are shared: this warp has none to read, or has read them)
-            if (shared || !p.overlap) hand_back(p.overlap ? tempty_bar(0) : tempty_bar(as));
-        }
-        if (lane == 0) bulk_wait_all();                                // stores must have read shared memory before it goes away
-        __syncwarp();
-    }
-
-    __syncwarp();
-    if (*abort_flag) let_flights_land();
-    tc_fence_before();
-    if constexpr (SPLIT) {
-        // every CTA joins a part of the columns, in the order of the parts of the reduction, and stays until the others have read its sums
-        cluster_sync_all();
-        if (worker < num_tiles) {
-            const F8Tile r = tiles.at(worker);
-            const int32_t mine0 = r.cols * part_k / split, mine1 = r.cols * (part_k + 1) / split;
-            const int32_t ch = r.c0 + (warp & 3) * 32 + lane;
-            const float bias = p.bias && ch < p.N ? __ldg(p.bias + (int64_t)r.g * p.N + ch) : 0.0f;
-            for (int32_t c = mine0 + (warp >> 2); c < mine1; c += F8_THREADS / 128) {
-                const uint32_t at = base + (uint32_t)(c * BM + (warp & 3) * 32 + lane) * 4u;
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < split) v[i] = ld_peer_f32(map_to_cta(at, (uint32_t)i));
-                float sum = v[0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i)
-                    if (i < split) sum += v[i];
-                if (ch < p.N) from_float(sum + bias, static_cast<TOUT *>(p.out)[(int64_t)(r.m0 + c) * p.ldo + ch]);
-            }
-        }
-        cluster_sync_all();
-    }
-    __syncthreads();
-    if (CTAS == 2) cluster_sync_all();     // the peer no longer touches this CTA's barriers, shared or tensor memory
-    tc_fence_after();
-    if (warp == 1) tmem_dealloc<CTAS>(tmem_base, S::TMEM);
-}
-
-// ---- host --------------------------------------------------------------------------------------------------------
-
-struct F8Call {
-    const char *what;
-    const void *w; int w_type; int64_t w_rows, w_cols, ld_w, stride_w;      // as they lie in memory, `groups` of them stride_w bytes apart
-    int32_t w_count;
-    const void *x; int x_type; int64_t x_rows, x_cols, ld_x;
-};
-
-int make_map_f8(const char *what, CUtensorMap *map, const void *ptr, int dims_n, int64_t cols, int64_t rows, int64_t count, int64_t ld, int64_t stride,
-                int box_cols, int box_rows, CUtensorMapSwizzle swizzle, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_UINT8)
-{
-    EncodeTiledFn fn = encode_fn();
-    QNN_REQUIRE(fn != nullptr, QNN_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available from this driver", what);
-    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
-    cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)stride};
-    cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
-    cuuint32_t estr[3] = {1, 1, 1};
-    CUresult r = fn(map, type, (cuuint32_t)dims_n, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    QNN_REQUIRE(r == CUDA_SUCCESS, QNN_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed with code %d", what, (int)r);
-    return QNN_OK;
-}
-
-// The shared-memory opt-in is per kernel and device and costs microseconds: asked for once each.
-template <typename Kern>
-int opt_in(Kern kern, int bytes, std::atomic<bool> (&done)[64])
-{
-    int dev = 0;
-    QNN_CUDA(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64 || !done[dev].load(std::memory_order_acquire)) {
-        QNN_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
-    }
-    return QNN_OK;
-}
-
-// CTA pairs a persistent grid can keep resident at once, asked once per device (0 = pairs cannot be launched)
-int pairs_resident()
-{
-    static std::atomic<int> cached[64];                 // 0 = not asked yet; stored as pairs + 1
+    static std::atomic<int> cached[64];                 // 0 = not asked yet; stored as clusters + 1
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     int v = cached[dev].load(std::memory_order_acquire);
     if (v == 0) {
-        using S = F8Cfg<256, FORWARD, 2, __nv_bfloat16>;
-        auto kern = gemm_f8_kernel<256, FORWARD, 2, __nv_bfloat16, false>;
+        using S = F8Cfg<NT, FORWARD, CTAS, __nv_bfloat16, SPLIT>;
+        auto kern = gemm_f8_kernel<NT, FORWARD, CTAS, __nv_bfloat16, SPLIT>;
         int n = 0;
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::TOTAL) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(2 * (unsigned)sm_count());
+            cfg.gridDim = dim3(CTAS * SPLIT * S::RESIDENT * (unsigned)sm_count());
             cfg.blockDim = dim3(F8_THREADS);
             cfg.dynamicSmemBytes = S::TOTAL;
             cudaLaunchAttribute attr[1];
             attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+            attr[0].val.clusterDim.x = CTAS * SPLIT; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
             cfg.attrs = attr; cfg.numAttrs = 1;
             if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
+        } else {
+            (void)cudaGetLastError();
         }
         v = n + 1;
         cached[dev].store(v, std::memory_order_release);
     }
     return v - 1;
 }
+int parts_resident(int width, int split)
+{
+    switch (split) {
+        case 2: return width == 16 ? clusters_resident<16, 1, 2>() : clusters_resident<128, 1, 2>();
+        case 4: return width == 16 ? clusters_resident<16, 1, 4>() : clusters_resident<128, 1, 4>();
+        default: return width == 16 ? clusters_resident<16, 1, 8>() : clusters_resident<128, 1, 8>();
+    }
+}
 
-// How a product runs: columns of a tile, CTAs that share a tile (ctas: a pair, split: parts of the reduction).
-struct F8Choice {
-    int width, ctas, split, nt;
-};
-constexpr int chunk_step(int mode, int width) { return mode == WGRAD || width >= 64 ? 32 : 16; }      // (blocks of 32 columns leave as one store)
+}  // namespace
+
+int pairs_resident_f8() { return clusters_resident<256, 2, 1>(); }
 
 // len: columns of a group (tokens; weight gradient: the width of dw); groups: how many are taken to have any; rows: the tiles' other
-// dimension; nkb: blocks of the reduction.  Clocks of a launch, as measured: a block of a tile costs what its loads do (2.2 clk for each
-// of the 128 + n / ctas rows of 128 bytes that a CTA loads), or its products (2 n); the results of a tile cost 11 clk a column, under
-// the products of the next one; joining parts of a reduction costs 2500.
-F8Choice choose_f8(int mode, int64_t len, int64_t groups, int64_t rows, int64_t nkb)
+// dimension; nkb: blocks of the reduction; cut: it may be cut.  Clocks of a launch, as measured: a block of a tile costs what its loads do (2.2 clk for each
+// of the 128 + n / ctas rows of 128 bytes that a CTA loads), or its products (2 n, at least 400); the results of a tile cost 11 clk a
+// column, under the products of the next one; joining parts of a reduction costs 2500, by sends 1000.
+F8Choice choose_f8(int mode, int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut)
 {
-    static const int widths[] = {32, 64, 128, 256};
+    static const int widths[] = {16, 32, 64, 128, 256};
     F8Choice best = {0, 1, 1, 0};
     double cost = 0.0;
     for (int w : widths) {
         if (mode == WGRAD && w < 128) continue;
         const int ctas = w == 256 ? 2 : 1, step = chunk_step(mode, w);
-        const int64_t workers = ctas == 1 ? sm_count() : pairs_resident();
+        const int64_t workers = ctas == 1 ? sm_count() : pairs_resident_f8();
         if (workers < 1) continue;
         const int64_t across = ceil_div(rows, (int64_t)BM * ctas) * groups, least = ceil_div(len, w);
         for (int64_t k = least; k <= least + 3 && (k == least || ceil_div(len, k) >= step); ++k) {
             const int64_t n = (int64_t)round_up((size_t)ceil_div(len, k), (size_t)step), tiles = k * across;
-            const double load = 2.2 * (128.0 + (double)n / ctas), block = load > 2.0 * (double)n ? load : 2.0 * (double)n, drain = 11.0 * (double)n;
-            for (int split = 1; split <= (ctas == 1 && mode != WGRAD ? 8 : 1); split *= 2) {
-                if (split > 1 && (nkb < 4 * split || tiles * split > workers)) break;
+            const double load = 2.2 * (128.0 + (double)n / ctas), issue = 2.0 * (double)n > 400.0 ? 2.0 * (double)n : 400.0, block = load > issue ? load : issue, drain = 11.0 * (double)n;
+            for (int split = w == 16 ? 2 : 1; split <= (ctas == 1 && cut ? 8 : 1); split *= 2) {
+                if (split > 1 && (nkb < 4 * split || tiles > parts_resident(w, split))) break;
                 const double part = (double)ceil_div(nkb, split) * block;
-                const double t = (double)ceil_div(tiles * split, workers) * (part > drain ? part : drain) + drain + (split > 1 ? 2500.0 : 0.0) + (ctas == 2 ? 1500.0 : 0.0);
+                const double t = (double)ceil_div(tiles * split, workers) * (part > drain ? part : drain) + drain + (split == 1 ? 0.0 : w == 16 ? 1000.0 : 2500.0) + (ctas == 2 ? 1500.0 : 0.0);
                 if (best.width == 0 || t < cost) { best = {w, ctas, split, (int)n}; cost = t; }
             }
         }
@@ -924,109 +78,7 @@ F8Choice choose_f8(int mode, int64_t len, int64_t groups, int64_t rows, int64_t 
     return best;
 }
 
-template <int NT, int MODE, int CTAS, typename TOUT, bool SPLIT = false>
-int launch_f8(const F8Call &c, F8Params p, const F8Choice &how, cudaStream_t st)
-{
-    using S = F8Cfg<NT, MODE, CTAS, TOUT>;
-    auto kern = gemm_f8_kernel<NT, MODE, CTAS, TOUT, SPLIT>;
-    constexpr int STEP = chunk_step(MODE, NT);
-    static_assert(NT % STEP == 0, "a chunk is never wider than a tile");
-    p.step = STEP;
-    p.nt = how.nt;
-    p.split = how.split;
-    p.tiles_c = (int32_t)ceil_div(p.N, BM * CTAS);
-    p.overlap = 2 * p.nt > S::SF_BASE;
-    p.acc1 = p.overlap ? NT - 32 : S::SF_BASE / 32 * 16;
-    if (MODE == WGRAD) {
-        p.chunk = p.nt;
-        p.chunks = (int32_t)ceil_div(p.C, p.chunk);
-    }
-    p.super = 16;
-    const int64_t tiles = MODE == WGRAD ? (int64_t)p.groups * p.tiles_c * p.chunks : (ceil_div(p.M, p.nt) + p.groups) * p.tiles_c;
-    QNN_REQUIRE(tiles < (int64_t)1 << 28, QNN_ERR_UNSUPPORTED, "%s: too many output tiles", c.what);
-    static std::atomic<bool> done[64];
-    if (int rc = opt_in(kern, S::TOTAL, done)) return rc;
-    CUtensorMap mw{}, mx{}, mx32{}, msw{}, msx{}, mo{};
-    // (an empty reduction loads nothing: any map will do)
-    const bool empty = c.w_rows == 0 || c.w_cols == 0 || c.x_rows == 0 || c.x_cols == 0;
-    p.has_maps = !empty;
-    if (!empty) {
-        const CUtensorMapSwizzle wide = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
-        if (int rc = make_map_f8(c.what, &mw, c.w, 3, c.w_cols, c.w_rows, c.w_count, c.ld_w, c.stride_w, BKB, BM, wide)) return rc;
-        if (int rc = make_map_f8(c.what, &mx, c.x, 2, c.x_cols, c.x_rows, 1, c.ld_x, 0, BKB, 128, wide)) return rc;
-        if (int rc = make_map_f8(c.what, &mx32, c.x, 2, c.x_cols, c.x_rows, 1, c.ld_x, 0, BKB, 32, wide)) return rc;
-        if (MODE == WGRAD) {
-            if (int rc = make_map_f8(c.what, &msw, p.w_scale, 2, c.w_cols, c.w_rows / 128, 1, p.ld_ws, 0, BM, 4, none)) return rc;
-            if (int rc = make_map_f8(c.what, &msx, p.x_scale, 2, c.x_cols, c.x_rows / 128, 1, p.ld_xs, 0, NT, 4, none)) return rc;
-        }
-    }
-    {
-        // (a bulk store clips a row in 16-byte units)
-        const int64_t es = (int64_t)sizeof(TOUT), cols = MODE == WGRAD ? p.C : p.N, rows = MODE == WGRAD ? p.N : p.M, count = MODE == WGRAD ? p.groups : 1;
-        const int64_t ld = p.ldo * es, stride = count == 1 ? ld : rows * ld;
-        p.tma_out = !SPLIT && p.vec_out && cols * es % 16 == 0 && ld < (int64_t)1 << 40 && stride < (int64_t)1 << 40;
-        if (p.tma_out)
-            if (int rc = make_map_f8(c.what, &mo, p.out, 3, cols, rows, count, ld, stride, 32, 32, es == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                                     es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16)) return rc;
-    }
-    // operand types, which dimension is contiguous, scales as powers of two, rows of the tile
-    p.idesc = (uint32_t)c.w_type << 7 | (uint32_t)c.x_type << 10 | (MODE != FORWARD ? 1u : 0u) << 15 | (MODE == WGRAD ? 1u : 0u) << 16 | 1u << 23 |
-              (uint32_t)((BM * CTAS) >> 7) << 27;
-    const int64_t resident = CTAS == 2 ? pairs_resident() : sm_count();
-    const int64_t ctas = SPLIT ? tiles * how.split : CTAS * (tiles < resident ? tiles : resident);
-    const unsigned cluster = SPLIT ? (unsigned)how.split : CTAS;
-    profile_before(st);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(F8_THREADS); cfg.dynamicSmemBytes = S::TOTAL; cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    unsigned na = 0;
-    if (cluster > 1) {
-        attr[na].id = cudaLaunchAttributeClusterDimension;
-        attr[na].val.clusterDim.x = cluster; attr[na].val.clusterDim.y = 1; attr[na].val.clusterDim.z = 1;
-        ++na;
-    }
-    if (pdl_enabled()) {
-        attr[na].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[na].val.programmaticStreamSerializationAllowed = 1;
-        ++na;
-    }
-    cfg.attrs = attr; cfg.numAttrs = na;
-    QNN_CUDA(cudaLaunchKernelEx(&cfg, kern, mw, mx, mx32, msw, msx, mo, p));
-    profile_after(st);
-    return check_launch(c.what);
-}
-
-template <int MODE, typename TOUT>
-int run_f8_typed(const F8Call &c, const F8Params &p, cudaStream_t st)
-{
-    F8Choice k;
-    if constexpr (MODE == WGRAD) {
-        k = choose_f8(MODE, p.C, p.groups, p.N, ceil_div(ceil_div(p.M, p.groups), 128) + (p.M == 0));
-        return k.width == 128 ? launch_f8<128, MODE, 1, TOUT>(c, p, k, st) : launch_f8<256, MODE, 2, TOUT>(c, p, k, st);
-    } else {
-        const int64_t groups = p.groups < p.M ? p.groups : p.M;
-        k = choose_f8(MODE, ceil_div(p.M, groups), groups, p.N, p.nkb);
-        if (p.groups > 1) k.nt = k.width;              // (groups differ: their chunks are evened out one by one)
-        if (k.split > 1) return k.width == 32   ? launch_f8<32, MODE, 1, TOUT, true>(c, p, k, st)
-                                : k.width == 64 ? launch_f8<64, MODE, 1, TOUT, true>(c, p, k, st)
-                                                : launch_f8<128, MODE, 1, TOUT, true>(c, p, k, st);
-        switch (k.width) {
-            case 32: return launch_f8<32, MODE, 1, TOUT>(c, p, k, st);
-            case 64: return launch_f8<64, MODE, 1, TOUT>(c, p, k, st);
-            case 128: return launch_f8<128, MODE, 1, TOUT>(c, p, k, st);
-            default: return launch_f8<256, MODE, 2, TOUT>(c, p, k, st);
-        }
-    }
-}
-template <int MODE>
-int run_f8(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st)
-{
-    switch (out_type) {
-        case QNN_TYPE_F32: return run_f8_typed<MODE, float>(c, p, st);
-        case QNN_TYPE_BF16: return run_f8_typed<MODE, __nv_bfloat16>(c, p, st);
-        default: return run_f8_typed<MODE, __half>(c, p, st);
-    }
-}
+namespace {
 
 bool f8_type_ok(int t) { return t == QNN_F8_E4M3 || t == QNN_F8_E5M2; }
 
@@ -1073,14 +125,25 @@ int gemm_f8(const char *what, const void *a, int a_type, int64_t lda, const void
     const int64_t rows = across ? K : N, cols = across ? N : K;
     QNN_REQUIRE(K == 0 || groups == 1 || ldb <= (((int64_t)1 << 40) - 1) / rows, QNN_ERR_UNSUPPORTED, "%s: matrices of b of 2^40 bytes and more", what);
     const F8Call c = {what, b, b_type, rows, cols, ldb, groups == 1 ? ldb : rows * ldb, (int32_t)groups, a, a_type, M, K, lda};
-    return across ? run_f8<ACROSS>(c, p, out_type, as_stream(stream)) : run_f8<FORWARD>(c, p, out_type, as_stream(stream));
+    return across ? run_f8_across(c, p, out_type, as_stream(stream)) : run_f8_forward(c, p, out_type, as_stream(stream));
 }
 
 }  // namespace
 
-int gemm_f8_status(int *code)
+int run_f8_forward(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st) { return run_f8<FORWARD>(c, p, out_type, st); }
+int f8_forward_status(int *code)
 {
     QNN_CUDA(status_read_clear(code));
+    return QNN_OK;
+}
+
+int gemm_f8_status(int *code)
+{
+    int c[3] = {0, 0, 0};
+    if (int rc = f8_forward_status(&c[0])) return rc;
+    if (int rc = f8_across_status(&c[1])) return rc;
+    if (int rc = f8_wgrad_status(&c[2])) return rc;
+    *code = c[0] ? c[0] : c[1] ? c[1] : c[2];
     return QNN_OK;
 }
 
@@ -1134,7 +197,7 @@ int qnn_gemm_f8_wgrad(const void *dy, int dy_type, int64_t ld_dy, const void *dy
     p.vec_out = aligned(dw, 16) && ld_dw * type_bytes(dw_type) % 16 == 0;
     const int64_t rows = M > 0 ? 128 * (M / 128 + groups) : 0;          // rows of all blocks, at most
     const F8Call c = {what, dy, dy_type, rows, N, ld_dy, ld_dy, 1, x, x_type, rows, K, ldx};
-    return run_f8<WGRAD>(c, p, dw_type, as_stream(stream));
+    return run_f8_wgrad(c, p, dw_type, as_stream(stream));
 }
 
 }  // extern "C"
