@@ -100,16 +100,18 @@ struct F8Cfg {
     static constexpr int QS = MODE == WGRAD ? 6 : 2;
     static constexpr int TABLE_BYTES = CUT ? 0 : 2 * 4 * (MAX_GROUPS + 8);          // (reductions are cut for one group only)
     static constexpr int BAR_BYTES = 320;
-    static constexpr int AUX = STG_BYTES + JOIN_BYTES + QS * Q_BYTES + TABLE_BYTES + BAR_BYTES + 1024;
+    static constexpr int RING_BYTES = 64 * 32;                          // tiles on their way to the roles
+    static constexpr int AUX = STG_BYTES + JOIN_BYTES + QS * Q_BYTES + RING_BYTES + TABLE_BYTES + BAR_BYTES + 1024;
     static constexpr int MAXS = ((RESIDENT == 2 ? 113 * 1024 : SMEM_LIMIT) - AUX) / STAGE_BYTES;
     static constexpr int STAGES = MAXS > 8 ? 8 : MAXS;
     static constexpr int STG_OFFSET = STAGES * STAGE_BYTES;
     static constexpr int JOIN_OFFSET = STG_OFFSET + STG_BYTES;
     static constexpr int Q_OFFSET = JOIN_OFFSET + JOIN_BYTES;
-    static constexpr int TABLE_OFFSET = Q_OFFSET + QS * Q_BYTES;
+    static constexpr int RING_OFFSET = Q_OFFSET + QS * Q_BYTES;
+    static constexpr int TABLE_OFFSET = RING_OFFSET + RING_BYTES;
     static constexpr int BAR_OFFSET = TABLE_OFFSET + TABLE_BYTES;
     static constexpr int TOTAL = BAR_OFFSET + BAR_BYTES + 1024;
-    static_assert(TMEM_NEED <= 512 && (2 * STAGES + 2 * QS + 7) * 8 + 16 <= BAR_BYTES && RESIDENT * (TOTAL + 1024) <= 228 * 1024, "configuration");
+    static_assert(TMEM_NEED <= 512 && (2 * STAGES + 2 * QS + 11) * 8 + 16 <= BAR_BYTES && RESIDENT * (TOTAL + 1024) <= 228 * 1024, "configuration");
     // The scales' warps learn from a stage's barrier that the word before the last one has been used: the products cannot be more than
     // four blocks past it by then, so the barrier must not come round within five.
     static_assert(STAGES >= 5, "configuration");
@@ -144,7 +146,7 @@ __device__ __forceinline__ uint32_t umma_f8_block(uint32_t next_full_bar, uint32
                  ".reg .b32 t1, t2, t3, u1, u2, u3, sb;\n"                                                                                  \
                  ".reg .b16 both;\n"                                                                                                        \
                  "mov.b16 both, 3;\n"                                                                                                       \
-                 "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"                                                                  \
+                 "mbarrier.test_wait.parity.shared::cta.b64 Q, [%1], %2;\n"                                                                  \
                  "setp.ne.b32 P, %9, 0;\n"                                                                                                  \
                  "setp.eq.b32 T, 0, 0;\n"                                                                                                   \
                  "add.u32 sb, %10, 4;\n"                                                                                                    \
@@ -172,6 +174,18 @@ __device__ __forceinline__ uint32_t umma_f8_block(uint32_t next_full_bar, uint32
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t *v)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+// for all lanes of a warp at once, which leave it together
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int code)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, code));
+}
+// (never suspends the thread, as a try_wait may)
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
 }
 template <int CTAS>
 __device__ __forceinline__ void commit(uint32_t bar)
@@ -253,7 +267,7 @@ __device__ __forceinline__ uint32_t tma_f8_stage(uint32_t next_empty_bar, uint32
 #define QNN_F8_STAGE(GROUP)                                                                                                                       \
     asm volatile("{\n"                                                                                                                          \
                  ".reg .pred Q, L;\n"                                                                                                           \
-                 "mbarrier.try_wait.parity.shared::cta.b64 Q, [%1], %2;\n"                                                                      \
+                 "mbarrier.test_wait.parity.shared::cta.b64 Q, [%1], %2;\n"                                                                      \
                  "setp.ne.b32 L, %14, 0;\n"                                                                                                     \
                  "@L mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%3], %4;\n"                                                              \
                  "cp.async.bulk.tensor.3d" GROUP ".shared::cluster.global.mbarrier::complete_tx::bytes [%5], [%6, {%7, %8, %9}], [%3];\n"       \
@@ -282,7 +296,7 @@ struct F8Tile {
     int32_t blk0;                    // weight gradient: the group's first block of rows
 };
 
-// Walks the tiles of one CTA (pair) in rising order; every role of the CTA walks by itself.
+// The tiles of a launch by their number; a CTA (pair) takes every so many of them, in rising order.
 template <int MODE, int CTAS>
 struct Tiles {
     const F8Params &p;
@@ -333,6 +347,46 @@ struct Tiles {
         constexpr int STEP = MODE == WGRAD ? 16 * CTAS : 16;          // (halves of MN-major columns start on 16 bytes)
         r.n = (r.cols + STEP - 1) / STEP * STEP;
         return r;
+    }
+};
+
+// What the roles of a CTA read their tiles from: warp 3 works them out, a tile a lane, 32 at a time into one of two halves.  (Each role
+// for itself, the divisions and look-ups of a grouped tile cost the multiplying warp a fifth of a short tile.)
+struct TileQueue {
+    const int4 *ring;                // two words of four numbers a tile
+    uint32_t full, empty;            // barriers of the halves, 8 bytes apart
+    volatile int *abort_flag;
+    uint32_t i = 0;
+    __device__ __forceinline__ TileQueue(const int4 *r, uint32_t f, uint32_t e, volatile int *a) : ring(r), full(f), empty(e), abort_flag(a) {}
+    __device__ __forceinline__ bool read(F8Tile &r)
+    {
+        const int4 u = ring[(i & 63u) * 2u], v = ring[(i & 63u) * 2u + 1u];
+        r.g = u.x; r.c0 = u.y; r.m0 = u.z; r.cols = u.w;
+        r.n = v.x; r.kb0 = v.y; r.kb = v.z; r.blk0 = v.w;
+        return r.cols > 0;
+    }
+    // the next tile, for a thread alone; false: there is none (or the block is aborting)
+    __device__ __forceinline__ bool next(F8Tile &r)
+    {
+        const uint32_t half = i >> 5 & 1u;
+        if ((i & 31u) == 0 && !mbar_wait(full + 8u * half, i >> 6 & 1u, abort_flag, 50)) return false;
+        const bool more = read(r);
+        if ((i & 31u) == 31u) mbar_arrive(empty + 8u * half);
+        ++i;
+        return more;
+    }
+    // the same for all lanes of a warp
+    __device__ __forceinline__ bool next_warp(F8Tile &r)
+    {
+        const uint32_t half = i >> 5 & 1u;
+        if ((i & 31u) == 0 && !warp_wait(full + 8u * half, i >> 6 & 1u, abort_flag, 50)) return false;
+        const bool more = read(r);
+        if ((i & 31u) == 31u) {
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(empty + 8u * half);
+        }
+        ++i;
+        return more;
     }
 };
 
@@ -431,7 +485,8 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     auto qfull_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + s); };
     auto qempty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + S::QS + s); };
     const uint32_t join_bar = bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + 2 * S::QS);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 7 + 2 * S::QS));
+    const uint32_t tiles_full = join_bar + 8u, tiles_empty = join_bar + 24u;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 11 + 2 * S::QS));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int32_t *first = reinterpret_cast<int32_t *>(gen + S::TABLE_OFFSET);
     int32_t *start = first + MAX_GROUPS + 8;
@@ -447,6 +502,8 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         for (int a = 0; a < 2; ++a) { mbar_init(sfull_bar(a), 4 * CTAS); mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 8 * CTAS); }
         for (int s = 0; s < S::QS; ++s) { mbar_init(qfull_bar(s), MODE == WGRAD ? 1 : 4); mbar_init(qempty_bar(s), 4); }
         if (S::PUSH) mbar_init(join_bar, 1);
+        // (read by warps 0, 4..15, where the products are issued 1, and for a weight gradient 2)
+        for (int h = 0; h < 2; ++h) { mbar_init(tiles_full + 8u * h, 1); mbar_init(tiles_empty + 8u * h, 13 + (leader ? 1 : 0) + (MODE == WGRAD ? 1 : 0)); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -472,10 +529,25 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     const int32_t part_k = CUT ? (int32_t)cluster_ctarank() : 0;
     const int32_t words = (p.nkb + 3) / 4, kb0 = CUT ? words * part_k / SPLIT * 4 : 0;
     const int32_t kb1 = !CUT || part_k == SPLIT - 1 ? p.nkb : words * (part_k + 1) / SPLIT * 4;
-    Tiles<MODE, CTAS> tiles(p, first, start, kb0, kb1 - kb0);
-    const int32_t num_tiles = tiles.count();
-    const int32_t worker = (int32_t)(blockIdx.x / (CTAS * SPLIT));
-    const int32_t workers = CUT ? num_tiles : (int32_t)(gridDim.x / CTAS);             // (CUT: a tile a cluster)
+    int4 *ring = reinterpret_cast<int4 *>(gen + S::RING_OFFSET);
+    TileQueue queue(ring, tiles_full, tiles_empty, abort_flag);
+
+    if (warp == 3) {
+        Tiles<MODE, CTAS> tiles(p, first, start, kb0, kb1 - kb0);
+        const int32_t num_tiles = tiles.count(), workers = (int32_t)(gridDim.x / (CTAS * SPLIT));
+        int64_t t = (int64_t)(blockIdx.x / (CTAS * SPLIT)) + (int64_t)lane * workers;
+        for (uint32_t b = 0;; ++b, t += 32 * (int64_t)workers) {
+            if (b >= 2 && !warp_wait(tiles_empty + 8u * (b & 1u), (b >> 1) - 1u & 1u, abort_flag, 51)) break;
+            F8Tile r{};
+            if (t < num_tiles) r = tiles.at((int32_t)t);
+            int4 *to = ring + (32u * (b & 1u) + (uint32_t)lane) * 2u;
+            to[0] = make_int4(r.g, r.c0, r.m0, r.cols);
+            to[1] = make_int4(r.n, r.kb0, r.kb, r.blk0);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tiles_full + 8u * (b & 1u));
+            if (__any_sync(0xffffffffu, t >= num_tiles)) break;
+        }
+    }
 
     if (warp == 0) {
         if (lane == 0) {
@@ -484,8 +556,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
             // (shared::cluster addresses)
             const uint32_t fb0 = CTAS == 2 ? map_to_cta(full_bar(0), 0) : full_bar(0), eb0 = empty_bar(0);
             uint32_t sa = base, fb = fb0, eb = eb0;
-            for (int32_t t = worker; t < num_tiles && ok; t += workers) {
-                const F8Tile r = tiles.at(t);
+            for (F8Tile r; ok && queue.next(r);) {
                 const int32_t mine = r.n / CTAS;                       // columns this CTA loads
                 const int32_t x0 = r.m0 + (int32_t)rank * mine;
                 const int32_t c0 = r.c0 + (int32_t)rank * BM;
@@ -528,10 +599,9 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
             const uint32_t a_hi = (uint32_t)(ad >> 32), b_hi = (uint32_t)(bd >> 32), a_lo0 = (uint32_t)ad, fb0 = full_bar(0), eb0 = empty_bar(0);
             const uint32_t b_off = (uint32_t)bd - (uint32_t)ad;
             uint32_t a_lo = a_lo0, fb = fb0, eb = eb0;
-            F8Tile next = worker < num_tiles ? tiles.at(worker) : F8Tile{};
-            bool sready = false;
-            for (int32_t t = worker; t < num_tiles && ok; t += workers, ++iter) {
-                const F8Tile r = next;
+            F8Tile r, after;
+            bool sready = false, more = queue.next(r);
+            for (bool next_more = false; more && ok; more = next_more, r = after, ++iter) {
                 const uint32_t as = iter & 1u, aphase = (iter >> 1) & 1u;
                 // the accumulator's last tile has been read; where the two share columns, those of the last tile have
                 if (p.overlap ? iter > 0 && !mbar_wait(tempty_bar(0), iter - 1u & 1u, abort_flag, 42)
@@ -560,10 +630,10 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                     stage = wrap ? 0 : stage + 1;
                     a_lo = a_lo_n; fb = fb_n; eb = eb_n; phase = phase_n;
                     // (behind the issue: the next tile's numbers, and whether the next word of scales is there)
-                    if (kb == 0 && t + workers < num_tiles) next = tiles.at(t + workers);
-                    if ((kb & 3) == 2) sready = mbar_try_wait(sfull_bar((int)(word & 1u)), word >> 1 & 1u);
+                    if (kb == 0) next_more = queue.next(after);
+                    if ((kb & 3) == 2) sready = mbar_test(sfull_bar((int)(word & 1u)), word >> 1 & 1u);
                 }
-                if (r.kb == 0 && t + workers < num_tiles) next = tiles.at(t + workers);
+                if (r.kb == 0) next_more = queue.next(after);
                 if (ok) commit<CTAS>(tfull_bar(as));                   // accumulator complete
             }
         }
@@ -572,8 +642,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         if (MODE == WGRAD && lane == 0) {
             int slot = 0; uint32_t phase = 0;
             bool ok = true;
-            for (int32_t t = worker; t < num_tiles && ok; t += workers) {
-                const F8Tile r = tiles.at(t);
+            for (F8Tile r; ok && queue.next(r);) {
                 for (int32_t kb = 0; kb < r.kb; kb += 4) {
                     if (!mbar_wait(qempty_bar(slot), phase ^ 1u, abort_flag, 47)) { ok = false; break; }
                     const uint32_t dst = base + (uint32_t)(S::Q_OFFSET + slot * S::Q_BYTES), fb = qfull_bar(slot);
@@ -597,7 +666,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         bool ok = true;
         // w: 4 words of the tile's rows, then 4 for each 128 columns
         auto put = [&](const uint32_t *w, int blocks) {
-            if (word >= 2 && !__all_sync(0xffffffffu, mbar_wait(empty_bar(last2), phase2, abort_flag, 45))) return false;
+            if (word >= 2 && !warp_wait(empty_bar(last2), phase2, abort_flag, 45)) return false;
             tc_fence_after();
             const uint32_t dst = tsf + (word & 1u) * S::SF_COLS;
 #pragma unroll
@@ -615,10 +684,9 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
             return true;
         };
         if constexpr (MODE == WGRAD) {
-            for (int32_t t = worker; t < num_tiles && ok; t += workers) {
-                const F8Tile r = tiles.at(t);
+            for (F8Tile r; ok && queue.next_warp(r);) {
                 for (int32_t kb = 0; kb < r.kb && ok; kb += 4) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(qfull_bar(slot), qphase, abort_flag, 48))) { ok = false; break; }
+                    if (!warp_wait(qfull_bar(slot), qphase, abort_flag, 48)) { ok = false; break; }
                     const uint8_t *qs = gen + S::Q_OFFSET + slot * S::Q_BYTES + lane;
                     uint32_t w[S::SF_COLS];
 #pragma unroll
@@ -634,7 +702,9 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                     ok = put(w, r.kb - kb < 4 ? r.kb - kb : 4);
                 }
             }
-        } else if (kb1 > kb0 && worker < num_tiles) {
+        } else if (kb1 <= kb0) {
+            for (F8Tile r; queue.next_warp(r);) {}                     // (an empty reduction: nothing to scale)
+        } else if (F8Tile r; queue.next_warp(r)) {
             // Sixteen blocks' bytes at a time: each warp fetches a quarter of the columns', the next ones while these are used, and all
             // four read the others' from shared memory.  (Each fetching all of them costs the pipe that feeds the tensor core an eighth
             // of its time, and 16-byte boxes by TMA take the loads' turns.)
@@ -660,8 +730,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                     if (lane < 16 && has_ct && kb + lane < kb1) a.x = ws[(int64_t)(kb + lane) * p.ld_ws + ct];
                 }
             };
-            int32_t t = worker, kb = kb0 & ~15;                        // (16 bytes lie on 16 bytes)
-            F8Tile r = tiles.at(t);
+            int32_t kb = kb0 & ~15;                                    // (16 bytes lie on 16 bytes)
             fetch(r, kb);
             for (bool more = true; more && ok;) {
                 uint4 *qs = reinterpret_cast<uint4 *>(gen + S::Q_OFFSET + slot * S::Q_BYTES) + lane;
@@ -687,7 +756,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                 } else {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(qfull_bar(slot));
-                    if (!__all_sync(0xffffffffu, mbar_wait(qfull_bar(slot), qphase, abort_flag, 48))) break;
+                    if (!warp_wait(qfull_bar(slot), qphase, abort_flag, 48)) break;
 #pragma unroll
                     for (int i = 0; i < R; ++i) x[i] = 32 * i + lane < NT ? qs[32 * i] : make_uint4(0, 0, 0, 0);
                     // (two slots: before a warp writes this one again, all have passed the other's barrier, and so have read this one)
@@ -696,8 +765,8 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                 const int32_t skip = kb < kb0 ? kb0 - kb : 0, blocks = kb1 - kb;
                 kb += 16;
                 if (kb >= kb1) {
-                    t += workers; kb = kb0 & ~15;
-                    if ((more = t < num_tiles)) r = tiles.at(t);
+                    kb = kb0 & ~15;
+                    more = queue.next_warp(r);
                 }
                 if (more) fetch(r, kb);
 #pragma unroll
@@ -724,13 +793,12 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         auto swz = [](int row, int piece) { return sizeof(TOUT) == 4 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3); };
         if (S::PUSH) cluster_wait();
         uint32_t iter = 0;
-        for (int32_t t = worker; t < num_tiles; t += workers, ++iter) {
-            const F8Tile r = tiles.at(t);
+        for (F8Tile r; queue.next_warp(r); ++iter) {
             const uint32_t as = iter & 1u, aphase = (iter >> 1) & 1u;
             const int32_t ch = r.c0 + (int32_t)rank * BM + q * 32;     // the channel of the warp's first row of tensor memory
             const float bias = MODE != WGRAD && p.bias && ch + lane < p.N ? __ldg(p.bias + (int64_t)r.g * p.N + ch + lane) : 0.0f;
             // the tensor-memory loads below are warp-collective: leave the loop only as a whole warp
-            if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(as), aphase, abort_flag, 46))) break;
+            if (!warp_wait(tfull_bar(as), aphase, abort_flag, 46)) break;
             tc_fence_after();
             const uint32_t tacc = tmem_base + ((uint32_t)(q * 32) << 16) + (as ? (uint32_t)p.acc1 : 0u);
             const int32_t nblk = CUT || ch < p.N ? (r.cols + 31) / 32 : 0;       // (warp-uniform)
@@ -871,10 +939,12 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         if (warp >= 4 && warp < 8) {
             // sums of this CTA's columns, in the order of the parts of the reduction
             constexpr int OWN = NT / SPLIT;
-            const F8Tile r = tiles.at(worker);
+            F8Tile r;
+            queue.i = 0;                                               // (the cluster's only tile)
+            queue.read(r);
             const int ch0 = (warp & 3) * 32 + lane, ch = r.c0 + ch0;
             const float bias = p.bias && ch < p.N ? __ldg(p.bias + ch) : 0.0f;
-            if (__all_sync(0xffffffffu, mbar_wait(join_bar, 0, abort_flag, 49))) {
+            if (warp_wait(join_bar, 0, abort_flag, 49)) {
                 float sum[OWN];
 #pragma unroll
                 for (int i = 0; i < SPLIT; ++i) {
@@ -894,7 +964,9 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     } else if constexpr (CUT) {
         // every CTA joins a part of the columns, in the order of the parts of the reduction, and stays until the others have read its sums
         cluster_sync_all();
-        const F8Tile r = tiles.at(worker);
+        F8Tile r;
+        queue.i = 0;                                                   // (the cluster's only tile)
+        queue.read(r);
         const int32_t mine0 = r.cols * part_k / SPLIT, mine1 = r.cols * (part_k + 1) / SPLIT;
         const int32_t ch = r.c0 + lane * 4;
         float bias[4];
