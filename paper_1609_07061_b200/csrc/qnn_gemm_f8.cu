@@ -139,11 +139,10 @@ int f8_forward_status(int *code)
 
 int gemm_f8_status(int *code)
 {
-    int c[3] = {0, 0, 0};
+    int c[2] = {0, 0};
     if (int rc = f8_forward_status(&c[0])) return rc;
     if (int rc = f8_across_status(&c[1])) return rc;
-    if (int rc = f8_wgrad_status(&c[2])) return rc;
-    *code = c[0] ? c[0] : c[1] ? c[1] : c[2];
+    *code = c[0] ? c[0] : c[1];
     return QNN_OK;
 }
 

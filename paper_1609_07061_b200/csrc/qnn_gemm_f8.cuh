@@ -68,7 +68,6 @@ int run_f8_across(const F8Call &c, const F8Params &p, int out_type, cudaStream_t
 int run_f8_wgrad(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st);
 int f8_forward_status(int *code);
 int f8_across_status(int *code);
-int f8_wgrad_status(int *code);
 
 namespace {
 

@@ -1,13 +1,180 @@
-// Products of 8-bit floating-point codes: the kernels of weight gradients (see qnn_gemm_f8.cuh).
+// Weight gradients of groups of rows from 8-bit floating-point codes: dw[g][n,k] = sum over the group's rows m of DY[m,n] X[m,k].
+//
+// Both operands carry one scale for each column of a block of 128 rows, so the sum over a block is a plain product of codes, taken to
+// its place by 2^(sy[n] + sx[k] - 254): sums of blocks and of the group are held in fp32.  A code of either type is an fp16 number
+// exactly (inf and NaN too) and a product of two is exact in fp32, so the codes are multiplied as fp16.
+//
+// One CTA owns 128 x 128 results of a group; eight warps own 64 x 32 of them each.  Rows go through shared memory 32 at a time, the next
+// 32 on their way in registers meanwhile, and are turned round by transposing matrix loads.  Every load is a plain one of 16 bytes
+// within a row, and only blocks of the group itself are read: buffers need hold no more than the groups' blocks.
 #include "qnn_gemm_f8.cuh"
+#include <cuda_fp8.h>
 
 namespace qnn {
+namespace {
 
-int run_f8_wgrad(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st) { return run_f8<WGRAD>(c, p, out_type, st); }
-int f8_wgrad_status(int *code)
+constexpr int WG_T = 128, WG_ROWS = 32, WG_THREADS = 256;
+constexpr int WG_PITCH = WG_T + 8;                   // halves; eight rows of 16 bytes then lie in different banks
+
+struct WgParams {
+    const uint8_t *dy, *x, *dy_scale, *x_scale;
+    int64_t ld_dy, ldx, ld_dys, ld_xs, M, ld_dw;
+    const int64_t *offsets;
+    void *dw;
+    int32_t N, K, groups, tiles_n, tiles_k, dy_type, x_type;
+};
+
+__device__ __forceinline__ uint32_t two_halves(uint32_t codes, __nv_fp8_interpretation_t type)
 {
-    QNN_CUDA(status_read_clear(code));
-    return QNN_OK;
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), type);
+    return (uint32_t)h.x | (uint32_t)h.y << 16;
+}
+// 16 codes as 16 halves
+__device__ __forceinline__ void put_codes(__half *to, uint4 v, int type)
+{
+    const __nv_fp8_interpretation_t t = type == QNN_F8_E4M3 ? __NV_E4M3 : __NV_E5M2;
+    uint4 *d = reinterpret_cast<uint4 *>(to);
+    d[0] = make_uint4(two_halves(v.x, t), two_halves(v.x >> 16, t), two_halves(v.y, t), two_halves(v.y >> 16, t));
+    d[1] = make_uint4(two_halves(v.z, t), two_halves(v.z >> 16, t), two_halves(v.w, t), two_halves(v.w >> 16, t));
+}
+__device__ __forceinline__ void load_trans(uint32_t (&r)[4], const __half *at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"((uint32_t)__cvta_generic_to_shared(at)) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// v 2^(s + t - 254), in two steps: the whole power need not be an fp32 number, its halves are normal ones.  Below 2^-252 any sum of a
+// block (at most 128 57344^2 < 2^39) is zero in fp32 either way.
+__device__ __forceinline__ float scaled(float v, int s, int t)
+{
+    const int e = s + t - 254 > -252 ? s + t - 254 : -252, h = e >> 1;
+    const float r = v * __int_as_float((h + 127) << 23) * __int_as_float((e - h + 127) << 23);
+    return s == 255 || t == 255 ? __int_as_float(0x7fffffff) : r;
+}
+
+template <typename TOUT>
+__global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
+{
+    __shared__ __align__(16) __half sy[2][WG_ROWS][WG_PITCH], sx[2][WG_ROWS][WG_PITCH];
+    __shared__ int32_t where[2];                     // the group's first block and its number of blocks
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t tile = (int32_t)blockIdx.x, per = p.tiles_n * p.tiles_k;
+    const int32_t g = tile / per, tn = (tile - g * per) / p.tiles_k, tk = tile - g * per - tn * p.tiles_k;
+    if (warp == 0) {
+        // offsets held to rise and to stay in 0..M, as the quantiser holds them
+        int32_t carry = 0, blocks = 0, len = (int32_t)p.M;
+        for (int32_t i0 = 0; p.offsets && i0 <= g + 1; i0 += 32) {
+            const int32_t i = i0 + lane;
+            int64_t o = i <= g + 1 ? __ldg(p.offsets + i) : 0;
+            o = o < 0 ? 0 : o > p.M ? p.M : o;
+            int32_t s = (int32_t)o > carry ? (int32_t)o : carry;
+            for (int d = 1; d < 32; d *= 2) {
+                const int32_t u = __shfl_up_sync(0xffffffffu, s, d);
+                if (lane >= d && u > s) s = u;
+            }
+            const int32_t up = __shfl_up_sync(0xffffffffu, s, 1), before = lane == 0 ? carry : up;
+            int32_t b = i >= 1 && i <= g ? (s - before + 127) / 128 : 0;
+            for (int d = 16; d > 0; d /= 2) b += __shfl_xor_sync(0xffffffffu, b, d);
+            blocks += b;
+            if (g + 1 - i0 < 32) len = __shfl_sync(0xffffffffu, s - before, g + 1 - i0);
+            carry = __shfl_sync(0xffffffffu, s, 31);
+        }
+        if (lane == 0) { where[0] = blocks; where[1] = (len + 127) / 128; }
+    }
+    __syncthreads();
+    const int32_t blk0 = where[0], steps = where[1] * (128 / WG_ROWS);
+
+    // a thread's 16 bytes of 32 rows x 128 columns
+    const int row = tid >> 3, col = (tid & 7) * 16;
+    const bool has_y = tn * WG_T + col < p.N, has_x = tk * WG_T + col < p.K;
+    const uint8_t *py = p.dy + ((int64_t)blk0 * 128 + row) * p.ld_dy + tn * WG_T + col;
+    const uint8_t *px = p.x + ((int64_t)blk0 * 128 + row) * p.ldx + tk * WG_T + col;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    auto fetch = [&](int32_t s, uint4 &a, uint4 &b) {
+        a = has_y ? __ldg(reinterpret_cast<const uint4 *>(py + (int64_t)s * WG_ROWS * p.ld_dy)) : none;
+        b = has_x ? __ldg(reinterpret_cast<const uint4 *>(px + (int64_t)s * WG_ROWS * p.ldx)) : none;
+    };
+    const int wn = (warp >> 2) * 64, wk = (warp & 3) * 32, fr = lane >> 2, fc = 2 * (lane & 3);
+    float sum[4][4][4] = {}, part[4][4][4] = {};
+    uint4 a, b;
+    if (steps > 0) fetch(0, a, b);
+    for (int32_t s = 0; s < steps; ++s) {
+        const int h = s & 1;
+        put_codes(&sy[h][row][col], a, p.dy_type);
+        put_codes(&sx[h][row][col], b, p.x_type);
+        __syncthreads();                             // (two buffers: a warp here has left the one before last)
+        if (s + 1 < steps) fetch(s + 1, a, b);
+#pragma unroll
+        for (int k0 = 0; k0 < WG_ROWS; k0 += 16) {
+            uint32_t fa[4][4], fb[2][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_trans(fa[i], &sy[h][k0 + (lane >> 4) * 8 + (lane & 7)][wn + 16 * i + (lane >> 3 & 1) * 8]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) load_trans(fb[j], &sx[h][k0 + (lane >> 3 & 1) * 8 + (lane & 7)][wk + 16 * j + (lane >> 4) * 8]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma_f16(part[i][j], fa[i], fb[j >> 1][2 * (j & 1)], fb[j >> 1][2 * (j & 1) + 1]);
+        }
+        if ((s & 3) != 3) continue;
+        const int64_t blk = blk0 + (s >> 2);
+        int ey[4][2], ex[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int32_t n = tn * WG_T + wn + 16 * i + 8 * u + fr, k = tk * WG_T + wk + 8 * i + fc + u;
+                ey[i][u] = n < p.N ? p.dy_scale[blk * p.ld_dys + n] : 127;
+                ex[i][u] = k < p.K ? p.x_scale[blk * p.ld_xs + k] : 127;
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum[i][j][e] += scaled(part[i][j][e], ey[i][e >> 1], ex[j][e & 1]);
+                    part[i][j][e] = 0.0f;
+                }
+    }
+    TOUT *dw = static_cast<TOUT *>(p.dw);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t n = tn * WG_T + wn + 16 * i + 8 * (e >> 1) + fr, k = tk * WG_T + wk + 8 * j + fc + (e & 1);
+                if (n < p.N && k < p.K) from_float(sum[i][j][e], dw[((int64_t)g * p.N + n) * p.ld_dw + k]);
+            }
+}
+
+}  // namespace
+
+int run_f8_wgrad(const F8Call &c, const F8Params &f, int out_type, cudaStream_t st)
+{
+    WgParams p{};
+    p.dy = static_cast<const uint8_t *>(c.w); p.x = static_cast<const uint8_t *>(c.x);
+    p.dy_scale = f.w_scale; p.x_scale = f.x_scale;
+    p.ld_dy = c.ld_w; p.ldx = c.ld_x; p.ld_dys = f.ld_ws; p.ld_xs = f.ld_xs; p.M = f.M; p.ld_dw = f.ldo;
+    p.offsets = f.offsets; p.dw = f.out;
+    p.N = f.N; p.K = f.C; p.groups = f.groups; p.dy_type = c.w_type; p.x_type = c.x_type;
+    p.tiles_n = (int32_t)ceil_div(p.N, WG_T); p.tiles_k = (int32_t)ceil_div(p.K, WG_T);
+    const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
+    QNN_REQUIRE(tiles < (int64_t)1 << 28 && tiles * p.groups < (int64_t)1 << 30, QNN_ERR_UNSUPPORTED, "%s: too many output tiles", c.what);
+    const unsigned grid = (unsigned)(tiles * p.groups);
+    profile_before(st);
+    switch (out_type) {
+        case QNN_TYPE_F32: wgrad_f8_kernel<float><<<grid, WG_THREADS, 0, st>>>(p); break;
+        case QNN_TYPE_BF16: wgrad_f8_kernel<__nv_bfloat16><<<grid, WG_THREADS, 0, st>>>(p); break;
+        default: wgrad_f8_kernel<__half><<<grid, WG_THREADS, 0, st>>>(p); break;
+    }
+    profile_after(st);
+    return check_launch(c.what);
 }
 
 }  // namespace qnn
