@@ -49,18 +49,17 @@ int parts_resident(int width, int split)
 
 int pairs_resident_f8() { return clusters_resident<256, 2, 1>(); }
 
-// len: columns of a group (tokens; weight gradient: the width of dw); groups: how many are taken to have any; rows: the tiles' other
+// len: tokens of a group; groups: how many are taken to have any; rows: the tiles' other
 // dimension; nkb: blocks of the reduction; cut: it may be cut.  Clocks of a launch, as measured: a block of a tile costs what its loads do (2.2 clk for each
 // of the 128 + n / ctas rows of 128 bytes that a CTA loads), or its products (2 n, at least 400); the results of a tile cost 11 clk a
 // column, under the products of the next one; joining parts of a reduction costs 2500, by sends 1000.
-F8Choice choose_f8(int mode, int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut)
+F8Choice choose_f8(int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut)
 {
     static const int widths[] = {16, 32, 64, 128, 256};
     F8Choice best = {0, 1, 1, 0};
     double cost = 0.0;
     for (int w : widths) {
-        if (mode == WGRAD && w < 128) continue;
-        const int ctas = w == 256 ? 2 : 1, step = chunk_step(mode, w);
+        const int ctas = w == 256 ? 2 : 1, step = chunk_step(w);
         const int64_t workers = ctas == 1 ? sm_count() : pairs_resident_f8();
         if (workers < 1) continue;
         const int64_t across = ceil_div(rows, (int64_t)BM * ctas) * groups, least = ceil_div(len, w);

@@ -1,16 +1,15 @@
 // Products of 8-bit floating-point codes (e4m3, e5m2) with a power-of-two scale for each block of 128 along the reduction:
 //   out[m, n]   = sum_k a[m,k] sa[m, k/128] b[g][n,k] sb[g][n/128, k/128] + bias[g][n]        rows m of group g (forward)
 //   out[m, n]   = sum_k a[m,k] sa[m, k/128] b[g][k,n] sb[g][k/128, n/128]                      the same weights read across (input gradient)
-//   dw[g][n, k] = sum_m y[m,n] sy[m/128, n] x[m,k] sx[m/128, k]                                rows m of group g (weight gradient)
 // The dense product is the grouped one with a single group.
 //
 // The tensor cores apply the scales themselves (tcgen05 kind::mxf8f6f4 with block scales: one byte for 32 elements, here the same
 // byte for the four steps of a block), so partial sums never leave tensor memory before a tile is done.
 //
-// One persistent kernel.  The weights (in a weight gradient: the output's rows) are the tile's 128 rows, the tokens its
+// One persistent kernel.  The weights are the tile's 128 rows, the tokens its
 // columns: their number is given to the instruction at run time, so a group of 37 rows costs 48 columns and not a tile.  Weights read
-// across, and both operands of a weight gradient, are taken as they lie in memory: the tensor core reads them MN-major.
-// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 2 loads scales, warps 4..11 store the previous tile,
+// across are taken as they lie in memory: the tensor core reads them MN-major.
+// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 3 works out the tiles, warps 4..11 store the previous one,
 // warps 12..15 put the scales into tensor memory.  All waits are bounded.
 #pragma once
 #include <cuda.h>
@@ -20,11 +19,11 @@
 
 namespace qnn {
 
-enum F8Mode { FORWARD = 0, ACROSS = 1, WGRAD = 2 };
+enum F8Mode { FORWARD = 0, ACROSS = 1 };
 
 struct F8Params {
     int64_t M;                       // rows of a (tokens) of all groups; offsets are held to 0..M
-    int32_t N;                       // channels: rows of the tile's operand (forward: n, across: n, weight gradient: n)
+    int32_t N;                       // channels: rows of the tile's operand
     int32_t C;                       // weight gradient: columns (k)
     int32_t nkb;                     // blocks of the reduction (forward, across)
     int32_t groups;
@@ -41,7 +40,7 @@ struct F8Params {
     int32_t step;                    // ... a multiple of this many, but for the last ones
     int32_t acc1;                    // tensor-memory column of the second accumulator
     int32_t overlap;                 // 1: its first 32 columns are the first one's last
-    int32_t chunks, chunk;           // chunks of columns and columns of each: weight gradient, or one group of all rows (offsets NULL)
+    int32_t chunks, chunk;           // chunks of tokens and tokens of each: one group of all rows (offsets NULL)
     int32_t super;                   // chunks of tokens that go through all channels before the next ones
     uint32_t idesc;                  // without N and the scales' byte
 };
@@ -57,10 +56,10 @@ struct F8Call {
 struct F8Choice {
     int width, ctas, split, nt;
 };
-constexpr int chunk_step(int mode, int width) { return mode == WGRAD || width >= 64 ? 32 : 16; }      // (blocks of 32 columns leave as one store)
+constexpr int chunk_step(int width) { return width >= 64 ? 32 : 16; }      // (blocks of 32 columns leave as one store)
 
 // (see qnn_gemm_f8.cu)
-F8Choice choose_f8(int mode, int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut);
+F8Choice choose_f8(int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut);
 int pairs_resident_f8();
 // one translation unit each; the status word of its waits: reads and clears it
 int run_f8_forward(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st);
@@ -93,10 +92,9 @@ struct F8Cfg {
     static constexpr int SF_BASE = NT == 256 ? 512 - 2 * SF_COLS : 2 * NT;
     static constexpr int TMEM_NEED = SF_BASE + 2 * SF_COLS;
     static constexpr int TMEM = TMEM_NEED <= 64 ? 64 : TMEM_NEED <= 128 ? 128 : TMEM_NEED <= 256 ? 256 : 512;
-    // Scales on their way: 16 blocks' bytes of every column, handed from warp to warp, or (weight gradient) four blocks' of every row and
-    // column, by TMA.
-    static constexpr int Q_BYTES = (MODE == WGRAD ? 4 * (BM + NT) + 127 : 16 * NT + 127) / 128 * 128;
-    static constexpr int QS = MODE == WGRAD ? 6 : 2;
+    // Scales on their way: 16 blocks' bytes of every column, handed from warp to warp.
+    static constexpr int Q_BYTES = (16 * NT + 127) / 128 * 128;
+    static constexpr int QS = 2;
     static constexpr int TABLE_BYTES = CUT ? 0 : 2 * 4 * (MAX_GROUPS + 8);          // (reductions are cut for one group only)
     static constexpr int BAR_BYTES = 320;
     static constexpr int RING_BYTES = 64 * 32;                          // tiles on their way to the roles
@@ -288,19 +286,18 @@ __device__ __forceinline__ uint32_t tma_f8_stage(uint32_t next_empty_bar, uint32
 struct F8Tile {
     int32_t g;                       // group
     int32_t c0;                      // first channel (of the pair)
-    int32_t m0;                      // first token; weight gradient: first column
+    int32_t m0;                      // first token
     int32_t cols;                    // columns with a result
     int32_t n;                       // columns multiplied: rounded up to what the instruction takes
     int32_t kb0, kb;                 // blocks of the reduction: the first one and how many
-    int32_t blk0;                    // weight gradient: the group's first block of rows
 };
 
 // The tiles of a launch by their number; a CTA (pair) takes every so many of them, in rising order.
 template <int MODE, int CTAS>
 struct Tiles {
     const F8Params &p;
-    const int32_t *first, *start;    // [groups + 1] first tile / (forward, across) first row or (weight gradient) first block
-    const int32_t kb0, kb;           // (forward, across) this CTA's part of the reduction
+    const int32_t *first, *start;    // [groups + 1] first tile / first row
+    const int32_t kb0, kb;           // this CTA's part of the reduction
     int32_t g = 0;
     __device__ __forceinline__ Tiles(const F8Params &p_, const int32_t *f, const int32_t *s, int32_t k0, int32_t k) : p(p_), first(f), start(s), kb0(k0), kb(k) {}
     // (without offsets there is one group of all rows, and nothing to look up)
@@ -308,43 +305,31 @@ struct Tiles {
     __device__ __forceinline__ F8Tile at(int32_t t)
     {
         F8Tile r;
-        int32_t i = t, s0 = 0, s1 = MODE == WGRAD ? (int32_t)((p.M + 127) / 128) : (int32_t)p.M;
+        int32_t i = t, s0 = 0, s1 = (int32_t)p.M;
         if (p.offsets) {
             while (t >= first[g + 1]) ++g;
             i -= first[g];
             s0 = start[g]; s1 = start[g + 1];
         }
         r.g = g;
-        if (MODE == WGRAD) {
-            const int32_t c = i / p.chunks, ch = i - c * p.chunks;
-            r.c0 = c * BM * CTAS;
-            r.m0 = ch * p.chunk;
-            r.cols = p.C - r.m0 < p.chunk ? p.C - r.m0 : p.chunk;
-            r.blk0 = s0;
-            r.kb0 = 0;
-            r.kb = s1 - s0;
-        } else {
-            const int32_t len = s1 - s0;
-            int32_t chunks = p.chunks, csize = p.chunk;
-            if (p.offsets) {
-                chunks = (len + p.nt - 1) / p.nt;
-                csize = ((len + chunks - 1) / chunks + p.step - 1) / p.step * p.step;
-            }
-            // (p.super chunks go through all channels before the next ones)
-            const int32_t sup = chunks > p.super ? i / (p.super * p.tiles_c) : 0;
-            const int32_t j = i - sup * p.super * p.tiles_c;
-            const int32_t wide = chunks - sup * p.super < p.super ? chunks - sup * p.super : p.super;
-            const int32_t c = wide == 1 ? j : j / wide;
-            const int32_t ch = sup * p.super + (j - c * wide);
-            r.c0 = c * BM * CTAS;
-            r.m0 = s0 + ch * csize;
-            r.cols = s1 - r.m0 < csize ? s1 - r.m0 : csize;
-            r.kb0 = kb0;
-            r.kb = kb;
-            r.blk0 = 0;
+        const int32_t len = s1 - s0;
+        int32_t chunks = p.chunks, csize = p.chunk;
+        if (p.offsets) {
+            chunks = (len + p.nt - 1) / p.nt;
+            csize = ((len + chunks - 1) / chunks + p.step - 1) / p.step * p.step;
         }
-        constexpr int STEP = MODE == WGRAD ? 16 * CTAS : 16;          // (halves of MN-major columns start on 16 bytes)
-        r.n = (r.cols + STEP - 1) / STEP * STEP;
+        // (p.super chunks go through all channels before the next ones)
+        const int32_t sup = chunks > p.super ? i / (p.super * p.tiles_c) : 0;
+        const int32_t j = i - sup * p.super * p.tiles_c;
+        const int32_t wide = chunks - sup * p.super < p.super ? chunks - sup * p.super : p.super;
+        const int32_t c = wide == 1 ? j : j / wide;
+        const int32_t ch = sup * p.super + (j - c * wide);
+        r.c0 = c * BM * CTAS;
+        r.m0 = s0 + ch * csize;
+        r.cols = s1 - r.m0 < csize ? s1 - r.m0 : csize;
+        r.kb0 = kb0;
+        r.kb = kb;
+        r.n = (r.cols + 15) / 16 * 16;
         return r;
     }
 };
@@ -361,7 +346,7 @@ struct TileQueue {
     {
         const int4 u = ring[(i & 63u) * 2u], v = ring[(i & 63u) * 2u + 1u];
         r.g = u.x; r.c0 = u.y; r.m0 = u.z; r.cols = u.w;
-        r.n = v.x; r.kb0 = v.y; r.kb = v.z; r.blk0 = v.w;
+        r.n = v.x; r.kb0 = v.y; r.kb = v.z;
         return r.cols > 0;
     }
     // the next tile, for a thread alone; false: there is none (or the block is aborting)
@@ -428,32 +413,30 @@ __device__ void fill_tables(const F8Params &p, int32_t *first, int32_t *start, i
         if (g <= G) start[g] = o[i] > before ? o[i] : before;
     }
     __syncthreads();
-    // tiles (and blocks) of each group, added up
-    int32_t tl[PER], bl[PER], tsum = 0, bsum = 0;
+    // tiles of each group, added up
+    int32_t tl[PER], tsum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int g = tid * PER + i;
         const int32_t len = g < G ? start[g + 1] - start[g] : 0;
-        tl[i] = tsum; bl[i] = bsum;
-        bsum += (len + 127) / 128;
-        if (g < G) tsum += MODE == WGRAD ? p.tiles_c * p.chunks : (len + p.nt - 1) / p.nt * p.tiles_c;
+        tl[i] = tsum;
+        if (g < G) tsum += (len + p.nt - 1) / p.nt * p.tiles_c;
     }
-    int32_t trun = tsum, brun = bsum;
+    int32_t trun = tsum;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const int32_t v = __shfl_up_sync(0xffffffffu, trun, d), u = __shfl_up_sync(0xffffffffu, brun, d);
-        if (lane >= d) { trun += v; brun += u; }
+        const int32_t v = __shfl_up_sync(0xffffffffu, trun, d);
+        if (lane >= d) trun += v;
     }
-    if (lane == 31) { scratch[W + warp] = trun; scratch[2 * W + warp] = brun; }
+    if (lane == 31) scratch[W + warp] = trun;
     __syncthreads();
-    trun -= tsum; brun -= bsum;
-    for (int w = 0; w < warp; ++w) { trun += scratch[W + w]; brun += scratch[2 * W + w]; }
+    trun -= tsum;
+    for (int w = 0; w < warp; ++w) trun += scratch[W + w];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int g = tid * PER + i;
         if (g <= G) {
             first[g] = trun + tl[i];
-            if (MODE == WGRAD) start[g] = brun + bl[i];
         }
     }
     __syncthreads();
@@ -465,12 +448,12 @@ __device__ void fill_tables(const F8Params &p, int32_t *first, int32_t *start, i
 template <int NT, int MODE, int CTAS, typename TOUT, int SPLIT>
 __global__ void __launch_bounds__(F8_THREADS, F8Cfg<NT, MODE, CTAS, TOUT, SPLIT>::RESIDENT)
 gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_x32,
-               const __grid_constant__ CUtensorMap tmap_sw, const __grid_constant__ CUtensorMap tmap_sx, const __grid_constant__ CUtensorMap tmap_out,
+               const __grid_constant__ CUtensorMap tmap_out,
                const F8Params p)
 {
     using S = F8Cfg<NT, MODE, CTAS, TOUT, SPLIT>;
     constexpr bool CUT = S::CUT;
-    static_assert(!CUT || (CTAS == 1 && MODE != WGRAD && S::STAGES * S::STAGE_BYTES >= NT * BM * 4), "the partial sums reuse the stages");
+    static_assert(!CUT || (CTAS == 1 && S::STAGES * S::STAGE_BYTES >= NT * BM * 4), "the partial sums reuse the stages");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;                      // swizzled tiles need 1024-byte alignment
@@ -499,10 +482,10 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(sfull_bar(a), 4 * CTAS); mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 8 * CTAS); }
-        for (int s = 0; s < S::QS; ++s) { mbar_init(qfull_bar(s), MODE == WGRAD ? 1 : 4); mbar_init(qempty_bar(s), 4); }
+        for (int s = 0; s < S::QS; ++s) { mbar_init(qfull_bar(s), 4); mbar_init(qempty_bar(s), 4); }
         if (S::PUSH) mbar_init(join_bar, 1);
-        // (read by warps 0, 4..15, where the products are issued 1, and for a weight gradient 2)
-        for (int h = 0; h < 2; ++h) { mbar_init(tiles_full + 8u * h, 1); mbar_init(tiles_empty + 8u * h, 13 + (leader ? 1 : 0) + (MODE == WGRAD ? 1 : 0)); }
+        // (read by warps 0, 4..15, and 1 where the products are issued)
+        for (int h = 0; h < 2; ++h) { mbar_init(tiles_full + 8u * h, 1); mbar_init(tiles_empty + 8u * h, 13 + (leader ? 1 : 0)); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -541,7 +524,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
             if (t < num_tiles) r = tiles.at((int32_t)t);
             int4 *to = ring + (32u * (b & 1u) + (uint32_t)lane) * 2u;
             to[0] = make_int4(r.g, r.c0, r.m0, r.cols);
-            to[1] = make_int4(r.n, r.kb0, r.kb, r.blk0);
+            to[1] = make_int4(r.n, r.kb0, r.kb, 0);
             __syncwarp();
             if (lane == 0) mbar_arrive(tiles_full + 8u * (b & 1u));
             if (__any_sync(0xffffffffu, t >= num_tiles)) break;
@@ -559,14 +542,14 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                 const int32_t mine = r.n / CTAS;                       // columns this CTA loads
                 const int32_t x0 = r.m0 + (int32_t)rank * mine;
                 const int32_t c0 = r.c0 + (int32_t)rank * BM;
-                // K-major: boxes of 128 rows, the rest in boxes of 32; MN-major: boxes of 128 columns
+                // boxes of 128 rows, the rest in boxes of 32
                 const int32_t n32 = (mine + 31) / 32;
-                const int32_t big = MODE == WGRAD ? (mine + 127) / 128 : S::BROWS >= 128 ? n32 / 4 + (n32 % 4 == 3 ? 1 : 0) : 0;
-                const int32_t small = MODE == WGRAD || n32 <= 4 * big ? 0 : n32 - 4 * big;
+                const int32_t big = S::BROWS >= 128 ? n32 / 4 + (n32 % 4 == 3 ? 1 : 0) : 0;
+                const int32_t small = n32 <= 4 * big ? 0 : n32 - 4 * big;
                 const int32_t boxes = big + small;
                 const uint32_t bytes = (uint32_t)(S::A_BYTES + big * 128 * BKB + small * 32 * BKB) * CTAS;
                 const CUtensorMap *map0 = big > 0 ? &tmap_x : &tmap_x32;
-                int32_t k = MODE == WGRAD ? r.blk0 * BKB : r.kb0 * BKB;           // along the reduction
+                int32_t k = r.kb0 * BKB;           // along the reduction
 #pragma unroll 1
                 for (int32_t kb = 0; kb < r.kb; ++kb, k += BKB) {
                     if (!ready && !mbar_wait(eb, phase ^ 1u, abort_flag, 41)) { ok = false; break; }
@@ -576,11 +559,10 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                     const uint32_t phase_n = wrap ? phase ^ 1u : phase;
                     const uint32_t sb = sa + S::A_BYTES;
                     ready = tma_f8_stage<CTAS>(eb_n, phase_n ^ 1u, fb, bytes, (uint32_t)leader, sa, &tmap_w, MODE == FORWARD ? k : c0, MODE == FORWARD ? c0 : k,
-                                               MODE == WGRAD ? 0 : r.g, sb, map0, MODE == WGRAD ? x0 : k, MODE == WGRAD ? k : x0) != 0;
+                                               r.g, sb, map0, k, x0) != 0;
                     for (int32_t i = 1; i < boxes; ++i) {
                         const int32_t at = i < big ? i * 128 : big * 128 + (i - big) * 32;
-                        if (MODE == WGRAD) tma_load_2d<CTAS>(sb + (uint32_t)(at * BKB), &tmap_x, x0 + at, k, fb);
-                        else tma_load_2d<CTAS>(sb + (uint32_t)(at * BKB), i < big ? &tmap_x : &tmap_x32, k, x0 + at, fb);
+                        tma_load_2d<CTAS>(sb + (uint32_t)(at * BKB), i < big ? &tmap_x : &tmap_x32, k, x0 + at, fb);
                     }
                     stage = wrap ? 0 : stage + 1;
                     sa = sa_n; fb = fb_n; eb = eb_n; phase = phase_n;
@@ -592,9 +574,9 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
             int stage = 0; uint32_t phase = 0, word = 0, iter = 0;
             bool ok = true, ready = false;
             // a step of 32 along the reduction: 32 bytes of a K-major row, 32 rows of an MN-major tile
-            constexpr uint32_t A_STEP = MODE == FORWARD ? 2 : (32 * BKB) >> 4, B_STEP = MODE == WGRAD ? (32 * BKB) >> 4 : 2;
+            constexpr uint32_t A_STEP = MODE == FORWARD ? 2 : (32 * BKB) >> 4, B_STEP = 2;
             const uint64_t ad = MODE == FORWARD ? make_kmajor_desc<BKB>(base) : make_across_desc(base);
-            const uint64_t bd = MODE == WGRAD ? make_across_desc(base + S::A_BYTES) : make_kmajor_desc<BKB>(base + S::A_BYTES);
+            const uint64_t bd = make_kmajor_desc<BKB>(base + S::A_BYTES);
             const uint32_t a_hi = (uint32_t)(ad >> 32), b_hi = (uint32_t)(bd >> 32), a_lo0 = (uint32_t)ad, fb0 = full_bar(0), eb0 = empty_bar(0);
             const uint32_t b_off = (uint32_t)bd - (uint32_t)ad;
             uint32_t a_lo = a_lo0, fb = fb0, eb = eb0;
@@ -636,22 +618,6 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                 if (ok) commit<CTAS>(tfull_bar(as));                   // accumulator complete
             }
         }
-    } else if (warp == 2) {
-        // weight gradient: scales into shared memory, well ahead of their use
-        if (MODE == WGRAD && lane == 0) {
-            int slot = 0; uint32_t phase = 0;
-            bool ok = true;
-            for (F8Tile r; ok && queue.next(r);) {
-                for (int32_t kb = 0; kb < r.kb; kb += 4) {
-                    if (!mbar_wait(qempty_bar(slot), phase ^ 1u, abort_flag, 47)) { ok = false; break; }
-                    const uint32_t dst = base + (uint32_t)(S::Q_OFFSET + slot * S::Q_BYTES), fb = qfull_bar(slot);
-                    expect_tx(fb, 4 * (BM + NT));
-                    tma_load_2d<1>(dst, &tmap_sw, r.c0 + (int32_t)rank * BM, r.blk0 + kb, fb);
-                    tma_load_2d<1>(dst + 4 * BM, &tmap_sx, r.m0, r.blk0 + kb, fb);
-                    if (++slot == S::QS) { slot = 0; phase ^= 1u; }
-                }
-            }
-        }
     } else if (warp >= 12) {
         // Scales: a word holds four blocks' bytes of a row; word r of a piece of 128 rows goes to lane r % 32 of column r / 32, the same in
         // each quarter of the lanes, one warp a quarter.  Two words have room.  A word's room is free when the products of the word before
@@ -682,26 +648,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
             if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
             return true;
         };
-        if constexpr (MODE == WGRAD) {
-            for (F8Tile r; ok && queue.next_warp(r);) {
-                for (int32_t kb = 0; kb < r.kb && ok; kb += 4) {
-                    if (!warp_wait(qfull_bar(slot), qphase, abort_flag, 48)) { ok = false; break; }
-                    const uint8_t *qs = gen + S::Q_OFFSET + slot * S::Q_BYTES + lane;
-                    uint32_t w[S::SF_COLS];
-#pragma unroll
-                    for (int i = 0; i < S::SF_COLS; ++i) {
-                        // (bytes of blocks behind the group's, and of rows and columns behind the last, are multiplied with nothing)
-                        const uint8_t *b = i < 4 ? qs + 32 * i : qs + 4 * BM + 32 * (i - 4);
-                        const int pitch = i < 4 ? BM : NT;
-                        w[i] = i < 4 || 32 * (i - 4) < NT ? (uint32_t)b[0] | (uint32_t)b[pitch] << 8 | (uint32_t)b[2 * pitch] << 16 | (uint32_t)b[3 * pitch] << 24 : 0u;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(qempty_bar(slot));
-                    if (++slot == S::QS) { slot = 0; qphase ^= 1u; }
-                    ok = put(w, r.kb - kb < 4 ? r.kb - kb : 4);
-                }
-            }
-        } else if (kb1 <= kb0) {
+        if (kb1 <= kb0) {
             for (F8Tile r; queue.next_warp(r);) {}                     // (an empty reduction: nothing to scale)
         } else if (F8Tile r; queue.next_warp(r)) {
             // Sixteen blocks' bytes at a time: each warp fetches a quarter of the columns', the next ones while these are used, and all
@@ -795,7 +742,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
         for (F8Tile r; queue.next_warp(r); ++iter) {
             const uint32_t as = iter & 1u, aphase = (iter >> 1) & 1u;
             const int32_t ch = r.c0 + (int32_t)rank * BM + q * 32;     // the channel of the warp's first row of tensor memory
-            const float bias = MODE != WGRAD && p.bias && ch + lane < p.N ? __ldg(p.bias + (int64_t)r.g * p.N + ch + lane) : 0.0f;
+            const float bias = p.bias && ch + lane < p.N ? __ldg(p.bias + (int64_t)r.g * p.N + ch + lane) : 0.0f;
             // the tensor-memory loads below are warp-collective: leave the loop only as a whole warp
             if (!warp_wait(tfull_bar(as), aphase, abort_flag, 46)) break;
             tc_fence_after();
@@ -839,7 +786,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
                         if (b * 32 + j < NT) sums[j * BM] = __uint_as_float(v[j]);
                     continue;
                 }
-                if constexpr (MODE != WGRAD && sizeof(TOUT) == 2) {
+                if constexpr (sizeof(TOUT) == 2) {
                     // Channels along lanes become channels along a row: blocks of 8 x 8 in fragments (lane 4 c + t: channel c, columns 2 t
                     // and 2 t + 1), stored transposed.
                     if (r.kb > 0) tmem_ld_frag(tacc + (uint32_t)(b * 32), v);
@@ -866,36 +813,20 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[j] = r.kb > 0 ? __uint_as_float(v[j]) + bias : bias;
                     staged_block_read();
-                    if (MODE == WGRAD) {
-                        // lanes are rows of the output
+                    // lanes are channels, next to each other in the output's rows
 #pragma unroll
-                        for (int c = 0; c < PIECES; ++c) {
-                            uint4 o;
-                            if constexpr (sizeof(TOUT) == 4)
-                                o = make_uint4(__float_as_uint(f[4 * c]), __float_as_uint(f[4 * c + 1]), __float_as_uint(f[4 * c + 2]), __float_as_uint(f[4 * c + 3]));
-                            else
-                                o = make_uint4(pack2(f[8 * c], f[8 * c + 1], TOUT()), pack2(f[8 * c + 2], f[8 * c + 3], TOUT()),
-                                               pack2(f[8 * c + 4], f[8 * c + 5], TOUT()), pack2(f[8 * c + 6], f[8 * c + 7], TOUT()));
-                            *reinterpret_cast<uint4 *>(stg + lane * PITCH + swz(lane, c) * 16) = o;
-                        }
-                    } else {
-                        // lanes are channels, next to each other in the output's rows
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) *reinterpret_cast<float *>(stg + j * PITCH + swz(j, lane / 4) * 16 + (lane % 4) * 4) = f[j];
-                    }
+                    for (int j = 0; j < 32; ++j) *reinterpret_cast<float *>(stg + j * PITCH + swz(j, lane / 4) * 16 + (lane % 4) * 4) = f[j];
                 }
                 // the staged block: `rows` rows of `cols` elements at dst
-                const int32_t rows_left = MODE == WGRAD ? p.N - ch : r.cols - b * 32, cols_left = MODE == WGRAD ? r.cols - b * 32 : p.N - ch;
+                const int32_t rows_left = r.cols - b * 32, cols_left = p.N - ch;
                 const int rows = rows_left < 32 ? rows_left : 32, cols = cols_left < 32 ? cols_left : 32;
-                TOUT *dst = static_cast<TOUT *>(p.out) + (MODE == WGRAD ? ((int64_t)r.g * p.N + ch) * p.ldo + r.m0 + b * 32
-                                                                        : (int64_t)(r.m0 + b * 32) * p.ldo + ch);
+                TOUT *dst = static_cast<TOUT *>(p.out) + (int64_t)(r.m0 + b * 32) * p.ldo + ch;
                 // A bulk store writes the whole block, but for what lies behind the matrix.
-                if (p.tma_out && (MODE == WGRAD ? cols == 32 || r.m0 + b * 32 + cols == p.C : rows == 32 || r.m0 + b * 32 + rows == p.M)) {
+                if (p.tma_out && (rows == 32 || r.m0 + b * 32 + rows == p.M)) {
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) {
-                        if (MODE == WGRAD) tma_store_3d(&tmap_out, r.m0 + b * 32, ch, r.g, smem_u32(stg));
-                        else tma_store_3d(&tmap_out, ch, r.m0 + b * 32, 0, smem_u32(stg));
+                        tma_store_3d(&tmap_out, ch, r.m0 + b * 32, 0, smem_u32(stg));
                         bulk_commit();
                     }
                     continue;
@@ -1033,7 +964,7 @@ int launch_f8(const F8Call &c, F8Params p, const F8Choice &how, cudaStream_t st)
 {
     using S = F8Cfg<NT, MODE, CTAS, TOUT, SPLIT>;
     auto kern = gemm_f8_kernel<NT, MODE, CTAS, TOUT, SPLIT>;
-    constexpr int STEP = chunk_step(MODE, NT);
+    constexpr int STEP = chunk_step(NT);
     static_assert(NT % STEP == 0, "a chunk is never wider than a tile");
     p.step = STEP;
     p.nt = how.nt;
@@ -1041,37 +972,33 @@ int launch_f8(const F8Call &c, F8Params p, const F8Choice &how, cudaStream_t st)
     p.overlap = 2 * p.nt > S::SF_BASE;
     p.acc1 = p.overlap ? NT - 32 : S::SF_BASE / 32 * 16;
     p.chunk = p.nt;
-    p.chunks = (int32_t)ceil_div(MODE == WGRAD ? p.C : p.M, p.chunk);
+    p.chunks = (int32_t)ceil_div(p.M, p.chunk);
     p.super = 16;
-    const int64_t tiles = MODE == WGRAD ? (int64_t)p.groups * p.tiles_c * p.chunks : (p.chunks + (p.offsets ? p.groups : 0)) * (int64_t)p.tiles_c;
+    const int64_t tiles = (p.chunks + (p.offsets ? p.groups : 0)) * (int64_t)p.tiles_c;
     QNN_REQUIRE(tiles < (int64_t)1 << 28, QNN_ERR_UNSUPPORTED, "%s: too many output tiles", c.what);
     static std::atomic<bool> done[64];
     if (int rc = opt_in(kern, S::TOTAL, done)) return rc;
-    CUtensorMap mw{}, mx{}, mx32{}, msw{}, msx{}, mo{};
+    CUtensorMap mw{}, mx{}, mx32{}, mo{};
     // (an empty reduction loads nothing: any map will do)
     const bool empty = c.w_rows == 0 || c.w_cols == 0 || c.x_rows == 0 || c.x_cols == 0;
     p.has_maps = !empty;
     if (!empty) {
-        const CUtensorMapSwizzle wide = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
+        const CUtensorMapSwizzle wide = CU_TENSOR_MAP_SWIZZLE_128B;
         if (int rc = make_map_f8(c.what, &mw, c.w, 3, c.w_cols, c.w_rows, c.w_count, c.ld_w, c.stride_w, BKB, BM, wide)) return rc;
         if (int rc = make_map_f8(c.what, &mx, c.x, 2, c.x_cols, c.x_rows, 1, c.ld_x, 0, BKB, 128, wide)) return rc;
         if (int rc = make_map_f8(c.what, &mx32, c.x, 2, c.x_cols, c.x_rows, 1, c.ld_x, 0, BKB, 32, wide)) return rc;
-        if (MODE == WGRAD) {
-            if (int rc = make_map_f8(c.what, &msw, p.w_scale, 2, c.w_cols, c.w_rows / 128, 1, p.ld_ws, 0, BM, 4, none)) return rc;
-            if (int rc = make_map_f8(c.what, &msx, p.x_scale, 2, c.x_cols, c.x_rows / 128, 1, p.ld_xs, 0, NT, 4, none)) return rc;
-        }
     }
     {
         // (a bulk store clips a row in 16-byte units)
-        const int64_t es = (int64_t)sizeof(TOUT), cols = MODE == WGRAD ? p.C : p.N, rows = MODE == WGRAD ? p.N : p.M, count = MODE == WGRAD ? p.groups : 1;
-        const int64_t ld = p.ldo * es, stride = count == 1 ? ld : rows * ld;
+        const int64_t es = (int64_t)sizeof(TOUT), cols = p.N, rows = p.M;
+        const int64_t ld = p.ldo * es, stride = ld;
         p.tma_out = !S::CUT && p.vec_out && cols * es % 16 == 0 && ld < (int64_t)1 << 40 && stride < (int64_t)1 << 40;
         if (p.tma_out)
-            if (int rc = make_map_f8(c.what, &mo, p.out, 3, cols, rows, count, ld, stride, 32, 32, es == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            if (int rc = make_map_f8(c.what, &mo, p.out, 3, cols, rows, 1, ld, stride, 32, 32, es == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                                      es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16)) return rc;
     }
     // operand types, which dimension is contiguous, scales as powers of two, rows of the tile
-    p.idesc = (uint32_t)c.w_type << 7 | (uint32_t)c.x_type << 10 | (MODE != FORWARD ? 1u : 0u) << 15 | (MODE == WGRAD ? 1u : 0u) << 16 | 1u << 23 |
+    p.idesc = (uint32_t)c.w_type << 7 | (uint32_t)c.x_type << 10 | (MODE != FORWARD ? 1u : 0u) << 15 | 1u << 23 |
               (uint32_t)((BM * CTAS) >> 7) << 27;
     const int64_t resident = CTAS == 2 ? pairs_resident_f8() : sm_count();
     const int64_t ctas = S::CUT ? tiles * SPLIT : CTAS * (tiles < resident ? tiles : resident);
@@ -1092,7 +1019,7 @@ int launch_f8(const F8Call &c, F8Params p, const F8Choice &how, cudaStream_t st)
         ++na;
     }
     cfg.attrs = attr; cfg.numAttrs = na;
-    QNN_CUDA(cudaLaunchKernelEx(&cfg, kern, mw, mx, mx32, msw, msx, mo, p));
+    QNN_CUDA(cudaLaunchKernelEx(&cfg, kern, mw, mx, mx32, mo, p));
     profile_after(st);
     return check_launch(c.what);
 }
@@ -1111,22 +1038,17 @@ template <int MODE, typename TOUT>
 int run_f8_typed(const F8Call &c, const F8Params &p, cudaStream_t st)
 {
     F8Choice k;
-    if constexpr (MODE == WGRAD) {
-        k = choose_f8(MODE, p.C, p.groups, p.N, ceil_div(ceil_div(p.M, p.groups), 128) + (p.M == 0), false);
-        return k.width == 128 ? launch_f8<128, MODE, 1, TOUT>(c, p, k, st) : launch_f8<256, MODE, 2, TOUT>(c, p, k, st);
-    } else {
-        const int64_t groups = p.groups < p.M ? p.groups : p.M;
-        k = choose_f8(MODE, ceil_div(p.M, groups), groups, p.N, p.nkb, p.offsets == nullptr);
-        if (p.offsets) k.nt = k.width;                 // (groups differ: their chunks are evened out one by one)
-        if (k.split > 1) return k.width == 16   ? launch_split<16, MODE, TOUT>(c, p, k, st)
-                                : k.width <= 64 ? launch_split<64, MODE, TOUT>(c, p, k, st)
-                                                : launch_split<128, MODE, TOUT>(c, p, k, st);
-        switch (k.width) {
-            case 32: return launch_f8<32, MODE, 1, TOUT>(c, p, k, st);
-            case 64: return launch_f8<64, MODE, 1, TOUT>(c, p, k, st);
-            case 128: return launch_f8<128, MODE, 1, TOUT>(c, p, k, st);
-            default: return launch_f8<256, MODE, 2, TOUT>(c, p, k, st);
-        }
+    const int64_t groups = p.groups < p.M ? p.groups : p.M;
+    k = choose_f8(ceil_div(p.M, groups), groups, p.N, p.nkb, p.offsets == nullptr);
+    if (p.offsets) k.nt = k.width;                 // (groups differ: their chunks are evened out one by one)
+    if (k.split > 1) return k.width == 16   ? launch_split<16, MODE, TOUT>(c, p, k, st)
+                            : k.width <= 64 ? launch_split<64, MODE, TOUT>(c, p, k, st)
+                                            : launch_split<128, MODE, TOUT>(c, p, k, st);
+    switch (k.width) {
+        case 32: return launch_f8<32, MODE, 1, TOUT>(c, p, k, st);
+        case 64: return launch_f8<64, MODE, 1, TOUT>(c, p, k, st);
+        case 128: return launch_f8<128, MODE, 1, TOUT>(c, p, k, st);
+        default: return launch_f8<256, MODE, 2, TOUT>(c, p, k, st);
     }
 }
 template <int MODE>
