@@ -4,8 +4,8 @@
 // its place by 2^(sy[n] + sx[k] - 254): sums of blocks and of the group are held in fp32.  A code of either type is an fp16 number
 // exactly (inf and NaN too) and a product of two is exact in fp32, so the codes are multiplied as fp16.
 //
-// One CTA owns 128 x 128 results of a group; eight warps own 64 x 32 of them each.  Rows go through shared memory 32 at a time, the next
-// 32 on their way in registers meanwhile, and are turned round by transposing matrix loads.  Every load is a plain one of 16 bytes
+// One CTA owns 128 x 128 results of a group; sixteen warps own 32 x 32 of them each.  Rows go through shared memory 64 at a time, the next
+// 64 on their way in registers meanwhile, and are turned round by transposing matrix loads.  Every load is a plain one of 16 bytes
 // within a row, and only blocks of the group itself are read: buffers need hold no more than the groups' blocks.
 #include "qnn_gemm_f8.cuh"
 #include <cuda_fp8.h>
@@ -13,15 +13,16 @@
 namespace qnn {
 namespace {
 
-constexpr int WG_T = 128, WG_ROWS = 32, WG_THREADS = 256;
+constexpr int WG_T = 128, WG_ROWS = 64, WG_THREADS = 512;
 constexpr int WG_PITCH = WG_T + 8;                   // halves; eight rows of 16 bytes then lie in different banks
+constexpr int WG_BYTES = 2 * 2 * WG_ROWS * WG_PITCH * 2;
 
 struct WgParams {
     const uint8_t *dy, *x, *dy_scale, *x_scale;
     int64_t ld_dy, ldx, ld_dys, ld_xs, M, ld_dw;
     const int64_t *offsets;
     void *dw;
-    int32_t N, K, groups, tiles_n, tiles_k, dy_type, x_type;
+    int32_t N, K, groups, tiles_n, tiles_k;
 };
 
 __device__ __forceinline__ uint32_t two_halves(uint32_t codes, __nv_fp8_interpretation_t type)
@@ -30,9 +31,10 @@ __device__ __forceinline__ uint32_t two_halves(uint32_t codes, __nv_fp8_interpre
     return (uint32_t)h.x | (uint32_t)h.y << 16;
 }
 // 16 codes as 16 halves
-__device__ __forceinline__ void put_codes(__half *to, uint4 v, int type)
+template <int TYPE>
+__device__ __forceinline__ void put_codes(__half *to, uint4 v)
 {
-    const __nv_fp8_interpretation_t t = type == QNN_F8_E4M3 ? __NV_E4M3 : __NV_E5M2;
+    constexpr __nv_fp8_interpretation_t t = TYPE == QNN_F8_E4M3 ? __NV_E4M3 : __NV_E5M2;
     uint4 *d = reinterpret_cast<uint4 *>(to);
     d[0] = make_uint4(two_halves(v.x, t), two_halves(v.x >> 16, t), two_halves(v.y, t), two_halves(v.y >> 16, t));
     d[1] = make_uint4(two_halves(v.z, t), two_halves(v.z >> 16, t), two_halves(v.w, t), two_halves(v.w >> 16, t));
@@ -56,10 +58,12 @@ __device__ __forceinline__ float scaled(float v, int s, int t)
     return s == 255 || t == 255 ? __int_as_float(0x7fffffff) : r;
 }
 
-template <typename TOUT>
+template <typename TOUT, int DY, int X>
 __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
 {
-    __shared__ __align__(16) __half sy[2][WG_ROWS][WG_PITCH], sx[2][WG_ROWS][WG_PITCH];
+    extern __shared__ __align__(16) uint8_t wg_smem[];
+    typedef __half Buffer[WG_ROWS][WG_PITCH];
+    Buffer *sy = reinterpret_cast<Buffer *>(wg_smem), *sx = sy + 2;
     __shared__ int32_t where[2];                     // the group's first block and its number of blocks
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t tile = (int32_t)blockIdx.x, per = p.tiles_n * p.tiles_k;
@@ -88,7 +92,7 @@ __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
     __syncthreads();
     const int32_t blk0 = where[0], steps = where[1] * (128 / WG_ROWS);
 
-    // a thread's 16 bytes of 32 rows x 128 columns
+    // a thread's 16 bytes of 64 rows x 128 columns
     const int row = tid >> 3, col = (tid & 7) * 16;
     const bool has_y = tn * WG_T + col < p.N, has_x = tk * WG_T + col < p.K;
     const uint8_t *py = p.dy + ((int64_t)blk0 * 128 + row) * p.ld_dy + tn * WG_T + col;
@@ -98,41 +102,44 @@ __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
         a = has_y ? __ldg(reinterpret_cast<const uint4 *>(py + (int64_t)s * WG_ROWS * p.ld_dy)) : none;
         b = has_x ? __ldg(reinterpret_cast<const uint4 *>(px + (int64_t)s * WG_ROWS * p.ldx)) : none;
     };
-    const int wn = (warp >> 2) * 64, wk = (warp & 3) * 32, fr = lane >> 2, fc = 2 * (lane & 3);
-    float sum[4][4][4] = {}, part[4][4][4] = {};
+    const int wn = (warp >> 2) * 32, wk = (warp & 3) * 32, fr = lane >> 2, fc = 2 * (lane & 3);
+    float sum[2][4][4] = {}, part[2][4][4] = {};
     uint4 a, b;
     if (steps > 0) fetch(0, a, b);
     for (int32_t s = 0; s < steps; ++s) {
         const int h = s & 1;
-        put_codes(&sy[h][row][col], a, p.dy_type);
-        put_codes(&sx[h][row][col], b, p.x_type);
+        put_codes<DY>(&sy[h][row][col], a);
+        put_codes<X>(&sx[h][row][col], b);
         __syncthreads();                             // (two buffers: a warp here has left the one before last)
         if (s + 1 < steps) fetch(s + 1, a, b);
 #pragma unroll
         for (int k0 = 0; k0 < WG_ROWS; k0 += 16) {
-            uint32_t fa[4][4], fb[2][4];
+            uint32_t fa[2][4], fb[2][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_trans(fa[i], &sy[h][k0 + (lane >> 4) * 8 + (lane & 7)][wn + 16 * i + (lane >> 3 & 1) * 8]);
+            for (int i = 0; i < 2; ++i) load_trans(fa[i], &sy[h][k0 + (lane >> 4) * 8 + (lane & 7)][wn + 16 * i + (lane >> 3 & 1) * 8]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) load_trans(fb[j], &sx[h][k0 + (lane >> 3 & 1) * 8 + (lane & 7)][wk + 16 * j + (lane >> 4) * 8]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) mma_f16(part[i][j], fa[i], fb[j >> 1][2 * (j & 1)], fb[j >> 1][2 * (j & 1) + 1]);
         }
-        if ((s & 3) != 3) continue;
-        const int64_t blk = blk0 + (s >> 2);
-        int ey[4][2], ex[4][2];
+        if ((s & 1) == 0) continue;
+        const int64_t blk = blk0 + (s >> 1);
+        int ey[2][2], ex[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int32_t n = tn * WG_T + wn + 16 * i + 8 * u + fr, k = tk * WG_T + wk + 8 * i + fc + u;
-                ey[i][u] = n < p.N ? p.dy_scale[blk * p.ld_dys + n] : 127;
+                const int32_t k = tk * WG_T + wk + 8 * i + fc + u;
+                if (i < 2) {
+                    const int32_t n = tn * WG_T + wn + 16 * i + 8 * u + fr;
+                    ey[i][u] = n < p.N ? p.dy_scale[blk * p.ld_dys + n] : 127;
+                }
                 ex[i][u] = k < p.K ? p.x_scale[blk * p.ld_xs + k] : 127;
             }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -143,7 +150,7 @@ __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
     }
     TOUT *dw = static_cast<TOUT *>(p.dw);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -151,6 +158,18 @@ __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
                 const int32_t n = tn * WG_T + wn + 16 * i + 8 * (e >> 1) + fr, k = tk * WG_T + wk + 8 * j + fc + (e & 1);
                 if (n < p.N && k < p.K) from_float(sum[i][j][e], dw[((int64_t)g * p.N + n) * p.ld_dw + k]);
             }
+}
+
+template <typename TOUT, int DY, int X>
+int launch_wgrad(const F8Call &c, const WgParams &p, unsigned grid, cudaStream_t st)
+{
+    static std::atomic<bool> done[64];
+    auto kern = wgrad_f8_kernel<TOUT, DY, X>;
+    if (int rc = opt_in(kern, WG_BYTES, done)) return rc;
+    profile_before(st);
+    kern<<<grid, WG_THREADS, WG_BYTES, st>>>(p);
+    profile_after(st);
+    return check_launch(c.what);
 }
 
 }  // namespace
@@ -162,19 +181,18 @@ int run_f8_wgrad(const F8Call &c, const F8Params &f, int out_type, cudaStream_t 
     p.dy_scale = f.w_scale; p.x_scale = f.x_scale;
     p.ld_dy = c.ld_w; p.ldx = c.ld_x; p.ld_dys = f.ld_ws; p.ld_xs = f.ld_xs; p.M = f.M; p.ld_dw = f.ldo;
     p.offsets = f.offsets; p.dw = f.out;
-    p.N = f.N; p.K = f.C; p.groups = f.groups; p.dy_type = c.w_type; p.x_type = c.x_type;
+    p.N = f.N; p.K = f.C; p.groups = f.groups;
     p.tiles_n = (int32_t)ceil_div(p.N, WG_T); p.tiles_k = (int32_t)ceil_div(p.K, WG_T);
     const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
     QNN_REQUIRE(tiles < (int64_t)1 << 28 && tiles * p.groups < (int64_t)1 << 30, QNN_ERR_UNSUPPORTED, "%s: too many output tiles", c.what);
     const unsigned grid = (unsigned)(tiles * p.groups);
-    profile_before(st);
-    switch (out_type) {
-        case QNN_TYPE_F32: wgrad_f8_kernel<float><<<grid, WG_THREADS, 0, st>>>(p); break;
-        case QNN_TYPE_BF16: wgrad_f8_kernel<__nv_bfloat16><<<grid, WG_THREADS, 0, st>>>(p); break;
-        default: wgrad_f8_kernel<__half><<<grid, WG_THREADS, 0, st>>>(p); break;
-    }
-    profile_after(st);
-    return check_launch(c.what);
+    const bool e4 = c.w_type == QNN_F8_E4M3, f4 = c.x_type == QNN_F8_E4M3;
+    auto typed = [&](auto out) {
+        typedef decltype(out) T;
+        return e4 ? (f4 ? launch_wgrad<T, QNN_F8_E4M3, QNN_F8_E4M3>(c, p, grid, st) : launch_wgrad<T, QNN_F8_E4M3, QNN_F8_E5M2>(c, p, grid, st))
+                  : (f4 ? launch_wgrad<T, QNN_F8_E5M2, QNN_F8_E4M3>(c, p, grid, st) : launch_wgrad<T, QNN_F8_E5M2, QNN_F8_E5M2>(c, p, grid, st));
+    };
+    return out_type == QNN_TYPE_F32 ? typed(float()) : out_type == QNN_TYPE_BF16 ? typed(__nv_bfloat16()) : typed(__half());
 }
 
 }  // namespace qnn
