@@ -126,27 +126,47 @@ __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
         }
         if ((s & 1) == 0) continue;
         const int64_t blk = blk0 + (s >> 1);
-        int ey[2][2], ex[4][2];
+        // scales as fp32 numbers 2^(s - 127), by their bits (0 and infinity: scales 0 and 255, which take the other way)
+        float ey[2][2], ex[4][2];
+        float y0 = 1.0f, y1 = 1.0f, x0 = 1.0f, x1 = 1.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int32_t k = tk * WG_T + wk + 8 * i + fc + u;
+                ex[i][u] = __int_as_float((k < p.K ? (int)p.x_scale[blk * p.ld_xs + k] : 127) << 23);
+                x0 = fminf(x0, ex[i][u]); x1 = fmaxf(x1, ex[i][u]);
                 if (i < 2) {
                     const int32_t n = tn * WG_T + wn + 16 * i + 8 * u + fr;
-                    ey[i][u] = n < p.N ? p.dy_scale[blk * p.ld_dys + n] : 127;
+                    ey[i][u] = __int_as_float((n < p.N ? (int)p.dy_scale[blk * p.ld_dys + n] : 127) << 23);
+                    y0 = fminf(y0, ey[i][u]); y1 = fmaxf(y1, ey[i][u]);
                 }
-                ex[i][u] = k < p.K ? p.x_scale[blk * p.ld_xs + k] : 127;
             }
+        // Where every product of two scales is a normal number it is exact: a multiplication and a multiply-add a result, which leave the
+        // integer pipe to the conversions of codes.
+        const float low = y0 * x0, high = y1 * x1;
+        if (__all_sync(0xffffffffu, y0 > 0.0f && x0 > 0.0f && low >= 1.17549435e-38f && high <= 3.40282347e38f)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[i][j][e] = fmaf(part[i][j][e], ey[i][e >> 1] * ex[j][e & 1], sum[i][j][e]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sum[i][j][e] += scaled(part[i][j][e], __float_as_int(ey[i][e >> 1]) >> 23, __float_as_int(ex[j][e & 1]) >> 23);
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sum[i][j][e] += scaled(part[i][j][e], ey[i][e >> 1], ex[j][e & 1]);
-                    part[i][j][e] = 0.0f;
-                }
+                for (int e = 0; e < 4; ++e) part[i][j][e] = 0.0f;
     }
     TOUT *dw = static_cast<TOUT *>(p.dw);
 #pragma unroll

@@ -355,3 +355,74 @@ def test_tensors_on_another_device_are_refused(q):
         with pytest.raises(ValueError):
             f(x.cpu())
     assert q.qnn_launch_count() == before
+
+
+@pytest.mark.parametrize("top,other", [(254, 0), (0, 254), (0, 0), (1, 126), (1, 127), (254, 127), (254, 128), (200, 60)])
+def test_weight_gradient_scales_at_the_ends(q, top, other):
+    """One channel's and one column's scale far from the others: powers of two that are no fp32 numbers by themselves, results exact."""
+    g, N, K = gen(top * 256 + other), 130, 140
+    y, x = Operand(g, B, N, E4M3, (B, 1), spread=0), Operand(g, B, K, E4M3, (B, 1), spread=0)
+    yv, xv = y.codes[:, :N].double(), x.codes[:, :K].double()
+    y.scale[0, 7] = top
+    x.scale[0, 9] = other
+    o = Guarded((N, K), torch.float32)
+    q.qnn_gemm_f8_wgrad(y.codes, y.ld, y.scale, y.lds, x.codes, x.ld, x.scale, x.lds, offsets_of([B]), 1, B, N, K, o.t, K)
+    o.check()
+    f = lambda s, n: torch.exp2(s[0, :n].double() - 127)
+    want = (yv.t() @ xv) * f(y.scale, N)[:, None] * f(x.scale, K)[None]
+    # a small integer (10 bits) times a power of two: fp32 holds it, but for what is rounded once (below 2^-126) or overflows
+    assert torch.equal(o.t, want.float())
+
+
+def test_weight_gradient_nan_scales_stay_in_their_channel_and_column(q):
+    g, sizes, N, K = gen(5), [130, 0, 100], 140, 150
+    y, x = Operand(g, 3 * B, N, E4M3, (B, 1)), Operand(g, 3 * B, K, E5M2, (B, 1))
+    y.codes.view(torch.uint8)[130:256] = 0
+    y.codes.view(torch.uint8)[356:] = 0
+    y.scale[1, 3] = 255
+    x.scale[2, 139] = 255
+    o = Guarded((3 * N, K), torch.float32)
+    q.qnn_gemm_f8_wgrad(y.codes, y.ld, y.scale, y.lds, x.codes, x.ld, x.scale, x.lds, offsets_of(sizes), 3, 230, N, K, o.t, K)
+    o.check()
+    bad = o.t.view(3, N, K).isnan()
+    want = torch.zeros_like(bad)
+    want[0, 3] = True
+    want[2, :, 139] = True
+    assert torch.equal(bad, want)
+
+
+def test_weight_gradient_offsets_that_fall_or_leave_the_rows(q):
+    """Held to rise and to stay within 0..M: the same as the offsets they are held to."""
+    g, N, K, M = gen(6), 33, 40, 300
+    y, x = Operand(g, 8 * B, N, E4M3, (B, 1)), Operand(g, 8 * B, K, E4M3, (B, 1))
+    out = []
+    for offs in ([-5, 200, 100, 900, 50], [0, 200, 200, 300, 300]):
+        o = Guarded((4 * N, K), torch.float32)
+        t = torch.tensor(offs, dtype=torch.int64, device="cuda")
+        q.qnn_gemm_f8_wgrad(y.codes, y.ld, y.scale, y.lds, x.codes, x.ld, x.scale, x.lds, t, 4, M, N, K, o.t, K)
+        o.check()
+        out.append(o.t.clone())
+    assert torch.equal(*out) and (out[0].view(4, N, K)[[1, 3]] == 0).all() and (out[0].view(4, N, K)[[0, 2]] != 0).any()
+
+
+def test_weight_gradient_captured_and_on_two_streams(q):
+    g, N, K = gen(7), 200, 260
+    y, x = Operand(g, 4 * B, N, E4M3, (B, 1)), Operand(g, 4 * B, K, E4M3, (B, 1))
+    off = offsets_of([2 * B, 2 * B])
+    outs = [torch.zeros(2 * N, K, device="cuda") for _ in range(4)]
+    call = lambda o: q.qnn_gemm_f8_wgrad(y.codes, y.ld, y.scale, y.lds, x.codes, x.ld, x.scale, x.lds, off, 2, 4 * B, N, K, o, K)
+    call(outs[0])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for s, o in zip(streams, outs[1:3]):
+        with torch.cuda.stream(s):
+            call(o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[3])
+    for _ in range(2):
+        outs[3].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(outs[0], o) for o in outs[1:]) and (outs[0] != 0).any()
