@@ -749,6 +749,7 @@ QNN_API int qnn_gemm_f8_grouped(const void *a, int a_type, int64_t lda, const vo
  *   dy, x       codes and scales as qnn_quantize_columns_f8 writes them for the same
  *               offsets, with N and K elements a row; M is the number of rows that
  *               call was given.  offsets may be NULL for a single group of all rows.
+ *               Only the groups' own blocks are read: buffers may end with the last.
  *   dw          device, [groups][N][ld_dw] of dw_type */
 QNN_API int qnn_gemm_f8_wgrad(const void *dy, int dy_type, int64_t ld_dy, const void *dy_scale, int64_t ld_dys, const void *x,
                               int x_type, int64_t ldx, const void *x_scale, int64_t ld_xs, const int64_t *offsets,

@@ -405,7 +405,7 @@ quant_rows_f8_kernel(const F8Source p)
         using V = decltype(kind);
         constexpr bool VALUES = !std::is_same<V, Nothing>::value;
         uint32_t carry[4] = {0u, 0u, 0u, 0u};
-        uint8_t *codes = p.codes + row0 * p.ldq + k0, *scale = p.scale + row0 * p.ld_scale + 8 * seg + half;  // (WIDE)
+        [[maybe_unused]] uint8_t *codes = p.codes + row0 * p.ldq + k0, *scale = p.scale + row0 * p.ld_scale + 8 * seg + half;  // (WIDE)
         V *values = static_cast<V *>(p.values) + (VALUES ? row0 * p.ld_values : 0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {

@@ -426,3 +426,147 @@ def test_weight_gradient_captured_and_on_two_streams(q):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(outs[0], o) for o in outs[1:]) and (outs[0] != 0).any()
+
+
+def within(got, a, b, terms):
+    """|got - a b| <= terms 2^-23 |a| |b|, and half a step of a 16-bit result."""
+    want, s = a @ b, a.abs() @ b.abs()
+    eps = torch.finfo(got.dtype).eps / 2
+    slack = terms * 2.0 ** -23 * s * (1 + eps) + (eps * want.abs() if got.dtype != torch.float32 else 0)
+    assert ((got.double() - want).abs() <= slack + 2.0 ** -149).all()
+
+
+def quantised(call, rows, K, scale_rows, scale_cols, code):
+    """(codes, scale bytes, what they stand for) of a quantising call."""
+    c = torch.zeros(rows, up(K, 16), dtype=torch.uint8, device="cuda").view(code)
+    s = torch.zeros(scale_rows, up(scale_cols, 16), dtype=torch.uint8, device="cuda")
+    v = torch.zeros(rows, K, device="cuda")
+    call(c, c.shape[1], s, s.shape[1], v)
+    return c, s, v
+
+
+@pytest.mark.parametrize("out", TYPES)
+def test_experts_forward_and_backward(q, out):
+    """Tokens in the order of their experts, a product, a gate, a product; then input and weight gradients from the same weights."""
+    g, T, K, N, sizes = gen(11), 150, 300, 260, [70, 0, 129, 101]       # every token goes to two experts
+    M, G = sum(sizes), len(sizes)
+    off, at = offsets_of(sizes), [0] + torch.tensor(sizes).cumsum(0).tolist()
+    index = (torch.randperm(M, generator=g, device="cuda") % T).to(torch.int64)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    x, w1, w2 = rand(T, K), rand(G, 2 * N, K), rand(G, K, N)
+
+    def rows(t, code, idx=None):
+        R, C = (len(idx), t.shape[1]) if idx is not None else t.shape
+        return quantised(lambda c, l, s, ls, v: q.qnn_quantize_blocks_f8(t, R, C, C, c, l, s, ls, index=idx, src_rows=t.shape[0] if idx is not None else 0,
+                                                                         values=v, ld_values=C), R, C, R, up(C, B) // B, code)
+
+    def weight(w):
+        parts = [quantised(lambda c, l, s, ls, v: q.qnn_quantize_tiles_f8(w[i], *w[i].shape, w.shape[2], c, l, s, ls, values=v, ld_values=w.shape[2]),
+                           *w[i].shape, up(w.shape[1], B) // B, up(w.shape[2], B) // B, E4M3) for i in range(G)]
+        return torch.stack([p[0].view(torch.uint8) for p in parts]).view(E4M3), torch.stack([p[1] for p in parts]), torch.stack([p[2] for p in parts])
+
+    def columns(t, code):
+        R = B * (M // B + G)
+        return quantised(lambda c, l, s, ls, v: q.qnn_quantize_columns_f8(t, M, t.shape[1], t.shape[1], off, G, c, l, s, ls, values=v, ld_values=t.shape[1]),
+                         R, t.shape[1], R // B, t.shape[1], code)
+
+    def product(a, w, n, k, across=False):
+        o = torch.zeros(M, n, dtype=out, device="cuda")
+        before = q.qnn_launch_count()
+        q.qnn_gemm_f8_grouped(a[0], a[0].shape[1], a[1], a[1].shape[1], w[0], w[0].shape[2], w[1], w[1].shape[2], off, G, M, n, k, o, n, b_transposed=across)
+        assert q.qnn_launch_count() == before + 1
+        for i in range(G):
+            m = w[2][i].double()
+            within(o[at[i]:at[i + 1]], a[2][at[i]:at[i + 1]].double(), m if across else m.t(), k)
+        return o
+
+    W1, W2 = weight(w1), weight(w2)
+    a1 = rows(x, E4M3, index)
+    assert torch.equal(a1[2], rows(x, E4M3)[2][index]), "an index that comes twice gives the same row twice"
+    h = product(a1, W1, 2 * N, K).float()
+    a2 = rows(torch.nn.functional.silu(h[:, :N]) * h[:, N:], E4M3)
+    y = product(a2, W2, K, N)
+    dy = rand(*y.shape)
+    product(rows(dy, E5M2), W2, N, K, across=True)
+    cy, cx = columns(dy, E5M2), columns(a2[2], E4M3)
+    dw = torch.full((G, K, N), 7.0, dtype=out, device="cuda")
+    q.qnn_gemm_f8_wgrad(cy[0], cy[0].shape[1], cy[1], cy[1].shape[1], cx[0], cx[0].shape[1], cx[1], cx[1].shape[1], off, G, M, K, N, dw, N)
+    blk = 0
+    for i, rows_i in enumerate(sizes):
+        r = slice(blk * B, (blk + up(rows_i, B) // B) * B)
+        blk += up(rows_i, B) // B
+        a, b = cy[2][r].double(), cx[2][r].double()
+        within(dw[i], a.t(), b, max(rows_i, 1))
+        if out == torch.float32 and rows_i:
+            # against differences: the loss sum(dy * (x w^T)) along a direction is linear, so its difference is the gradient's product with it
+            d = rand(K, N).double()
+            loss = lambda w: (a * (b @ w.t())).sum()
+            slope, bound = (loss(d) - loss(-d)) / 2, ((a.abs().t() @ b.abs()) * d.abs()).sum() * rows_i * 2.0 ** -23
+            assert (slope - (dw[i].double() * d).sum()).abs() <= bound + 1e-9 * slope.abs()
+
+
+@pytest.mark.parametrize("across", [False, True], ids=["forward", "across"])
+@pytest.mark.parametrize("M", [1, 16, 40, 130, 700])
+def test_nan_scales_stay_in_their_rows_and_channels(q, M, across):
+    g, N, K = gen(M), 300, 400
+    a = Operand(g, M, K, E4M3, (1, B))
+    w = Operand(g, K if across else N, N if across else K, E4M3, (B, B))
+    a.scale[M // 2, 1] = 255
+    if M > 1:
+        w.scale[(2, 1) if across else (1, 2)] = 255                     # channels 128..255
+    o = Guarded((M, N), torch.float32)
+    q.qnn_gemm_f8(a.codes, a.ld, a.scale, a.lds, w.codes, w.ld, w.scale, w.lds, M, N, K, o.t, N, b_transposed=across)
+    o.check()
+    want = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    want[M // 2] = True
+    if M > 1:
+        want[:, 128:256] = True
+    assert torch.equal(o.t.isnan(), want)
+
+
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("M,N", [(1, 5), (40, 300), (3000, 2000)])
+def test_an_empty_reduction_gives_the_bias(q, M, N, out):
+    c, s = torch.zeros(up(max(M, N), 16), 16, dtype=torch.uint8, device="cuda").view(E4M3), torch.zeros(up(max(M, N), 16), 16, dtype=torch.uint8, device="cuda")
+    bias = torch.arange(N, device="cuda", dtype=torch.float32)
+    for b in (bias, None):
+        o = Guarded((M, N), out)
+        q.qnn_gemm_f8(c, 16, s, 16, c, 16, s, 16, M, N, 0, o.t, N, bias=b)
+        o.check()
+        assert torch.equal(o.t, (bias if b is not None else bias * 0).to(out).expand(M, N))
+
+
+def test_grouped_offsets_that_fall_or_leave_the_rows(q):
+    g, M, N, K = gen(9), 300, 130, 200
+    a = Operand(g, M, K, E4M3, (1, B))
+    codes, scales, _ = weights(g, 4, N, K, E4M3)
+    out = []
+    for offs in ([-5, 200, 100, 900, 50], [0, 200, 200, 300, 300]):
+        o = Guarded((M, N), torch.float32)
+        t = torch.tensor(offs, dtype=torch.int64, device="cuda")
+        q.qnn_gemm_f8_grouped(a.codes, a.ld, a.scale, a.lds, codes, codes.shape[2], scales, scales.shape[2], t, 4, M, N, K, o.t, N)
+        o.check()
+        out.append(o.t.clone())
+    assert torch.equal(*out)
+
+
+@pytest.mark.parametrize("M", [1, 40, 129, 700])
+def test_products_captured_and_on_two_streams(q, M):
+    g, N, K = gen(M), 512, 1024
+    a, w = Operand(g, M, K, E4M3, (1, B)), Operand(g, N, K, E4M3, (B, B))
+    outs = [torch.zeros(M, N, device="cuda") for _ in range(4)]
+    call = lambda o: q.qnn_gemm_f8(a.codes, a.ld, a.scale, a.lds, w.codes, w.ld, w.scale, w.lds, M, N, K, o, N)
+    call(outs[0])
+    torch.cuda.synchronize()
+    for s, o in zip([torch.cuda.Stream(), torch.cuda.Stream()], outs[1:3]):
+        with torch.cuda.stream(s):
+            call(o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[3])
+    for _ in range(2):
+        outs[3].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(outs[0], o) for o in outs[1:]) and (outs[0] != 0).any()
