@@ -7,8 +7,9 @@
 // One CTA owns 128 x 128 results of a group; sixteen warps own 32 x 32 of them each.  Rows go through shared memory 64 at a time, the next
 // 64 on their way in registers meanwhile, and are turned round by transposing matrix loads.  Every load is a plain one of 16 bytes
 // within a row, and only blocks of the group itself are read: buffers need hold no more than the groups' blocks.
-// Bound by the integer pipe, which the conversions and addresses load to 43 % (tensor pipe 24 %, at 1500 rows in 3 groups, 1000 x 2040):
-// 16384 rows over 32 groups, 4096 x 2048, take 2203 us (125 TFLOP/s); scales on the integer pipe 2590, eight warps and 32 rows 3008.
+// 16384 rows over 32 groups, 4096 x 2048 (e5m2): 2149 us, 128 TFLOP/s.  Warps waited for a busy arithmetic pipe most (integer 43 %,
+// tensor 24 %, before scales left the former: 2590 us).  Conversions are not what bounds it now: e5m2 by the conversion instruction
+// takes 2203.  Eight warps of 64 x 32, which read shared memory less often, take 2547.
 #include "qnn_gemm_f8.cuh"
 #include <cuda_fp8.h>
 
@@ -27,19 +28,27 @@ struct WgParams {
     int32_t N, K, groups, tiles_n, tiles_k;
 };
 
-__device__ __forceinline__ uint32_t two_halves(uint32_t codes, __nv_fp8_interpretation_t type)
+// two codes as halves: an e5m2 code is the upper byte of its fp16 number
+template <int TYPE>
+__device__ __forceinline__ uint32_t low_halves(uint32_t codes)
 {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), type);
+    if constexpr (TYPE == QNN_F8_E5M2) return __byte_perm(codes, 0u, 0x1404);
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), __NV_E4M3);
     return (uint32_t)h.x | (uint32_t)h.y << 16;
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t high_halves(uint32_t codes)
+{
+    if constexpr (TYPE == QNN_F8_E5M2) return __byte_perm(codes, 0u, 0x3424);
+    return low_halves<TYPE>(codes >> 16);
 }
 // 16 codes as 16 halves
 template <int TYPE>
 __device__ __forceinline__ void put_codes(__half *to, uint4 v)
 {
-    constexpr __nv_fp8_interpretation_t t = TYPE == QNN_F8_E4M3 ? __NV_E4M3 : __NV_E5M2;
     uint4 *d = reinterpret_cast<uint4 *>(to);
-    d[0] = make_uint4(two_halves(v.x, t), two_halves(v.x >> 16, t), two_halves(v.y, t), two_halves(v.y >> 16, t));
-    d[1] = make_uint4(two_halves(v.z, t), two_halves(v.z >> 16, t), two_halves(v.w, t), two_halves(v.w >> 16, t));
+    d[0] = make_uint4(low_halves<TYPE>(v.x), high_halves<TYPE>(v.x), low_halves<TYPE>(v.y), high_halves<TYPE>(v.y));
+    d[1] = make_uint4(low_halves<TYPE>(v.z), high_halves<TYPE>(v.z), low_halves<TYPE>(v.w), high_halves<TYPE>(v.w));
 }
 __device__ __forceinline__ void load_trans(uint32_t (&r)[4], const __half *at)
 {
