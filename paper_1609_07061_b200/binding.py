@@ -683,14 +683,15 @@ except ImportError:
 
         @staticmethod
         def _f8(t, where):
-            kinds = {torch.float8_e4m3fn: QNN_F8_E4M3, torch.float8_e5m2: QNN_F8_E5M2}
+            # (types that an older torch may lack)
+            kinds = {getattr(torch, "float8_e4m3fn", None): QNN_F8_E4M3, getattr(torch, "float8_e5m2", None): QNN_F8_E5M2}
             if t is not None and t.dtype not in kinds:
                 raise TypeError(f"{where}: {t.dtype} where float8_e4m3fn or float8_e5m2 is needed")
             return QNN_F8_E4M3 if t is None else kinds[t.dtype]
 
         @staticmethod
         def _scale8(t, where):
-            if t is not None and t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+            if t is not None and t.dtype not in (torch.uint8, getattr(torch, "float8_e8m0fnu", None)):
                 raise TypeError(f"{where}: {t.dtype} where uint8 or float8_e8m0fnu is needed")
             return _p(t)
 

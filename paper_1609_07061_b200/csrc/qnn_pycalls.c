@@ -10,7 +10,8 @@
 
 static PyObject *s_dtype, *s_data_ptr, *s_get_device;    /* attribute names */
 static PyObject *t_f32, *t_bf16, *t_f16, *t_i8, *t_i64;  /* torch's type objects: one of each exists */
-static PyObject *t_e4m3, *t_e5m2, *t_u8, *t_e8m0;
+static PyObject *t_u8;
+static PyObject *t_e4m3, *t_e5m2, *t_e8m0;               /* NULL where torch has no such type: no tensor can have it then */
 
 static void *ptr(PyObject *o) { return o == Py_None ? NULL : PyLong_AsVoidPtr(o); }
 /* pointer of a tensor of any type; None gives NULL */
@@ -222,6 +223,12 @@ static PyMethodDef methods[] = {METHOD(qnn_quantize_rows_i8), METHOD(qnn_rmsnorm
                                 METHOD(qnn_quantize_columns_f8), METHOD(qnn_gemm_f8), METHOD(qnn_gemm_f8_grouped), METHOD(qnn_gemm_f8_wgrad),
                                 METHOD(qnn_token_logprobs), METHOD(qnn_token_logprobs_backward),
                                 {NULL, NULL, 0, NULL}};
+static PyObject *if_there(PyObject *torch, const char *name)
+{
+    PyObject *t = PyObject_GetAttrString(torch, name);
+    if (t == NULL && PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Clear();
+    return t;
+}
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qnn_calls", "Argument marshalling of libqnn.so calls.", -1, methods,
                                     NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__qnn_calls(void)
@@ -236,12 +243,12 @@ PyMODINIT_FUNC PyInit__qnn_calls(void)
     t_i8 = PyObject_GetAttrString(torch, "int8");
     t_i64 = PyObject_GetAttrString(torch, "int64");
     s_get_device = PyUnicode_InternFromString("get_device");
-    t_e4m3 = PyObject_GetAttrString(torch, "float8_e4m3fn");
-    t_e5m2 = PyObject_GetAttrString(torch, "float8_e5m2");
     t_u8 = PyObject_GetAttrString(torch, "uint8");
-    t_e8m0 = PyObject_GetAttrString(torch, "float8_e8m0fnu");
+    t_e4m3 = if_there(torch, "float8_e4m3fn");
+    t_e5m2 = if_there(torch, "float8_e5m2");
+    t_e8m0 = if_there(torch, "float8_e8m0fnu");
     Py_DECREF(torch);
-    if (!s_get_device || !t_e4m3 || !t_e5m2 || !t_u8 || !t_e8m0) return NULL;
+    if (!s_get_device || !t_u8 || PyErr_Occurred()) return NULL;
     if (!s_dtype || !s_data_ptr || !t_f32 || !t_bf16 || !t_f16 || !t_i8 || !t_i64) return NULL;
     return PyModule_Create(&module);
 }
