@@ -637,6 +637,21 @@ def qnn_xnor_gemm_noalloc(a, lda, b, ldb, M, N, K, out, ldo):
 try:
     from . import _qnn_calls  # (after the library's own check above)
 except ImportError:
+    class _Fits:
+        """The library's functions, for whole numbers that fit their parameters: ctypes drops the bits that do not."""
+
+        def __getattr__(self, name):
+            call, kinds = getattr(_lib, name), _SIGS[name][1]
+
+            def checked(*a):
+                for v, kind in zip(a, kinds):
+                    if kind in (i32, i64) and not -(1 << 8 * ctypes.sizeof(kind) - 1) <= v < 1 << 8 * ctypes.sizeof(kind) - 1:
+                        raise OverflowError(f"{name}: {v} does not fit a C int of {8 * ctypes.sizeof(kind)} bits")
+                return call(*a)
+            return checked
+
+    _fits = _Fits()
+
     class _qnn_calls:
         """The module's functions through ctypes: same names, arguments and refusals."""
 
@@ -658,27 +673,27 @@ except ImportError:
         @classmethod
         def qnn_quantize_rows_i8(cls, x, rows, K, ldx, codes, ldq, scale, values, ldv, stream):
             w = "qnn_quantize_rows_i8"
-            return _lib.qnn_quantize_rows_i8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(codes, torch.int8, w), ldq,
+            return _fits.qnn_quantize_rows_i8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(codes, torch.int8, w), ldq,
                                              cls._need(scale, torch.float32, w), _p(values), cls._real(values, w), ldv, stream)
 
         @classmethod
         def qnn_rmsnorm_quant_i8(cls, x, r, rows, K, ldx, ldr, gamma, eps, codes, ldq, scale, total, ld_sum, values, ldv, stream):
             w, dt = "qnn_rmsnorm_quant_i8", torch.float32 if x is None else x.dtype
-            return _lib.qnn_rmsnorm_quant_i8(_p(x), cls._need(r, dt, w), cls._real(x, w), rows, K, ldx, ldr, cls._need(gamma, dt, w), eps,
+            return _fits.qnn_rmsnorm_quant_i8(_p(x), cls._need(r, dt, w), cls._real(x, w), rows, K, ldx, ldr, cls._need(gamma, dt, w), eps,
                                              cls._need(codes, torch.int8, w), ldq, cls._need(scale, torch.float32, w),
                                              cls._need(total, dt, w), ld_sum, _p(values), cls._real(values, w), ldv, stream)
 
         @classmethod
         def qnn_silu_mul_quant_i8(cls, gate, up, rows, K, ldg, ldu, codes, ldq, scale, values, ldv, stream):
             w, dt = "qnn_silu_mul_quant_i8", torch.float32 if gate is None else gate.dtype
-            return _lib.qnn_silu_mul_quant_i8(_p(gate), cls._need(up, dt, w), cls._real(gate, w), rows, K, ldg, ldu,
+            return _fits.qnn_silu_mul_quant_i8(_p(gate), cls._need(up, dt, w), cls._real(gate, w), rows, K, ldg, ldu,
                                               cls._need(codes, torch.int8, w), ldq, cls._need(scale, torch.float32, w), _p(values),
                                               cls._real(values, w), ldv, stream)
 
         @classmethod
         def qnn_gemm_i8_scaled(cls, a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, stream):
             w, f, i = "qnn_gemm_i8_scaled", torch.float32, torch.int8
-            return _lib.qnn_gemm_i8_scaled(cls._need(a, i, w), lda, cls._need(a_scale, f, w), cls._need(b, i, w), ldb,
+            return _fits.qnn_gemm_i8_scaled(cls._need(a, i, w), lda, cls._need(a_scale, f, w), cls._need(b, i, w), ldb,
                                            cls._need(b_scale, f, w), cls._need(bias, f, w), M, N, K, _p(out), cls._real(out, w), ldo, stream)
 
         @staticmethod
@@ -705,35 +720,35 @@ except ImportError:
         def qnn_quantize_blocks_f8(cls, x, rows, K, ldx, index, src_rows, codes, ldq, scale, lds, values, ldv, device, stream):
             w = "qnn_quantize_blocks_f8"
             cls._here(device, w, x, index, codes, scale, values)
-            return _lib.qnn_quantize_blocks_f8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(index, torch.int64, w), src_rows, _p(codes),
+            return _fits.qnn_quantize_blocks_f8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(index, torch.int64, w), src_rows, _p(codes),
                                                cls._f8(codes, w), ldq, cls._scale8(scale, w), lds, _p(values), cls._real(values, w), ldv, stream)
 
         @classmethod
         def qnn_quantize_tiles_f8(cls, x, rows, K, ldx, codes, ldq, scale, lds, values, ldv, device, stream):
             w = "qnn_quantize_tiles_f8"
             cls._here(device, w, x, codes, scale, values)
-            return _lib.qnn_quantize_tiles_f8(_p(x), cls._real(x, w), rows, K, ldx, _p(codes), cls._f8(codes, w), ldq, cls._scale8(scale, w),
+            return _fits.qnn_quantize_tiles_f8(_p(x), cls._real(x, w), rows, K, ldx, _p(codes), cls._f8(codes, w), ldq, cls._scale8(scale, w),
                                               lds, _p(values), cls._real(values, w), ldv, stream)
 
         @classmethod
         def qnn_quantize_columns_f8(cls, x, rows, K, ldx, offsets, groups, codes, ldq, scale, lds, values, ldv, device, stream):
             w = "qnn_quantize_columns_f8"
             cls._here(device, w, x, offsets, codes, scale, values)
-            return _lib.qnn_quantize_columns_f8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(offsets, torch.int64, w), groups, _p(codes),
+            return _fits.qnn_quantize_columns_f8(_p(x), cls._real(x, w), rows, K, ldx, cls._need(offsets, torch.int64, w), groups, _p(codes),
                                                 cls._f8(codes, w), ldq, cls._scale8(scale, w), lds, _p(values), cls._real(values, w), ldv, stream)
 
         @classmethod
         def qnn_gemm_f8(cls, a, lda, a_s, ld_as, b, ldb, b_s, ld_bs, across, bias, M, N, K, out, ldo, device, stream):
             w = "qnn_gemm_f8"
             cls._here(device, w, a, a_s, b, b_s, bias, out)
-            return _lib.qnn_gemm_f8(_p(a), cls._f8(a, w), lda, cls._scale8(a_s, w), ld_as, _p(b), cls._f8(b, w), ldb, cls._scale8(b_s, w),
+            return _fits.qnn_gemm_f8(_p(a), cls._f8(a, w), lda, cls._scale8(a_s, w), ld_as, _p(b), cls._f8(b, w), ldb, cls._scale8(b_s, w),
                                     ld_bs, across, cls._need(bias, torch.float32, w), M, N, K, _p(out), cls._real(out, w), ldo, stream)
 
         @classmethod
         def qnn_gemm_f8_grouped(cls, a, lda, a_s, ld_as, b, ldb, b_s, ld_bs, across, bias, offsets, groups, M, N, K, out, ldo, device, stream):
             w = "qnn_gemm_f8_grouped"
             cls._here(device, w, a, a_s, b, b_s, bias, offsets, out)
-            return _lib.qnn_gemm_f8_grouped(_p(a), cls._f8(a, w), lda, cls._scale8(a_s, w), ld_as, _p(b), cls._f8(b, w), ldb,
+            return _fits.qnn_gemm_f8_grouped(_p(a), cls._f8(a, w), lda, cls._scale8(a_s, w), ld_as, _p(b), cls._f8(b, w), ldb,
                                             cls._scale8(b_s, w), ld_bs, across, cls._need(bias, torch.float32, w),
                                             cls._need(offsets, torch.int64, w), groups, M, N, K, _p(out), cls._real(out, w), ldo, stream)
 
@@ -741,7 +756,7 @@ except ImportError:
         def qnn_gemm_f8_wgrad(cls, dy, ld_dy, dy_s, ld_dys, x, ldx, x_s, ld_xs, offsets, groups, M, N, K, dw, ld_dw, device, stream):
             w = "qnn_gemm_f8_wgrad"
             cls._here(device, w, dy, dy_s, x, x_s, offsets, dw)
-            return _lib.qnn_gemm_f8_wgrad(_p(dy), cls._f8(dy, w), ld_dy, cls._scale8(dy_s, w), ld_dys, _p(x), cls._f8(x, w), ldx,
+            return _fits.qnn_gemm_f8_wgrad(_p(dy), cls._f8(dy, w), ld_dy, cls._scale8(dy_s, w), ld_dys, _p(x), cls._f8(x, w), ldx,
                                           cls._scale8(x_s, w), ld_xs, cls._need(offsets, torch.int64, w), groups, M, N, K, _p(dw),
                                           cls._real(dw, w), ld_dw, stream)
 
@@ -750,14 +765,14 @@ except ImportError:
             w, f = "qnn_token_logprobs", torch.float32
             if not -2 ** 31 <= topk < 2 ** 31:
                 raise OverflowError("argument does not fit a C int")
-            return _lib.qnn_token_logprobs(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(logprob, f, w),
+            return _fits.qnn_token_logprobs(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(logprob, f, w),
                                            cls._need(entropy, f, w), cls._need(lse, f, w), topk, cls._need(top_logprob, f, w),
                                            cls._need(top_ids, torch.int64, w), stream)
 
         @classmethod
         def qnn_token_logprobs_backward(cls, z, T, V, ldl, ids, lse, entropy, g_logprob, g_entropy, d, ldd, stream):
             w, f = "qnn_token_logprobs_backward", torch.float32
-            return _lib.qnn_token_logprobs_backward(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(lse, f, w),
+            return _fits.qnn_token_logprobs_backward(_p(z), cls._real(z, w), T, V, ldl, cls._need(ids, torch.int64, w), cls._need(lse, f, w),
                                                     cls._need(entropy, f, w), cls._need(g_logprob, f, w), cls._need(g_entropy, f, w),
                                                     cls._need(d, f if z is None else z.dtype, w), ldd, stream)
 
