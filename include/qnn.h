@@ -744,6 +744,16 @@ QNN_API int qnn_gemm_f8_grouped(const void *a, int a_type, int64_t lda, const vo
                                 const float *bias, const int64_t *offsets, int64_t groups, int64_t M, int64_t N, int64_t K,
                                 void *out, int out_type, int64_t ldo, void *stream);
 
+/* Which kernel a product of this size runs on (for reports and tests, as
+ * qnn_select_algo): width | split << 12 | columns << 16, or 0 where none of them does
+ * (nothing to compute, sizes that are refused).  groups: 0 for qnn_gemm_f8, else
+ * qnn_gemm_f8_grouped's.
+ *   width    tokens that a tile of the kernel has room for; 256: a tile of 256
+ *            channels, shared by two thread blocks, otherwise 128
+ *   split    thread blocks that share K
+ *   columns  tokens of a tile of this product at most */
+QNN_API int qnn_gemm_f8_kernel(int64_t M, int64_t N, int64_t K, int64_t groups);
+
 /* Weight gradient of each group: dw[g][n,k] = sum over the group's rows m of
  * DY[m,n] X[m,k]; 0 for a group without rows.
  *   dy, x       codes and scales as qnn_quantize_columns_f8 writes them for the same

@@ -143,6 +143,7 @@ _SIGS = {
     "qnn_quantize_columns_f8": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, i32, i64, vp, i64, vp, i32, i64, vp]),
     "qnn_gemm_f8": (i32, [vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, i32, vp, i64, i64, i64, vp, i32, i64, vp]),
     "qnn_gemm_f8_grouped": (i32, [vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, i32, vp, vp, i64, i64, i64, i64, vp, i32, i64, vp]),
+    "qnn_gemm_f8_kernel": (i32, [i64, i64, i64, i64]),
     "qnn_gemm_f8_wgrad": (i32, [vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, vp, i32, i64, vp]),
     "qnn_workspace_bytes": (sz, [i32, i64, i64, i64, i32, i32, i32]),
     "qnn_select_algo": (i32, [i64, i64, i64, i32, i32, i32, i32]),
@@ -859,6 +860,12 @@ def qnn_gemm_f8_grouped(a, lda, a_scale, ld_as, b, ldb, b_scale, ld_bs, offsets,
                                        out, ldo, *_here())
     if s:
         raise QnnError(s, "qnn_gemm_f8_grouped")
+
+
+def qnn_gemm_f8_kernel(M, N, K, groups=0):
+    """(width, split, columns) of the kernel that a product of this size runs on, see qnn.h; (0, 0, 0) for none."""
+    k = _lib.qnn_gemm_f8_kernel(M, N, K, groups)
+    return k & 0xfff, k >> 12 & 15, k >> 16
 
 
 def qnn_gemm_f8_wgrad(dy, ld_dy, dy_scale, ld_dys, x, ldx, x_scale, ld_xs, offsets, groups, M, N, K, dw, ld_dw):

@@ -49,11 +49,13 @@ int parts_resident(int width, int split)
 
 int pairs_resident_f8() { return clusters_resident<256, 2, 1>(); }
 
+namespace {
+
 // len: tokens of a group; groups: how many are taken to have any; rows: the tiles' other
 // dimension; nkb: blocks of the reduction; cut: it may be cut.  Clocks of a launch, as measured: a block of a tile costs what its loads do (2.2 clk for each
 // of the 128 + n / ctas rows of 128 bytes that a CTA loads), or its products (2 n, at least 400); the results of a tile cost 11 clk a
 // column, under the products of the next one; joining parts of a reduction costs 2500, by sends 1000.
-F8Choice choose_f8(int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut)
+F8Choice cheapest(int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut)
 {
     static const int widths[] = {16, 32, 64, 128, 256};
     F8Choice best = {0, 1, 1, 0};
@@ -75,6 +77,17 @@ F8Choice choose_f8(int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool 
         }
     }
     return best;
+}
+
+}  // namespace
+
+F8Choice choose_f8(int64_t M, int64_t groups, int64_t N, int64_t nkb, bool one_group)
+{
+    const int64_t taken = groups < M ? groups : M;
+    F8Choice k = cheapest(ceil_div(M, taken), taken, N, nkb, one_group);
+    if (!one_group) k.nt = k.width;                // (groups differ: their chunks are evened out one by one)
+    if (k.split > 1 && k.width == 32) k.width = 64;    // (32 columns, in the kernel for 64)
+    return k;
 }
 
 namespace {
@@ -150,6 +163,14 @@ int gemm_f8_status(int *code)
 using namespace qnn;
 
 extern "C" {
+
+int qnn_gemm_f8_kernel(int64_t M, int64_t N, int64_t K, int64_t groups)
+{
+    const int64_t most = (int64_t)1 << 30;
+    if (M <= 0 || N <= 0 || K < 0 || groups < 0 || M > most || N > most || K > most || groups > MAX_GROUPS) return 0;
+    const F8Choice k = choose_f8(M, groups ? groups : 1, N, ceil_div(K, 128), groups == 0);
+    return k.width | k.split << 12 | k.nt << 16;
+}
 
 int qnn_gemm_f8(const void *a, int a_type, int64_t lda, const void *a_scale, int64_t ld_as, const void *b, int b_type, int64_t ldb, const void *b_scale,
                 int64_t ld_bs, int b_transposed, const float *bias, int64_t M, int64_t N, int64_t K, void *out, int out_type, int64_t ldo, void *stream)

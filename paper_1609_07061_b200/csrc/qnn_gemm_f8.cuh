@@ -52,14 +52,15 @@ struct F8Call {
     const void *x; int x_type; int64_t x_rows, x_cols, ld_x;
 };
 
-// How a product runs: columns of a tile, CTAs that share a tile (ctas: a pair, split: parts of the reduction).
+// How a product runs: columns that the kernel's tile has room for, CTAs that share a tile (ctas: a pair, split: parts of the
+// reduction), columns of the tiles of this product.
 struct F8Choice {
     int width, ctas, split, nt;
 };
 constexpr int chunk_step(int width) { return width >= 64 ? 32 : 16; }      // (blocks of 32 columns leave as one store)
 
 // (see qnn_gemm_f8.cu)
-F8Choice choose_f8(int64_t len, int64_t groups, int64_t rows, int64_t nkb, bool cut);
+F8Choice choose_f8(int64_t M, int64_t groups, int64_t N, int64_t nkb, bool one_group);
 int pairs_resident_f8();
 // one translation unit each; the status word of its waits: reads and clears it
 int run_f8_forward(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st);
@@ -1037,12 +1038,9 @@ int launch_split(const F8Call &c, const F8Params &p, const F8Choice &k, cudaStre
 template <int MODE, typename TOUT>
 int run_f8_typed(const F8Call &c, const F8Params &p, cudaStream_t st)
 {
-    F8Choice k;
-    const int64_t groups = p.groups < p.M ? p.groups : p.M;
-    k = choose_f8(ceil_div(p.M, groups), groups, p.N, p.nkb, p.offsets == nullptr);
-    if (p.offsets) k.nt = k.width;                 // (groups differ: their chunks are evened out one by one)
+    const F8Choice k = choose_f8(p.M, p.groups, p.N, p.nkb, p.offsets == nullptr);
     if (k.split > 1) return k.width == 16   ? launch_split<16, MODE, TOUT>(c, p, k, st)
-                            : k.width <= 64 ? launch_split<64, MODE, TOUT>(c, p, k, st)
+                            : k.width == 64 ? launch_split<64, MODE, TOUT>(c, p, k, st)
                                             : launch_split<128, MODE, TOUT>(c, p, k, st);
     switch (k.width) {
         case 32: return launch_f8<32, MODE, 1, TOUT>(c, p, k, st);
