@@ -493,7 +493,7 @@ __device__ __forceinline__ void find_block(const int64_t *offsets, int32_t group
 
 constexpr int TILE_THREADS = 256;
 
-// 128 rows x 128 columns at a time: 16 lanes hold a row's 128 columns, eight each, and a thread every sixteenth row.  Elements stay as they
+// 128 rows x 128 columns: 16 lanes hold a row's 128 columns, eight each, and a thread every sixteenth row.  Elements stay as they
 // lie in memory until they are encoded, so that four blocks (of 16-bit types) fit an SM: one's loads go on while the others join and write.
 template <typename T, bool VEC, bool COLUMNS, bool E5>
 __global__ void __launch_bounds__(TILE_THREADS, sizeof(T) == 4 ? 2 : 4)
@@ -504,7 +504,7 @@ quant_tiles_f8_kernel(const F8Source p)
     __shared__ __align__(8) uint8_t bytes[128];
     __shared__ int64_t where[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, l16 = tid & 15, r16 = tid >> 4;
-    const int32_t blk = blockIdx.y, tiles = (p.K + 127) / 128;
+    const int32_t blk = blockIdx.y, tile = blockIdx.x;
     const int32_t K16 = (p.K + 15) & ~15;
     griddep_wait();
     int64_t row0 = (int64_t)blk * 128, left = p.rows - row0;
@@ -519,93 +519,91 @@ quant_tiles_f8_kernel(const F8Source p)
     }
     const int rows = left < 128 ? (int)left : 128;
     const T *src = static_cast<const T *>(p.x) + row0 * p.ldx;
-    for (int32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int32_t k = tile * 128 + 8 * l16;
-        Eight<T> v[8];
+    const int32_t k = tile * 128 + 8 * l16;
+    Eight<T> v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = i * 16 + r16;
+        v[i] = read8<T, VEC>(r < rows ? src + (int64_t)r * p.ldx : nullptr, k, p.K);
+    }
+    griddep_launch_dependents();
+    uint32_t s8[2];                                  // this thread's columns' scale bytes
+    if (COLUMNS) {
+        uint32_t m[W];
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            uint32_t t = mag<T>(v[0].w[c]);
+#pragma unroll
+            for (int i = 1; i < 8; ++i) t = mag_max<T>(t, mag<T>(v[i].w[c]));
+            m[c] = mag_max<T>(t, __shfl_xor_sync(0xffffffffu, t, 16));
+        }
+        if (lane < 16)
+#pragma unroll
+            for (int u = 0; u < W / 4; ++u) tops[warp][l16 * (W / 4) + u] = make_uint4(m[4 * u], m[4 * u + 1], m[4 * u + 2], m[4 * u + 3]);
+        __syncthreads();
+        if (tid < 128) {
+            uint32_t t = 0;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if constexpr (sizeof(T) == 4) t = max(t, reinterpret_cast<const uint32_t *>(tops[w])[tid]);
+                else t = max(t, (uint32_t)reinterpret_cast<const uint16_t *>(tops[w])[tid]);
+            }
+            const uint32_t b = scale_byte<E5>(mag_bits(t, T()));
+            bytes[tid] = (uint8_t)b;
+            if (tile * 128 + tid < p.K) p.scale[(int64_t)blk * p.ld_scale + tile * 128 + tid] = (uint8_t)b;
+        }
+        __syncthreads();
+        const uint2 b8 = *reinterpret_cast<const uint2 *>(&bytes[8 * l16]);
+        s8[0] = b8.x; s8[1] = b8.y;
+    } else {
+        uint32_t t = mag8(v[0]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) t = mag_max<T>(t, mag8(v[i]));
+        t = __reduce_max_sync(0xffffffffu, mag_bits(t, T()));
+        uint32_t *part = reinterpret_cast<uint32_t *>(tops[0]);
+        if (lane == 0) part[warp] = t;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t = max(t, part[w]);
+        const uint32_t b = scale_byte<E5>(t);
+        if (tid == 0) p.scale[(int64_t)blk * p.ld_scale + tile] = (uint8_t)b;
+        s8[0] = s8[1] = b * 0x01010101u;
+    }
+    f32x2 inv[4], val[4];
+    uint2 keep = make_uint2(0u, 0u);                 // codes of columns with a NaN scale are 0
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint32_t a = s8[c / 2] >> (16 * (c & 1)) & 0xffu, b = s8[c / 2] >> (16 * (c & 1) + 8) & 0xffu;
+        inv[c] = pair(scale_inverse(a), scale_inverse(b));
+        val[c] = pair(scale_value(a), scale_value(b));
+        const uint32_t both = ((a != 255u ? 0xffu : 0u) | (b != 255u ? 0xff00u : 0u)) << (16 * (c & 1));
+        if (c < 2) keep.x |= both;
+        else keep.y |= both;
+    }
+    // (columns: the rows that fill a group up to whole blocks are written too, as zeros)
+    auto encode = [&](auto kind) {
+        using V = decltype(kind);
+        constexpr bool VALUES = !std::is_same<V, Nothing>::value;
+        const int64_t out0 = (int64_t)blk * 128 + r16;
+        uint8_t *codes = p.codes + out0 * p.ldq + k;
+        V *values = static_cast<V *>(p.values) + (VALUES ? out0 * p.ld_values : 0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = i * 16 + r16;
-            v[i] = read8<T, VEC>(r < rows ? src + (int64_t)r * p.ldx : nullptr, k, p.K);
-        }
-        if (tile + (int32_t)gridDim.x >= tiles) griddep_launch_dependents();
-        uint32_t s8[2];                                  // this thread's columns' scale bytes
-        if (COLUMNS) {
-            uint32_t m[W];
-#pragma unroll
-            for (int c = 0; c < W; ++c) {
-                uint32_t t = mag<T>(v[0].w[c]);
-#pragma unroll
-                for (int i = 1; i < 8; ++i) t = mag_max<T>(t, mag<T>(v[i].w[c]));
-                m[c] = mag_max<T>(t, __shfl_xor_sync(0xffffffffu, t, 16));
+            const bool there = (COLUMNS || i * 16 + r16 < rows) && k < K16;
+            f32x2 f[4];
+            floats_of(v[i], f);
+            uint2 q = encode8<E5>(f, inv);
+            q.x &= keep.x; q.y &= keep.y;
+            if (there) *reinterpret_cast<uint2 *>(codes) = q;
+            codes += 16 * p.ldq;
+            if constexpr (VALUES) {
+                decode8<E5>(q, val, f);
+                put_values(values, k, p.K, f, p.vec_values != 0, there && k < p.K);
+                values += 16 * p.ld_values;
             }
-            if (lane < 16)
-#pragma unroll
-                for (int u = 0; u < W / 4; ++u) tops[warp][l16 * (W / 4) + u] = make_uint4(m[4 * u], m[4 * u + 1], m[4 * u + 2], m[4 * u + 3]);
-            __syncthreads();
-            if (tid < 128) {
-                uint32_t t = 0;
-#pragma unroll
-                for (int w = 0; w < 8; ++w) {
-                    if constexpr (sizeof(T) == 4) t = max(t, reinterpret_cast<const uint32_t *>(tops[w])[tid]);
-                    else t = max(t, (uint32_t)reinterpret_cast<const uint16_t *>(tops[w])[tid]);
-                }
-                const uint32_t b = scale_byte<E5>(mag_bits(t, T()));
-                bytes[tid] = (uint8_t)b;
-                if (tile * 128 + tid < p.K) p.scale[(int64_t)blk * p.ld_scale + tile * 128 + tid] = (uint8_t)b;
-            }
-            __syncthreads();
-            const uint2 b8 = *reinterpret_cast<const uint2 *>(&bytes[8 * l16]);
-            s8[0] = b8.x; s8[1] = b8.y;
-        } else {
-            uint32_t t = mag8(v[0]);
-#pragma unroll
-            for (int i = 1; i < 8; ++i) t = mag_max<T>(t, mag8(v[i]));
-            t = __reduce_max_sync(0xffffffffu, mag_bits(t, T()));
-            uint32_t *part = reinterpret_cast<uint32_t *>(tops[tile / (int32_t)gridDim.x & 1]);
-            if (lane == 0) part[warp] = t;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < 8; ++w) t = max(t, part[w]);
-            const uint32_t b = scale_byte<E5>(t);
-            if (tid == 0) p.scale[(int64_t)blk * p.ld_scale + tile] = (uint8_t)b;
-            s8[0] = s8[1] = b * 0x01010101u;
         }
-        f32x2 inv[4], val[4];
-        uint2 keep = make_uint2(0u, 0u);                 // codes of columns with a NaN scale are 0
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const uint32_t a = s8[c / 2] >> (16 * (c & 1)) & 0xffu, b = s8[c / 2] >> (16 * (c & 1) + 8) & 0xffu;
-            inv[c] = pair(scale_inverse(a), scale_inverse(b));
-            val[c] = pair(scale_value(a), scale_value(b));
-            const uint32_t both = ((a != 255u ? 0xffu : 0u) | (b != 255u ? 0xff00u : 0u)) << (16 * (c & 1));
-            if (c < 2) keep.x |= both;
-            else keep.y |= both;
-        }
-        // (columns: the rows that fill a group up to whole blocks are written too, as zeros)
-        auto encode = [&](auto kind) {
-            using V = decltype(kind);
-            constexpr bool VALUES = !std::is_same<V, Nothing>::value;
-            const int64_t out0 = (int64_t)blk * 128 + r16;
-            uint8_t *codes = p.codes + out0 * p.ldq + k;
-            V *values = static_cast<V *>(p.values) + (VALUES ? out0 * p.ld_values : 0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool there = (COLUMNS || i * 16 + r16 < rows) && k < K16;
-                f32x2 f[4];
-                floats_of(v[i], f);
-                uint2 q = encode8<E5>(f, inv);
-                q.x &= keep.x; q.y &= keep.y;
-                if (there) *reinterpret_cast<uint2 *>(codes) = q;
-                codes += 16 * p.ldq;
-                if constexpr (VALUES) {
-                    decode8<E5>(q, val, f);
-                    put_values(values, k, p.K, f, p.vec_values != 0, there && k < p.K);
-                    values += 16 * p.ld_values;
-                }
-            }
-        };
-        with_values(p, encode);
-    }
+    };
+    with_values(p, encode);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
