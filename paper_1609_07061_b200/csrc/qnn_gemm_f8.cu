@@ -207,16 +207,13 @@ int qnn_gemm_f8_wgrad(const void *dy, int dy_type, int64_t ld_dy, const void *dy
         if (int rc = check_operand(what, "dy", dy, ld_dy, dy_scale, ld_dys, N, N)) return rc;
         if (int rc = check_operand(what, "x", x, ldx, x_scale, ld_xs, K, K)) return rc;
     }
-    F8Params p{};
-    p.M = M; p.N = (int32_t)N; p.C = (int32_t)K; p.groups = (int32_t)groups;
-    p.offsets = offsets;
-    p.w_scale = static_cast<const uint8_t *>(dy_scale); p.ld_ws = ld_dys;
-    p.x_scale = static_cast<const uint8_t *>(x_scale); p.ld_xs = ld_xs;
-    p.out = dw; p.ldo = ld_dw;
-    p.vec_out = aligned(dw, 16) && ld_dw * type_bytes(dw_type) % 16 == 0;
-    const int64_t rows = M > 0 ? 128 * (M / 128 + groups) : 0;          // rows of all blocks, at most
-    const F8Call c = {what, dy, dy_type, rows, N, ld_dy, ld_dy, 1, x, x_type, rows, K, ldx};
-    return run_f8_wgrad(c, p, dw_type, as_stream(stream));
+    WgParams p{};
+    p.dy = static_cast<const uint8_t *>(dy); p.ld_dy = ld_dy; p.dy_scale = static_cast<const uint8_t *>(dy_scale); p.ld_dys = ld_dys;
+    p.x = static_cast<const uint8_t *>(x); p.ldx = ldx; p.x_scale = static_cast<const uint8_t *>(x_scale); p.ld_xs = ld_xs;
+    p.offsets = offsets; p.groups = (int32_t)groups;
+    p.M = M; p.N = (int32_t)N; p.K = (int32_t)K;
+    p.dw = dw; p.ld_dw = ld_dw;
+    return run_f8_wgrad(what, p, dy_type, x_type, dw_type, as_stream(stream));
 }
 
 }  // extern "C"

@@ -9,12 +9,11 @@
 // One persistent kernel.  The weights are the tile's 128 rows, the tokens its
 // columns: their number is given to the instruction at run time, so a group of 37 rows costs 48 columns and not a tile.  Weights read
 // across are taken as they lie in memory: the tensor core reads them MN-major.
-// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 3 works out the tiles, warps 4..11 store the previous one,
+// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 2 fetches the tensor maps, warp 3 works out the tiles, warps 4..11 store the previous one,
 // warps 12..15 put the scales into tensor memory.  All waits are bounded.
 #pragma once
 #include <cuda.h>
-#include <atomic>
-#include "qnn_types.cuh"
+#include "qnn_f8.cuh"
 #include "qnn_tc_ptx.cuh"
 
 namespace qnn {
@@ -24,8 +23,7 @@ enum F8Mode { FORWARD = 0, ACROSS = 1 };
 struct F8Params {
     int64_t M;                       // rows of a (tokens) of all groups; offsets are held to 0..M
     int32_t N;                       // channels: rows of the tile's operand
-    int32_t C;                       // weight gradient: columns (k)
-    int32_t nkb;                     // blocks of the reduction (forward, across)
+    int32_t nkb;                     // blocks of the reduction
     int32_t groups;
     const int64_t *offsets;          // [groups + 1] or NULL: one group of all rows
     const uint8_t *w_scale; int64_t ld_ws, stride_ws;      // scales of the tile's rows
@@ -65,13 +63,11 @@ int pairs_resident_f8();
 // one translation unit each; the status word of its waits: reads and clears it
 int run_f8_forward(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st);
 int run_f8_across(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st);
-int run_f8_wgrad(const F8Call &c, const F8Params &p, int out_type, cudaStream_t st);
 int f8_forward_status(int *code);
 int f8_across_status(int *code);
 
 namespace {
 
-constexpr int MAX_GROUPS = QNN_F8_MAX_GROUPS;
 constexpr int F8_THREADS = 512;
 template <int NT, int MODE, int CTAS, typename TOUT, int SPLIT = 1>
 struct F8Cfg {
@@ -109,7 +105,7 @@ struct F8Cfg {
     static constexpr int TABLE_OFFSET = RING_OFFSET + RING_BYTES;
     static constexpr int BAR_OFFSET = TABLE_OFFSET + TABLE_BYTES;
     static constexpr int TOTAL = BAR_OFFSET + BAR_BYTES + 1024;
-    static_assert(TMEM_NEED <= 512 && (2 * STAGES + 2 * QS + 11) * 8 + 16 <= BAR_BYTES && RESIDENT * (TOTAL + 1024) <= 228 * 1024, "configuration");
+    static_assert(TMEM_NEED <= 512 && (2 * STAGES + QS + 11) * 8 + 16 <= BAR_BYTES && RESIDENT * (TOTAL + 1024) <= 228 * 1024, "configuration");
     // The scales' warps learn from a stage's barrier that the word before the last one has been used: the products cannot be more than
     // four blocks past it by then, so the barrier must not come round within five.
     static_assert(STAGES >= 5, "configuration");
@@ -294,7 +290,7 @@ struct F8Tile {
 };
 
 // The tiles of a launch by their number; a CTA (pair) takes every so many of them, in rising order.
-template <int MODE, int CTAS>
+template <int CTAS>
 struct Tiles {
     const F8Params &p;
     const int32_t *first, *start;    // [groups + 1] first tile / first row
@@ -377,7 +373,6 @@ struct TileQueue {
 
 // first[], start[] in shared memory from the offsets in global memory, by all threads of the block.  Offsets that fall, or leave
 // 0..M, are held to rise and to stay inside, so that no group reaches rows that are not there.
-template <int MODE>
 __device__ void fill_tables(const F8Params &p, int32_t *first, int32_t *start, int32_t *scratch)
 {
     constexpr int W = F8_THREADS / 32;
@@ -466,10 +461,9 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     auto tfull_bar = [&](int a) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 2 + a); };
     auto tempty_bar = [&](int a) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 4 + a); };
     auto qfull_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + s); };
-    auto qempty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + S::QS + s); };
-    const uint32_t join_bar = bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + 2 * S::QS);
+    const uint32_t join_bar = bar0 + 8u * (uint32_t)(2 * S::STAGES + 6 + S::QS);
     const uint32_t tiles_full = join_bar + 8u, tiles_empty = join_bar + 24u;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 11 + 2 * S::QS));
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + S::BAR_OFFSET + 8 * (2 * S::STAGES + 11 + S::QS));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int32_t *first = reinterpret_cast<int32_t *>(gen + S::TABLE_OFFSET);
     int32_t *start = first + MAX_GROUPS + 8;
@@ -483,7 +477,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(sfull_bar(a), 4 * CTAS); mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 8 * CTAS); }
-        for (int s = 0; s < S::QS; ++s) { mbar_init(qfull_bar(s), 4); mbar_init(qempty_bar(s), 4); }
+        for (int s = 0; s < S::QS; ++s) mbar_init(qfull_bar(s), 4);
         if (S::PUSH) mbar_init(join_bar, 1);
         // (read by warps 0, 4..15, and 1 where the products are issued)
         for (int h = 0; h < 2; ++h) { mbar_init(tiles_full + 8u * h, 1); mbar_init(tiles_empty + 8u * h, 13 + (leader ? 1 : 0)); }
@@ -506,7 +500,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     // only now may the next kernel be scheduled: one that shares this SM could take the tensor memory this CTA waits for
     griddep_launch_dependents();
     griddep_wait();
-    if (p.offsets) fill_tables<MODE>(p, first, start, reinterpret_cast<int32_t *>(gen + S::STG_OFFSET));
+    if (p.offsets) fill_tables(p, first, start, reinterpret_cast<int32_t *>(gen + S::STG_OFFSET));
 
     // a part of the reduction is whole words of scales
     const int32_t part_k = CUT ? (int32_t)cluster_ctarank() : 0;
@@ -516,7 +510,7 @@ gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant
     TileQueue queue(ring, tiles_full, tiles_empty, abort_flag);
 
     if (warp == 3) {
-        Tiles<MODE, CTAS> tiles(p, first, start, kb0, kb1 - kb0);
+        Tiles<CTAS> tiles(p, first, start, kb0, kb1 - kb0);
         const int32_t num_tiles = tiles.count(), workers = (int32_t)(gridDim.x / (CTAS * SPLIT));
         int64_t t = (int64_t)(blockIdx.x / (CTAS * SPLIT)) + (int64_t)lane * workers;
         for (uint32_t b = 0;; ++b, t += 32 * (int64_t)workers) {
@@ -944,19 +938,6 @@ int make_map_f8(const char *what, CUtensorMap *map, const void *ptr, int dims_n,
     CUresult r = fn(map, type, (cuuint32_t)dims_n, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     QNN_REQUIRE(r == CUDA_SUCCESS, QNN_ERR_CUDA, "%s: cuTensorMapEncodeTiled failed with code %d", what, (int)r);
-    return QNN_OK;
-}
-
-// The shared-memory opt-in is per kernel and device and costs microseconds: asked for once each.
-template <typename Kern>
-int opt_in(Kern kern, int bytes, std::atomic<bool> (&done)[64])
-{
-    int dev = 0;
-    QNN_CUDA(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64 || !done[dev].load(std::memory_order_acquire)) {
-        QNN_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
-    }
     return QNN_OK;
 }
 

@@ -10,8 +10,8 @@
 // 16384 rows over 32 groups, 4096 x 2048 (e5m2): 2149 us, 128 TFLOP/s.  Warps waited for a busy arithmetic pipe most (integer 43 %,
 // tensor 24 %, before scales left the former: 2590 us).  Conversions are not what bounds it now: e5m2 by the conversion instruction
 // takes 2203.  Eight warps of 64 x 32, which read shared memory less often, take 2547.
-#include "qnn_gemm_f8.cuh"
 #include <cuda_fp8.h>
+#include "qnn_f8.cuh"
 
 namespace qnn {
 namespace {
@@ -19,14 +19,6 @@ namespace {
 constexpr int WG_T = 128, WG_ROWS = 64, WG_THREADS = 512;
 constexpr int WG_PITCH = WG_T + 8;                   // halves; eight rows of 16 bytes then lie in different banks
 constexpr int WG_BYTES = 2 * 2 * WG_ROWS * WG_PITCH * 2;
-
-struct WgParams {
-    const uint8_t *dy, *x, *dy_scale, *x_scale;
-    int64_t ld_dy, ldx, ld_dys, ld_xs, M, ld_dw;
-    const int64_t *offsets;
-    void *dw;
-    int32_t N, K, groups, tiles_n, tiles_k;
-};
 
 // two codes as halves: an e5m2 code is the upper byte of its fp16 number
 template <int TYPE>
@@ -192,7 +184,7 @@ __global__ void __launch_bounds__(WG_THREADS) wgrad_f8_kernel(const WgParams p)
 }
 
 template <typename TOUT, int DY, int X>
-int launch_wgrad(const F8Call &c, const WgParams &p, unsigned grid, cudaStream_t st)
+int launch_wgrad(const char *what, const WgParams &p, unsigned grid, cudaStream_t st)
 {
     static std::atomic<bool> done[64];
     auto kern = wgrad_f8_kernel<TOUT, DY, X>;
@@ -200,28 +192,22 @@ int launch_wgrad(const F8Call &c, const WgParams &p, unsigned grid, cudaStream_t
     profile_before(st);
     kern<<<grid, WG_THREADS, WG_BYTES, st>>>(p);
     profile_after(st);
-    return check_launch(c.what);
+    return check_launch(what);
 }
 
 }  // namespace
 
-int run_f8_wgrad(const F8Call &c, const F8Params &f, int out_type, cudaStream_t st)
+int run_f8_wgrad(const char *what, WgParams p, int dy_type, int x_type, int out_type, cudaStream_t st)
 {
-    WgParams p{};
-    p.dy = static_cast<const uint8_t *>(c.w); p.x = static_cast<const uint8_t *>(c.x);
-    p.dy_scale = f.w_scale; p.x_scale = f.x_scale;
-    p.ld_dy = c.ld_w; p.ldx = c.ld_x; p.ld_dys = f.ld_ws; p.ld_xs = f.ld_xs; p.M = f.M; p.ld_dw = f.ldo;
-    p.offsets = f.offsets; p.dw = f.out;
-    p.N = f.N; p.K = f.C; p.groups = f.groups;
     p.tiles_n = (int32_t)ceil_div(p.N, WG_T); p.tiles_k = (int32_t)ceil_div(p.K, WG_T);
     const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
-    QNN_REQUIRE(tiles < (int64_t)1 << 28 && tiles * p.groups < (int64_t)1 << 30, QNN_ERR_UNSUPPORTED, "%s: too many output tiles", c.what);
+    QNN_REQUIRE(tiles < (int64_t)1 << 28 && tiles * p.groups < (int64_t)1 << 30, QNN_ERR_UNSUPPORTED, "%s: too many output tiles", what);
     const unsigned grid = (unsigned)(tiles * p.groups);
-    const bool e4 = c.w_type == QNN_F8_E4M3, f4 = c.x_type == QNN_F8_E4M3;
+    const bool e4 = dy_type == QNN_F8_E4M3, f4 = x_type == QNN_F8_E4M3;
     auto typed = [&](auto out) {
         typedef decltype(out) T;
-        return e4 ? (f4 ? launch_wgrad<T, QNN_F8_E4M3, QNN_F8_E4M3>(c, p, grid, st) : launch_wgrad<T, QNN_F8_E4M3, QNN_F8_E5M2>(c, p, grid, st))
-                  : (f4 ? launch_wgrad<T, QNN_F8_E5M2, QNN_F8_E4M3>(c, p, grid, st) : launch_wgrad<T, QNN_F8_E5M2, QNN_F8_E5M2>(c, p, grid, st));
+        return e4 ? (f4 ? launch_wgrad<T, QNN_F8_E4M3, QNN_F8_E4M3>(what, p, grid, st) : launch_wgrad<T, QNN_F8_E4M3, QNN_F8_E5M2>(what, p, grid, st))
+                  : (f4 ? launch_wgrad<T, QNN_F8_E5M2, QNN_F8_E4M3>(what, p, grid, st) : launch_wgrad<T, QNN_F8_E5M2, QNN_F8_E5M2>(what, p, grid, st));
     };
     return out_type == QNN_TYPE_F32 ? typed(float()) : out_type == QNN_TYPE_BF16 ? typed(__nv_bfloat16()) : typed(__half());
 }
