@@ -84,17 +84,16 @@ static void *scale8(PyObject *t, const char *where)
     }
     return any(t);
 }
-/* every tensor among the n arguments must be on the current device, whose index is `device` */
-static void here(PyObject *const *a, Py_ssize_t n, PyObject *device, const char *where)
+/* the tensors among the arguments, a bit each (None: not given), must be on the current device, whose index is `device` */
+static void here(PyObject *const *a, unsigned tensors, PyObject *device, const char *where)
 {
     const long dev = PyLong_AsLong(device);
-    Py_ssize_t i;
-    for (i = 0; i < n && !PyErr_Occurred(); ++i) {
+    for (; tensors != 0 && !PyErr_Occurred(); tensors >>= 1, ++a) {
         PyObject *v;
-        if (a[i] == Py_None || PyLong_Check(a[i])) continue;
-        v = PyObject_CallMethodNoArgs(a[i], s_get_device);
+        if ((tensors & 1) == 0 || *a == Py_None) continue;
+        v = PyObject_CallMethodNoArgs(*a, s_get_device);
         if (v == NULL) return;
-        if (PyLong_AsLong(v) != dev) PyErr_Format(PyExc_ValueError, "%s: a tensor on another device than the current one", where);
+        if (PyLong_AsLong(v) != dev && !PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: a tensor on another device than the current one", where);
         Py_DECREF(v);
     }
 }
@@ -159,28 +158,28 @@ ENTRY(qnn_gemm_i8_scaled, 13,
       qnn_gemm_i8_scaled(x, lda, sa, wt, ldb, sb, bias, M, N, K, out, type, ldo, stream))
 
 ENTRY(qnn_quantize_blocks_f8, 14,
-      const char *w = "qnn_quantize_blocks_f8"; int type COMMA vtype COMMA ctype; here(a, 12, a[12], w); real(a[0], &type, w);
+      const char *w = "qnn_quantize_blocks_f8"; int type COMMA vtype COMMA ctype; here(a, 0x551, a[12], w); real(a[0], &type, w);
       void *x = any(a[0]); int64_t rows = i64(a[1]) COMMA K = i64(a[2]) COMMA ldx = i64(a[3]); void *index = need(a[4], t_i64, w);
       int64_t src = i64(a[5]); void *codes = f8(a[6], &ctype, w); int64_t ldq = i64(a[7]); void *scale = scale8(a[8], w);
       int64_t lds = i64(a[9]); real(a[10], &vtype, w); void *values = any(a[10]); int64_t ldv = i64(a[11]); void *stream = ptr(a[13]),
       qnn_quantize_blocks_f8(x, type, rows, K, ldx, index, src, codes, ctype, ldq, scale, lds, values, vtype, ldv, stream))
 
 ENTRY(qnn_quantize_tiles_f8, 12,
-      const char *w = "qnn_quantize_tiles_f8"; int type COMMA vtype COMMA ctype; here(a, 10, a[10], w); real(a[0], &type, w);
+      const char *w = "qnn_quantize_tiles_f8"; int type COMMA vtype COMMA ctype; here(a, 0x151, a[10], w); real(a[0], &type, w);
       void *x = any(a[0]); int64_t rows = i64(a[1]) COMMA K = i64(a[2]) COMMA ldx = i64(a[3]); void *codes = f8(a[4], &ctype, w);
       int64_t ldq = i64(a[5]); void *scale = scale8(a[6], w); int64_t lds = i64(a[7]); real(a[8], &vtype, w);
       void *values = any(a[8]); int64_t ldv = i64(a[9]); void *stream = ptr(a[11]),
       qnn_quantize_tiles_f8(x, type, rows, K, ldx, codes, ctype, ldq, scale, lds, values, vtype, ldv, stream))
 
 ENTRY(qnn_quantize_columns_f8, 14,
-      const char *w = "qnn_quantize_columns_f8"; int type COMMA vtype COMMA ctype; here(a, 12, a[12], w); real(a[0], &type, w);
+      const char *w = "qnn_quantize_columns_f8"; int type COMMA vtype COMMA ctype; here(a, 0x551, a[12], w); real(a[0], &type, w);
       void *x = any(a[0]); int64_t rows = i64(a[1]) COMMA K = i64(a[2]) COMMA ldx = i64(a[3]); void *offsets = need(a[4], t_i64, w);
       int64_t groups = i64(a[5]); void *codes = f8(a[6], &ctype, w); int64_t ldq = i64(a[7]); void *scale = scale8(a[8], w);
       int64_t lds = i64(a[9]); real(a[10], &vtype, w); void *values = any(a[10]); int64_t ldv = i64(a[11]); void *stream = ptr(a[13]),
       qnn_quantize_columns_f8(x, type, rows, K, ldx, offsets, groups, codes, ctype, ldq, scale, lds, values, vtype, ldv, stream))
 
 ENTRY(qnn_gemm_f8, 17,
-      const char *w = "qnn_gemm_f8"; int type COMMA at COMMA bt; here(a, 15, a[15], w); real(a[13], &type, w);
+      const char *w = "qnn_gemm_f8"; int type COMMA at COMMA bt; here(a, 0x2255, a[15], w); real(a[13], &type, w);
       void *x = f8(a[0], &at, w); int64_t lda = i64(a[1]); void *sa = scale8(a[2], w); int64_t ldsa = i64(a[3]);
       void *wt = f8(a[4], &bt, w); int64_t ldb = i64(a[5]); void *sb = scale8(a[6], w); int64_t ldsb = i64(a[7]); int across = i32(a[8]);
       void *bias = need(a[9], t_f32, w); int64_t M = i64(a[10]) COMMA N = i64(a[11]) COMMA K = i64(a[12]);
@@ -188,7 +187,7 @@ ENTRY(qnn_gemm_f8, 17,
       qnn_gemm_f8(x, at, lda, sa, ldsa, wt, bt, ldb, sb, ldsb, across, bias, M, N, K, out, type, ldo, stream))
 
 ENTRY(qnn_gemm_f8_grouped, 19,
-      const char *w = "qnn_gemm_f8_grouped"; int type COMMA at COMMA bt; here(a, 17, a[17], w); real(a[15], &type, w);
+      const char *w = "qnn_gemm_f8_grouped"; int type COMMA at COMMA bt; here(a, 0x8655, a[17], w); real(a[15], &type, w);
       void *x = f8(a[0], &at, w); int64_t lda = i64(a[1]); void *sa = scale8(a[2], w); int64_t ldsa = i64(a[3]);
       void *wt = f8(a[4], &bt, w); int64_t ldb = i64(a[5]); void *sb = scale8(a[6], w); int64_t ldsb = i64(a[7]); int across = i32(a[8]);
       void *bias = need(a[9], t_f32, w); void *offsets = need(a[10], t_i64, w); int64_t groups = i64(a[11]);
@@ -196,7 +195,7 @@ ENTRY(qnn_gemm_f8_grouped, 19,
       qnn_gemm_f8_grouped(x, at, lda, sa, ldsa, wt, bt, ldb, sb, ldsb, across, bias, offsets, groups, M, N, K, out, type, ldo, stream))
 
 ENTRY(qnn_gemm_f8_wgrad, 17,
-      const char *w = "qnn_gemm_f8_wgrad"; int type COMMA at COMMA bt; here(a, 15, a[15], w); real(a[13], &type, w);
+      const char *w = "qnn_gemm_f8_wgrad"; int type COMMA at COMMA bt; here(a, 0x2155, a[15], w); real(a[13], &type, w);
       void *dy = f8(a[0], &at, w); int64_t ldy = i64(a[1]); void *sy = scale8(a[2], w); int64_t ldsy = i64(a[3]);
       void *x = f8(a[4], &bt, w); int64_t ldx = i64(a[5]); void *sx = scale8(a[6], w); int64_t ldsx = i64(a[7]);
       void *offsets = need(a[8], t_i64, w); int64_t groups = i64(a[9]) COMMA M = i64(a[10]) COMMA N = i64(a[11]) COMMA K = i64(a[12]);
