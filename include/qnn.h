@@ -695,6 +695,7 @@ QNN_API int qnn_token_logprobs_backward(const void *logits, int type, int64_t T,
  *            every row are written as 0, bytes beyond that are left untouched
  *  - values  device, [rows, ld_values] of values_type, or NULL: what the codes
  *            stand for, code * 2^(s - 127) rounded to values_type
+ *  - codes, scales and values overlap neither x nor one another
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED (a size above 2^30; tiles and columns:
  * 65536 blocks of 128 rows and more), CUDA. */
 

@@ -137,3 +137,42 @@ def test_rows_far_apart(q):
     y.codes.view(torch.uint8)[rows:] = 0
     q.qnn_gemm_f8_wgrad(y.codes, y.ld, y.scale, y.lds, cq, 208, cs, 208, None, 1, rows, rows, K, out, far)
     assert torch.equal(out[:, :K], (y.exact[:rows].t() @ x[:, :K].double()).float().to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("out", TYPES)
+def test_an_empty_reduction_by_group_gives_the_groups_bias(q, out):
+    sizes, first, N = [40, 0, 300, 1], 2, 200
+    M, G = first + sum(sizes) + 5, len(sizes)
+    c, s = torch.zeros(512, 16, dtype=torch.uint8, device="cuda").view(E4M3), torch.zeros(512, 16, dtype=torch.uint8, device="cuda")
+    bias = torch.arange(G * N, device="cuda", dtype=torch.float32).view(G, N)
+    for b in (bias, None):
+        o = Guarded((M, N), out)
+        q.qnn_gemm_f8_grouped(c, 16, s, 16, c, 16, s, 16, offsets_of(sizes, first), G, M, N, 0, o.t, N, bias=b)
+        o.check()
+        at = first
+        for i, n in enumerate(sizes):
+            assert torch.equal(o.t[at:at + n], ((b if b is not None else 0 * bias)[i]).to(out).expand(n, N))
+            at += n
+        for r in (slice(0, first), slice(at, M)):
+            assert (o.t[r].view(torch.uint8) == 0xA5).all()
+
+
+def test_products_beside_one_another_on_three_streams(q):
+    """Products of every kind at once: clusters and pairs of one stream's call wait for SMs, shared and tensor memory of the other's."""
+    g, jobs = gen(8), []
+    for M, N, K in [(1, 4096, 4096), (250, 1030, 4700), (2000, 2000, 600), (7, 2000, 4200), (950, 520, 2300), (4000, 2100, 600), (40, 3000, 260)]:
+        a, w = Operand(g, M, K, E4M3, (1, B)), Operand(g, N, K, E4M3, (B, B))
+        jobs.append((a, w, M, N, K, (a.exact @ w.exact.t()).float()))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [[torch.zeros(j[2], j[3], device="cuda") for j in jobs] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for n, (st, out) in enumerate(zip(streams, outs)):
+            with torch.cuda.stream(st):
+                for i in range(len(jobs)):
+                    a, w, M, N, K, _ = jobs[(i * (n + 1)) % len(jobs)]
+                    q.qnn_gemm_f8(a.codes, a.ld, a.scale, a.lds, w.codes, w.ld, w.scale, w.lds, M, N, K, out[(i * (n + 1)) % len(jobs)], N)
+    torch.cuda.synchronize()
+    for out in outs:
+        for o, j in zip(out, jobs):
+            assert torch.equal(o, j[5])

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from test_gpu_f8_kernels import product
-from test_gpu_f8_ops import B, E4M3, E5M2, TYPES, Operand, gen, q, up  # noqa: F401
+from test_gpu_f8_ops import B, E4M3, E5M2, TYPES, Operand, Out, gen, q, ref_blocks, up  # noqa: F401
 from util import Guarded
 
 pytestmark = pytest.mark.gpu
@@ -107,3 +107,28 @@ def test_sums_keep_25_bits_below_their_largest_term(q, M, N):
             q.qnn_gemm_f8(a.to(E5M2), K, scale, 16, b.to(E5M2), K, scale, 16, M, N, K, o.t, N)
             o.check()
             assert (o.t == 2.0 ** (20 - j)).all(), (at, j)
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("code", [E4M3, E5M2])
+def test_quantisers_at_the_ends_of_16_bit_types(q, code, dtype):
+    """Zeros, the least subnormal, the largest number, infinities and NaN of the type, each in a block of its own."""
+    info = torch.finfo(dtype)
+    tiny = info.smallest_normal * info.eps
+    rows = [[0.0], [-0.0], [tiny], [-tiny, tiny * 3], [info.smallest_normal], [info.max, 1.0], [-info.max, info.max / 2], [float("inf"), 1.0],
+            [1.0, float("-inf")], [float("nan"), 2.0], [info.max, float("nan")], [17.0, 19.0, 448.0], [1.75, 1.0], [1.75 + 2 * info.eps, 1.0]]
+    t = torch.zeros(len(rows), B, device="cuda", dtype=dtype)
+    for i, r in enumerate(rows):
+        t[i, :len(r)] = torch.tensor(r, dtype=torch.float64).to(dtype)
+    o = Out(len(rows), B, len(rows), 1, code, torch.float32)
+    q.qnn_quantize_blocks_f8(t, len(rows), B, B, o.q, o.ldq, o.scale.t, o.lds, values=o.values.t, ld_values=o.ldv)
+    o.check(*ref_blocks(t.double(), 1, B, code), (1, B))
+    assert (o.scale.t[:, 0] == 255).tolist() == [not torch.tensor(r).isfinite().all() for r in rows]
+    cols = t.t().contiguous()
+    o = Out(2 * B, len(rows), 2, len(rows), code, torch.float32)
+    q.qnn_quantize_columns_f8(cols, B, len(rows), len(rows), None, 1, o.q, o.ldq, o.scale.t, o.lds, values=o.values.t, ld_values=o.ldv)
+    o.check(*ref_blocks(cols.double(), B, 1, code), (B, 1), rows=B)
+    for i in range(len(rows)):
+        o = Out(1, B, 1, 1, code, torch.float32)
+        q.qnn_quantize_tiles_f8(t[i:i + 1], 1, B, B, o.q, o.ldq, o.scale.t, o.lds, values=o.values.t, ld_values=o.ldv)
+        o.check(*ref_blocks(t[i:i + 1].double(), B, B, code), (B, B))
