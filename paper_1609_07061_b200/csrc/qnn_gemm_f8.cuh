@@ -9,8 +9,15 @@
 // One persistent kernel.  The weights are the tile's 128 rows, the tokens its
 // columns: their number is given to the instruction at run time, so a group of 37 rows costs 48 columns and not a tile.  Weights read
 // across are taken as they lie in memory: the tensor core reads them MN-major.
-// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 2 fetches the tensor maps, warp 3 works out the tiles, warps 4..11 store the previous one,
-// warps 12..15 put the scales into tensor memory.  All waits are bounded.
+// Warp 0 loads codes by TMA, warp 1 multiplies into one of two accumulators, warp 2 fetches the tensor maps, warp 3 works out the tiles,
+// warps 4..11 store the previous one, warps 12..15 put the scales into tensor memory.  All waits are bounded.
+//
+// No access leaves the caller's buffers: tensor maps describe exactly these, so what lies outside is filled with zeros or not
+// stored; offsets are held to 0..M before they are used, and a tile's rows end with its group; scales are read 16 bytes at a time from
+// multiples of 16 inside a row.
+//
+// 10000 x 4096 x 4096, e4m3 to bf16: 117 us from cold, 2870 T operations/s; repeated it is held by the power limit, 145 us at 1335 MHz, 193000
+// clocks (zeros in the place of the tokens: 101 us at 1878 MHz, 191000 clocks).  The tensor pipe is busy 70 % of the active clocks.
 #pragma once
 #include <cuda.h>
 #include "qnn_f8.cuh"

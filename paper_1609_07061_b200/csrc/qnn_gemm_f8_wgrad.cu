@@ -7,9 +7,11 @@
 // One CTA owns 128 x 128 results of a group; sixteen warps own 32 x 32 of them each.  Rows go through shared memory 64 at a time, the next
 // 64 on their way in registers meanwhile, and are turned round by transposing matrix loads.  Every load is a plain one of 16 bytes
 // within a row, and only blocks of the group itself are read: buffers need hold no more than the groups' blocks.
-// 16384 rows over 32 groups, 4096 x 2048 (e5m2): 2149 us, 128 TFLOP/s.  Warps waited for a busy arithmetic pipe most (integer 43 %,
-// tensor 24 %, before scales left the former: 2590 us).  Conversions are not what bounds it now: e5m2 by the conversion instruction
-// takes 2203.  Eight warps of 64 x 32, which read shared memory less often, take 2547.
+// 16384 rows over 32 groups, 4096 x 2048 (e5m2): 2159 us, 127 TFLOP/s; 4096 x 4096 x 4096 in one group 700 us, 196 TFLOP/s.  Far from
+// its floor (98 and 41 us).  At 4096 rows, 8 groups, 2048 x 2048 the tensor pipe is busy 26 % of the time, the integer pipe 23 %; warps
+// wait most for the queue of loads and stores (scales come a byte at a time, results leave one by one), then for shared memory.
+// Conversions are not what bounds it: e5m2 by the conversion instruction takes 2203 instead of 2149.  Eight warps of 64 x 32, which
+// read shared memory less often, take 2547.
 #include <cuda_fp8.h>
 #include "qnn_f8.cuh"
 

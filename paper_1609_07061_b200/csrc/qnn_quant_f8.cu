@@ -4,8 +4,12 @@
 // The scale is the least power of two at which the block's largest magnitude fits the codes: read off the exponent and the mantissa
 // of that magnitude, so dividing by it is exact and a code is one rounding of the value (to nearest, ties to even).
 //
-// All of it is bound by memory: every element is read once into registers, the blocks' maxima are joined across lanes (rows: 16 lanes
-// hold a block) or through shared memory (tiles, columns), and codes, scales and values are written from the registers.
+// Every element is read once into registers, the blocks' maxima are joined across lanes (rows: 16 lanes hold a block) or through shared
+// memory (tiles, columns), and codes, scales and values are written from the registers.
+//
+// Tiles of fp32 are bound by memory: 11008 x 4096 with bf16 values 48.7 us, 6.5 TB/s.  16-bit elements are bound by the integer pipe
+// before that, and by how long loads take: 16384 rows x 2048 by index 26.1 us (pipe busy 77 %, DRAM 26 %), columns of 16384 x 4096 in
+// 32 groups 71.2 us (62 %, 54 %), 5000 x 4097 in tiles, whose rows lie off 16 bytes, 41 us from cold (73 %, 16 %).
 #include <type_traits>
 #include "qnn_types.cuh"
 
